@@ -16,7 +16,8 @@ Qwen-2.5 and Gemma-3 shaped heads) and generic odd ones.
 
 Logits are normal with a standard deviation of 3, which at these vocabularies puts most of a row's probability on a
 few tens of tokens, as a language model's rows do.  A drafter's logits follow the target's with an error of their
-own, on the clusters that hold its best tokens.
+own, on the clusters that hold its best tokens.  Temperatures and tail weights are 32-bit arguments, so the cases
+take values that 32 bits hold exactly.
 """
 from __future__ import annotations
 
@@ -60,8 +61,8 @@ def listed():
         # one user's drafting cycle: five drafts sampled from shortlists, judged together
         _chain("chain_b1", B=1, n=5, V=128256, M=1024, k=32),
         # a serving batch with chains of different lengths, tempered on both sides, drafts from the tail mixture
-        _chain("chain_serving_b16", B=16, n=4, V=151936, M=2048, k=64, temperature=0.7, draft_temperature=0.8,
-               tail=0.1, ragged=True),
+        _chain("chain_serving_b16", B=16, n=4, V=151936, M=2048, k=64, temperature=0.75,
+               draft_temperature=0.875, tail=0.125, ragged=True),
         # the largest vocabulary and batch
         _chain("chain_large_b128", B=128, n=4, V=262144, M=4096, k=64),
         # a small model's greedy tree in fp32 at an odd vocabulary: the smallest call, where launches count
@@ -92,12 +93,12 @@ def draw(rng):
     kind = rng.choice(["chain", "chain", "tree", "distill", "distill", "router"])
     V = between(8192, 262144)
     dtype = rng.choice(["bf16", "bf16", "f32"])
-    temperature = rng.choice([0.0, 0.6, 1.0, 1.0])
+    temperature = rng.choice([0.0, 0.625, 1.0, 1.0])
     if kind == "chain":
         M = between(64, min(4096, V // 32))
         return _chain(B=between(1, 64), n=rng.randint(1, 8), V=V, M=M, k=between(2, min(64, M // 4)), dtype=dtype,
-                      temperature=temperature, draft_temperature=rng.choice([1.0, 0.8]),
-                      tail=rng.choice([0.0, 0.0, 0.1]), ragged=rng.random() < 0.5, outright=rng.random() < 0.25)
+                      temperature=temperature, draft_temperature=rng.choice([1.0, 0.75]),
+                      tail=rng.choice([0.0, 0.0, 0.125]), ragged=rng.random() < 0.5, outright=rng.random() < 0.25)
     if kind == "tree":
         return _tree(B=between(1, 16), depth=rng.randint(2, 6), width=rng.randint(2, 10), V=V, dtype=dtype,
                      temperature=temperature)
