@@ -48,6 +48,9 @@ extern "C" {
 #define DYNA_ABI_VERSION 2
 #define DYNA_MAX_M 8192     /* clusters */
 #define DYNA_MAX_KT 64      /* tokens per context in top-k output */
+#define DYNA_MAX_STEPS 32   /* drafts of a verified chain */
+#define DYNA_MAX_NODES 1024 /* nodes of a verified tree, its root included */
+#define DYNA_MAX_TEACHER 1024 /* entries of a teacher's top list */
 
 typedef enum {
     DYNA_OK = 0,
@@ -368,6 +371,156 @@ int32_t dyna_cluster_budget(int32_t t, int32_t k0, int32_t k1, int32_t k_min, in
  * Returns -1 for t < 0 or k_max < 1.  The value is the n_rows a caller
  * passes to dyna_dense_head for the static head at that position. */
 int32_t dyna_static_budget(int32_t t, int32_t k_max);
+
+/* ------------------------------------------------------------------ */
+/* Verification with the target model (Algorithm 1, last step; Sec. 3  */
+/* and Sec. 5: the emitted tokens are distributed as the target's).     */
+/* ------------------------------------------------------------------ */
+
+/* Rules of both calls:
+ *  target   device, tdtype, logits of the target model: row j of request b is
+ *           V consecutive elements at b * batch_stride + j * row_stride
+ *           (strides in elements, any alignment of the element).  p_j =
+ *           softmax(row / temperature).  NaN counts as -inf (a masked token),
+ *           +inf as the largest finite number.
+ *  temperature  >= 0; 0 is greedy: a draft stands when it is the row's largest
+ *           logit (ties to the lower id), the token behind them is the largest
+ *           of its row, uniforms may be NULL, and log-probabilities are those
+ *           of softmax(row).
+ *  A draft of token x, proposed with probability q, stands when u q < p(x).
+ *  The token behind the last draft that stands is drawn by the inverse CDF in
+ *  ascending token id: the first token whose cumulative weight exceeds u times
+ *  the total, else the last one with any weight.  It is -1 where the target
+ *  allows no token (every logit -inf).
+ *  out_len [B]       device: drafts that stand
+ *  out_ids [B, n+1] or [B, N]  device: those drafts' tokens, the drawn token, -1 behind
+ *  out_logprobs      same shape, may be NULL: log p of each emitted token in
+ *                    its target row, -inf where the id is -1
+ *  ws                dyna_verify_workspace_bytes of the same sizes; it holds
+ *                    nothing between calls.  Calls that may overlap (two
+ *                    streams, two captured graphs) need one each.
+ * The rows are summed in 32 bits with 64-bit partial sums; the row a token is
+ * drawn from is read again in 64 bits. */
+
+/* One drafted position of every chain.  As a draft head writes it (SAMPLE),
+ * or tokens alone (logits NULL) for drafts proposed outright: argmax drafts,
+ * tokens looked up elsewhere. */
+typedef struct dyna_draft_step {
+    const int32_t* tokens;    /* device [B]; an id outside [0, V) ends its chain */
+    const float* logprobs;    /* device [B]: log q(token); with logits */
+    const float* logits;      /* device [B, cap] draft logits, or NULL */
+    const int32_t* clusters;  /* device [B, k]: the selected clusters, any order; NULL: logits
+                               * over the token ids [0, cap) (dyna_dense_head) */
+    int32_t k, cap;
+    int32_t shared;           /* 1: logits over the union of the B rows' clusters (DYNA_SEL_UNION) */
+    float temperature;        /* of the draft's softmax, > 0; with logits */
+    float tail_beta;          /* its tail mixture weight in [0, 1); with clusters */
+} dyna_draft_step;
+
+/* (cluster, layout row) of every token: token_rows [V, 2], device, 8-byte
+ * aligned.  Made once from a layout; dyna_verify_chain finds a token's
+ * shortlist slot with it. */
+dyna_status dyna_token_rows(const dyna_layout* L, int32_t* token_rows, hipStream_t stream);
+
+/* rows: n + 1 of a chain of n drafts, N of a tree; M: clusters of the layout
+ * (0 without one). */
+size_t dyna_verify_workspace_bytes(int32_t B, int32_t rows, int32_t V, int32_t M);
+
+/* Chains of up to n drafts.  Row i of `target` judges draft i (0-based), the
+ * row behind the last draft gives the token after it.
+ *  steps [n]         HOST array (its pointers are device pointers)
+ *  lens [B]          device, may be NULL (n): drafts of each request, clamped to [0, n]
+ *  uniforms [B, n+1] device: column i tests draft i, column n draws
+ * The first draft that falls ends the chain.  The token in its place is drawn
+ * from max(p - q, 0), q the draft's whole distribution, (1 - beta) softmax over
+ * its shortlist and beta spread over the rest; for a draft proposed outright
+ * from p without its token; from p where those leave nothing.
+ * L and token_rows may be NULL when no step has clusters; L->V == V. */
+dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32_t V, int64_t row_stride,
+                              int64_t batch_stride, int32_t B, int32_t n, const dyna_draft_step* steps,
+                              const int32_t* lens, float temperature, const dyna_layout* L,
+                              const int32_t* token_rows, const float* uniforms, int32_t* out_len,
+                              int32_t* out_ids, float* out_logprobs, void* ws, size_t ws_bytes,
+                              hipStream_t stream);
+
+/* Trees of drafts proposed outright (the beam's, dyna_beam_expand).  Node 0 is
+ * the last committed token; row j of `target` is the target's after node j.
+ *  tokens [B, N]     device; column 0 is not read
+ *  parents [N] or [B, N]  device (parent_stride 0 or N): parents[j] < j; a node
+ *                    with another parent or a token outside [0, V) is absent,
+ *                    and so are the nodes under it
+ *  uniforms [B, N]   device: column j tests node j, column 0 draws
+ *  out_nodes [B, N]  device, may be NULL: the nodes that stand, -1 behind
+ * At a node its children are tried in ascending j.  A child stands when
+ * u_j R < p(x_j), R = 1 less p of the children that fell before it; the walk
+ * goes on from it.  A token that an earlier sibling proposed falls.  Where no
+ * child stands, the token is drawn from p without the children's tokens (from
+ * p where that leaves nothing). */
+dyna_status dyna_verify_tree(const void* target, int32_t tdtype, int32_t V, int64_t row_stride,
+                             int64_t batch_stride, int32_t B, int32_t N, const int32_t* tokens,
+                             const int32_t* parents, int32_t parent_stride, float temperature,
+                             const float* uniforms, int32_t* out_len, int32_t* out_ids, float* out_logprobs,
+                             int32_t* out_nodes, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------ */
+/* Learning from the target's top tokens (Sec. 4.2, "Training the       */
+/* router": S+, the top-L tokens).                                      */
+/* ------------------------------------------------------------------ */
+
+/* A teacher's list of a row: ids [N, K] (device) and values [N, K], as
+ * dyna_dense_head's top-k_t writes them (ids, log-probabilities).  An id
+ * outside [0, V), and an id that stands earlier in its row, is no entry.
+ * weights [N]: device, may be NULL (ones): d objective / d loss of each row.  A
+ * row of weight 0 is padding: nothing of it is read, its loss and gradient are
+ * 0.  K and L up to DYNA_MAX_TEACHER. */
+
+size_t dyna_distill_workspace_bytes(int32_t N, int32_t V);
+
+/* Distillation loss of N rows of student logits, q = softmax(z / temperature):
+ *   tail 0: p = softmax(values / temperature) over the entries,
+ *           loss = sum_k p_k (log p_k - log q(i_k));
+ *   tail 1: p_k = exp(values) (log-probabilities of the teacher's whole row);
+ *           + p_r (log p_r - log q_r), p_r = max(0, 1 - sum p_k) and q_r the
+ *           student's probability outside the list.
+ *  logits         device, dtype, row r is V elements at r * row_stride, any alignment
+ *  out_loss [N]   device fp32 (not weighted)
+ *  out_stats [N, 2] device fp64, may be NULL: log sum exp(z / temperature) over all
+ *                 tokens and over those outside the list, for dyna_distill_grad
+ *                 (0 for a padding row)
+ *  grad           device, dtype, row r at r * grad_stride, may be NULL: weights[r] *
+ *                 d loss[r] / d logits[r]; elements behind a row are left as they
+ *                 were; must not overlap logits
+ * A row without entries (or with every value -inf, tail 0) has loss and
+ * gradient 0.  A masked logit (-inf) has q = 0: the loss is +inf where the
+ * teacher gives it weight, the gradient stays finite.  A NaN or +inf logit or
+ * value makes its row NaN. */
+dyna_status dyna_distill(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
+                         const int32_t* ids, const void* values, int32_t vdtype, int32_t K, int32_t tail,
+                         float temperature, const float* weights, float* out_loss, double* out_stats,
+                         void* grad, int64_t grad_stride, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* The gradient alone, from a forward call's out_stats and the same other
+ * arguments: a backward pass whose weights come later. */
+dyna_status dyna_distill_grad(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
+                              const int32_t* ids, const void* values, int32_t vdtype, int32_t K, int32_t tail,
+                              float temperature, const float* weights, const double* stats, void* grad,
+                              int64_t grad_stride, hipStream_t stream);
+
+/* The router's loss (Sec. 4.2: multi-label binary cross-entropy): y_m = 1 where
+ * a listed token lies in cluster m,
+ *   loss = sum_m pos_weight y_m softplus(-s_m) + (1 - y_m) softplus(s_m).
+ *  scores         device, dtype, row r is M elements at r * row_stride
+ *  ids [N, L]     device: the teacher's top tokens; repeats and ids outside [0, V) add nothing
+ *  cluster_of [V] device: the partition
+ *  pos_weight     > 0
+ *  out_loss [N]   device fp32 (not weighted), may be NULL with grad
+ *  grad           as above, may be NULL with out_loss.  May be `scores` itself
+ *                 (same strides); otherwise the two must not overlap.
+ * M <= DYNA_MAX_M. */
+dyna_status dyna_router_loss(const void* scores, int32_t dtype, int32_t M, int64_t row_stride, int32_t N,
+                             const int32_t* ids, int32_t L, const int32_t* cluster_of, int32_t V,
+                             float pos_weight, const float* weights, float* out_loss, void* grad,
+                             int64_t grad_stride, hipStream_t stream);
 
 /* ------------------------------------------------------------------ */
 /* Diagnostics.                                                        */

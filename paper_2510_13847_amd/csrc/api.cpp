@@ -226,7 +226,7 @@ static Carve carve(const dyna_layout* L, const dyna_router* r, int32_t B, int32_
         if (!(cond)) return set_error(DYNA_ERR_INVALID_ARG, __VA_ARGS__); \
     } while (0)
 
-static dyna_status check_layout(const dyna_layout* L) {
+dyna_status check_layout(const dyna_layout* L) {
     REQUIRE(L != nullptr, "layout is NULL");
     REQUIRE(L->V >= 1 && L->d >= 8 && L->M >= 1, "layout: bad sizes V=%d d=%d M=%d", L->V, L->d, L->M);
     REQUIRE(L->M <= L->V, "layout: M=%d > V=%d", L->M, L->V);

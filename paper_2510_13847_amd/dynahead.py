@@ -23,6 +23,7 @@ SEL_ARGMAX, SEL_TOPK, SEL_SAMPLE, SEL_UNION = 1, 2, 4, 8
 OPT_LOGITS_PATH, OPT_ROUTER_PATH, OPT_KERNEL_TIMING, OPT_GEMV_ROWS, OPT_FUSED_B1, OPT_MFMA_UNROLL = 1, 2, 3, 4, 5, 6
 OPT_GATHER_CFG, OPT_GREEDY_GRID, OPT_UNION_CFG, OPT_KMEANS_CFG, OPT_WAIT_BOUND_US = 7, 8, 9, 10, 11
 MAX_KT = 64
+MAX_STEPS, MAX_NODES, MAX_TEACHER = 32, 1024, 1024
 
 
 class DynaError(RuntimeError):
@@ -44,6 +45,12 @@ class _Router(ctypes.Structure):
                 ("b1", ctypes.c_void_p), ("W2", ctypes.c_void_p), ("b2", ctypes.c_void_p)]
 
 
+class _DraftStep(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("logprobs", ctypes.c_void_p), ("logits", ctypes.c_void_p),
+                ("clusters", ctypes.c_void_p), ("k", ctypes.c_int32), ("cap", ctypes.c_int32),
+                ("shared", ctypes.c_int32), ("temperature", ctypes.c_float), ("tail_beta", ctypes.c_float)]
+
+
 _lib = None
 ABI_VERSION = 2  # DYNA_ABI_VERSION of include/dynahead.h
 
@@ -51,6 +58,7 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _F = ctypes.c_float
 _Z = ctypes.c_size_t
+_L = ctypes.c_int64
 
 _SIGNATURES = {
     "dyna_abi_version": (_I, []),
@@ -78,6 +86,14 @@ _SIGNATURES = {
     "dyna_kmeans_update": (_I, [_P, _I, _I, _I, _P, _I, _P, _P, ctypes.c_size_t, _P]),
     "dyna_kmeans": (_I, [_P, _I, _I, _I, _I, _P, _I, _P, _P, _P, ctypes.c_size_t, _P]),
     "dyna_static_budget": (_I, [_I, _I]),
+    "dyna_token_rows": (_I, [_P, _P, _P]),
+    "dyna_verify_workspace_bytes": (_Z, [_I, _I, _I, _I]),
+    "dyna_verify_chain": (_I, [_P, _I, _I, _L, _L, _I, _I, _P, _P, _F, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dyna_verify_tree": (_I, [_P, _I, _I, _L, _L, _I, _I, _P, _P, _I, _F, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dyna_distill_workspace_bytes": (_Z, [_I, _I]),
+    "dyna_distill": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _I, _I, _F, _P, _P, _P, _P, _L, _P, _Z, _P]),
+    "dyna_distill_grad": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _I, _I, _F, _P, _P, _P, _L, _P]),
+    "dyna_router_loss": (_I, [_P, _I, _I, _L, _I, _P, _I, _P, _I, _F, _P, _P, _P, _L, _P]),
     "dyna_dense_head": (_I, [_P, _I, _I, _I, _P, _I, _I, _I, _I, _F, _P, _P, _P, _P, _P, _P, _P,
                              _Z, _P]),
 }
@@ -484,3 +500,311 @@ def kmeans(W, M: int, init_ids, iters: int, ws=None, stream=None, keep_centroids
     _check(lib().dyna_kmeans(_ptr(W), _dtype_code(W), V, d, M, _ptr(init_ids), iters, _ptr(cl), _ptr(mu),
                              _ptr(ws), ws.numel(), _stream(stream)))
     return cl, mu
+
+
+# ---------------------------------------------------------------- verification with the target model
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _typed(t, name, dtype, shape):
+    """A contiguous device tensor of this dtype and shape (None in a place of `shape`: any)."""
+    _need(t, name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+
+
+class _Launch:
+    """The device of a call's tensors, made the current one while it launches, and its stream there."""
+
+    def __init__(self, device, stream):
+        import torch
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the tensors are on {device}")
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.stream = stream
+
+    def __enter__(self):
+        import torch
+        if self.guard is not None:
+            self.guard.__enter__()
+        return (torch.cuda.current_stream() if self.stream is None else self.stream).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+@dataclass
+class DraftStep:
+    """One drafted position of B chains, as a draft head wrote it (tensors are
+    kept alive here): the sampled tokens with the log-probability of each, the
+    draft logits they were sampled from and the clusters those span.  Tokens
+    alone are drafts proposed outright (argmax drafts)."""
+    tokens: object
+    logprobs: Optional[object] = None
+    logits: Optional[object] = None
+    clusters: Optional[object] = None
+    temperature: float = 1.0
+    tail_beta: float = 0.0
+    shared: bool = False
+
+    def __post_init__(self):
+        import torch
+        _typed(self.tokens, "tokens", torch.int32, (None,))
+        B, k, cap = self.tokens.shape[0], 0, 0
+        if self.logits is not None:
+            _typed(self.logits, "logits", torch.float32, (B, None))
+            _typed(self.logprobs, "logprobs", torch.float32, (B,))
+            cap = self.logits.shape[1]
+        if self.clusters is not None:
+            _typed(self.clusters, "clusters", torch.int32, (B, None))
+            k = self.clusters.shape[1]
+        _same_device(self.tokens.device, logprobs=self.logprobs, logits=self.logits, clusters=self.clusters)
+        self.B, self.device = B, self.tokens.device
+        self._c = _DraftStep(_ptr(self.tokens), _ptr(self.logprobs), _ptr(self.logits), _ptr(self.clusters), k, cap,
+                             int(self.shared), self.temperature, self.tail_beta)
+
+    @classmethod
+    def of(cls, head) -> "DraftStep":
+        """The step a DraftHead (keep_logits, keep_clusters) or DenseHead
+        (keep_logits) holds: its sample and the distribution it came from, or
+        its best tokens, proposed outright, when it does not sample."""
+        if head.sample is None:
+            return cls(head.ids[:, 0].contiguous())
+        if head.logits is None or (isinstance(head, DraftHead) and head.clusters is None):
+            raise ValueError("a sampled step needs a head that keeps its logits and clusters")
+        if isinstance(head, DenseHead):
+            return cls(head.sample, head.sample_logprob, head.logits, temperature=head.temperature)
+        return cls(head.sample, head.sample_logprob, head.logits, head.clusters, head.temperature, head.tail_beta,
+                   bool(head.mode & SEL_UNION) and head.B > 1)
+
+
+def token_rows(layout: Layout, stream=None):
+    """dyna_token_rows -> [V, 2] int32: (cluster, layout row) of every token."""
+    import torch
+    out = torch.empty((layout.V, 2), dtype=torch.int32, device=layout.perm.device)
+    with _Launch(out.device, stream) as s:
+        _check(lib().dyna_token_rows(layout.c, _ptr(out), s))
+    return out
+
+
+def verify_workspace(B, rows, V, M=0, device="cuda"):
+    import torch
+    n = int(lib().dyna_verify_workspace_bytes(B, rows, V, M))
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+
+
+def _target_rows(target, B, rows, V):
+    if not target.is_cuda:
+        raise ValueError("target must be a device tensor")
+    if tuple(target.shape) != (B, rows, V):
+        raise ValueError(f"target must have shape {(B, rows, V)}, not {tuple(target.shape)}")
+    if V > 1 and target.stride(2) != 1:
+        raise ValueError("target's last dimension must be contiguous")
+
+
+class _Verifier:
+    def __init__(self, B, rows, V, temperature, M, device):
+        import torch
+        self.B, self.rows, self.V, self.temperature = B, rows, V, float(temperature)
+        dev = torch.empty(0, device=device).device
+        self.device = dev
+        self.lengths = torch.empty(B, dtype=torch.int32, device=dev)
+        self.ids = torch.empty((B, rows), dtype=torch.int32, device=dev)
+        self.logprobs = torch.empty((B, rows), dtype=torch.float32, device=dev)
+        self.ws = verify_workspace(B, rows, V, M, dev)
+
+    def _uniforms(self, uniforms):
+        import torch
+        if uniforms is not None:
+            _typed(uniforms, "uniforms", torch.float32, (self.B, self.rows))
+        elif self.temperature > 0.0:
+            raise ValueError("uniforms are required with a temperature above 0")
+
+
+class ChainVerifier(_Verifier):
+    """Preallocated outputs + workspace for repeated dyna_verify_chain calls:
+    lengths [B], ids and logprobs [B, n + 1].  temperature 0 is greedy; layout
+    is that of the draft heads whose logits span clusters."""
+
+    def __init__(self, B: int, n: int, V: int, temperature: float = 1.0, layout: Optional[Layout] = None,
+                 device="cuda"):
+        super().__init__(B, n + 1, V, temperature, layout.M if layout is not None else 0, device)
+        self.n, self.layout = n, layout
+        self.token_rows = token_rows(layout) if layout is not None else None
+        self._steps = (_DraftStep * max(n, 1))()
+
+    def __call__(self, target, steps, uniforms=None, lens=None, stream=None):
+        """target [B, n + 1, V] logits, steps: n DraftSteps, uniforms [B, n + 1],
+        lens [B] int32 (drafts of each request)."""
+        import torch
+        _target_rows(target, self.B, self.rows, self.V)
+        self._uniforms(uniforms)
+        if lens is not None:
+            _typed(lens, "lens", torch.int32, (self.B,))
+        if len(steps) != self.n:
+            raise ValueError(f"{len(steps)} steps, not {self.n}")
+        for i, s in enumerate(steps):
+            if s.B != self.B:
+                raise ValueError(f"step {i} has {s.B} rows, not {self.B}")
+            if s.device != self.device:
+                raise ValueError(f"step {i} is on {s.device}, not on {self.device}")
+            if s.clusters is not None and self.layout is None:
+                raise ValueError(f"step {i} has clusters: the verifier needs their layout")
+            self._steps[i] = s._c
+        _same_device(self.device, target=target, uniforms=uniforms, lens=lens)
+        L = self.layout
+        with _Launch(self.device, stream) as s:
+            _check(lib().dyna_verify_chain(_ptr(target), _dtype_code(target), self.V, target.stride(1),
+                                           target.stride(0), self.B, self.n, self._steps, _ptr(lens),
+                                           self.temperature, L.c if L is not None else None, _ptr(self.token_rows),
+                                           _ptr(uniforms), _ptr(self.lengths), _ptr(self.ids), _ptr(self.logprobs),
+                                           _ptr(self.ws), self.ws.numel(), s))
+        return self
+
+
+class TreeVerifier(_Verifier):
+    """Preallocated outputs + workspace for repeated dyna_verify_tree calls:
+    lengths [B]; ids, logprobs and nodes [B, N]."""
+
+    def __init__(self, B: int, N: int, V: int, temperature: float = 1.0, device="cuda"):
+        import torch
+        super().__init__(B, N, V, temperature, 0, device)
+        self.N = N
+        self.nodes = torch.empty((B, N), dtype=torch.int32, device=self.device)
+
+    def __call__(self, target, tokens, parents, uniforms=None, stream=None):
+        """target [B, N, V] logits, tokens [B, N], parents [N] or [B, N], uniforms [B, N]."""
+        import torch
+        _target_rows(target, self.B, self.N, self.V)
+        self._uniforms(uniforms)
+        _typed(tokens, "tokens", torch.int32, (self.B, self.N))
+        _typed(parents, "parents", torch.int32, (self.N,) if parents.dim() == 1 else (self.B, self.N))
+        _same_device(self.device, target=target, tokens=tokens, parents=parents, uniforms=uniforms)
+        with _Launch(self.device, stream) as s:
+            _check(lib().dyna_verify_tree(_ptr(target), _dtype_code(target), self.V, target.stride(1),
+                                          target.stride(0), self.B, self.N, _ptr(tokens), _ptr(parents),
+                                          0 if parents.dim() == 1 else self.N, self.temperature, _ptr(uniforms),
+                                          _ptr(self.lengths), _ptr(self.ids), _ptr(self.logprobs), _ptr(self.nodes),
+                                          _ptr(self.ws), self.ws.numel(), s))
+        return self
+
+
+def verify_chain(target, steps, uniforms=None, lens=None, temperature=1.0, layout=None, stream=None):
+    """One dyna_verify_chain call with fresh outputs (see ChainVerifier for repeated calls)."""
+    v = ChainVerifier(target.shape[0], len(steps), target.shape[2], temperature, layout, target.device)
+    return v(target, steps, uniforms, lens, stream)
+
+
+def verify_tree(target, tokens, parents, uniforms=None, temperature=1.0, stream=None):
+    """One dyna_verify_tree call with fresh outputs (see TreeVerifier for repeated calls)."""
+    v = TreeVerifier(target.shape[0], target.shape[1], target.shape[2], temperature, target.device)
+    return v(target, tokens, parents, uniforms, stream)
+
+
+# ---------------------------------------------------------------- learning from the target's top tokens
+def _matrix(t, name):
+    """A [rows, cols] device tensor with contiguous rows -> (dtype code, row stride)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    return _dtype_code(t), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _grad_like(out, t, name="out"):
+    import torch
+    if out is None:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    if out.shape != t.shape or out.dtype != t.dtype:
+        raise ValueError(f"{name} must have the shape and dtype of its input")
+    return out
+
+
+def distill_workspace(N: int, V: int, device="cuda"):
+    import torch
+    return torch.empty(max(int(lib().dyna_distill_workspace_bytes(N, V)), 1), dtype=torch.uint8, device=device)
+
+
+def _teacher_list(t, ids, values, weights):
+    import torch
+    N = t.shape[0]
+    _typed(ids, "ids", torch.int32, (N, None))
+    if values is not None:
+        _need(values, "values")
+        if values.shape != ids.shape:
+            raise ValueError("ids and values must have one shape")
+    if weights is not None:
+        _typed(weights, "weights", torch.float32, (N,))
+    _same_device(t.device, ids=ids, values=values, weights=weights)
+
+
+def distill(logits, ids, values, temperature=1.0, tail=False, weights=None, want_grad=True, want_stats=False,
+            out=None, ws=None, stream=None):
+    """dyna_distill -> (loss [N], stats [N, 2] or None, grad [N, V] or None).
+
+    logits [N, V]: the student's; ids, values [N, K]: the teacher's top list, as
+    DenseHead's top-k_t writes it; weights [N]: d objective / d loss of each row
+    (0: padding).  grad is weights * d loss / d logits: the training loop passes
+    it on with ``logits.backward(grad)``.  out: an existing gradient to write."""
+    import torch
+    code, stride = _matrix(logits, "logits")
+    _teacher_list(logits, ids, values, weights)
+    N, V = logits.shape
+    dev = logits.device
+    with _Launch(dev, stream) as s, torch.cuda.stream(stream):
+        loss = torch.empty(N, dtype=torch.float32, device=dev)
+        stats = torch.empty((N, 2), dtype=torch.float64, device=dev) if want_stats else None
+        grad = _grad_like(out, logits) if want_grad else None
+        gstride = _matrix(grad, "out")[1] if want_grad else V
+        ws = distill_workspace(N, V, dev) if ws is None else ws
+        _same_device(dev, out=grad, ws=ws)
+        _check(lib().dyna_distill(_ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values), _dtype_code(values),
+                                  ids.shape[1], int(tail), temperature, _ptr(weights), _ptr(loss), _ptr(stats),
+                                  _ptr(grad), gstride, _ptr(ws), ws.numel(), s))
+    return loss, stats, grad
+
+
+def distill_grad(logits, stats, ids, values, temperature=1.0, tail=False, weights=None, out=None, stream=None):
+    """dyna_distill_grad -> grad [N, V], from the stats of an earlier distill call."""
+    import torch
+    code, stride = _matrix(logits, "logits")
+    _teacher_list(logits, ids, values, weights)
+    N, V = logits.shape
+    _typed(stats, "stats", torch.float64, (N, 2))
+    with _Launch(logits.device, stream) as s, torch.cuda.stream(stream):
+        grad = _grad_like(out, logits)
+        _same_device(logits.device, stats=stats, out=grad)
+        _check(lib().dyna_distill_grad(_ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values), _dtype_code(values),
+                                       ids.shape[1], int(tail), temperature, _ptr(weights), _ptr(stats), _ptr(grad),
+                                       _matrix(grad, "out")[1], s))
+    return grad
+
+
+def router_loss(scores, ids, cluster_of, pos_weight=1.0, weights=None, want_grad=True, out=None, stream=None):
+    """dyna_router_loss -> (loss [N], grad [N, M] or None).
+
+    scores [N, M]: the router's; ids [N, L]: the teacher's top tokens, whose
+    clusters are the labels; grad as in distill (out may be `scores` itself)."""
+    import torch
+    code, stride = _matrix(scores, "scores")
+    _teacher_list(scores, ids, None, weights)
+    _typed(cluster_of, "cluster_of", torch.int32, (None,))
+    N, M = scores.shape
+    dev = scores.device
+    with _Launch(dev, stream) as s, torch.cuda.stream(stream):
+        loss = torch.empty(N, dtype=torch.float32, device=dev)
+        grad = _grad_like(out, scores) if want_grad else None
+        gstride = _matrix(grad, "out")[1] if want_grad else M
+        _same_device(dev, cluster_of=cluster_of, out=grad)
+        _check(lib().dyna_router_loss(_ptr(scores), code, M, stride, N, _ptr(ids), ids.shape[1], _ptr(cluster_of),
+                                      cluster_of.numel(), pos_weight, _ptr(weights), _ptr(loss), _ptr(grad), gstride,
+                                      s))
+    return loss, grad
