@@ -503,40 +503,42 @@ def kmeans(W, M: int, init_ids, iters: int, ws=None, stream=None, keep_centroids
 
 
 # ---------------------------------------------------------------- verification with the target model
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
-
-
-def _typed(t, name, dtype, shape):
-    """A contiguous device tensor of this dtype and shape (None in a place of `shape`: any)."""
-    _need(t, name)
-    if t.dtype != dtype:
+def _typed(t, name, dtype, shape, device):
+    """A contiguous tensor of this dtype, shape and device."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
 
 
-class _Launch:
-    """The device of a call's tensors, made the current one while it launches, and its stream there."""
+def _dims(t, name, n):
+    _need(t, name, contiguous=False)
+    if t.dim() != n:
+        raise ValueError(f"{name} must have {n} dimension{'s' if n > 1 else ''}")
+    return t.shape
 
-    def __init__(self, device, stream):
-        import torch
-        if stream is not None and stream.device != device:
-            raise ValueError(f"stream is on {stream.device}, the tensors are on {device}")
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.stream = stream
 
-    def __enter__(self):
-        import torch
-        if self.guard is not None:
-            self.guard.__enter__()
-        return (torch.cuda.current_stream() if self.stream is None else self.stream).cuda_stream
+def _stream_device(stream, device):
+    if stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, the tensors are on {device}")
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+
+def _launch(device, call, *args):
+    """call(*args, stream) on the device of its tensors (made the current one for
+    the time of the call) and that device's current stream."""
+    import torch
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if device.index == torch._C._cuda_getDevice():
+        _check(call(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, stream))
 
 
 @dataclass
@@ -555,17 +557,17 @@ class DraftStep:
 
     def __post_init__(self):
         import torch
-        _typed(self.tokens, "tokens", torch.int32, (None,))
-        B, k, cap = self.tokens.shape[0], 0, 0
+        (B,), dev, k, cap = _dims(self.tokens, "tokens", 1), self.tokens.device, 0, 0
+        _typed(self.tokens, "tokens", torch.int32, (B,), dev)
         if self.logits is not None:
-            _typed(self.logits, "logits", torch.float32, (B, None))
-            _typed(self.logprobs, "logprobs", torch.float32, (B,))
-            cap = self.logits.shape[1]
+            cap = _dims(self.logits, "logits", 2)[1]
+            _typed(self.logits, "logits", torch.float32, (B, cap), dev)
+            _need(self.logprobs, "logprobs")
+            _typed(self.logprobs, "logprobs", torch.float32, (B,), dev)
         if self.clusters is not None:
-            _typed(self.clusters, "clusters", torch.int32, (B, None))
-            k = self.clusters.shape[1]
-        _same_device(self.tokens.device, logprobs=self.logprobs, logits=self.logits, clusters=self.clusters)
-        self.B, self.device = B, self.tokens.device
+            k = _dims(self.clusters, "clusters", 2)[1]
+            _typed(self.clusters, "clusters", torch.int32, (B, k), dev)
+        self.B, self.device = B, dev
         self._c = _DraftStep(_ptr(self.tokens), _ptr(self.logprobs), _ptr(self.logits), _ptr(self.clusters), k, cap,
                              int(self.shared), self.temperature, self.tail_beta)
 
@@ -587,9 +589,12 @@ class DraftStep:
 def token_rows(layout: Layout, stream=None):
     """dyna_token_rows -> [V, 2] int32: (cluster, layout row) of every token."""
     import torch
+    if stream is not None:
+        _stream_device(stream, layout.perm.device)
+        with torch.cuda.stream(stream):
+            return token_rows(layout)
     out = torch.empty((layout.V, 2), dtype=torch.int32, device=layout.perm.device)
-    with _Launch(out.device, stream) as s:
-        _check(lib().dyna_token_rows(layout.c, _ptr(out), s))
+    _launch(out.device, lib().dyna_token_rows, layout.c, _ptr(out))
     return out
 
 
@@ -597,15 +602,6 @@ def verify_workspace(B, rows, V, M=0, device="cuda"):
     import torch
     n = int(lib().dyna_verify_workspace_bytes(B, rows, V, M))
     return torch.empty(max(n, 1), dtype=torch.uint8, device=device)
-
-
-def _target_rows(target, B, rows, V):
-    if not target.is_cuda:
-        raise ValueError("target must be a device tensor")
-    if tuple(target.shape) != (B, rows, V):
-        raise ValueError(f"target must have shape {(B, rows, V)}, not {tuple(target.shape)}")
-    if V > 1 and target.stride(2) != 1:
-        raise ValueError("target's last dimension must be contiguous")
 
 
 class _Verifier:
@@ -619,12 +615,23 @@ class _Verifier:
         self.logprobs = torch.empty((B, rows), dtype=torch.float32, device=dev)
         self.ws = verify_workspace(B, rows, V, M, dev)
 
-    def _uniforms(self, uniforms):
+    def _inputs(self, target, uniforms):
+        """The target's dtype code and strides, after the checks both forms share."""
         import torch
+        if not target.is_cuda:
+            raise ValueError("target must be a device tensor")
+        if target.device != self.device:
+            raise ValueError(f"target is on {target.device}, not on {self.device}")
+        if target.shape != (self.B, self.rows, self.V):
+            raise ValueError(f"target must have shape {(self.B, self.rows, self.V)}, not {tuple(target.shape)}")
+        batch, row, one = target.stride()
+        if one != 1 and self.V > 1:
+            raise ValueError("target's last dimension must be contiguous")
         if uniforms is not None:
-            _typed(uniforms, "uniforms", torch.float32, (self.B, self.rows))
+            _typed(uniforms, "uniforms", torch.float32, (self.B, self.rows), self.device)
         elif self.temperature > 0.0:
             raise ValueError("uniforms are required with a temperature above 0")
+        return _dtype_code(target), row, batch
 
 
 class ChainVerifier(_Verifier):
@@ -638,15 +645,20 @@ class ChainVerifier(_Verifier):
         self.n, self.layout = n, layout
         self.token_rows = token_rows(layout) if layout is not None else None
         self._steps = (_DraftStep * max(n, 1))()
+        self._fixed = (layout.c if layout is not None else None, _ptr(self.token_rows), _ptr(self.lengths),
+                       _ptr(self.ids), _ptr(self.logprobs), _ptr(self.ws), self.ws.numel())
 
     def __call__(self, target, steps, uniforms=None, lens=None, stream=None):
         """target [B, n + 1, V] logits, steps: n DraftSteps, uniforms [B, n + 1],
         lens [B] int32 (drafts of each request)."""
         import torch
-        _target_rows(target, self.B, self.rows, self.V)
-        self._uniforms(uniforms)
+        if stream is not None:
+            _stream_device(stream, self.device)
+            with torch.cuda.stream(stream):
+                return self(target, steps, uniforms, lens)
+        code, row, batch = self._inputs(target, uniforms)
         if lens is not None:
-            _typed(lens, "lens", torch.int32, (self.B,))
+            _typed(lens, "lens", torch.int32, (self.B,), self.device)
         if len(steps) != self.n:
             raise ValueError(f"{len(steps)} steps, not {self.n}")
         for i, s in enumerate(steps):
@@ -657,14 +669,8 @@ class ChainVerifier(_Verifier):
             if s.clusters is not None and self.layout is None:
                 raise ValueError(f"step {i} has clusters: the verifier needs their layout")
             self._steps[i] = s._c
-        _same_device(self.device, target=target, uniforms=uniforms, lens=lens)
-        L = self.layout
-        with _Launch(self.device, stream) as s:
-            _check(lib().dyna_verify_chain(_ptr(target), _dtype_code(target), self.V, target.stride(1),
-                                           target.stride(0), self.B, self.n, self._steps, _ptr(lens),
-                                           self.temperature, L.c if L is not None else None, _ptr(self.token_rows),
-                                           _ptr(uniforms), _ptr(self.lengths), _ptr(self.ids), _ptr(self.logprobs),
-                                           _ptr(self.ws), self.ws.numel(), s))
+        _launch(self.device, lib().dyna_verify_chain, _ptr(target), code, self.V, row, batch, self.B, self.n,
+                self._steps, _ptr(lens), self.temperature, *self._fixed[:2], _ptr(uniforms), *self._fixed[2:])
         return self
 
 
@@ -677,21 +683,22 @@ class TreeVerifier(_Verifier):
         super().__init__(B, N, V, temperature, 0, device)
         self.N = N
         self.nodes = torch.empty((B, N), dtype=torch.int32, device=self.device)
+        self._fixed = (_ptr(self.lengths), _ptr(self.ids), _ptr(self.logprobs), _ptr(self.nodes), _ptr(self.ws),
+                       self.ws.numel())
 
     def __call__(self, target, tokens, parents, uniforms=None, stream=None):
         """target [B, N, V] logits, tokens [B, N], parents [N] or [B, N], uniforms [B, N]."""
         import torch
-        _target_rows(target, self.B, self.N, self.V)
-        self._uniforms(uniforms)
-        _typed(tokens, "tokens", torch.int32, (self.B, self.N))
-        _typed(parents, "parents", torch.int32, (self.N,) if parents.dim() == 1 else (self.B, self.N))
-        _same_device(self.device, target=target, tokens=tokens, parents=parents, uniforms=uniforms)
-        with _Launch(self.device, stream) as s:
-            _check(lib().dyna_verify_tree(_ptr(target), _dtype_code(target), self.V, target.stride(1),
-                                          target.stride(0), self.B, self.N, _ptr(tokens), _ptr(parents),
-                                          0 if parents.dim() == 1 else self.N, self.temperature, _ptr(uniforms),
-                                          _ptr(self.lengths), _ptr(self.ids), _ptr(self.logprobs), _ptr(self.nodes),
-                                          _ptr(self.ws), self.ws.numel(), s))
+        if stream is not None:
+            _stream_device(stream, self.device)
+            with torch.cuda.stream(stream):
+                return self(target, tokens, parents, uniforms)
+        code, row, batch = self._inputs(target, uniforms)
+        _typed(tokens, "tokens", torch.int32, (self.B, self.N), self.device)
+        shared = parents.dim() == 1
+        _typed(parents, "parents", torch.int32, (self.N,) if shared else (self.B, self.N), self.device)
+        _launch(self.device, lib().dyna_verify_tree, _ptr(target), code, self.V, row, batch, self.B, self.N,
+                _ptr(tokens), _ptr(parents), 0 if shared else self.N, self.temperature, _ptr(uniforms), *self._fixed)
         return self
 
 
@@ -719,13 +726,17 @@ def _matrix(t, name):
     return _dtype_code(t), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
 
 
-def _grad_like(out, t, name="out"):
+def _gradient(out, t):
+    """The gradient to write (a fresh one without `out`) and its row stride."""
     import torch
     if out is None:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device), t.shape[1]
     if out.shape != t.shape or out.dtype != t.dtype:
-        raise ValueError(f"{name} must have the shape and dtype of its input")
-    return out
+        raise ValueError("out must have the shape and dtype of its input")
+    stride = _matrix(out, "out")[1]
+    if out.device != t.device:
+        raise ValueError(f"out is on {out.device}, not on {t.device}")
+    return out, stride
 
 
 def distill_workspace(N: int, V: int, device="cuda"):
@@ -734,16 +745,16 @@ def distill_workspace(N: int, V: int, device="cuda"):
 
 
 def _teacher_list(t, ids, values, weights):
+    """Checks a teacher's list against rows t -> entries of each row."""
     import torch
-    N = t.shape[0]
-    _typed(ids, "ids", torch.int32, (N, None))
+    N, dev = t.shape[0], t.device
+    K = _dims(ids, "ids", 2)[1]
+    _typed(ids, "ids", torch.int32, (N, K), dev)
     if values is not None:
-        _need(values, "values")
-        if values.shape != ids.shape:
-            raise ValueError("ids and values must have one shape")
+        _typed(values, "values", torch.bfloat16 if values.dtype is torch.bfloat16 else torch.float32, (N, K), dev)
     if weights is not None:
-        _typed(weights, "weights", torch.float32, (N,))
-    _same_device(t.device, ids=ids, values=values, weights=weights)
+        _typed(weights, "weights", torch.float32, (N,), dev)
+    return K
 
 
 def distill(logits, ids, values, temperature=1.0, tail=False, weights=None, want_grad=True, want_stats=False,
@@ -755,36 +766,42 @@ def distill(logits, ids, values, temperature=1.0, tail=False, weights=None, want
     (0: padding).  grad is weights * d loss / d logits: the training loop passes
     it on with ``logits.backward(grad)``.  out: an existing gradient to write."""
     import torch
-    code, stride = _matrix(logits, "logits")
-    _teacher_list(logits, ids, values, weights)
-    N, V = logits.shape
     dev = logits.device
-    with _Launch(dev, stream) as s, torch.cuda.stream(stream):
-        loss = torch.empty(N, dtype=torch.float32, device=dev)
-        stats = torch.empty((N, 2), dtype=torch.float64, device=dev) if want_stats else None
-        grad = _grad_like(out, logits) if want_grad else None
-        gstride = _matrix(grad, "out")[1] if want_grad else V
-        ws = distill_workspace(N, V, dev) if ws is None else ws
-        _same_device(dev, out=grad, ws=ws)
-        _check(lib().dyna_distill(_ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values), _dtype_code(values),
-                                  ids.shape[1], int(tail), temperature, _ptr(weights), _ptr(loss), _ptr(stats),
-                                  _ptr(grad), gstride, _ptr(ws), ws.numel(), s))
+    if stream is not None:
+        _stream_device(stream, dev)
+        with torch.cuda.stream(stream):
+            return distill(logits, ids, values, temperature, tail, weights, want_grad, want_stats, out, ws)
+    code, stride = _matrix(logits, "logits")
+    K = _teacher_list(logits, ids, values, weights)
+    N, V = logits.shape
+    loss = torch.empty(N, dtype=torch.float32, device=dev)
+    stats = torch.empty((N, 2), dtype=torch.float64, device=dev) if want_stats else None
+    grad, gstride = _gradient(out, logits) if want_grad else (None, V)
+    if ws is None:
+        ws = distill_workspace(N, V, dev)
+    elif ws.device != dev:
+        raise ValueError(f"ws is on {ws.device}, not on {dev}")
+    _launch(dev, lib().dyna_distill, _ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values), _dtype_code(values),
+            K, int(tail), temperature, _ptr(weights), _ptr(loss), _ptr(stats), _ptr(grad), gstride, _ptr(ws),
+            ws.numel())
     return loss, stats, grad
 
 
 def distill_grad(logits, stats, ids, values, temperature=1.0, tail=False, weights=None, out=None, stream=None):
     """dyna_distill_grad -> grad [N, V], from the stats of an earlier distill call."""
     import torch
+    dev = logits.device
+    if stream is not None:
+        _stream_device(stream, dev)
+        with torch.cuda.stream(stream):
+            return distill_grad(logits, stats, ids, values, temperature, tail, weights, out)
     code, stride = _matrix(logits, "logits")
-    _teacher_list(logits, ids, values, weights)
+    K = _teacher_list(logits, ids, values, weights)
     N, V = logits.shape
-    _typed(stats, "stats", torch.float64, (N, 2))
-    with _Launch(logits.device, stream) as s, torch.cuda.stream(stream):
-        grad = _grad_like(out, logits)
-        _same_device(logits.device, stats=stats, out=grad)
-        _check(lib().dyna_distill_grad(_ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values), _dtype_code(values),
-                                       ids.shape[1], int(tail), temperature, _ptr(weights), _ptr(stats), _ptr(grad),
-                                       _matrix(grad, "out")[1], s))
+    _typed(stats, "stats", torch.float64, (N, 2), dev)
+    grad, gstride = _gradient(out, logits)
+    _launch(dev, lib().dyna_distill_grad, _ptr(logits), code, V, stride, N, _ptr(ids), _ptr(values),
+            _dtype_code(values), K, int(tail), temperature, _ptr(weights), _ptr(stats), _ptr(grad), gstride)
     return grad
 
 
@@ -794,17 +811,18 @@ def router_loss(scores, ids, cluster_of, pos_weight=1.0, weights=None, want_grad
     scores [N, M]: the router's; ids [N, L]: the teacher's top tokens, whose
     clusters are the labels; grad as in distill (out may be `scores` itself)."""
     import torch
-    code, stride = _matrix(scores, "scores")
-    _teacher_list(scores, ids, None, weights)
-    _typed(cluster_of, "cluster_of", torch.int32, (None,))
-    N, M = scores.shape
     dev = scores.device
-    with _Launch(dev, stream) as s, torch.cuda.stream(stream):
-        loss = torch.empty(N, dtype=torch.float32, device=dev)
-        grad = _grad_like(out, scores) if want_grad else None
-        gstride = _matrix(grad, "out")[1] if want_grad else M
-        _same_device(dev, cluster_of=cluster_of, out=grad)
-        _check(lib().dyna_router_loss(_ptr(scores), code, M, stride, N, _ptr(ids), ids.shape[1], _ptr(cluster_of),
-                                      cluster_of.numel(), pos_weight, _ptr(weights), _ptr(loss), _ptr(grad), gstride,
-                                      s))
+    if stream is not None:
+        _stream_device(stream, dev)
+        with torch.cuda.stream(stream):
+            return router_loss(scores, ids, cluster_of, pos_weight, weights, want_grad, out)
+    code, stride = _matrix(scores, "scores")
+    L = _teacher_list(scores, ids, None, weights)
+    V = _dims(cluster_of, "cluster_of", 1)[0]
+    _typed(cluster_of, "cluster_of", torch.int32, (V,), dev)
+    N, M = scores.shape
+    loss = torch.empty(N, dtype=torch.float32, device=dev)
+    grad, gstride = _gradient(out, scores) if want_grad else (None, M)
+    _launch(dev, lib().dyna_router_loss, _ptr(scores), code, M, stride, N, _ptr(ids), L, _ptr(cluster_of), V,
+            pos_weight, _ptr(weights), _ptr(loss), _ptr(grad), gstride)
     return loss, grad
