@@ -50,6 +50,16 @@ struct Row8<float> {
 __device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    __asm__("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// Largest of eight; NaN operands give way to the others.
+__device__ __forceinline__ float max8(const float (&x)[8]) {
+    return max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+}
+
 // x[0..8) = p[0..n), `fill` past n.
 template <typename T>
 __device__ __forceinline__ void load_part(const T* p, int n, float fill, float (&x)[8]) {
@@ -100,21 +110,31 @@ __device__ __forceinline__ void store_part(T* p, int n, const float (&x)[8]) {
 __device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, kNegInf), kF32Max); }
 
 // ---------------------------------------------------------------- reductions
-// Sum of a double over the wave, the same value on every lane (fixed order).
-__device__ __forceinline__ double wave_sum_f64(double x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-    return x;
+// Inclusive sum over the wave's lanes, in the fixed order of DPP row shifts and
+// broadcasts.
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ double dpp_f64(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint64_t lo = dpp<CTRL, ROW_MASK>(0u, (uint32_t)u), hi = dpp<CTRL, ROW_MASK>(0u, (uint32_t)(u >> 32));
+    return __builtin_bit_cast(double, (hi << 32) | lo);
 }
 __device__ __forceinline__ double wave_scan_f64(double x) {
-    const int lane = lane_id();
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const double y = __shfl_up(x, o, kWave);
-        if (lane >= o) x += y;
-    }
+    x += dpp_f64<kRowShr1, 0xf>(x);
+    x += dpp_f64<kRowShr2, 0xf>(x);
+    x += dpp_f64<kRowShr4, 0xf>(x);
+    x += dpp_f64<kRowShr8, 0xf>(x);
+    x += dpp_f64<kRowBcast15, 0xa>(x);
+    x += dpp_f64<kRowBcast31, 0xc>(x);
     return x;
 }
+__device__ __forceinline__ double readlane_f64(double x, int l) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint64_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, l);
+    const uint64_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+    return __builtin_bit_cast(double, (hi << 32) | lo);
+}
+// Sum over the wave, the same value on every lane.
+__device__ __forceinline__ double wave_sum_f64(double x) { return readlane_f64(wave_scan_f64(x), kWave - 1); }
 __device__ __forceinline__ float wave_max_all(float x) {
     return readlane_f32(wave_max_f32(x), kWave - 1);
 }
@@ -160,9 +180,44 @@ __device__ __forceinline__ double block_scan_f64(double x, double* tmp, double* 
     return base + (inc - x);
 }
 
-// exp((z - m) * inv_t), 0 for a masked z; m is finite wherever a z is.
-__device__ __forceinline__ double weight_f64(float z, float m, double inv_t) {
-    return z > kNegInf ? exp(((double)z - (double)m) * inv_t) : 0.0;
+// ---------------------------------------------------------------- weights in 64 bits
+// exp((z - m) / T) for whole rows in 64 bits, where the device's fp64 rate is
+// the bound: 2^(y / 16) with y = (z - m) 16 log2(e) / T split into a whole
+// number and f in [-1/2, 1/2]; 2^(f / 16) by its Taylor series to the sixth
+// power (its remainder is below 2^-51), 2^(j / 16) from a table of 16 in LDS,
+// which the 64 lanes read without bank conflicts.  15 fp64 instructions where
+// the library's exp takes about 30.
+struct Weigher {
+    const double* table;  // LDS [16]
+    double c;             // 16 log2(e) / T
+    __device__ __forceinline__ double operator()(float z, float m) const {
+        // a masked z (or a chunk without any) gives 2^-1100, which is 0
+        double y = fmax(((double)z - (double)m) * c, -17600.0);
+        const double magic = 0x1.8p52;
+        const double t = y + magic;
+        const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+        const double f = y - (t - magic);
+        constexpr double L = 0.69314718055994530942 / 16.0;
+        double p = L * L * L * L * L * L / 720.0;
+        p = fma(p, f, L * L * L * L * L / 120.0);
+        p = fma(p, f, L * L * L * L / 24.0);
+        p = fma(p, f, L * L * L / 6.0);
+        p = fma(p, f, L * L / 2.0);
+        p = fma(p, f, L);
+        p = fma(p, f, 1.0);
+        return ldexp(p * table[k & 15], k >> 4);
+    }
+};
+constexpr double k16Log2e = 16.0 * 1.4426950408889634074;
+
+// Fills the table by the first lanes of a workgroup, or of every wave with a
+// table of its own; a barrier, or the wave's LDS order, has to follow.
+__device__ __forceinline__ void fill_weight_table(double* table) {
+    if (threadIdx.x < 16) table[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+}
+__device__ __forceinline__ void fill_wave_table(double* table) {
+    if (lane_id() < 16) table[lane_id()] = exp2((double)lane_id() / 16.0);
+    wave_lds_order();
 }
 
 }  // namespace dyna

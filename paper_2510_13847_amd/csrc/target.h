@@ -6,7 +6,8 @@
 
 namespace dyna {
 
-constexpr int kChunk = 2048;  // vocabulary entries of a draw's work item: 256 threads of 8
+constexpr int kChunk = 512;       // vocabulary entries of a draw's work item: a wave's 64 lanes of 8
+constexpr int kPartStep = 2048;  // rows are cut in steps of 256 threads of 8
 
 // Where a request's walk ended.
 struct WalkEnd {
@@ -33,11 +34,11 @@ struct ChunkPart {
     float pad;
 };
 
-// The rejected draft's own distribution.
+// Softmax pieces of kChunk slots of the rejected draft's own row.
 struct DraftPart {
-    double s;     // sum of exp((z - m) / T_draft) over the shortlist
+    double s;     // sum of exp((z - m) / T_draft)
     float m;
-    int32_t len;  // shortlist length
+    int32_t len;  // the row's shortlist length
 };
 
 struct StepTable {
@@ -60,6 +61,7 @@ struct VerifyArgs {
     const int32_t* lens;     // [B] or nullptr
     // layout of the shortlists (nullptr: no step has one)
     const int32_t* offsets;
+    const int32_t* perm;
     const int32_t* token_rows;
     int32_t M;
     double inv_t;            // 1 / temperature (greedy: 1)
@@ -74,15 +76,30 @@ struct VerifyArgs {
     WalkEnd* ends;           // [B]
     int32_t n_chunks;
     ChunkPart* chunks;       // [B, n_chunks]
-    double* left;            // [B, n_chunks] residual mass
-    DraftPart* drafts;       // [B]
+    double* left;            // [B, n_chunks] what the drafts leave of a chunk's p
+    int32_t n_pieces;
+    DraftPart* pieces;       // [B, n_pieces]
     int32_t* slot_of;        // [B, M] first slot less first layout row of a selected cluster
 };
 
 size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a, void* ws);
+// What a call's steps need of the drawing kernels.
+struct DrawNeeds {
+    int32_t pieces = 0;    // kChunk slots of the longest draft row; 0: no step has draft logits
+    int32_t entries = 0;   // most clusters a step's list can name, among the steps that `listed` holds for
+    bool streamed = false; // a step whose chunks are read again (not `listed`)
+};
+// A step whose shortlist is short enough for one workgroup to go through, and
+// without a tail mixture, so that tokens off it keep their p.
+constexpr int kListedSlots = 32768, kListedClusters = 2048;
+__host__ __device__ inline bool step_listed(const dyna_draft_step& d, int32_t B, int32_t M) {
+    const int64_t named = (int64_t)(d.shared ? B : 1) * d.k;
+    return d.clusters != nullptr && d.tail_beta == 0.0f && d.cap <= kListedSlots &&
+           (named < M ? named : M) <= kListedClusters;
+}
 dyna_status launch_token_rows(const int32_t* perm, const int32_t* offsets, int32_t V, int32_t M, int32_t* token_rows,
                               hipStream_t stream);
-dyna_status launch_verify(const VerifyArgs& a, const StepTable& steps, bool residual, hipStream_t stream);
+dyna_status launch_verify(const VerifyArgs& a, const StepTable& steps, const DrawNeeds& needs, hipStream_t stream);
 
 // Softmax pieces of a part of a student's row, the listed tokens left out.
 struct RestPart {

@@ -10,7 +10,7 @@
 namespace dyna {
 namespace {
 
-constexpr int32_t kMaxVocab = 1 << 22;
+constexpr int32_t kMaxVocab = 1 << 21;
 constexpr int64_t kMaxBlocks = 1 << 23;  // workgroups of 256 threads in one launch: below 2^32 threads
 
 bool valid_dtype(int32_t t) { return t == DYNA_F32 || t == DYNA_BF16; }
@@ -56,8 +56,8 @@ dyna_status check_verify_sizes(int32_t tdtype, int32_t V, int32_t B, int32_t row
     REQUIRE(V >= 1, "V=%d < 1", V);
     if (V > kMaxVocab) return set_error(DYNA_ERR_UNSUPPORTED, "V=%d > %d", V, kMaxVocab);
     REQUIRE(B >= 0, "B=%d < 0", B);
-    const int64_t chunks = (V + kChunk - 1) / kChunk;
-    if ((int64_t)B * rows * chunks > kMaxBlocks)
+    const int64_t steps = (V + kPartStep - 1) / kPartStep, chunks = (V + kChunk - 1) / kChunk;
+    if ((int64_t)B * rows * steps > kMaxBlocks || (int64_t)B * chunks > kMaxBlocks)
         return set_error(DYNA_ERR_UNSUPPORTED, "%d requests of %d rows of %d logits in one call", B, rows, V);
     return DYNA_OK;
 }
@@ -122,7 +122,8 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
     REQUIRE(n == 0 || steps != nullptr, "steps is NULL");
     REQUIRE(out_len && out_ids && ws && aligned_to(ws, 256), "NULL argument or ws not 256-byte aligned");
     StepTable table{};
-    bool residual = false, clusters = false;
+    DrawNeeds needs{};
+    bool clusters = false;
     for (int i = 0; i < n; ++i) {
         const dyna_draft_step& d = steps[i];
         REQUIRE(d.tokens != nullptr, "step %d: tokens is NULL", i);
@@ -131,8 +132,9 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
         REQUIRE(d.logprobs != nullptr, "step %d: logprobs is NULL", i);
         REQUIRE(d.temperature > 0.0f && d.temperature < 3.0e38f, "step %d: temperature must be positive and finite", i);
         REQUIRE(d.cap >= 0, "step %d: cap=%d", i, d.cap);
-        residual = true;
+        needs.pieces = std::max<int32_t>(needs.pieces, std::max<int32_t>(1, (std::min(d.cap, V) + kChunk - 1) / kChunk));
         if (d.clusters == nullptr) {
+            needs.streamed = true;
             REQUIRE(d.cap <= V, "step %d: cap=%d > V=%d", i, d.cap, V);
             REQUIRE(d.tail_beta == 0.0f, "step %d: tail_beta without clusters", i);
             continue;
@@ -153,6 +155,11 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
             const int64_t rows = d.shared ? std::min<int64_t>(V, (int64_t)B * L->cap_by_k[d.k]) : L->cap_by_k[d.k];
             if (d.cap < rows)
                 return set_error(DYNA_ERR_CAPACITY, "step %d: cap=%d < %lld", i, d.cap, (long long)rows);
+            if (step_listed(d, B, L->M))
+                needs.entries = (int32_t)std::max<int64_t>(
+                    needs.entries, std::min<int64_t>(L->M, (int64_t)(d.shared ? B : 1) * d.k));
+            else
+                needs.streamed = true;
         }
     }
     VerifyArgs a{};
@@ -170,13 +177,14 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
     a.greedy = temperature == 0.0f;
     a.lens = lens;
     a.offsets = clusters ? L->offsets : nullptr;
+    a.perm = clusters ? L->perm : nullptr;
     a.token_rows = token_rows;
     a.inv_t = a.greedy ? 1.0 : 1.0 / (double)temperature;
     a.uniforms = uniforms;
     a.out_len = out_len;
     a.out_ids = out_ids;
     a.out_logprobs = out_logprobs;
-    return launch_verify(a, table, residual, stream);
+    return launch_verify(a, table, needs, stream);
 }
 
 DYNA_API dyna_status dyna_verify_tree(const void* target, int32_t tdtype, int32_t V, int64_t row_stride,
@@ -212,7 +220,7 @@ DYNA_API dyna_status dyna_verify_tree(const void* target, int32_t tdtype, int32_
     a.out_ids = out_ids;
     a.out_logprobs = out_logprobs;
     a.out_nodes = out_nodes;
-    return launch_verify(a, StepTable{}, false, stream);
+    return launch_verify(a, StepTable{}, DrawNeeds{}, stream);
 }
 
 // ------------------------------------------------------------------ learning

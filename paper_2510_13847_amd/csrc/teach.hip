@@ -398,9 +398,9 @@ dyna_status run_distill(const DistillArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t distill_ws_bytes(int32_t N, int32_t V, DistillArgs* a, void* ws) {
-    const int64_t most = (V + kChunk - 1) / kChunk, least = (V + kMaxSplitLen - 1) / kMaxSplitLen;
+    const int64_t most = (V + kPartStep - 1) / kPartStep, least = (V + kMaxSplitLen - 1) / kMaxSplitLen;
     int64_t splits = std::min<int64_t>(most, std::max<int64_t>(least, (2048 + (int64_t)N - 1) / N));
-    const int64_t len = ((V + splits - 1) / splits + kChunk - 1) / kChunk * kChunk;
+    const int64_t len = ((V + splits - 1) / splits + kPartStep - 1) / kPartStep * kPartStep;
     splits = (V + len - 1) / len;
     if (a) {
         a->splits = (int32_t)splits;

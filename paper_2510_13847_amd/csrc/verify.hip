@@ -51,8 +51,83 @@ __device__ __forceinline__ const T* row_ptr(const VerifyArgs& a, int b, int j) {
 }
 
 // ---------------------------------------------------------------- rows
-// Largest logit, its lowest index and the sum of exponentials of one part of
-// one row, where a walk can need them.
+// Softmax pieces of a thread's share of a row: largest logit and its lowest
+// index, sum of exp2((z - m) c).
+struct Running {
+    float m = kNegInf;
+    double s = 0.0;
+    int best = -1;
+    float c;
+
+    __device__ __forceinline__ explicit Running(float c_) : c(c_) {}
+
+    // NV vectors of eight logits, the i-th at v + i * step.  The exponentials
+    // take z c - m c in one fused step; its rounding of m c is the same for
+    // every term and is put right on their sum.
+    template <int NV>
+    __device__ __forceinline__ bool take(const float (&z)[NV][8], int v, int step) {
+        float top = max8(z[0]);
+#pragma unroll
+        for (int i = 1; i < NV; ++i) top = fmaxf(top, max8(z[i]));
+        const float ref = fmaxf(m, top);
+        const float mc = ref * c, lost = fmaf(ref, c, -mc);
+        float e = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = __builtin_amdgcn_exp2f(fmaf(z[i][k], c, -mc));
+            e += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        }
+        // a NaN or +inf logit, nothing but masked ones so far, or a product
+        // that its own rounding matters to
+        if (!(e < __builtin_inff()) || !(fabsf(mc) < 1e6f)) return false;
+        if (top > m) {
+            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+#pragma unroll
+            for (int i = NV - 1; i >= 0; --i)
+#pragma unroll
+                for (int k = 7; k >= 0; --k)
+                    if (z[i][k] == top) best = v + i * step + k;
+        }
+        s += (double)(e * __builtin_amdgcn_exp2f(-lost));
+        return true;
+    }
+    // The same with every logit cleaned first.
+    template <int NV>
+    __device__ __forceinline__ void take_any(float (&z)[NV][8], int v, int step) {
+        if (take(z, v, step)) return;
+        float top = kNegInf;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                z[i][k] = clean(z[i][k]);
+                top = fmaxf(top, z[i][k]);
+            }
+        if (top > m) {
+            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+#pragma unroll
+            for (int i = NV - 1; i >= 0; --i)
+#pragma unroll
+                for (int k = 7; k >= 0; --k)
+                    if (z[i][k] == top) best = v + i * step + k;
+        }
+        if (m == kNegInf) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += (double)__builtin_amdgcn_exp2f((z[i][k] - m) * c);
+    }
+};
+
+// Vectors a thread has in flight.  One was measured too: the batches' rows
+// then stream at 4.6 TB/s.
+constexpr int kFlight = 4;
+
+// Pieces of one part of one row, where a walk can need them.
 template <typename T>
 __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
     __shared__ float tmp_f[kVT / kWave];
@@ -70,41 +145,30 @@ __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
         for (int i = j + 1 + (int)threadIdx.x; i < a.N; i += kVT) kid |= node_parent(a, b, i) == j;
         if (!__syncthreads_or(kid)) return;
     }
-    const int v0 = part * a.split_len, v1 = min(a.V, v0 + a.split_len);
+    const int v1 = min(a.V, (part + 1) * a.split_len);
     const T* x = row_ptr<T>(a, b, j);
-    const float c = (float)(a.inv_t * 1.4426950408889634);
-    float m = kNegInf;
-    double s = 0.0;
-    int best = a.V;
-    for (int v = v0 + (int)threadIdx.x * 8; v < v1; v += kVT * 8) {
-        float z[8];
-        load_part(x + v, v1 - v, kNegInf, z);
-        float top = kNegInf;
+    constexpr int kStep = kVT * 8;
+    Running run((float)(a.inv_t * 1.4426950408889634));
+    int v = part * a.split_len + (int)threadIdx.x * 8;
+    for (; v + (kFlight - 1) * kStep + 8 <= v1; v += kFlight * kStep) {
+        Row8<T> r[kFlight];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            z[i] = clean(z[i]);
-            top = fmaxf(top, z[i]);
-        }
-        if (top > m) {
-            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
-            m = top;
+        for (int i = 0; i < kFlight; ++i) r[i].load(x + v + i * kStep);
+        float z[kFlight][8];
 #pragma unroll
-            for (int i = 7; i >= 0; --i)
-                if (z[i] == top) best = v + i;
-        }
-        if (m > kNegInf) {
-            float e = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e += __builtin_amdgcn_exp2f((z[i] - m) * c);
-            s += (double)e;
-        }
+        for (int i = 0; i < kFlight; ++i) r[i].get(z[i]);
+        run.take_any(z, v, kStep);
     }
-    const float top = block_max_f32<kVT>(m, tmp_f);
-    const double part_s = m > kNegInf ? s * (double)__builtin_amdgcn_exp2f((m - top) * c) : 0.0;
-    const double total = block_sum_f64<kVT>(part_s, tmp_d);
-    const uint64_t key = wave_max_u64(m > kNegInf ? sel_key(m, (uint32_t)best) : 0ull);
+    for (; v < v1; v += kStep) {
+        float z[1][8];
+        load_part(x + v, v1 - v, kNegInf, z[0]);
+        run.take_any(z, v, kStep);
+    }
+    const float top = block_max_f32<kVT>(run.m, tmp_f);
+    const double mine = run.m > kNegInf ? run.s * (double)__builtin_amdgcn_exp2f((run.m - top) * run.c) : 0.0;
+    const uint64_t key = wave_max_u64(run.m > kNegInf ? sel_key(run.m, (uint32_t)run.best) : 0ull);
     if (lane_id() == 0) tmp_k[threadIdx.x / kWave] = key;
-    __syncthreads();
+    const double total = block_sum_f64<kVT>(mine, tmp_d);
     if (threadIdx.x == 0) {
         uint64_t k = tmp_k[0];
         for (int w = 1; w < kVT / kWave; ++w) k = tmp_k[w] > k ? tmp_k[w] : k;
@@ -117,11 +181,13 @@ struct WalkLds {
     double p[DYNA_MAX_NODES];     // target probability of the node's token in its parent's row
     double sum[DYNA_MAX_NODES];
     float top[DYNA_MAX_NODES];
+    float z[DYNA_MAX_NODES];      // the token's logit there
     int32_t best[DYNA_MAX_NODES];
     int32_t token[DYNA_MAX_NODES];
     int32_t parent[DYNA_MAX_NODES];
-    uint8_t stands[DYNA_MAX_NODES];
     int32_t path[DYNA_MAX_NODES];
+    uint8_t stands[DYNA_MAX_NODES];
+    double table[16];
     int32_t depth, node;
 };
 
@@ -134,42 +200,63 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
     const int b = blockIdx.x, t = threadIdx.x;
     const int N = a.N;
     const int len = a.chain ? chain_len(a, b) : N - 1;
+    const Weigher weight{w.table, a.inv_t * k16Log2e};
+    fill_weight_table(w.table);
     for (int j = t; j < N; j += kVT) {
-        w.token[j] = j == 0 ? -1 : node_token(a, st, b, len, j);
-        w.parent[j] = j == 0 ? -1 : node_parent(a, b, j);
-        // rows that row_parts_kernel left out are not read below
+        const int x = j == 0 ? -1 : node_token(a, st, b, len, j), par = j == 0 ? -1 : node_parent(a, b, j);
+        w.token[j] = x;
+        w.parent[j] = par;
+        w.z[j] = x >= 0 && par >= 0 ? clean(to_f32(row_ptr<T>(a, b, par)[x])) : kNegInf;
+    }
+    __syncthreads();
+    // 16 lanes join a row's parts (what stands in place of parts that were not
+    // written is not used)
+    constexpr int kTeam = 16;
+    for (int j0 = 0; j0 < N; j0 += kVT / kTeam) {
+        const int j = j0 + t / kTeam, i0 = t % kTeam;
+        const bool have = j < N && (a.chain ? (j < len || (j == len && a.greedy)) : true);
+        const RowPart* p = a.parts + ((int64_t)b * N + (have ? j : 0)) * a.splits;
         float m = kNegInf;
         double s = 0.0;
-        int best = -1;
-        const bool have = a.chain ? (j < len || (j == len && a.greedy)) : true;
-        if (have) {
-            const RowPart* p = a.parts + ((int64_t)b * N + j) * a.splits;
-            for (int i = 0; i < a.splits; ++i) {
-                const RowPart r = p[i];
-                if (r.m > m) {
-                    s *= exp(((double)m - (double)r.m) * a.inv_t);
-                    m = r.m;
-                    best = r.best;
-                }
-                if (r.m > kNegInf) s += r.s * exp(((double)r.m - (double)m) * a.inv_t);
+        int best = INT32_MAX;
+        if (have)
+#pragma unroll 4
+            for (int i = i0; i < a.splits; i += kTeam) {
+                const float x = p[i].m;
+                best = x > m ? p[i].best : best;
+                m = fmaxf(m, x);
             }
+        float top = m;
+#pragma unroll
+        for (int o = kTeam / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+        if (have)
+#pragma unroll 4
+            for (int i = i0; i < a.splits; i += kTeam) s += p[i].s * weight(p[i].m, top);
+        best = m == top ? best : INT32_MAX;
+#pragma unroll
+        for (int o = kTeam / 2; o > 0; o >>= 1) {
+            s += __shfl_xor(s, o, kWave);
+            best = min(best, __shfl_xor(best, o, kWave));
         }
-        w.top[j] = m;
-        w.sum[j] = s;
-        w.best[j] = best;
+        if (j < N && i0 == 0) {
+            w.top[j] = top;
+            w.sum[j] = s;
+            w.best[j] = top > kNegInf ? best : -1;
+        }
     }
     __syncthreads();
     for (int j = t; j < N; j += kVT) {
         const int x = w.token[j], par = w.parent[j];
         double p = 0.0;
-        if (x >= 0 && par >= 0) {
-            const float z = clean(to_f32(row_ptr<T>(a, b, par)[x]));
-            p = weight_f64(z, w.top[par], a.inv_t);
-            p = p > 0.0 ? p / w.sum[par] : 0.0;
+        if (x >= 0 && par >= 0 && w.z[j] > kNegInf) {
+            p = weight(w.z[j], w.top[par]) / w.sum[par];
             // a token that a sibling before it has proposed cannot stand again
-            if (!a.chain)
-                for (int i = par + 1; i < j; ++i)
-                    if (w.parent[i] == par && w.token[i] == x) p = 0.0;
+            if (!a.chain) {
+                bool again = false;
+#pragma unroll 8
+                for (int i = par + 1; i < j; ++i) again |= (w.parent[i] == par) & (w.token[i] == x);
+                p = again ? 0.0 : p;
+            }
         }
         w.p[j] = p;
     }
@@ -186,8 +273,8 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
                 ok = (double)a.uniforms[(int64_t)b * N + j - 1] * q < w.p[j];
             } else {
                 double mass = 1.0;
-                for (int i = par + 1; i < j; ++i)
-                    if (w.parent[i] == par) mass -= w.p[i];
+#pragma unroll 8
+                for (int i = par + 1; i < j; ++i) mass -= w.parent[i] == par ? w.p[i] : 0.0;
                 ok = (double)a.uniforms[(int64_t)b * N + j] * mass < w.p[j];
             }
         }
@@ -247,222 +334,378 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
 }
 
 // ---------------------------------------------------------------- draw
-// Tokens [c * kChunk, ...) of a request that were rejected outright at node:
-// the tokens of its children, marked in an LDS bit set.
+constexpr int kWaves = kVT / kWave;
+
+// Tokens [v0, v0 + kChunk) of a request that were rejected outright at the node
+// the walk ended in (its children's tokens), as a wave's bit set in LDS.
 __device__ __forceinline__ void mark_rejected(const VerifyArgs& a, const StepTable& st, int b, const WalkEnd& e,
                                               int v0, uint32_t* bits) {
-    for (int i = threadIdx.x; i < kChunk / 32; i += kVT) bits[i] = 0u;
-    __syncthreads();
-    if (e.mode == kDrawTarget) {
-        const int len = a.chain ? chain_len(a, b) : a.N - 1;
-        const int last = a.chain ? min(len, e.node + 1) : a.N - 1;
-        for (int j = e.node + 1 + (int)threadIdx.x; j <= last; j += kVT) {
-            if (node_parent(a, b, j) != e.node) continue;
-            const int x = node_token(a, st, b, len, j) - v0;
-            if (x >= 0 && x < kChunk) atomicOr(&bits[x >> 5], 1u << (x & 31));
-        }
+    if (lane_id() < kChunk / 32) bits[lane_id()] = 0u;
+    wave_lds_order();
+    const int len = a.chain ? chain_len(a, b) : a.N - 1;
+    const int last = a.chain ? min(len, e.node + 1) : a.N - 1;
+    for (int j = e.node + 1 + lane_id(); j <= last; j += kWave) {
+        if (node_parent(a, b, j) != e.node) continue;
+        const int x = node_token(a, st, b, len, j) - v0;
+        if (x >= 0 && x < kChunk) atomicOr(&bits[x >> 5], 1u << (x & 31));
     }
-    __syncthreads();
+    wave_lds_order();
 }
 __device__ __forceinline__ uint32_t marks8(const uint32_t* bits, int x) { return (bits[x >> 5] >> (x & 31)) & 0xffu; }
 
-// Chunks 0..n_chunks-1: softmax pieces of the row the walk ended in.  One more
-// workgroup per request reads the rejected draft's shortlist row.
+// The step's clusters of request b as a bit set in LDS (ids outside [0, M) and
+// repeats add nothing); returns, on every thread, the tokens they hold.
+template <int NT>
+__device__ __forceinline__ int pick_clusters(const VerifyArgs& a, const dyna_draft_step& d, int b, uint32_t* picked,
+                                             int* total) {
+    const int t = threadIdx.x;
+    for (int i = t; i < (a.M + 31) / 32; i += NT) picked[i] = 0u;
+    if (t == 0) *total = 0;
+    __syncthreads();
+    const int first = d.shared ? 0 : b * d.k, count = d.shared ? a.B * d.k : d.k;
+    int n = 0;
+    for (int i = t; i < count; i += NT) {
+        const int m = d.clusters[first + i];
+        if (m < 0 || m >= a.M) continue;
+        const int size = a.offsets[m + 1] - a.offsets[m];
+        if (!(atomicOr(&picked[m >> 5], 1u << (m & 31)) & (1u << (m & 31)))) n += size;
+    }
+    if (n) atomicAdd(total, n);
+    __syncthreads();
+    return *total;
+}
+
+// Per request, waves c < n_chunks: softmax pieces of a chunk of the row the walk
+// ended in.  Behind them, workgroups: the same of kWaves chunks of the rejected
+// draft's row; and one that writes where each selected cluster's slots start,
+// for the steps whose chunks are read again.
 template <typename T>
-__global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int per) {
-    __shared__ float tmp_f[kVT / kWave];
-    __shared__ double tmp_d[kVT / kWave];
-    __shared__ int tmp_i[kVT / kWave + 1];
-    __shared__ uint32_t bits[kChunk / 32];
-    extern __shared__ uint32_t picked[];  // [M / 32] bit set of selected clusters
-    const int b = blockIdx.x / per, c = blockIdx.x % per, t = threadIdx.x;
+__global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int n_pieces,
+                                                         int per) {
+    __shared__ double table[kWaves][16];
+    __shared__ uint32_t bits[kWaves][kChunk / 32];
+    __shared__ int tmp_i[kWaves + 1];
+    extern __shared__ uint32_t picked[];  // [M / 32]
+    const int b = blockIdx.x / per, g = blockIdx.x % per, t = threadIdx.x, wave = t / kWave, lane = lane_id();
     const WalkEnd e = a.ends[b];
-    if (c < a.n_chunks) {
-        const int v0 = c * kChunk;
-        mark_rejected(a, st, b, e, v0, bits);
-        const int v = v0 + t * 8;
+    fill_wave_table(table[wave]);
+    if (g < chunk_groups) {
+        const int c = g * kWaves + wave;
+        if (c >= a.n_chunks) return;
+        const Weigher weight{table[wave], a.inv_t * k16Log2e};
+        const int v0 = c * kChunk, v = v0 + lane * 8;
         float z[8];
         load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
-        float m = kNegInf;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            z[i] = clean(z[i]);
-            m = fmaxf(m, z[i]);
-        }
-        m = block_max_f32<kVT>(m, tmp_f);
-        const uint32_t out = marks8(bits, t * 8);
-        double all = 0.0, ex = 0.0;
+        for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
+        const float m = wave_max_all(max8(z));
+        double all = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double w = weight_f64(z[i], m, a.inv_t);
-            all += w;
-            if (!((out >> i) & 1u)) ex += w;
+        for (int i = 0; i < 8; ++i) all += weight(z[i], m);
+        all = wave_sum_f64(all);
+        double ex = all;
+        if (e.mode == kDrawTarget) {
+            // the sum without the rejected tokens is taken apart: a difference
+            // would be rounding alone where they hold the chunk's weight
+            mark_rejected(a, st, b, e, v0, bits[wave]);
+            const uint32_t out = marks8(bits[wave], lane * 8);
+            if (__any(out != 0)) {
+                ex = 0.0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ex += (out >> i) & 1u ? 0.0 : weight(z[i], m);
+                ex = wave_sum_f64(ex);
+            }
         }
-        all = block_sum_f64<kVT>(all, tmp_d);
-        ex = block_sum_f64<kVT>(ex, tmp_d);
-        if (t == 0) a.chunks[(int64_t)b * a.n_chunks + c] = ChunkPart{all, ex, m, 0.0f};
+        if (lane == 0) a.chunks[(int64_t)b * a.n_chunks + c] = ChunkPart{all, ex, m, 0.0f};
         return;
     }
     if (e.mode != kDrawResidual) return;
     const dyna_draft_step& d = st.s[e.node];
     int len = d.cap;
-    if (d.clusters != nullptr) {
-        const int M = a.M, words = (M + 31) / 32;
-        for (int i = t; i < words; i += kVT) picked[i] = 0u;
-        __syncthreads();
-        const int first = d.shared ? 0 : b * d.k, count = d.shared ? a.B * d.k : d.k;
-        for (int i = t; i < count; i += kVT) {
-            const int m = d.clusters[first + i];
-            if (m >= 0 && m < M) atomicOr(&picked[m >> 5], 1u << (m & 31));
-        }
-        __syncthreads();
-        const int each = (M + kVT - 1) / kVT, m0 = min(M, t * each), m1 = min(M, m0 + each);
-        int sum = 0;
-        for (int m = m0; m < m1; ++m)
-            if ((picked[m >> 5] >> (m & 31)) & 1u) sum += a.offsets[m + 1] - a.offsets[m];
-        int total = 0;
-        int base = block_exclusive_scan<kVT>(sum, tmp_i, &total);
-        for (int m = m0; m < m1; ++m) {
-            int s = kNoSlot;
-            if ((picked[m >> 5] >> (m & 31)) & 1u) {
-                s = base - a.offsets[m];
-                base += a.offsets[m + 1] - a.offsets[m];
-            }
-            a.slot_of[(int64_t)b * M + m] = s;
-        }
-        len = min(total, d.cap);
-    }
-    const float* z = d.logits + (int64_t)b * d.cap;
-    const double inv_t = 1.0 / (double)d.temperature;
-    float m = kNegInf;
-    for (int i = t; i < len; i += kVT) m = fmaxf(m, clean(z[i]));
-    m = block_max_f32<kVT>(m, tmp_f);
-    double s = 0.0;
-    for (int i = t; i < len; i += kVT) s += weight_f64(clean(z[i]), m, inv_t);
-    s = block_sum_f64<kVT>(s, tmp_d);
-    if (t == 0) a.drafts[b] = DraftPart{s, m, len};
-}
-
-// Largest logit and sum of exponentials of a whole row from its chunks; `ex`
-// the same without the rejected tokens.
-__device__ __forceinline__ void row_total(const VerifyArgs& a, int b, float* tmp_f, double* tmp_d, float* m,
-                                          double* all, double* ex) {
-    const ChunkPart* p = a.chunks + (int64_t)b * a.n_chunks;
-    float top = kNegInf;
-    for (int c = threadIdx.x; c < a.n_chunks; c += kVT) top = fmaxf(top, p[c].m);
-    top = block_max_f32<kVT>(top, tmp_f);
-    double s = 0.0, x = 0.0;
-    for (int c = threadIdx.x; c < a.n_chunks; c += kVT) {
-        const double f = weight_f64(p[c].m, top, a.inv_t);
-        s += p[c].all * f;
-        x += p[c].ex * f;
-    }
-    *m = top;
-    *all = block_sum_f64<kVT>(s, tmp_d);
-    *ex = block_sum_f64<kVT>(x, tmp_d);
-}
-
-// max(p - q, 0) of the eight tokens from v on.
-template <typename T>
-__device__ __forceinline__ void residual8(const VerifyArgs& a, const StepTable& st, int b, const WalkEnd& e, int v,
-                                          float m, double all, double (&r)[8]) {
-    const dyna_draft_step& d = st.s[e.node];
-    const DraftPart dp = a.drafts[b];
-    const double inv_tq = 1.0 / (double)d.temperature;
-    const double beta = dp.len < a.V ? (double)d.tail_beta : 0.0;
-    const double in = dp.s > 0.0 ? (1.0 - beta) / dp.s : 0.0;
-    const double out = beta > 0.0 ? beta / (double)(a.V - dp.len) : 0.0;
-    const double inv_all = all > 0.0 ? 1.0 / all : 0.0;
-    float z[8];
-    load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
-    const float* zq = d.logits + (int64_t)b * d.cap;
+    if (d.clusters != nullptr) len = min(d.cap, pick_clusters<kVT>(a, d, b, picked, tmp_i));
+    const int piece = (g - chunk_groups) * kWaves + wave;
+    if (g - chunk_groups < (n_pieces + kWaves - 1) / kWaves) {
+        if (piece >= n_pieces) return;
+        const Weigher weight{table[wave], 1.0 / (double)d.temperature * k16Log2e};
+        const int s0 = piece * kChunk + lane * 8;
+        float z[8];
+        load_part(d.logits + (int64_t)b * d.cap + s0, len - s0, kNegInf, z);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        double q = out;
-        if (v + i < a.V) {
-            int slot = -1;
-            if (d.clusters == nullptr) {
-                slot = v + i;
-            } else {
-                const int cl = a.token_rows[2 * (int64_t)(v + i)], row = a.token_rows[2 * (int64_t)(v + i) + 1];
-                const int s = cl >= 0 && cl < a.M ? a.slot_of[(int64_t)b * a.M + cl] : kNoSlot;
-                if (s != kNoSlot) slot = s + row;
-            }
-            if (slot >= 0 && slot < dp.len) q = in * weight_f64(clean(zq[slot]), dp.m, inv_tq);
-        }
-        const double p = weight_f64(clean(z[i]), m, a.inv_t) * inv_all;
-        r[i] = p > q ? p - q : 0.0;
+        for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
+        const float m = wave_max_all(max8(z));
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += weight(z[i], m);
+        s = wave_sum_f64(s);
+        if (lane == 0) a.pieces[(int64_t)b * a.n_pieces + piece] = DraftPart{s, m, len};
+        return;
+    }
+    if (d.clusters == nullptr || step_listed(d, a.B, a.M)) return;
+    __syncthreads();
+    // consecutive clusters a round, so that offsets are read in order
+    int base = 0;
+    for (int m0 = 0; m0 < a.M; m0 += kVT) {
+        const int m = m0 + t;
+        const bool in = m < a.M && ((picked[m >> 5] >> (m & 31)) & 1u);
+        const int o0 = in ? a.offsets[m] : 0, size = in ? a.offsets[m + 1] - o0 : 0;
+        int total = 0;
+        const int at = block_exclusive_scan<kVT>(size, tmp_i, &total);
+        if (m < a.M) a.slot_of[(int64_t)b * a.M + m] = in ? base + at - o0 : kNoSlot;
+        base += total;
     }
 }
 
+// The two distributions of a residual, from their pieces.
+struct Drawn {
+    float m;           // target row: largest logit
+    double all;        // sum of exp((z - m) / T)
+    double inv_all;
+    float qm;          // draft row
+    double q_in;       // (1 - beta) / its sum, 0 without one
+    double q_out;      // probability of a token off the shortlist
+    int len;           // slots
+};
+
+template <int NT>
+struct JoinLds {
+    float f[2][NT / kWave];
+    double d[2][NT / kWave];
+};
+
+// Joins the chunks' pieces, and the draft row's when `residual`.
+template <int NT>
+__device__ __forceinline__ Drawn join_parts(const VerifyArgs& a, const StepTable& st, int b, const WalkEnd& e,
+                                            bool residual, int n_pieces, const double* table, JoinLds<NT>& w) {
+    const ChunkPart* p = a.chunks + (int64_t)b * a.n_chunks;
+    const dyna_draft_step& d = st.s[residual ? e.node : 0];
+    const DraftPart* q = a.pieces + (int64_t)b * a.n_pieces;
+    const int t = threadIdx.x, wave = t / kWave;
+    Drawn r{};
+    r.len = residual ? q[0].len : 0;
+    const int nq = min(n_pieces, (r.len + kChunk - 1) / kChunk);
+    float m = kNegInf, qm = kNegInf;
+    for (int c = t; c < a.n_chunks; c += NT) m = fmaxf(m, p[c].m);
+    for (int i = t; i < nq; i += NT) qm = fmaxf(qm, q[i].m);
+    m = wave_max_all(m);
+    qm = wave_max_all(qm);
+    if (lane_id() == 0) {
+        w.f[0][wave] = m;
+        w.f[1][wave] = qm;
+    }
+    __syncthreads();
+    r.m = r.qm = kNegInf;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) {
+        r.m = fmaxf(r.m, w.f[0][i]);
+        r.qm = fmaxf(r.qm, w.f[1][i]);
+    }
+    const Weigher weight{table, a.inv_t * k16Log2e};
+    double s = 0.0, x = 0.0;
+    for (int c = t; c < a.n_chunks; c += NT) s += p[c].all * weight(p[c].m, r.m);
+    s = wave_sum_f64(s);
+    if (residual) {
+        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+        for (int i = t; i < nq; i += NT) x += q[i].s * wq(q[i].m, r.qm);
+        x = wave_sum_f64(x);
+    }
+    if (lane_id() == 0) {
+        w.d[0][wave] = s;
+        w.d[1][wave] = x;
+    }
+    __syncthreads();
+    s = x = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) {
+        s += w.d[0][i];
+        x += w.d[1][i];
+    }
+    r.all = s;
+    r.inv_all = s > 0.0 ? 1.0 / s : 0.0;
+    if (residual) {
+        const double beta = r.len < a.V ? (double)d.tail_beta : 0.0;
+        r.q_in = x > 0.0 ? (1.0 - beta) / x : 0.0;
+        r.q_out = beta > 0.0 ? beta / (double)(a.V - r.len) : 0.0;
+    }
+    return r;
+}
+
+// Slot of token v in a step whose chunks are read again, -1 off the shortlist.
+__device__ __forceinline__ int streamed_slot(const VerifyArgs& a, const dyna_draft_step& d, int b, int v) {
+    if (d.clusters == nullptr) return v;
+    const int m = a.token_rows[2 * (int64_t)v], j = a.token_rows[2 * (int64_t)v + 1];
+    const int s = m >= 0 && m < a.M ? a.slot_of[(int64_t)b * a.M + m] : kNoSlot;
+    return s != kNoSlot ? s + j : -1;
+}
+
+// max(p - q, 0) chunk by chunk, for steps with a tail mixture, contiguous logits
+// or a long shortlist.
 template <typename T>
-__global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable st) {
-    __shared__ float tmp_f[kVT / kWave];
-    __shared__ double tmp_d[kVT / kWave];
-    const int b = blockIdx.x / a.n_chunks, c = blockIdx.x % a.n_chunks;
+__global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable st, int per, int n_pieces) {
+    __shared__ double table[16];
+    __shared__ JoinLds<kVT> w;
+    const int b = blockIdx.x / per, g = blockIdx.x % per;
     const WalkEnd e = a.ends[b];
     if (e.mode != kDrawResidual) return;
-    float m;
-    double all, ex;
-    row_total(a, b, tmp_f, tmp_d, &m, &all, &ex);
-    double r[8], s = 0.0;
-    residual8<T>(a, st, b, e, c * kChunk + (int)threadIdx.x * 8, m, all, r);
+    const dyna_draft_step& d = st.s[e.node];
+    if (step_listed(d, a.B, a.M)) return;
+    fill_weight_table(table);
+    const int c = g * kWaves + (int)threadIdx.x / kWave, v = c * kChunk + lane_id() * 8;
+    const float* zq = d.logits + (int64_t)b * d.cap;
+    const int len = a.pieces[(int64_t)b * a.n_pieces].len;
+    float z[8], y[8];
+    load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
+    uint32_t in = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += r[i];
-    s = block_sum_f64<kVT>(s, tmp_d);
-    if (threadIdx.x == 0) a.left[(int64_t)b * a.n_chunks + c] = s;
+    for (int i = 0; i < 8; ++i) {
+        y[i] = kNegInf;
+        if (v + i < a.V) {
+            const int slot = streamed_slot(a, d, b, v + i);
+            if (slot >= 0 && slot < len) {
+                y[i] = clean(zq[slot]);
+                in |= 1u << i;
+            }
+        }
+    }
+    const Drawn r = join_parts<kVT>(a, st, b, e, true, n_pieces, table, w);  // its barriers order the table
+    const Weigher weight{table, a.inv_t * k16Log2e}, wq{table, 1.0 / (double)d.temperature * k16Log2e};
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        double q = r.q_out;
+        if (__any((in >> i) & 1u)) q = (in >> i) & 1u ? r.q_in * wq(y[i], r.qm) : q;
+        s += fmax(weight(clean(z[i]), r.m) * r.inv_all - q, 0.0);
+    }
+    s = wave_sum_f64(s);
+    if (lane_id() == 0 && c < a.n_chunks) a.left[(int64_t)b * a.n_chunks + c] = s;
 }
 
+// Less than this of p's mass left by the drafts counts as nothing, and less than
+// kRounding of a chunk's own mass as rounding: the chunks' sums are differences.
+constexpr double kNothing = 0x1p-40;
+constexpr double kRounding = 0x1p-45;
+constexpr double kFixOne = 0x1p62;
+
 // The draw: the chunk in which the cumulative weight passes u of the total,
-// then the token inside it.
-template <typename T>
-__global__ __launch_bounds__(kVT) void draw_kernel(VerifyArgs a, StepTable st) {
-    __shared__ float tmp_f[kVT / kWave];
-    __shared__ double tmp_d[kVT / kWave];
-    __shared__ uint32_t bits[kChunk / 32];
+// then the token inside it.  One workgroup per request.
+//
+// A listed step's residual differs from p on its shortlist alone: a chunk keeps
+// its sum of p, and the shortlist's tokens, looked up slot by slot, take
+// min(p, q) from their chunks, as whole multiples of 2^-62 so that the order of
+// the additions in LDS does not matter.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces, int entries) {
+    __shared__ double table[16];
+    __shared__ JoinLds<NT> w;
+    __shared__ double sums[NT / kWave];
+    __shared__ int tmp_i[NT / kWave + 1], tmp_j[NT / kWave + 1];
     __shared__ int hit, last;
     __shared__ double before;
-    const int b = blockIdx.x, t = threadIdx.x;
+    __shared__ uint32_t bits[kChunk / 32];
+    extern __shared__ char lds[];
+    const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks;
+    double* chunk_w = reinterpret_cast<double*>(lds);                       // [n]
+    int* list_slot = reinterpret_cast<int*>(chunk_w + n);                   // [entries] first slot
+    int* list_row = list_slot + entries;                                    // [entries] first layout row
+    int* list_id = list_row + entries;                                      // [entries] cluster
+    uint32_t* picked = reinterpret_cast<uint32_t*>(list_id + entries);      // [M / 32]
     const WalkEnd e = a.ends[b];
-    const int n = a.n_chunks;
-    float m;
-    double all, ex;
-    row_total(a, b, tmp_f, tmp_d, &m, &all, &ex);
+    fill_weight_table(table);
+    const Weigher weight{table, a.inv_t * k16Log2e};
+    bool residual = e.mode == kDrawResidual;
+    const dyna_draft_step& d = st.s[residual ? e.node : 0];
+    const bool listed = residual && step_listed(d, a.B, a.M);
+    const double u = (double)a.uniforms[(int64_t)b * a.N + (a.chain ? a.N - 1 : 0)];
+    if (t == 0) hit = n, last = -1;
+    for (int c = t; c < n; c += NT) chunk_w[c] = 0.0;  // all bits 0: also the whole multiples' zero
+    const Drawn r = join_parts<NT>(a, st, b, e, residual, n_pieces, table, w);
     const ChunkPart* p = a.chunks + (int64_t)b * n;
-    const double* left = a.left + (int64_t)b * n;
     const int64_t o = (int64_t)b * a.N + e.depth;
-    if (!(all > 0.0)) {  // no token the target allows
+    if (!(r.all > 0.0)) {  // no token the target allows
         if (t == 0) {
             a.out_ids[o] = -1;
             if (a.out_logprobs) a.out_logprobs[o] = kNegInf;
         }
         return;
     }
-    bool residual = e.mode == kDrawResidual;
-    if (residual) {
-        double s = 0.0;
-        for (int c = t; c < n; c += kVT) s += left[c];
-        residual = block_sum_f64<kVT>(s, tmp_d) > 0.0;
+    const T* row = row_ptr<T>(a, b, e.node);
+    const float* zq = d.logits + (int64_t)b * d.cap;
+    int n_list = 0;
+    if (listed) {
+        // selected clusters in ascending id with their first slots
+        pick_clusters<NT>(a, d, b, picked, tmp_i);
+        __syncthreads();
+        int slots = 0;
+        for (int m0 = 0; m0 < a.M; m0 += NT) {
+            const int m = m0 + t;
+            const bool in = m < a.M && ((picked[m >> 5] >> (m & 31)) & 1u);
+            const int o0 = in ? a.offsets[m] : 0, size = in ? a.offsets[m + 1] - o0 : 0;
+            int total = 0, count = 0;
+            const int at = block_exclusive_scan<NT>(size, tmp_i, &total);
+            const int i = block_exclusive_scan<NT>(in, tmp_j, &count);
+            if (in) {
+                list_slot[n_list + i] = slots + at;
+                list_row[n_list + i] = o0;
+                list_id[n_list + i] = m;
+            }
+            slots += total;
+            n_list += count;
+        }
+        __syncthreads();
+        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+        long long* change = reinterpret_cast<long long*>(chunk_w);
+#pragma unroll 4
+        for (int s = t; s < r.len; s += NT) {
+            int lo = 0, hi = n_list;  // the last entry with list_slot <= s
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (list_slot[mid] <= s) lo = mid;
+                else hi = mid;
+            }
+            const int v = a.perm[list_row[lo] + s - list_slot[lo]];
+            if (v < 0 || v >= a.V) continue;
+            const double pv = weight(clean(to_f32(row[v])), r.m) * r.inv_all;
+            const double qv = r.q_in * wq(clean(zq[s]), r.qm);
+            atomicAdd(reinterpret_cast<unsigned long long*>(&change[v / kChunk]),
+                      (unsigned long long)(long long)(fmin(pv, qv) * kFixOne));
+        }
+        __syncthreads();
     }
-    const bool without = !residual && ex > 0.0;  // else the whole row
-    auto chunk_weight = [&](int c) {
-        if (residual) return left[c];
-        return (without ? p[c].ex : p[c].all) * weight_f64(p[c].m, m, a.inv_t);
+    // a thread's chunks are consecutive; their weights stay in LDS
+    const int each = (n + NT - 1) / NT, c0 = min(n, t * each), c1 = min(n, c0 + each);
+    auto weigh_chunks = [&](bool from_residual, bool without) {
+        double s = 0.0;
+        for (int c = c0; c < c1; ++c) {
+            double x;
+            if (from_residual && !listed) {
+                x = a.left[(int64_t)b * n + c];
+            } else {
+                x = (without ? p[c].ex : p[c].all) * weight(p[c].m, r.m);
+                if (from_residual) {
+                    x *= r.inv_all;
+                    const double kept = x - (double)__builtin_bit_cast(long long, chunk_w[c]) / kFixOne;
+                    x = kept > x * kRounding ? kept : 0.0;
+                }
+            }
+            chunk_w[c] = x;
+            s += x;
+        }
+        return s;
     };
-    if (t == 0) hit = n, last = -1;
-    const int each = (n + kVT - 1) / kVT, c0 = min(n, t * each), c1 = min(n, c0 + each);
-    double mine = 0.0;
-    for (int c = c0; c < c1; ++c) mine += chunk_weight(c);
-    double total;
-    double run = block_scan_f64<kVT>(mine, tmp_d, &total);
-    const double goal = (double)a.uniforms[(int64_t)b * a.N + (a.chain ? a.N - 1 : 0)] * total;
+    double total, run;
+    bool without = !residual;
+    run = block_scan_f64<NT>(weigh_chunks(residual, without), sums, &total);
+    if (residual ? !(total > kNothing) : !(total > 0.0)) {  // from p itself
+        residual = without = false;
+        run = block_scan_f64<NT>(weigh_chunks(false, false), sums, &total);
+    }
+    const double goal = u * total;
     {
         double f = run;
         int first = n, lastc = -1;
         for (int c = c0; c < c1; ++c) {
-            const double w = chunk_weight(c);
-            f += w;
-            if (w > 0.0) {
+            const double x = chunk_w[c];
+            f += x;
+            if (x > 0.0) {
                 lastc = c;
                 if (f > goal && first == n) first = c;
             }
@@ -474,51 +717,77 @@ __global__ __launch_bounds__(kVT) void draw_kernel(VerifyArgs a, StepTable st) {
     const int chunk = hit < n ? hit : last;
     if (chunk >= c0 && chunk < c1) {
         double f = run;
-        for (int c = c0; c < chunk; ++c) f += chunk_weight(c);
+        for (int c = c0; c < chunk; ++c) f += chunk_w[c];
         before = f;
     }
     __syncthreads();
+    if (t >= kWave) return;
+    // the chunk's tokens, eight to a lane.  Weights inside it are relative to
+    // its own largest logit, as when its sum was taken: a chunk of weight holds
+    // a token of weight
     const double base = before;
     const int v0 = chunk * kChunk, v = v0 + t * 8;
-    // weights inside the chunk are relative to its own largest logit, as when
-    // its sum was taken: a chunk of weight holds a token of weight
-    double w[8], scale = 1.0;
+    float z[8];
+    load_part(row + v, a.V - v, kNegInf, z);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
+    double x[8], scale = 1.0;
     if (residual) {
-        residual8<T>(a, st, b, e, v, m, all, w);
+        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int slot = -1;
+            if (v + i < a.V) {
+                if (listed) {
+                    const int m = a.token_rows[2 * (int64_t)(v + i)], j = a.token_rows[2 * (int64_t)(v + i) + 1];
+                    int lo = 0, hi = n_list;  // the last entry with list_id <= m
+                    while (hi - lo > 1) {
+                        const int mid = (lo + hi) >> 1;
+                        if (list_id[mid] <= m) lo = mid;
+                        else hi = mid;
+                    }
+                    if (n_list > 0 && list_id[lo] == m) slot = list_slot[lo] + j - list_row[lo];
+                } else {
+                    slot = streamed_slot(a, d, b, v + i);
+                }
+            }
+            const double q = slot >= 0 && slot < r.len ? r.q_in * wq(clean(zq[slot]), r.qm) : r.q_out;
+            x[i] = fmax(weight(z[i], r.m) * r.inv_all - q, 0.0);
+        }
     } else {
+        if (without) mark_rejected(a, st, b, e, v0, bits);
+        const uint32_t out = without ? marks8(bits, t * 8) : 0u;
         const float top = p[chunk].m;
-        scale = weight_f64(top, m, a.inv_t);
-        mark_rejected(a, st, b, without ? e : WalkEnd{0, 0, kDrawNone, 0}, v0, bits);
-        float z[8];
-        load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
-        const uint32_t out = marks8(bits, t * 8);
+        scale = weight(top, r.m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = (out >> i) & 1u ? 0.0 : weight_f64(clean(z[i]), top, a.inv_t);
+        for (int i = 0; i < 8; ++i) x[i] = (out >> i) & 1u ? 0.0 : weight(z[i], top);
     }
-    mine = 0.0;
+    double mine = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mine += w[i];
-    if (t == 0) hit = kChunk, last = -1;
-    double f = block_scan_f64<kVT>(mine, tmp_d, &total);
-    int first = kChunk, lastv = -1;
+    for (int i = 0; i < 8; ++i) mine += x[i];
+    double f = wave_scan_f64(mine) - mine;
+    int first = -1, lastv = -1;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        f += w[i];
-        if (w[i] > 0.0) {
-            lastv = t * 8 + i;
-            if (base + scale * f > goal && first == kChunk) first = t * 8 + i;
+        f += x[i];
+        if (x[i] > 0.0) {
+            lastv = i;
+            if (base + scale * f > goal && first < 0) first = i;
         }
     }
-    if (first < kChunk) atomicMin(&hit, first);
-    if (lastv >= 0) atomicMax(&last, lastv);
-    __syncthreads();
-    if (t == 0) {
-        // rounding can leave the last cumulative sum at or below the goal: then the last token with any weight
-        const int x = v0 + (hit < kChunk ? hit : last);
-        a.out_ids[o] = x;
+    // rounding can leave the last cumulative sum at or below the goal: then the
+    // last token with any weight
+    const uint64_t hits = __ballot(first >= 0), some = __ballot(lastv >= 0);
+    const int lane = hits ? __builtin_ctzll(hits) : some ? 63 - __builtin_clzll(some) : 0;
+    if (t == lane) {
+        const int i = hits ? first : max(lastv, 0);
+        a.out_ids[o] = v + i;
         if (a.out_logprobs) {
-            const float z = clean(to_f32(row_ptr<T>(a, b, e.node)[x]));
-            a.out_logprobs[o] = (float)(((double)z - (double)m) * a.inv_t - log(all));
+            float zx = kNegInf;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k == i) zx = z[k];
+            a.out_logprobs[o] = (float)(((double)zx - (double)r.m) * a.inv_t - log(r.all));
         }
     }
 }
@@ -541,16 +810,20 @@ __global__ __launch_bounds__(kVT) void token_rows_kernel(const int32_t* perm, co
 }
 
 template <typename T>
-dyna_status run(const VerifyArgs& a, const StepTable& st, bool residual, hipStream_t s) {
+dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hipStream_t s) {
     row_parts_kernel<T><<<(uint32_t)((int64_t)a.B * a.N * a.splits), kVT, 0, s>>>(a);
     walk_kernel<T><<<a.B, kVT, 0, s>>>(a, st);
-    if (!a.greedy) {
-        const int per = a.n_chunks + (residual ? 1 : 0);
-        const uint32_t lds = residual ? 4u * (uint32_t)((a.M + 31) / 32) : 0u;
-        draw_parts_kernel<T><<<(uint32_t)((int64_t)a.B * per), kVT, lds, s>>>(a, st, per);
-        if (residual) residual_kernel<T><<<(uint32_t)((int64_t)a.B * a.n_chunks), kVT, 0, s>>>(a, st);
-        draw_kernel<T><<<a.B, kVT, 0, s>>>(a, st);
-    }
+    if (a.greedy) return check_launch("verify");
+    const int groups = (a.n_chunks + kWaves - 1) / kWaves;
+    const bool clusters = q.pieces > 0 && a.M > 0;
+    const int per = groups + (q.pieces + kWaves - 1) / kWaves + (clusters && q.streamed ? 1 : 0);
+    const uint32_t set = clusters ? 4u * (uint32_t)((a.M + 31) / 32) : 0u;
+    draw_parts_kernel<T><<<(uint32_t)((int64_t)a.B * per), kVT, set, s>>>(a, st, groups, q.pieces, per);
+    if (q.streamed)
+        residual_kernel<T><<<(uint32_t)((int64_t)a.B * groups), kVT, 0, s>>>(a, st, groups, q.pieces);
+    const uint32_t lds = 8u * (uint32_t)a.n_chunks + 12u * (uint32_t)q.entries + (q.entries ? set : 0u);
+    if (q.entries) draw_kernel<T, 1024><<<a.B, 1024, lds, s>>>(a, st, q.pieces, q.entries);
+    else draw_kernel<T, 256><<<a.B, 256, lds, s>>>(a, st, q.pieces, 0);
     return check_launch("verify");
 }
 
@@ -562,13 +835,13 @@ dyna_status launch_token_rows(const int32_t* perm, const int32_t* offsets, int32
     return check_launch("token rows");
 }
 
-// Parts of a row: enough workgroups for the chip when there are few rows, in
-// steps of 2048 entries.
+// Parts of a row: 20480 entries (ten steps of a workgroup), or fewer where the
+// rows alone would leave the chip without 2048 workgroups.
 size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a, void* ws) {
     const int64_t rows = (int64_t)B * N;
-    const int64_t most = (V + kChunk - 1) / kChunk;
-    int64_t splits = std::min<int64_t>(most, std::max<int64_t>(1, (2048 + rows - 1) / rows));
-    const int64_t len = ((V + splits - 1) / splits + kChunk - 1) / kChunk * kChunk;
+    const int64_t steps = (V + kPartStep - 1) / kPartStep, most = (V + kChunk - 1) / kChunk;
+    int64_t splits = std::min(steps, std::max<int64_t>((V + 20479) / 20480, (2048 + rows - 1) / rows));
+    const int64_t len = (steps + splits - 1) / splits * kPartStep;
     splits = (V + len - 1) / len;
     char* p = static_cast<char*>(ws);
     size_t off = 0;
@@ -586,13 +859,14 @@ size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a
     v.ends = static_cast<WalkEnd*>(take(sizeof(WalkEnd) * (size_t)B));
     v.chunks = static_cast<ChunkPart*>(take(sizeof(ChunkPart) * (size_t)(B * most)));
     v.left = static_cast<double*>(take(sizeof(double) * (size_t)(B * most)));
-    v.drafts = static_cast<DraftPart*>(take(sizeof(DraftPart) * (size_t)B));
+    v.n_pieces = (int32_t)most;
+    v.pieces = static_cast<DraftPart*>(take(sizeof(DraftPart) * (size_t)(B * most)));
     v.slot_of = static_cast<int32_t*>(take(sizeof(int32_t) * (size_t)B * (size_t)M));
     return off;
 }
 
-dyna_status launch_verify(const VerifyArgs& a, const StepTable& steps, bool residual, hipStream_t stream) {
-    return a.tdtype == DYNA_BF16 ? run<uint16_t>(a, steps, residual, stream) : run<float>(a, steps, residual, stream);
+dyna_status launch_verify(const VerifyArgs& a, const StepTable& steps, const DrawNeeds& needs, hipStream_t stream) {
+    return a.tdtype == DYNA_BF16 ? run<uint16_t>(a, steps, needs, stream) : run<float>(a, steps, needs, stream);
 }
 
 }  // namespace dyna

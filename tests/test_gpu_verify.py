@@ -128,6 +128,8 @@ CHAINS = [  # V, B, n, dtype, T, kind, kwargs
     (50021, 3, 5, "bf16", 1.0, "clusters", dict(M=300, k=24)),
     (50021, 2, 32, "bf16", 1.0, "outright", {}),
     (131077, 2, 4, "f32", 0.6, "dense", dict(td=1.1)),
+    (100003, 2, 2, "bf16", 1.0, "clusters", dict(M=40, k=25)),              # a shortlist longer than 32768
+    (20011, 2, 2, "f32", 1.0, "clusters", dict(M=2500, k=2100)),            # more clusters than a list in LDS holds
 ]
 
 
