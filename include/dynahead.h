@@ -380,7 +380,7 @@ int32_t dyna_static_budget(int32_t t, int32_t k_max);
 /* Rules of both calls:
  *  target   device, tdtype, logits of the target model: row j of request b is
  *           V consecutive elements at b * batch_stride + j * row_stride
- *           (strides in elements, any alignment of the element).  p_j =
+ *           (strides in elements, any alignment of the element; V <= 2^20).  p_j =
  *           softmax(row / temperature).  NaN counts as -inf (a masked token),
  *           +inf as the largest finite number.
  *  temperature  >= 0; 0 is greedy: a draft stands when it is the row's largest
@@ -482,7 +482,7 @@ size_t dyna_distill_workspace_bytes(int32_t N, int32_t V);
  *   tail 1: p_k = exp(values) (log-probabilities of the teacher's whole row);
  *           + p_r (log p_r - log q_r), p_r = max(0, 1 - sum p_k) and q_r the
  *           student's probability outside the list.
- *  logits         device, dtype, row r is V elements at r * row_stride, any alignment
+ *  logits         device, dtype, row r is V <= 2^20 elements at r * row_stride, any alignment
  *  out_loss [N]   device fp32 (not weighted)
  *  out_stats [N, 2] device fp64, may be NULL: log sum exp(z / temperature) over all
  *                 tokens and over those outside the list, for dyna_distill_grad

@@ -210,13 +210,20 @@ struct Weigher {
 };
 constexpr double k16Log2e = 16.0 * 1.4426950408889634074;
 
+// 2^(j / 16), j < 16.
+__device__ const double kWeightTable[16] = {
+    1.0,                  0x1.0b5586cf9890fp+0, 0x1.172b83c7d517bp+0, 0x1.2387a6e756238p+0,
+    0x1.306fe0a31b715p+0, 0x1.3dea64c123422p+0, 0x1.4bfdad5362a27p+0, 0x1.5ab07dd485429p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.7a11473eb0187p+0, 0x1.8ace5422aa0dbp+0, 0x1.9c49182a3f090p+0,
+    0x1.ae89f995ad3adp+0, 0x1.c199bdd85529cp+0, 0x1.d5818dcfba487p+0, 0x1.ea4afa2a490dap+0};
+
 // Fills the table by the first lanes of a workgroup, or of every wave with a
 // table of its own; a barrier, or the wave's LDS order, has to follow.
 __device__ __forceinline__ void fill_weight_table(double* table) {
-    if (threadIdx.x < 16) table[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
+    if (threadIdx.x < 16) table[threadIdx.x] = kWeightTable[threadIdx.x];
 }
 __device__ __forceinline__ void fill_wave_table(double* table) {
-    if (lane_id() < 16) table[lane_id()] = exp2((double)lane_id() / 16.0);
+    if (lane_id() < 16) table[lane_id()] = kWeightTable[lane_id()];
     wave_lds_order();
 }
 

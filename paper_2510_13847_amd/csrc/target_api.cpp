@@ -10,7 +10,7 @@
 namespace dyna {
 namespace {
 
-constexpr int32_t kMaxVocab = 1 << 21;
+constexpr int32_t kMaxVocab = 1 << 20;
 constexpr int64_t kMaxBlocks = 1 << 23;  // workgroups of 256 threads in one launch: below 2^32 threads
 
 bool valid_dtype(int32_t t) { return t == DYNA_F32 || t == DYNA_BF16; }

@@ -20,6 +20,8 @@ namespace {
 
 constexpr int kVT = 256;  // threads of every kernel here
 constexpr int kNoSlot = INT32_MIN;
+// Chunks of all requests from which on a wave takes four of them.
+constexpr int kManyChunks = 16384;
 
 // ---------------------------------------------------------------- inputs
 __device__ __forceinline__ int chain_len(const VerifyArgs& a, int b) {
@@ -141,9 +143,11 @@ __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
         const int len = chain_len(a, b);
         if (j > len || (j == len && !a.greedy)) return;
     } else if (!a.greedy) {
-        int kid = 0;
-        for (int i = j + 1 + (int)threadIdx.x; i < a.N; i += kVT) kid |= node_parent(a, b, i) == j;
-        if (!__syncthreads_or(kid)) return;
+        // every wave looks for itself: most rows of a tree are leaves, and their
+        // workgroups leave without a barrier
+        bool kid = false;
+        for (int i = j + 1 + lane_id(); i < a.N; i += kWave) kid |= node_parent(a, b, i) == j;
+        if (!__any(kid)) return;
     }
     const int v1 = min(a.V, (part + 1) * a.split_len);
     const T* x = row_ptr<T>(a, b, j);
@@ -180,6 +184,7 @@ __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
 struct WalkLds {
     double p[DYNA_MAX_NODES];     // target probability of the node's token in its parent's row
     double sum[DYNA_MAX_NODES];
+    double bar[DYNA_MAX_NODES];
     float top[DYNA_MAX_NODES];
     float z[DYNA_MAX_NODES];      // the token's logit there
     int32_t best[DYNA_MAX_NODES];
@@ -207,6 +212,13 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
         w.token[j] = x;
         w.parent[j] = par;
         w.z[j] = x >= 0 && par >= 0 ? clean(to_f32(row_ptr<T>(a, b, par)[x])) : kNegInf;
+        // what p has to pass: u q(x), or u alone for a token proposed outright
+        double bar = 0.0;
+        if (!a.greedy && j > 0) {
+            bar = (double)a.uniforms[(int64_t)b * N + (a.chain ? j - 1 : j)];
+            if (a.chain && x >= 0 && st.s[j - 1].logits != nullptr) bar *= exp((double)st.s[j - 1].logprobs[b]);
+        }
+        w.bar[j] = bar;
     }
     __syncthreads();
     // 16 lanes join a row's parts (what stands in place of parts that were not
@@ -268,14 +280,12 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
             if (a.greedy) {
                 ok = x == w.best[par];
             } else if (a.chain) {
-                const dyna_draft_step& d = st.s[j - 1];
-                const double q = d.logits != nullptr ? exp((double)d.logprobs[b]) : 1.0;
-                ok = (double)a.uniforms[(int64_t)b * N + j - 1] * q < w.p[j];
+                ok = w.bar[j] < w.p[j];
             } else {
                 double mass = 1.0;
 #pragma unroll 8
                 for (int i = par + 1; i < j; ++i) mass -= w.parent[i] == par ? w.p[i] : 0.0;
-                ok = (double)a.uniforms[(int64_t)b * N + j] * mass < w.p[j];
+                ok = w.bar[j] * mass < w.p[j];
             }
         }
         w.stands[j] = ok;
@@ -379,50 +389,58 @@ __device__ __forceinline__ int pick_clusters(const VerifyArgs& a, const dyna_dra
 // ended in.  Behind them, workgroups: the same of kWaves chunks of the rejected
 // draft's row; and one that writes where each selected cluster's slots start,
 // for the steps whose chunks are read again.
-template <typename T>
+template <typename T, int CW>
 __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int n_pieces,
                                                          int per) {
     __shared__ double table[kWaves][16];
     __shared__ uint32_t bits[kWaves][kChunk / 32];
-    __shared__ int tmp_i[kWaves + 1];
+    __shared__ int tmp_i[kWaves + 1], tokens;
     extern __shared__ uint32_t picked[];  // [M / 32]
     const int b = blockIdx.x / per, g = blockIdx.x % per, t = threadIdx.x, wave = t / kWave, lane = lane_id();
     const WalkEnd e = a.ends[b];
     fill_wave_table(table[wave]);
     if (g < chunk_groups) {
-        const int c = g * kWaves + wave;
-        if (c >= a.n_chunks) return;
         const Weigher weight{table[wave], a.inv_t * k16Log2e};
-        const int v0 = c * kChunk, v = v0 + lane * 8;
-        float z[8];
-        load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
+        const T* row = row_ptr<T>(a, b, e.node);
+        const int c0 = (g * kWaves + wave) * CW;
+        float z[CW][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
-        const float m = wave_max_all(max8(z));
-        double all = 0.0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) all += weight(z[i], m);
-        all = wave_sum_f64(all);
-        double ex = all;
-        if (e.mode == kDrawTarget) {
-            // the sum without the rejected tokens is taken apart: a difference
-            // would be rounding alone where they hold the chunk's weight
-            mark_rejected(a, st, b, e, v0, bits[wave]);
-            const uint32_t out = marks8(bits[wave], lane * 8);
-            if (__any(out != 0)) {
-                ex = 0.0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ex += (out >> i) & 1u ? 0.0 : weight(z[i], m);
-                ex = wave_sum_f64(ex);
-            }
+        for (int k = 0; k < CW; ++k) {
+            const int v = (c0 + k) * kChunk + lane * 8;
+            load_part(row + v, a.V - v, kNegInf, z[k]);
         }
-        if (lane == 0) a.chunks[(int64_t)b * a.n_chunks + c] = ChunkPart{all, ex, m, 0.0f};
+#pragma unroll
+        for (int k = 0; k < CW; ++k) {
+            const int c = c0 + k;
+            if (c >= a.n_chunks) return;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[k][i] = clean(z[k][i]);
+            const float m = wave_max_all(max8(z[k]));
+            double all = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) all += weight(z[k][i], m);
+            all = wave_sum_f64(all);
+            double ex = all;
+            if (e.mode == kDrawTarget) {
+                // the sum without the rejected tokens is taken apart: a difference
+                // would be rounding alone where they hold the chunk's weight
+                mark_rejected(a, st, b, e, c * kChunk, bits[wave]);
+                const uint32_t out = marks8(bits[wave], lane * 8);
+                if (__any(out != 0)) {
+                    ex = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ex += (out >> i) & 1u ? 0.0 : weight(z[k][i], m);
+                    ex = wave_sum_f64(ex);
+                }
+            }
+            if (lane == 0) a.chunks[(int64_t)b * a.n_chunks + c] = ChunkPart{all, ex, m, 0.0f};
+        }
         return;
     }
     if (e.mode != kDrawResidual) return;
     const dyna_draft_step& d = st.s[e.node];
     int len = d.cap;
-    if (d.clusters != nullptr) len = min(d.cap, pick_clusters<kVT>(a, d, b, picked, tmp_i));
+    if (d.clusters != nullptr) len = min(d.cap, pick_clusters<kVT>(a, d, b, picked, &tokens));
     const int piece = (g - chunk_groups) * kWaves + wave;
     if (g - chunk_groups < (n_pieces + kWaves - 1) / kWaves) {
         if (piece >= n_pieces) return;
@@ -460,6 +478,7 @@ struct Drawn {
     float m;           // target row: largest logit
     double all;        // sum of exp((z - m) / T)
     double inv_all;
+    double ex;         // the same without the rejected tokens
     float qm;          // draft row
     double q_in;       // (1 - beta) / its sum, 0 without one
     double q_out;      // probability of a token off the shortlist
@@ -469,23 +488,30 @@ struct Drawn {
 template <int NT>
 struct JoinLds {
     float f[2][NT / kWave];
-    double d[2][NT / kWave];
+    double d[3][NT / kWave];
 };
 
-// Joins the chunks' pieces, and the draft row's when `residual`.
+// Joins the chunks' pieces, and the draft row's when `residual`; weights, where
+// given, receives each chunk's sum (without the rejected tokens for a draw from
+// the target) relative to the row's largest logit.
 template <int NT>
 __device__ __forceinline__ Drawn join_parts(const VerifyArgs& a, const StepTable& st, int b, const WalkEnd& e,
-                                            bool residual, int n_pieces, const double* table, JoinLds<NT>& w) {
+                                            int n_pieces, const double* table, JoinLds<NT>& w,
+                                            double* weights = nullptr) {
+    const bool residual = e.mode == kDrawResidual;
     const ChunkPart* p = a.chunks + (int64_t)b * a.n_chunks;
-    const dyna_draft_step& d = st.s[residual ? e.node : 0];
     const DraftPart* q = a.pieces + (int64_t)b * a.n_pieces;
     const int t = threadIdx.x, wave = t / kWave;
+    // the first piece of each thread stays in registers: there are rarely more
+    const ChunkPart none{0.0, 0.0, kNegInf, 0.0f};
+    const ChunkPart p0 = t < a.n_chunks ? p[t] : none;
+    const DraftPart q0 = residual && t < n_pieces ? q[t] : DraftPart{0.0, kNegInf, 0};
     Drawn r{};
     r.len = residual ? q[0].len : 0;
-    const int nq = min(n_pieces, (r.len + kChunk - 1) / kChunk);
-    float m = kNegInf, qm = kNegInf;
-    for (int c = t; c < a.n_chunks; c += NT) m = fmaxf(m, p[c].m);
-    for (int i = t; i < nq; i += NT) qm = fmaxf(qm, q[i].m);
+    float m = p0.m, qm = q0.m;
+    for (int c = t + NT; c < a.n_chunks; c += NT) m = fmaxf(m, p[c].m);
+    if (residual)
+        for (int i = t + NT; i < n_pieces; i += NT) qm = fmaxf(qm, q[i].m);
     m = wave_max_all(m);
     qm = wave_max_all(qm);
     if (lane_id() == 0) {
@@ -500,29 +526,42 @@ __device__ __forceinline__ Drawn join_parts(const VerifyArgs& a, const StepTable
         r.qm = fmaxf(r.qm, w.f[1][i]);
     }
     const Weigher weight{table, a.inv_t * k16Log2e};
-    double s = 0.0, x = 0.0;
-    for (int c = t; c < a.n_chunks; c += NT) s += p[c].all * weight(p[c].m, r.m);
+    double s = 0.0, y = 0.0, x = 0.0;
+    for (int c = t; c < a.n_chunks; c += NT) {
+        const ChunkPart& pc = c == t ? p0 : p[c];
+        const double f = weight(pc.m, r.m);
+        s += pc.all * f;
+        y += pc.ex * f;
+        if (weights) weights[c] = (residual ? pc.all : pc.ex) * f;
+    }
     s = wave_sum_f64(s);
+    y = wave_sum_f64(y);
     if (residual) {
-        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-        for (int i = t; i < nq; i += NT) x += q[i].s * wq(q[i].m, r.qm);
+        const Weigher wq{table, 1.0 / (double)st.s[e.node].temperature * k16Log2e};
+        for (int i = t; i < n_pieces; i += NT) {
+            const DraftPart& qi = i == t ? q0 : q[i];
+            x += qi.s * wq(qi.m, r.qm);
+        }
         x = wave_sum_f64(x);
     }
     if (lane_id() == 0) {
         w.d[0][wave] = s;
         w.d[1][wave] = x;
+        w.d[2][wave] = y;
     }
     __syncthreads();
-    s = x = 0.0;
+    s = x = y = 0.0;
 #pragma unroll
     for (int i = 0; i < NT / kWave; ++i) {
         s += w.d[0][i];
         x += w.d[1][i];
+        y += w.d[2][i];
     }
     r.all = s;
+    r.ex = y;
     r.inv_all = s > 0.0 ? 1.0 / s : 0.0;
     if (residual) {
-        const double beta = r.len < a.V ? (double)d.tail_beta : 0.0;
+        const double beta = r.len < a.V ? (double)st.s[e.node].tail_beta : 0.0;
         r.q_in = x > 0.0 ? (1.0 - beta) / x : 0.0;
         r.q_out = beta > 0.0 ? beta / (double)(a.V - r.len) : 0.0;
     }
@@ -566,7 +605,7 @@ __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable s
             }
         }
     }
-    const Drawn r = join_parts<kVT>(a, st, b, e, true, n_pieces, table, w);  // its barriers order the table
+    const Drawn r = join_parts<kVT>(a, st, b, e, n_pieces, table, w);  // its barriers order the table
     const Weigher weight{table, a.inv_t * k16Log2e}, wq{table, 1.0 / (double)d.temperature * k16Log2e};
     double s = 0.0;
 #pragma unroll
@@ -594,20 +633,21 @@ constexpr double kFixOne = 0x1p62;
 // the additions in LDS does not matter.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces, int entries) {
+    constexpr int kW = NT / kWave;
     __shared__ double table[16];
     __shared__ JoinLds<NT> w;
-    __shared__ double sums[NT / kWave];
-    __shared__ int tmp_i[NT / kWave + 1], tmp_j[NT / kWave + 1];
-    __shared__ int hit, last;
-    __shared__ double before;
+    __shared__ double sums[kW], before[kW];
+    __shared__ int tmp_i[kW + 1], tokens;
+    __shared__ int first_of[kW], last_of[kW];  // each wave's first chunk past the goal and last one of weight
     __shared__ uint32_t bits[kChunk / 32];
     extern __shared__ char lds[];
-    const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks;
-    double* chunk_w = reinterpret_cast<double*>(lds);                       // [n]
-    int* list_slot = reinterpret_cast<int*>(chunk_w + n);                   // [entries] first slot
-    int* list_row = list_slot + entries;                                    // [entries] first layout row
-    int* list_id = list_row + entries;                                      // [entries] cluster
-    uint32_t* picked = reinterpret_cast<uint32_t*>(list_id + entries);      // [M / 32]
+    const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks, wave = t / kWave;
+    double* chunk_w = reinterpret_cast<double*>(lds);                             // [n]
+    unsigned long long* taken = reinterpret_cast<unsigned long long*>(chunk_w + n);  // [n] if entries
+    int* list_slot = reinterpret_cast<int*>(taken + (entries ? n : 0));           // [entries] first slot
+    int* list_row = list_slot + entries;                                          // [entries] first layout row
+    int* list_id = list_row + entries;                                            // [entries] cluster
+    uint32_t* picked = reinterpret_cast<uint32_t*>(list_id + entries);            // [M / 32]
     const WalkEnd e = a.ends[b];
     fill_weight_table(table);
     const Weigher weight{table, a.inv_t * k16Log2e};
@@ -615,9 +655,9 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     const dyna_draft_step& d = st.s[residual ? e.node : 0];
     const bool listed = residual && step_listed(d, a.B, a.M);
     const double u = (double)a.uniforms[(int64_t)b * a.N + (a.chain ? a.N - 1 : 0)];
-    if (t == 0) hit = n, last = -1;
-    for (int c = t; c < n; c += NT) chunk_w[c] = 0.0;  // all bits 0: also the whole multiples' zero
-    const Drawn r = join_parts<NT>(a, st, b, e, residual, n_pieces, table, w);
+    if (listed)
+        for (int c = t; c < n; c += NT) taken[c] = 0;
+    const Drawn r = join_parts<NT>(a, st, b, e, n_pieces, table, w, chunk_w);
     const ChunkPart* p = a.chunks + (int64_t)b * n;
     const int64_t o = (int64_t)b * a.N + e.depth;
     if (!(r.all > 0.0)) {  // no token the target allows
@@ -629,130 +669,174 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     }
     const T* row = row_ptr<T>(a, b, e.node);
     const float* zq = d.logits + (int64_t)b * d.cap;
-    int n_list = 0;
+    int n_list = 0, rounds = 0;  // entries, and steps of a search among them
     if (listed) {
-        // selected clusters in ascending id with their first slots
-        pick_clusters<NT>(a, d, b, picked, tmp_i);
-        __syncthreads();
+        // selected clusters in ascending id with their first slots: one scan
+        // carries the entries (high half) and their tokens
+        pick_clusters<NT>(a, d, b, picked, &tokens);
         int slots = 0;
         for (int m0 = 0; m0 < a.M; m0 += NT) {
             const int m = m0 + t;
             const bool in = m < a.M && ((picked[m >> 5] >> (m & 31)) & 1u);
             const int o0 = in ? a.offsets[m] : 0, size = in ? a.offsets[m + 1] - o0 : 0;
-            int total = 0, count = 0;
-            const int at = block_exclusive_scan<NT>(size, tmp_i, &total);
-            const int i = block_exclusive_scan<NT>(in, tmp_j, &count);
+            // in a listed step all tokens together are at most kListedSlots = 2^15
+            int total = 0;
+            const int at = block_exclusive_scan<NT>(in ? (1 << 16) + size : 0, tmp_i, &total);
             if (in) {
-                list_slot[n_list + i] = slots + at;
-                list_row[n_list + i] = o0;
-                list_id[n_list + i] = m;
+                const int i = n_list + (at >> 16);
+                list_slot[i] = slots + (at & 0xffff);
+                list_row[i] = o0;
+                list_id[i] = m;
             }
-            slots += total;
-            n_list += count;
+            slots += total & 0xffff;
+            n_list += total >> 16;
         }
         __syncthreads();
+        while ((1 << rounds) < n_list) ++rounds;
         const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-        long long* change = reinterpret_cast<long long*>(chunk_w);
-#pragma unroll 4
-        for (int s = t; s < r.len; s += NT) {
-            int lo = 0, hi = n_list;  // the last entry with list_slot <= s
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (list_slot[mid] <= s) lo = mid;
-                else hi = mid;
+        constexpr int kAhead = 8;  // slots of a thread whose loads are in flight together
+        for (int s0 = t; s0 < r.len; s0 += kAhead * NT) {
+            int v[kAhead], at[kAhead];
+            float z[kAhead], y[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) at[i] = 0;
+            // the last entry whose first slot is at or before s
+            for (int k = rounds - 1; k >= 0; --k) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int mid = at[i] + (1 << k);
+                    at[i] = mid < n_list && list_slot[min(mid, n_list - 1)] <= min(s0 + i * NT, r.len - 1) ? mid : at[i];
+                }
             }
-            const int v = a.perm[list_row[lo] + s - list_slot[lo]];
-            if (v < 0 || v >= a.V) continue;
-            const double pv = weight(clean(to_f32(row[v])), r.m) * r.inv_all;
-            const double qv = r.q_in * wq(clean(zq[s]), r.qm);
-            atomicAdd(reinterpret_cast<unsigned long long*>(&change[v / kChunk]),
-                      (unsigned long long)(long long)(fmin(pv, qv) * kFixOne));
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int s = min(s0 + i * NT, r.len - 1);
+                v[i] = a.perm[list_row[at[i]] + s - list_slot[at[i]]];
+                y[i] = zq[s];
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                v[i] = s0 + i * NT < r.len && v[i] >= 0 && v[i] < a.V ? v[i] : -1;
+                z[i] = to_f32(row[max(v[i], 0)]);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (!__any(v[i] >= 0)) break;
+                const double pv = weight(clean(z[i]), r.m) * r.inv_all;
+                const double qv = r.q_in * wq(clean(y[i]), r.qm);
+                if (v[i] >= 0)
+                    atomicAdd(&taken[v[i] / kChunk], (unsigned long long)(long long)(fmin(pv, qv) * kFixOne));
+            }
         }
         __syncthreads();
     }
-    // a thread's chunks are consecutive; their weights stay in LDS
+    // a thread's chunks are consecutive
     const int each = (n + NT - 1) / NT, c0 = min(n, t * each), c1 = min(n, c0 + each);
-    auto weigh_chunks = [&](bool from_residual, bool without) {
-        double s = 0.0;
-        for (int c = c0; c < c1; ++c) {
-            double x;
-            if (from_residual && !listed) {
-                x = a.left[(int64_t)b * n + c];
+    if (each > 1) __syncthreads();  // their weights come from other threads
+    double mine = 0.0, total;
+    for (int c = c0; c < c1; ++c) {
+        double x = chunk_w[c];
+        if (residual) {
+            if (listed) {
+                x *= r.inv_all;
+                const double kept = x - (double)(long long)taken[c] / kFixOne;
+                x = kept > x * kRounding ? kept : 0.0;
             } else {
-                x = (without ? p[c].ex : p[c].all) * weight(p[c].m, r.m);
-                if (from_residual) {
-                    x *= r.inv_all;
-                    const double kept = x - (double)__builtin_bit_cast(long long, chunk_w[c]) / kFixOne;
-                    x = kept > x * kRounding ? kept : 0.0;
-                }
+                x = a.left[(int64_t)b * n + c];
             }
             chunk_w[c] = x;
-            s += x;
         }
-        return s;
-    };
-    double total, run;
+        mine += x;
+    }
+    double run = block_scan_f64<NT>(mine, sums, &total);
     bool without = !residual;
-    run = block_scan_f64<NT>(weigh_chunks(residual, without), sums, &total);
-    if (residual ? !(total > kNothing) : !(total > 0.0)) {  // from p itself
+    if (residual ? !(total > kNothing) : !(total > 0.0)) {  // nothing left: from p itself
         residual = without = false;
-        run = block_scan_f64<NT>(weigh_chunks(false, false), sums, &total);
+        mine = 0.0;
+        for (int c = c0; c < c1; ++c) mine += chunk_w[c] = p[c].all * weight(p[c].m, r.m);
+        run = block_scan_f64<NT>(mine, sums, &total);
     }
     const double goal = u * total;
     {
-        double f = run;
-        int first = n, lastc = -1;
+        double f = run, f_at = 0.0, f_last = 0.0;
+        int first = INT32_MAX, lastc = -1;
         for (int c = c0; c < c1; ++c) {
             const double x = chunk_w[c];
-            f += x;
             if (x > 0.0) {
                 lastc = c;
-                if (f > goal && first == n) first = c;
+                f_last = f;
+                if (f + x > goal && first == INT32_MAX) {
+                    first = c;
+                    f_at = f;
+                }
             }
+            f += x;
         }
-        if (first < n) atomicMin(&hit, first);
-        if (lastc >= 0) atomicMax(&last, lastc);
-    }
-    __syncthreads();
-    const int chunk = hit < n ? hit : last;
-    if (chunk >= c0 && chunk < c1) {
-        double f = run;
-        for (int c = c0; c < chunk; ++c) f += chunk_w[c];
-        before = f;
+        const uint64_t hits = __ballot(first != INT32_MAX), some = __ballot(lastc >= 0);
+        const int lane = hits ? __builtin_ctzll(hits) : some ? 63 - __builtin_clzll(some) : 0;
+        if (lane_id() == lane) {
+            first_of[wave] = first;
+            last_of[wave] = lastc;
+            before[wave] = first != INT32_MAX ? f_at : f_last;
+        }
     }
     __syncthreads();
     if (t >= kWave) return;
+    // rounding can leave the last cumulative sum at or below the goal: then the
+    // last chunk with any weight
+    int from = -1;
+    for (int i = 0; i < kW && from < 0; ++i)
+        if (first_of[i] != INT32_MAX) from = i;
+    const bool past = from >= 0;
+    for (int i = kW - 1; i >= 0 && from < 0; --i)
+        if (last_of[i] >= 0) from = i;
+    from = max(from, 0);
+    const int chunk = past ? first_of[from] : max(last_of[from], 0);
+    const double base = before[from];
     // the chunk's tokens, eight to a lane.  Weights inside it are relative to
     // its own largest logit, as when its sum was taken: a chunk of weight holds
     // a token of weight
-    const double base = before;
     const int v0 = chunk * kChunk, v = v0 + t * 8;
     float z[8];
     load_part(row + v, a.V - v, kNegInf, z);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
     double x[8], scale = 1.0;
     if (residual) {
-        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+        int slot[8];
+        if (listed) {
+            int m[8], j[8], at[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int slot = -1;
-            if (v + i < a.V) {
-                if (listed) {
-                    const int m = a.token_rows[2 * (int64_t)(v + i)], j = a.token_rows[2 * (int64_t)(v + i) + 1];
-                    int lo = 0, hi = n_list;  // the last entry with list_id <= m
-                    while (hi - lo > 1) {
-                        const int mid = (lo + hi) >> 1;
-                        if (list_id[mid] <= m) lo = mid;
-                        else hi = mid;
-                    }
-                    if (n_list > 0 && list_id[lo] == m) slot = list_slot[lo] + j - list_row[lo];
-                } else {
-                    slot = streamed_slot(a, d, b, v + i);
+            for (int i = 0; i < 8; ++i) {
+                const int64_t k = 2 * (int64_t)min(v + i, a.V - 1);
+                m[i] = a.token_rows[k];
+                j[i] = a.token_rows[k + 1];
+                at[i] = 0;
+            }
+            for (int k = rounds - 1; k >= 0; --k) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int mid = at[i] + (1 << k);
+                    at[i] = mid < n_list && list_id[min(mid, n_list - 1)] <= m[i] ? mid : at[i];
                 }
             }
-            const double q = slot >= 0 && slot < r.len ? r.q_in * wq(clean(zq[slot]), r.qm) : r.q_out;
-            x[i] = fmax(weight(z[i], r.m) * r.inv_all - q, 0.0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                slot[i] = n_list > 0 && list_id[at[i]] == m[i] ? list_slot[at[i]] + j[i] - list_row[at[i]] : -1;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) slot[i] = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
+        }
+        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = slot[i] >= 0 && slot[i] < r.len;
+            y[i] = in ? zq[slot[i]] : 0.0f;
+            slot[i] = in ? 1 : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const double q = slot[i] ? r.q_in * wq(clean(y[i]), r.qm) : r.q_out;
+            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q, 0.0);
         }
     } else {
         if (without) mark_rejected(a, st, b, e, v0, bits);
@@ -760,9 +844,9 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
         const float top = p[chunk].m;
         scale = weight(top, r.m);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (out >> i) & 1u ? 0.0 : weight(z[i], top);
+        for (int i = 0; i < 8; ++i) x[i] = (out >> i) & 1u ? 0.0 : weight(clean(z[i]), top);
     }
-    double mine = 0.0;
+    mine = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) mine += x[i];
     double f = wave_scan_f64(mine) - mine;
@@ -775,8 +859,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
             if (base + scale * f > goal && first < 0) first = i;
         }
     }
-    // rounding can leave the last cumulative sum at or below the goal: then the
-    // last token with any weight
+    // as above: the last token with any weight where no sum passes the goal
     const uint64_t hits = __ballot(first >= 0), some = __ballot(lastv >= 0);
     const int lane = hits ? __builtin_ctzll(hits) : some ? 63 - __builtin_clzll(some) : 0;
     if (t == lane) {
@@ -786,7 +869,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
             float zx = kNegInf;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (k == i) zx = z[k];
+                if (k == i) zx = clean(z[k]);
             a.out_logprobs[o] = (float)(((double)zx - (double)r.m) * a.inv_t - log(r.all));
         }
     }
@@ -814,16 +897,24 @@ dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hi
     row_parts_kernel<T><<<(uint32_t)((int64_t)a.B * a.N * a.splits), kVT, 0, s>>>(a);
     walk_kernel<T><<<a.B, kVT, 0, s>>>(a, st);
     if (a.greedy) return check_launch("verify");
-    const int groups = (a.n_chunks + kWaves - 1) / kWaves;
     const bool clusters = q.pieces > 0 && a.M > 0;
-    const int per = groups + (q.pieces + kWaves - 1) / kWaves + (clusters && q.streamed ? 1 : 0);
     const uint32_t set = clusters ? 4u * (uint32_t)((a.M + 31) / 32) : 0u;
-    draw_parts_kernel<T><<<(uint32_t)((int64_t)a.B * per), kVT, set, s>>>(a, st, groups, q.pieces, per);
+    const int extra = (q.pieces + kWaves - 1) / kWaves + (clusters && q.streamed ? 1 : 0);
+    auto parts = [&](auto chunks_per_wave) {
+        constexpr int CW = decltype(chunks_per_wave)::value;
+        const int groups = (a.n_chunks + kWaves * CW - 1) / (kWaves * CW), per = groups + extra;
+        draw_parts_kernel<T, CW><<<(uint32_t)((int64_t)a.B * per), kVT, set, s>>>(a, st, groups, q.pieces, per);
+    };
+    if ((int64_t)a.B * a.n_chunks >= kManyChunks) parts(std::integral_constant<int, 4>{});
+    else parts(std::integral_constant<int, 1>{});
+    const int groups = (a.n_chunks + kWaves - 1) / kWaves;
     if (q.streamed)
         residual_kernel<T><<<(uint32_t)((int64_t)a.B * groups), kVT, 0, s>>>(a, st, groups, q.pieces);
-    const uint32_t lds = 8u * (uint32_t)a.n_chunks + 12u * (uint32_t)q.entries + (q.entries ? set : 0u);
-    if (q.entries) draw_kernel<T, 1024><<<a.B, 1024, lds, s>>>(a, st, q.pieces, q.entries);
-    else draw_kernel<T, 256><<<a.B, 256, lds, s>>>(a, st, q.pieces, 0);
+    const uint32_t each = 8u * (uint32_t)a.n_chunks;
+    if (q.entries)
+        draw_kernel<T, 1024><<<a.B, 1024, 2 * each + 12u * (uint32_t)q.entries + set, s>>>(a, st, q.pieces, q.entries);
+    else
+        draw_kernel<T, 256><<<a.B, 256, each, s>>>(a, st, q.pieces, 0);
     return check_launch("verify");
 }
 
