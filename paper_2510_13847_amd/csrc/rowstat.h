@@ -191,8 +191,12 @@ struct Weigher {
     const double* table;  // LDS [16]
     double c;             // 16 log2(e) / T
     __device__ __forceinline__ double operator()(float z, float m) const {
-        // a masked z (or a chunk without any) gives 2^-1100, which is 0
-        double y = fmax(((double)z - (double)m) * c, -17600.0);
+        return power(((double)z - (double)m) * c);
+    }
+    // 2^(y / 16); a masked z (or a row of nothing else) makes y -inf or NaN,
+    // here 2^-1100, which is 0
+    __device__ __forceinline__ double power(double y) const {
+        y = fmax(y, -17600.0);
         const double magic = 0x1.8p52;
         const double t = y + magic;
         const int k = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);

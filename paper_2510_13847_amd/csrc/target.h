@@ -41,6 +41,11 @@ struct DraftPart {
     int32_t len;  // the row's shortlist length
 };
 
+struct ListedCluster {
+    int32_t slot;  // first slot
+    int32_t row;   // first layout row
+};
+
 struct StepTable {
     dyna_draft_step s[DYNA_MAX_STEPS];
 };
@@ -80,22 +85,23 @@ struct VerifyArgs {
     int32_t n_pieces;
     DraftPart* pieces;       // [B, n_pieces]
     int32_t* slot_of;        // [B, M] first slot less first layout row of a selected cluster
+    ListedCluster* list;     // [B, list_stride] selected clusters in ascending id
+    int32_t* list_len;       // [B]
+    int32_t list_stride;
 };
 
 size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a, void* ws);
 // What a call's steps need of the drawing kernels.
 struct DrawNeeds {
     int32_t pieces = 0;    // kChunk slots of the longest draft row; 0: no step has draft logits
-    int32_t entries = 0;   // most clusters a step's list can name, among the steps that `listed` holds for
-    bool streamed = false; // a step whose chunks are read again (not `listed`)
+    int32_t entries = 0;   // most clusters a step's list can name, among the steps that step_listed holds for
+    bool streamed = false; // a step whose chunks are read again
 };
-// A step whose shortlist is short enough for one workgroup to go through, and
-// without a tail mixture, so that tokens off it keep their p.
+// A step whose shortlist is short enough for one workgroup to go through.
 constexpr int kListedSlots = 32768, kListedClusters = 2048;
 __host__ __device__ inline bool step_listed(const dyna_draft_step& d, int32_t B, int32_t M) {
     const int64_t named = (int64_t)(d.shared ? B : 1) * d.k;
-    return d.clusters != nullptr && d.tail_beta == 0.0f && d.cap <= kListedSlots &&
-           (named < M ? named : M) <= kListedClusters;
+    return d.clusters != nullptr && d.cap <= kListedSlots && (named < M ? named : M) <= kListedClusters;
 }
 dyna_status launch_token_rows(const int32_t* perm, const int32_t* offsets, int32_t V, int32_t M, int32_t* token_rows,
                               hipStream_t stream);

@@ -199,15 +199,15 @@ struct WalkLds {
 // One workgroup per request.  Whether a draft stands, once its siblings before
 // it have fallen, does not depend on the walk, so all are tested at once; the
 // walk then only follows the drafts that stand.
-template <typename T>
-__global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     __shared__ WalkLds w;
     const int b = blockIdx.x, t = threadIdx.x;
     const int N = a.N;
     const int len = a.chain ? chain_len(a, b) : N - 1;
     const Weigher weight{w.table, a.inv_t * k16Log2e};
     fill_weight_table(w.table);
-    for (int j = t; j < N; j += kVT) {
+    for (int j = t; j < N; j += NT) {
         const int x = j == 0 ? -1 : node_token(a, st, b, len, j), par = j == 0 ? -1 : node_parent(a, b, j);
         w.token[j] = x;
         w.parent[j] = par;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
     // 16 lanes join a row's parts (what stands in place of parts that were not
     // written is not used)
     constexpr int kTeam = 16;
-    for (int j0 = 0; j0 < N; j0 += kVT / kTeam) {
+    for (int j0 = 0; j0 < N; j0 += NT / kTeam) {
         const int j = j0 + t / kTeam, i0 = t % kTeam;
         const bool have = j < N && (a.chain ? (j < len || (j == len && a.greedy)) : true);
         const RowPart* p = a.parts + ((int64_t)b * N + (have ? j : 0)) * a.splits;
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
         }
     }
     __syncthreads();
-    for (int j = t; j < N; j += kVT) {
+    for (int j = t; j < N; j += NT) {
         const int x = w.token[j], par = w.parent[j];
         double p = 0.0;
         if (x >= 0 && par >= 0 && w.z[j] > kNegInf) {
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
         w.p[j] = p;
     }
     __syncthreads();
-    for (int j = t; j < N; j += kVT) {
+    for (int j = t; j < N; j += NT) {
         const int x = w.token[j], par = w.parent[j];
         bool ok = false;
         if (x >= 0 && par >= 0) {
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kVT) void walk_kernel(VerifyArgs a, StepTable st) {
     __syncthreads();
     const int depth = w.depth, node = w.node;
     const int64_t o = (int64_t)b * N;
-    for (int i = t; i < N; i += kVT) {
+    for (int i = t; i < N; i += NT) {
         int id = -1, at = -1;
         float lp = kNegInf;
         if (i < depth) {
@@ -385,18 +385,44 @@ __device__ __forceinline__ int pick_clusters(const VerifyArgs& a, const dyna_dra
     return *total;
 }
 
+template <int NT>
+__device__ __forceinline__ unsigned long long block_exclusive_scan_u64(unsigned long long x, unsigned long long* tmp,
+                                                                       unsigned long long* total) {
+    const int lane = lane_id();
+    unsigned long long inc = x;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const unsigned long long y = __shfl_up(inc, o, kWave);
+        if (lane >= o) inc += y;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) tmp[threadIdx.x / kWave] = inc;
+    __syncthreads();
+    unsigned long long base = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) {
+        if (w == (int)threadIdx.x / kWave) base = all;
+        all += tmp[w];
+    }
+    *total = all;
+    return base + inc - x;
+}
+
 // Per request, waves c < n_chunks: softmax pieces of a chunk of the row the walk
 // ended in.  Behind them, workgroups: the same of kWaves chunks of the rejected
 // draft's row; and one that writes where each selected cluster's slots start,
-// for the steps whose chunks are read again.
+// as a list, or by cluster for shortlists too long for one.
 template <typename T, int CW>
 __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int n_pieces,
                                                          int per) {
     __shared__ double table[kWaves][16];
     __shared__ uint32_t bits[kWaves][kChunk / 32];
-    __shared__ int tmp_i[kWaves + 1], tokens;
+    __shared__ unsigned long long tmp_u[kWaves];
+    __shared__ int tokens;
     extern __shared__ uint32_t picked[];  // [M / 32]
-    const int b = blockIdx.x / per, g = blockIdx.x % per, t = threadIdx.x, wave = t / kWave, lane = lane_id();
+    // the longest ones first
+    const int b = blockIdx.x / per, g = per - 1 - (int)(blockIdx.x % per), t = threadIdx.x, wave = t / kWave;
+    const int lane = lane_id();
     const WalkEnd e = a.ends[b];
     fill_wave_table(table[wave]);
     if (g < chunk_groups) {
@@ -458,19 +484,36 @@ __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable
         if (lane == 0) a.pieces[(int64_t)b * a.n_pieces + piece] = DraftPart{s, m, len};
         return;
     }
-    if (d.clusters == nullptr || step_listed(d, a.B, a.M)) return;
-    __syncthreads();
-    // consecutive clusters a round, so that offsets are read in order
-    int base = 0;
-    for (int m0 = 0; m0 < a.M; m0 += kVT) {
-        const int m = m0 + t;
-        const bool in = m < a.M && ((picked[m >> 5] >> (m & 31)) & 1u);
-        const int o0 = in ? a.offsets[m] : 0, size = in ? a.offsets[m + 1] - o0 : 0;
-        int total = 0;
-        const int at = block_exclusive_scan<kVT>(size, tmp_i, &total);
-        if (m < a.M) a.slot_of[(int64_t)b * a.M + m] = in ? base + at - o0 : kNoSlot;
-        base += total;
+    if (d.clusters == nullptr) return;
+    const bool listed = step_listed(d, a.B, a.M);
+    ListedCluster* list = a.list + (int64_t)b * a.list_stride;
+    // a thread takes the 32 clusters of a word of the set (M <= 8192: one word);
+    // one scan carries the clusters (high half) and their tokens
+    static_assert(DYNA_MAX_M <= 32 * kVT, "a word of the set to a thread");
+    const uint32_t mine = t < (a.M + 31) / 32 ? picked[t] : 0u;
+    unsigned long long sum = 0, total = 0;
+    for (uint32_t left = mine; left; left &= left - 1) {
+        const int m = t * 32 + __builtin_ctz(left);
+        sum += (1ull << 32) + (uint32_t)(a.offsets[m + 1] - a.offsets[m]);
     }
+    const unsigned long long at = block_exclusive_scan_u64<kVT>(sum, tmp_u, &total);
+    int n = (int)(at >> 32), slot = (int)(uint32_t)at;
+    for (uint32_t left = mine; left; left &= left - 1) {
+        const int m = t * 32 + __builtin_ctz(left), o0 = a.offsets[m];
+        if (listed) list[n++] = ListedCluster{slot, o0};
+        slot += a.offsets[m + 1] - o0;
+    }
+    if (!listed) {
+        slot = (int)(uint32_t)at;
+        for (int i = 0; i < 32 && t * 32 + i < a.M; ++i) {
+            const int m = t * 32 + i, o0 = a.offsets[m];
+            const bool in = (mine >> i) & 1u;
+            a.slot_of[(int64_t)b * a.M + m] = in ? slot - o0 : kNoSlot;
+            if (in) slot += a.offsets[m + 1] - o0;
+        }
+    }
+    n = (int)(total >> 32);
+    if (t == 0) a.list_len[b] = n;
 }
 
 // The two distributions of a residual, from their pieces.
@@ -576,8 +619,9 @@ __device__ __forceinline__ int streamed_slot(const VerifyArgs& a, const dyna_dra
     return s != kNoSlot ? s + j : -1;
 }
 
-// max(p - q, 0) chunk by chunk, for steps with a tail mixture, contiguous logits
-// or a long shortlist.
+// max(p - q, 0) chunk by chunk.  Long shortlists and contiguous logits take each
+// token's q; a listed step's tokens all take the tail's constant here, and the
+// drawing kernel puts the shortlist's right.
 template <typename T>
 __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable st, int per, int n_pieces) {
     __shared__ double table[16];
@@ -586,22 +630,25 @@ __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable s
     const WalkEnd e = a.ends[b];
     if (e.mode != kDrawResidual) return;
     const dyna_draft_step& d = st.s[e.node];
-    if (step_listed(d, a.B, a.M)) return;
+    const bool listed = step_listed(d, a.B, a.M);
+    if (listed && d.tail_beta == 0.0f) return;
     fill_weight_table(table);
     const int c = g * kWaves + (int)threadIdx.x / kWave, v = c * kChunk + lane_id() * 8;
     const float* zq = d.logits + (int64_t)b * d.cap;
-    const int len = a.pieces[(int64_t)b * a.n_pieces].len;
     float z[8], y[8];
     load_part(row_ptr<T>(a, b, e.node) + v, a.V - v, kNegInf, z);
     uint32_t in = 0;
+    if (!listed) {
+        const int len = a.pieces[(int64_t)b * a.n_pieces].len;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        y[i] = kNegInf;
-        if (v + i < a.V) {
-            const int slot = streamed_slot(a, d, b, v + i);
-            if (slot >= 0 && slot < len) {
-                y[i] = clean(zq[slot]);
-                in |= 1u << i;
+        for (int i = 0; i < 8; ++i) {
+            y[i] = kNegInf;
+            if (v + i < a.V) {
+                const int slot = streamed_slot(a, d, b, v + i);
+                if (slot >= 0 && slot < len) {
+                    y[i] = clean(zq[slot]);
+                    in |= 1u << i;
+                }
             }
         }
     }
@@ -627,27 +674,26 @@ constexpr double kFixOne = 0x1p62;
 // The draw: the chunk in which the cumulative weight passes u of the total,
 // then the token inside it.  One workgroup per request.
 //
-// A listed step's residual differs from p on its shortlist alone: a chunk keeps
-// its sum of p, and the shortlist's tokens, looked up slot by slot, take
-// min(p, q) from their chunks, as whole multiples of 2^-62 so that the order of
-// the additions in LDS does not matter.
+// A listed step's residual is known off its shortlist: a chunk's sum of p, or of
+// max(p - q_out, 0) with a tail.  The shortlist's tokens, slot by slot, change
+// their chunks by max(p - q, 0) - max(p - q_out, 0), without a tail -min(p, q),
+// as whole multiples of 2^-62, so that the order of the additions in LDS does
+// not matter.
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces, int entries) {
+__global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces) {
     constexpr int kW = NT / kWave;
     __shared__ double table[16];
     __shared__ JoinLds<NT> w;
     __shared__ double sums[kW], before[kW];
-    __shared__ int tmp_i[kW + 1], tokens;
     __shared__ int first_of[kW], last_of[kW];  // each wave's first chunk past the goal and last one of weight
     __shared__ uint32_t bits[kChunk / 32];
     extern __shared__ char lds[];
     const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks, wave = t / kWave;
     double* chunk_w = reinterpret_cast<double*>(lds);                             // [n]
-    unsigned long long* taken = reinterpret_cast<unsigned long long*>(chunk_w + n);  // [n] if entries
-    int* list_slot = reinterpret_cast<int*>(taken + (entries ? n : 0));           // [entries] first slot
-    int* list_row = list_slot + entries;                                          // [entries] first layout row
-    int* list_id = list_row + entries;                                            // [entries] cluster
-    uint32_t* picked = reinterpret_cast<uint32_t*>(list_id + entries);            // [M / 32]
+    // and, if entries: [n] changes, [kChunk] the drawn chunk's q, [entries] the list
+    unsigned long long* change = reinterpret_cast<unsigned long long*>(chunk_w + n);
+    double* chunk_q = reinterpret_cast<double*>(change + n);
+    ListedCluster* list = reinterpret_cast<ListedCluster*>(chunk_q + kChunk);
     const WalkEnd e = a.ends[b];
     fill_weight_table(table);
     const Weigher weight{table, a.inv_t * k16Log2e};
@@ -655,9 +701,15 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     const dyna_draft_step& d = st.s[residual ? e.node : 0];
     const bool listed = residual && step_listed(d, a.B, a.M);
     const double u = (double)a.uniforms[(int64_t)b * a.N + (a.chain ? a.N - 1 : 0)];
-    if (listed)
-        for (int c = t; c < n; c += NT) taken[c] = 0;
-    const Drawn r = join_parts<NT>(a, st, b, e, n_pieces, table, w, chunk_w);
+    int n_list = 0, rounds = 0;  // entries, and steps of a search among them
+    if (listed) {
+        n_list = a.list_len[b];
+        while ((1 << rounds) < n_list) ++rounds;
+        for (int i = t; i < n_list; i += NT) list[i] = a.list[(int64_t)b * a.list_stride + i];
+        for (int c = t; c < n; c += NT) change[c] = 0;
+        for (int i = t; i < kChunk; i += NT) chunk_q[i] = -1.0;  // off the shortlist
+    }
+    const Drawn r = join_parts<NT>(a, st, b, e, n_pieces, table, w, chunk_w);  // its barriers order what stands above
     const ChunkPart* p = a.chunks + (int64_t)b * n;
     const int64_t o = (int64_t)b * a.N + e.depth;
     if (!(r.all > 0.0)) {  // no token the target allows
@@ -669,63 +721,58 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     }
     const T* row = row_ptr<T>(a, b, e.node);
     const float* zq = d.logits + (int64_t)b * d.cap;
-    int n_list = 0, rounds = 0;  // entries, and steps of a search among them
-    if (listed) {
-        // selected clusters in ascending id with their first slots: one scan
-        // carries the entries (high half) and their tokens
-        pick_clusters<NT>(a, d, b, picked, &tokens);
-        int slots = 0;
-        for (int m0 = 0; m0 < a.M; m0 += NT) {
-            const int m = m0 + t;
-            const bool in = m < a.M && ((picked[m >> 5] >> (m & 31)) & 1u);
-            const int o0 = in ? a.offsets[m] : 0, size = in ? a.offsets[m + 1] - o0 : 0;
-            // in a listed step all tokens together are at most kListedSlots = 2^15
-            int total = 0;
-            const int at = block_exclusive_scan<NT>(in ? (1 << 16) + size : 0, tmp_i, &total);
-            if (in) {
-                const int i = n_list + (at >> 16);
-                list_slot[i] = slots + (at & 0xffff);
-                list_row[i] = o0;
-                list_id[i] = m;
+    constexpr int kAhead = 8;  // slots of a thread whose loads are in flight together
+    // tokens of the slots s0 + i NT, -1 past the row's length
+    auto tokens_at = [&](int s0, int (&v)[kAhead]) {
+        int at[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) at[i] = 0;
+        // the last entry whose first slot is at or before the slot
+        for (int k = rounds - 1; k >= 0; --k) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int mid = at[i] + (1 << k);
+                at[i] = mid < n_list && list[min(mid, n_list - 1)].slot <= min(s0 + i * NT, r.len - 1) ? mid : at[i];
             }
-            slots += total & 0xffff;
-            n_list += total >> 16;
         }
-        __syncthreads();
-        while ((1 << rounds) < n_list) ++rounds;
-        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-        constexpr int kAhead = 8;  // slots of a thread whose loads are in flight together
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const ListedCluster k = list[at[i]];
+            v[i] = a.perm[k.row + min(s0 + i * NT, r.len - 1) - k.slot];
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = s0 + i * NT < r.len && v[i] >= 0 && v[i] < a.V ? v[i] : -1;
+    };
+    int v_first[kAhead];  // of the first round, which rarely is not the last
+    if (listed) {
+        const double c = a.inv_t * k16Log2e, cq = 1.0 / (double)d.temperature * k16Log2e;
+        const Weigher wq{table, cq};
+        const double yp = 16.0 * log2(r.inv_all), yq = 16.0 * log2(r.q_in);
         for (int s0 = t; s0 < r.len; s0 += kAhead * NT) {
-            int v[kAhead], at[kAhead];
+            int v[kAhead];
             float z[kAhead], y[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) at[i] = 0;
-            // the last entry whose first slot is at or before s
-            for (int k = rounds - 1; k >= 0; --k) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int mid = at[i] + (1 << k);
-                    at[i] = mid < n_list && list_slot[min(mid, n_list - 1)] <= min(s0 + i * NT, r.len - 1) ? mid : at[i];
-                }
-            }
+            tokens_at(s0, v);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int s = min(s0 + i * NT, r.len - 1);
-                v[i] = a.perm[list_row[at[i]] + s - list_slot[at[i]]];
-                y[i] = zq[s];
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                v[i] = s0 + i * NT < r.len && v[i] >= 0 && v[i] < a.V ? v[i] : -1;
+                y[i] = zq[min(s0 + i * NT, r.len - 1)];
                 z[i] = to_f32(row[max(v[i], 0)]);
+                if (s0 == t) v_first[i] = v[i];
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (!__any(v[i] >= 0)) break;
-                const double pv = weight(clean(z[i]), r.m) * r.inv_all;
-                const double qv = r.q_in * wq(clean(y[i]), r.qm);
+                double off;
+                if (r.q_out == 0.0) {  // one exponential, of the smaller exponent
+                    const double ep = ((double)clean(z[i]) - (double)r.m) * c + yp;
+                    // (a draft row without any weight takes nothing)
+                    const double eq = r.q_in > 0.0 ? ((double)clean(y[i]) - (double)r.qm) * cq + yq : -__builtin_inf();
+                    off = -weight.power(fmin(ep, eq));
+                } else {
+                    const double pv = weight(clean(z[i]), r.m) * r.inv_all, qv = r.q_in * wq(clean(y[i]), r.qm);
+                    off = fmax(pv - qv, 0.0) - fmax(pv - r.q_out, 0.0);
+                }
                 if (v[i] >= 0)
-                    atomicAdd(&taken[v[i] / kChunk], (unsigned long long)(long long)(fmin(pv, qv) * kFixOne));
+                    atomicAdd(&change[v[i] / kChunk], (unsigned long long)(long long)(off * kFixOne));
             }
         }
         __syncthreads();
@@ -737,12 +784,10 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     for (int c = c0; c < c1; ++c) {
         double x = chunk_w[c];
         if (residual) {
+            x = listed && r.q_out == 0.0 ? x * r.inv_all : a.left[(int64_t)b * n + c];
             if (listed) {
-                x *= r.inv_all;
-                const double kept = x - (double)(long long)taken[c] / kFixOne;
+                const double kept = x + (double)(long long)change[c] / kFixOne;
                 x = kept > x * kRounding ? kept : 0.0;
-            } else {
-                x = a.left[(int64_t)b * n + c];
             }
             chunk_w[c] = x;
         }
@@ -781,7 +826,6 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
         }
     }
     __syncthreads();
-    if (t >= kWave) return;
     // rounding can leave the last cumulative sum at or below the goal: then the
     // last chunk with any weight
     int from = -1;
@@ -793,51 +837,50 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     from = max(from, 0);
     const int chunk = past ? first_of[from] : max(last_of[from], 0);
     const double base = before[from];
-    // the chunk's tokens, eight to a lane.  Weights inside it are relative to
-    // its own largest logit, as when its sum was taken: a chunk of weight holds
-    // a token of weight
     const int v0 = chunk * kChunk, v = v0 + t * 8;
+    // the chunk's tokens, eight to a lane of the first wave
     float z[8];
-    load_part(row + v, a.V - v, kNegInf, z);
+    if (t < kWave) load_part(row + v, a.V - v, kNegInf, z);
+    if (residual && listed) {
+        // the shortlist's tokens in this chunk, found as above
+        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
+        for (int s0 = t; s0 < r.len; s0 += kAhead * NT) {
+            int u[kAhead];
+            if (s0 == t) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) u[i] = v_first[i];
+            } else {
+                tokens_at(s0, u);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (u[i] >= v0 && u[i] < v0 + kChunk)
+                    chunk_q[u[i] - v0] = r.q_in * wq(clean(zq[s0 + i * NT]), r.qm);
+        }
+        __syncthreads();
+    }
+    if (t >= kWave) return;
+    // weights inside a chunk are relative to its own largest logit, as when its
+    // sum was taken: a chunk of weight holds a token of weight
     double x[8], scale = 1.0;
     if (residual) {
-        int slot[8];
+        double q[8];
         if (listed) {
-            int m[8], j[8], at[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int64_t k = 2 * (int64_t)min(v + i, a.V - 1);
-                m[i] = a.token_rows[k];
-                j[i] = a.token_rows[k + 1];
-                at[i] = 0;
+                q[i] = chunk_q[t * 8 + i];
+                q[i] = q[i] < 0.0 ? r.q_out : q[i];
             }
-            for (int k = rounds - 1; k >= 0; --k) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int mid = at[i] + (1 << k);
-                    at[i] = mid < n_list && list_id[min(mid, n_list - 1)] <= m[i] ? mid : at[i];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                slot[i] = n_list > 0 && list_id[at[i]] == m[i] ? list_slot[at[i]] + j[i] - list_row[at[i]] : -1;
         } else {
+            const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) slot[i] = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
-        }
-        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool in = slot[i] >= 0 && slot[i] < r.len;
-            y[i] = in ? zq[slot[i]] : 0.0f;
-            slot[i] = in ? 1 : 0;
+            for (int i = 0; i < 8; ++i) {
+                const int slot = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
+                q[i] = slot >= 0 && slot < r.len ? r.q_in * wq(clean(zq[slot]), r.qm) : r.q_out;
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const double q = slot[i] ? r.q_in * wq(clean(y[i]), r.qm) : r.q_out;
-            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q, 0.0);
-        }
+        for (int i = 0; i < 8; ++i) x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q[i], 0.0);
     } else {
         if (without) mark_rejected(a, st, b, e, v0, bits);
         const uint32_t out = without ? marks8(bits, t * 8) : 0u;
@@ -895,11 +938,13 @@ __global__ __launch_bounds__(kVT) void token_rows_kernel(const int32_t* perm, co
 template <typename T>
 dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hipStream_t s) {
     row_parts_kernel<T><<<(uint32_t)((int64_t)a.B * a.N * a.splits), kVT, 0, s>>>(a);
-    walk_kernel<T><<<a.B, kVT, 0, s>>>(a, st);
+    // 16 lanes to a row: all rows of a tree of up to 64 nodes at once
+    if (a.N > 16) walk_kernel<T, 1024><<<a.B, 1024, 0, s>>>(a, st);
+    else walk_kernel<T, kVT><<<a.B, kVT, 0, s>>>(a, st);
     if (a.greedy) return check_launch("verify");
     const bool clusters = q.pieces > 0 && a.M > 0;
     const uint32_t set = clusters ? 4u * (uint32_t)((a.M + 31) / 32) : 0u;
-    const int extra = (q.pieces + kWaves - 1) / kWaves + (clusters && q.streamed ? 1 : 0);
+    const int extra = (q.pieces + kWaves - 1) / kWaves + (clusters ? 1 : 0);
     auto parts = [&](auto chunks_per_wave) {
         constexpr int CW = decltype(chunks_per_wave)::value;
         const int groups = (a.n_chunks + kWaves * CW - 1) / (kWaves * CW), per = groups + extra;
@@ -912,9 +957,9 @@ dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hi
         residual_kernel<T><<<(uint32_t)((int64_t)a.B * groups), kVT, 0, s>>>(a, st, groups, q.pieces);
     const uint32_t each = 8u * (uint32_t)a.n_chunks;
     if (q.entries)
-        draw_kernel<T, 1024><<<a.B, 1024, 2 * each + 12u * (uint32_t)q.entries + set, s>>>(a, st, q.pieces, q.entries);
+        draw_kernel<T, 1024><<<a.B, 1024, 2 * each + 8u * (uint32_t)(kChunk + q.entries), s>>>(a, st, q.pieces);
     else
-        draw_kernel<T, 256><<<a.B, 256, each, s>>>(a, st, q.pieces, 0);
+        draw_kernel<T, 256><<<a.B, 256, each, s>>>(a, st, q.pieces);
     return check_launch("verify");
 }
 
@@ -953,6 +998,9 @@ size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a
     v.n_pieces = (int32_t)most;
     v.pieces = static_cast<DraftPart*>(take(sizeof(DraftPart) * (size_t)(B * most)));
     v.slot_of = static_cast<int32_t*>(take(sizeof(int32_t) * (size_t)B * (size_t)M));
+    v.list_stride = std::min(M, kListedClusters);
+    v.list = static_cast<ListedCluster*>(take(sizeof(ListedCluster) * (size_t)B * (size_t)v.list_stride));
+    v.list_len = static_cast<int32_t*>(take(sizeof(int32_t) * (size_t)B));
     return off;
 }
 
