@@ -140,13 +140,14 @@ __device__ __forceinline__ float wave_max_all(float x) {
 }
 
 // Over a workgroup of NT threads, the same value on every thread.  `tmp` holds
-// NT / 64 entries; the first barrier also orders tmp's earlier readers.
+// NT / 64 entries; the first barrier also orders tmp's earlier readers.  The
+// barriers order LDS alone: loads from memory stay in flight across them.
 template <int NT>
 __device__ __forceinline__ double block_sum_f64(double x, double* tmp) {
     x = wave_sum_f64(x);
-    __syncthreads();
+    lds_barrier();
     if (lane_id() == 0) tmp[threadIdx.x / kWave] = x;
-    __syncthreads();
+    lds_barrier();
     double s = 0.0;
 #pragma unroll
     for (int w = 0; w < NT / kWave; ++w) s += tmp[w];
@@ -155,9 +156,9 @@ __device__ __forceinline__ double block_sum_f64(double x, double* tmp) {
 template <int NT>
 __device__ __forceinline__ float block_max_f32(float x, float* tmp) {
     x = wave_max_all(x);
-    __syncthreads();
+    lds_barrier();
     if (lane_id() == 0) tmp[threadIdx.x / kWave] = x;
-    __syncthreads();
+    lds_barrier();
     float m = tmp[0];
 #pragma unroll
     for (int w = 1; w < NT / kWave; ++w) m = fmaxf(m, tmp[w]);
@@ -167,9 +168,9 @@ __device__ __forceinline__ float block_max_f32(float x, float* tmp) {
 template <int NT>
 __device__ __forceinline__ double block_scan_f64(double x, double* tmp, double* total) {
     const double inc = wave_scan_f64(x);
-    __syncthreads();
+    lds_barrier();
     if (lane_id() == kWave - 1) tmp[threadIdx.x / kWave] = inc;
-    __syncthreads();
+    lds_barrier();
     double base = 0.0, all = 0.0;
 #pragma unroll
     for (int w = 0; w < NT / kWave; ++w) {

@@ -41,9 +41,10 @@ struct DraftPart {
     int32_t len;  // the row's shortlist length
 };
 
-struct ListedCluster {
-    int32_t slot;  // first slot
-    int32_t row;   // first layout row
+// A shortlist slot: its token and the target's logit there.
+struct SlotToken {
+    int32_t v;
+    float z;
 };
 
 struct StepTable {
@@ -85,17 +86,17 @@ struct VerifyArgs {
     int32_t n_pieces;
     DraftPart* pieces;       // [B, n_pieces]
     int32_t* slot_of;        // [B, M] first slot less first layout row of a selected cluster
-    ListedCluster* list;     // [B, list_stride] selected clusters in ascending id
-    int32_t* list_len;       // [B]
-    int32_t list_stride;
+    SlotToken* slots;        // [B, slot_stride] the tokens of a listed step's shortlist
+    int32_t slot_stride;
 };
 
 size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a, void* ws);
 // What a call's steps need of the drawing kernels.
 struct DrawNeeds {
     int32_t pieces = 0;    // kChunk slots of the longest draft row; 0: no step has draft logits
-    int32_t entries = 0;   // most clusters a step's list can name, among the steps that step_listed holds for
+    int32_t entries = 0;   // most clusters a step can name, among the steps that step_listed holds for
     bool streamed = false; // a step whose chunks are read again
+    bool mapped = false;   // a step whose clusters need slot_of
 };
 // A step whose shortlist is short enough for one workgroup to go through.
 constexpr int kListedSlots = 32768, kListedClusters = 2048;

@@ -159,6 +159,7 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
                 needs.entries = (int32_t)std::max<int64_t>(
                     needs.entries, std::min<int64_t>(L->M, (int64_t)(d.shared ? B : 1) * d.k));
             needs.streamed |= d.tail_beta > 0.0f || !step_listed(d, B, L->M);
+            needs.mapped |= !step_listed(d, B, L->M);
         }
     }
     VerifyArgs a{};

@@ -408,10 +408,39 @@ __device__ __forceinline__ unsigned long long block_exclusive_scan_u64(unsigned 
     return base + inc - x;
 }
 
-// Per request, waves c < n_chunks: softmax pieces of a chunk of the row the walk
-// ended in.  Behind them, workgroups: the same of kWaves chunks of the rejected
-// draft's row; and one that writes where each selected cluster's slots start,
-// as a list, or by cluster for shortlists too long for one.
+struct ListedCluster {
+    int32_t slot;  // first slot
+    int32_t row;   // first layout row
+};
+
+// Selected clusters in ascending id with their first slots, a thread taking the
+// 32 clusters of a word of the set; returns their number.
+template <typename F>
+__device__ __forceinline__ int list_clusters(const VerifyArgs& a, const uint32_t* picked, unsigned long long* tmp,
+                                             F emit) {
+    static_assert(DYNA_MAX_M <= 32 * kVT, "a word of the set to a thread");
+    const int t = threadIdx.x;
+    const uint32_t mine = t < (a.M + 31) / 32 ? picked[t] : 0u;
+    // one scan carries the clusters (high half) and their tokens
+    unsigned long long sum = 0, total = 0;
+    for (uint32_t left = mine; left; left &= left - 1) {
+        const int m = t * 32 + __builtin_ctz(left);
+        sum += (1ull << 32) + (uint32_t)(a.offsets[m + 1] - a.offsets[m]);
+    }
+    const unsigned long long at = block_exclusive_scan_u64<kVT>(sum, tmp, &total);
+    int n = (int)(at >> 32), slot = (int)(uint32_t)at;
+    for (uint32_t left = mine; left; left &= left - 1) {
+        const int m = t * 32 + __builtin_ctz(left), o0 = a.offsets[m];
+        emit(n++, m, ListedCluster{slot, o0});
+        slot += a.offsets[m + 1] - o0;
+    }
+    return (int)(total >> 32);
+}
+
+// Per request, workgroups g < chunk_groups: softmax pieces of the chunks of the
+// row the walk ended in, CW to a wave.  Behind them: the same of 4 chunks of the
+// rejected draft's row, with the tokens of those slots and the target's logits
+// there; and one that maps clusters to slots for shortlists too long for that.
 template <typename T, int CW>
 __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int n_pieces,
                                                          int per) {
@@ -465,15 +494,40 @@ __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable
     }
     if (e.mode != kDrawResidual) return;
     const dyna_draft_step& d = st.s[e.node];
+    const bool listed = step_listed(d, a.B, a.M);
     int len = d.cap;
     if (d.clusters != nullptr) len = min(d.cap, pick_clusters<kVT>(a, d, b, picked, &tokens));
-    const int piece = (g - chunk_groups) * kWaves + wave;
     if (g - chunk_groups < (n_pieces + kWaves - 1) / kWaves) {
-        if (piece >= n_pieces) return;
-        const Weigher weight{table[wave], 1.0 / (double)d.temperature * k16Log2e};
-        const int s0 = piece * kChunk + lane * 8;
+        const int piece = (g - chunk_groups) * kWaves + wave, s0 = piece * kChunk + lane * 8;
         float z[8];
         load_part(d.logits + (int64_t)b * d.cap + s0, len - s0, kNegInf, z);
+        if (listed && (g - chunk_groups) * kWaves * kChunk < len) {
+            ListedCluster* list = reinterpret_cast<ListedCluster*>(picked + (a.M + 63) / 64 * 2);
+            const int n = list_clusters(a, picked, tmp_u, [&](int i, int, ListedCluster k) { list[i] = k; });
+            __syncthreads();
+            int at = 0, step = 1;  // the last entry whose first slot is at or before s0
+            while (step < n) step *= 2;
+            for (step /= 2; step > 0; step /= 2) at = at + step < n && list[at + step].slot <= s0 ? at + step : at;
+            int next = at + 1 < n ? list[at + 1].slot : INT32_MAX, row_of = list[at].row - list[at].slot;
+            int v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                while (s0 + i >= next) {  // (an empty cluster has its successor's slot)
+                    ++at;
+                    next = at + 1 < n ? list[at + 1].slot : INT32_MAX;
+                    row_of = list[at].row - list[at].slot;
+                }
+                v[i] = s0 + i < len ? a.perm[row_of + s0 + i] : -1;
+            }
+            const T* row = row_ptr<T>(a, b, e.node);
+            SlotToken* out = a.slots + (int64_t)b * a.slot_stride;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] >= 0 && v[i] < a.V) out[s0 + i] = SlotToken{v[i], to_f32(row[v[i]])};
+                else if (s0 + i < len) out[s0 + i] = SlotToken{-1, kNegInf};
+        }
+        if (piece >= n_pieces) return;
+        const Weigher weight{table[wave], 1.0 / (double)d.temperature * k16Log2e};
 #pragma unroll
         for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
         const float m = wave_max_all(max8(z));
@@ -484,36 +538,11 @@ __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable
         if (lane == 0) a.pieces[(int64_t)b * a.n_pieces + piece] = DraftPart{s, m, len};
         return;
     }
-    if (d.clusters == nullptr) return;
-    const bool listed = step_listed(d, a.B, a.M);
-    ListedCluster* list = a.list + (int64_t)b * a.list_stride;
-    // a thread takes the 32 clusters of a word of the set (M <= 8192: one word);
-    // one scan carries the clusters (high half) and their tokens
-    static_assert(DYNA_MAX_M <= 32 * kVT, "a word of the set to a thread");
-    const uint32_t mine = t < (a.M + 31) / 32 ? picked[t] : 0u;
-    unsigned long long sum = 0, total = 0;
-    for (uint32_t left = mine; left; left &= left - 1) {
-        const int m = t * 32 + __builtin_ctz(left);
-        sum += (1ull << 32) + (uint32_t)(a.offsets[m + 1] - a.offsets[m]);
-    }
-    const unsigned long long at = block_exclusive_scan_u64<kVT>(sum, tmp_u, &total);
-    int n = (int)(at >> 32), slot = (int)(uint32_t)at;
-    for (uint32_t left = mine; left; left &= left - 1) {
-        const int m = t * 32 + __builtin_ctz(left), o0 = a.offsets[m];
-        if (listed) list[n++] = ListedCluster{slot, o0};
-        slot += a.offsets[m + 1] - o0;
-    }
-    if (!listed) {
-        slot = (int)(uint32_t)at;
-        for (int i = 0; i < 32 && t * 32 + i < a.M; ++i) {
-            const int m = t * 32 + i, o0 = a.offsets[m];
-            const bool in = (mine >> i) & 1u;
-            a.slot_of[(int64_t)b * a.M + m] = in ? slot - o0 : kNoSlot;
-            if (in) slot += a.offsets[m + 1] - o0;
-        }
-    }
-    n = (int)(total >> 32);
-    if (t == 0) a.list_len[b] = n;
+    if (d.clusters == nullptr || listed) return;
+    int* slot_of = a.slot_of + (int64_t)b * a.M;
+    for (int m = t; m < a.M; m += kVT)
+        if (!((picked[m >> 5] >> (m & 31)) & 1u)) slot_of[m] = kNoSlot;
+    list_clusters(a, picked, tmp_u, [&](int, int m, ListedCluster k) { slot_of[m] = k.slot - k.row; });
 }
 
 // The two distributions of a residual, from their pieces.
@@ -561,7 +590,7 @@ __device__ __forceinline__ Drawn join_parts(const VerifyArgs& a, const StepTable
         w.f[0][wave] = m;
         w.f[1][wave] = qm;
     }
-    __syncthreads();
+    lds_barrier();
     r.m = r.qm = kNegInf;
 #pragma unroll
     for (int i = 0; i < NT / kWave; ++i) {
@@ -592,7 +621,7 @@ __device__ __forceinline__ Drawn join_parts(const VerifyArgs& a, const StepTable
         w.d[1][wave] = x;
         w.d[2][wave] = y;
     }
-    __syncthreads();
+    lds_barrier();
     s = x = y = 0.0;
 #pragma unroll
     for (int i = 0; i < NT / kWave; ++i) {
@@ -690,10 +719,9 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     extern __shared__ char lds[];
     const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks, wave = t / kWave;
     double* chunk_w = reinterpret_cast<double*>(lds);                             // [n]
-    // and, if entries: [n] changes, [kChunk] the drawn chunk's q, [entries] the list
+    // and, for listed steps: [n] changes, [kChunk] the drawn chunk's q
     unsigned long long* change = reinterpret_cast<unsigned long long*>(chunk_w + n);
     double* chunk_q = reinterpret_cast<double*>(change + n);
-    ListedCluster* list = reinterpret_cast<ListedCluster*>(chunk_q + kChunk);
     const WalkEnd e = a.ends[b];
     fill_weight_table(table);
     const Weigher weight{table, a.inv_t * k16Log2e};
@@ -701,11 +729,25 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     const dyna_draft_step& d = st.s[residual ? e.node : 0];
     const bool listed = residual && step_listed(d, a.B, a.M);
     const double u = (double)a.uniforms[(int64_t)b * a.N + (a.chain ? a.N - 1 : 0)];
-    int n_list = 0, rounds = 0;  // entries, and steps of a search among them
+    const T* row = row_ptr<T>(a, b, e.node);
+    const float* zq = d.logits + (int64_t)b * d.cap;
+    const int len = listed ? a.pieces[(int64_t)b * a.n_pieces].len : 0;
+    constexpr int kAhead = 8;  // slots of a thread whose loads are in flight together
+    const SlotToken* slots = a.slots + (int64_t)b * a.slot_stride;
+    auto load_slots = [&](int s0, SlotToken (&x)[kAhead], float (&y)[kAhead]) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = s0 + i * NT;
+            x[i] = s < len ? slots[s] : SlotToken{-1, 0.0f};
+            y[i] = s < len ? zq[s] : 0.0f;
+        }
+    };
+    // a thread's first slots, rarely not its only ones: they come in while the
+    // pieces are joined
+    SlotToken x_first[kAhead];
+    float y_first[kAhead];
     if (listed) {
-        n_list = a.list_len[b];
-        while ((1 << rounds) < n_list) ++rounds;
-        for (int i = t; i < n_list; i += NT) list[i] = a.list[(int64_t)b * a.list_stride + i];
+        load_slots(t, x_first, y_first);
         for (int c = t; c < n; c += NT) change[c] = 0;
         for (int i = t; i < kChunk; i += NT) chunk_q[i] = -1.0;  // off the shortlist
     }
@@ -719,67 +761,35 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
         }
         return;
     }
-    const T* row = row_ptr<T>(a, b, e.node);
-    const float* zq = d.logits + (int64_t)b * d.cap;
-    constexpr int kAhead = 8;  // slots of a thread whose loads are in flight together
-    // tokens of the slots s0 + i NT, -1 past the row's length
-    auto tokens_at = [&](int s0, int (&v)[kAhead]) {
-        int at[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) at[i] = 0;
-        // the last entry whose first slot is at or before the slot
-        for (int k = rounds - 1; k >= 0; --k) {
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int mid = at[i] + (1 << k);
-                at[i] = mid < n_list && list[min(mid, n_list - 1)].slot <= min(s0 + i * NT, r.len - 1) ? mid : at[i];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const ListedCluster k = list[at[i]];
-            v[i] = a.perm[k.row + min(s0 + i * NT, r.len - 1) - k.slot];
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) v[i] = s0 + i * NT < r.len && v[i] >= 0 && v[i] < a.V ? v[i] : -1;
-    };
-    int v_first[kAhead];  // of the first round, which rarely is not the last
     if (listed) {
         const double c = a.inv_t * k16Log2e, cq = 1.0 / (double)d.temperature * k16Log2e;
         const Weigher wq{table, cq};
         const double yp = 16.0 * log2(r.inv_all), yq = 16.0 * log2(r.q_in);
-        for (int s0 = t; s0 < r.len; s0 += kAhead * NT) {
-            int v[kAhead];
-            float z[kAhead], y[kAhead];
-            tokens_at(s0, v);
+        for (int s0 = t; s0 < len; s0 += kAhead * NT) {
+            if (s0 != t) load_slots(s0, x_first, y_first);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                y[i] = zq[min(s0 + i * NT, r.len - 1)];
-                z[i] = to_f32(row[max(v[i], 0)]);
-                if (s0 == t) v_first[i] = v[i];
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (!__any(v[i] >= 0)) break;
+                const int v = x_first[i].v;
+                if (!__any(v >= 0)) continue;
+                const float z = clean(x_first[i].z), y = clean(y_first[i]);
                 double off;
                 if (r.q_out == 0.0) {  // one exponential, of the smaller exponent
-                    const double ep = ((double)clean(z[i]) - (double)r.m) * c + yp;
+                    const double ep = ((double)z - (double)r.m) * c + yp;
                     // (a draft row without any weight takes nothing)
-                    const double eq = r.q_in > 0.0 ? ((double)clean(y[i]) - (double)r.qm) * cq + yq : -__builtin_inf();
+                    const double eq = r.q_in > 0.0 ? ((double)y - (double)r.qm) * cq + yq : -__builtin_inf();
                     off = -weight.power(fmin(ep, eq));
                 } else {
-                    const double pv = weight(clean(z[i]), r.m) * r.inv_all, qv = r.q_in * wq(clean(y[i]), r.qm);
+                    const double pv = weight(z, r.m) * r.inv_all, qv = r.q_in * wq(y, r.qm);
                     off = fmax(pv - qv, 0.0) - fmax(pv - r.q_out, 0.0);
                 }
-                if (v[i] >= 0)
-                    atomicAdd(&change[v[i] / kChunk], (unsigned long long)(long long)(off * kFixOne));
+                if (v >= 0) atomicAdd(&change[v / kChunk], (unsigned long long)(long long)(off * kFixOne));
             }
         }
-        __syncthreads();
+        lds_barrier();
     }
     // a thread's chunks are consecutive
     const int each = (n + NT - 1) / NT, c0 = min(n, t * each), c1 = min(n, c0 + each);
-    if (each > 1) __syncthreads();  // their weights come from other threads
+    if (each > 1) lds_barrier();  // their weights come from other threads
     double mine = 0.0, total;
     for (int c = c0; c < c1; ++c) {
         double x = chunk_w[c];
@@ -825,7 +835,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
             before[wave] = first != INT32_MAX ? f_at : f_last;
         }
     }
-    __syncthreads();
+    lds_barrier();
     // rounding can leave the last cumulative sum at or below the goal: then the
     // last chunk with any weight
     int from = -1;
@@ -842,22 +852,16 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     float z[8];
     if (t < kWave) load_part(row + v, a.V - v, kNegInf, z);
     if (residual && listed) {
-        // the shortlist's tokens in this chunk, found as above
+        // the shortlist's tokens in this chunk
         const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-        for (int s0 = t; s0 < r.len; s0 += kAhead * NT) {
-            int u[kAhead];
-            if (s0 == t) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) u[i] = v_first[i];
-            } else {
-                tokens_at(s0, u);
-            }
+        for (int s0 = t; s0 < len; s0 += kAhead * NT) {
+            if (len > kAhead * NT) load_slots(s0, x_first, y_first);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (u[i] >= v0 && u[i] < v0 + kChunk)
-                    chunk_q[u[i] - v0] = r.q_in * wq(clean(zq[s0 + i * NT]), r.qm);
+                if (x_first[i].v >= v0 && x_first[i].v < v0 + kChunk)
+                    chunk_q[x_first[i].v - v0] = r.q_in * wq(clean(y_first[i]), r.qm);
         }
-        __syncthreads();
+        lds_barrier();
     }
     if (t >= kWave) return;
     // weights inside a chunk are relative to its own largest logit, as when its
@@ -943,8 +947,8 @@ dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hi
     else walk_kernel<T, kVT><<<a.B, kVT, 0, s>>>(a, st);
     if (a.greedy) return check_launch("verify");
     const bool clusters = q.pieces > 0 && a.M > 0;
-    const uint32_t set = clusters ? 4u * (uint32_t)((a.M + 31) / 32) : 0u;
-    const int extra = (q.pieces + kWaves - 1) / kWaves + (clusters ? 1 : 0);
+    const uint32_t set = clusters ? 8u * (uint32_t)((a.M + 63) / 64 + q.entries) : 0u;
+    const int extra = (q.pieces + kWaves - 1) / kWaves + (q.mapped ? 1 : 0);
     auto parts = [&](auto chunks_per_wave) {
         constexpr int CW = decltype(chunks_per_wave)::value;
         const int groups = (a.n_chunks + kWaves * CW - 1) / (kWaves * CW), per = groups + extra;
@@ -957,7 +961,7 @@ dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hi
         residual_kernel<T><<<(uint32_t)((int64_t)a.B * groups), kVT, 0, s>>>(a, st, groups, q.pieces);
     const uint32_t each = 8u * (uint32_t)a.n_chunks;
     if (q.entries)
-        draw_kernel<T, 1024><<<a.B, 1024, 2 * each + 8u * (uint32_t)(kChunk + q.entries), s>>>(a, st, q.pieces);
+        draw_kernel<T, 1024><<<a.B, 1024, 2 * each + 8u * (uint32_t)kChunk, s>>>(a, st, q.pieces);
     else
         draw_kernel<T, 256><<<a.B, 256, each, s>>>(a, st, q.pieces);
     return check_launch("verify");
@@ -998,9 +1002,8 @@ size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a
     v.n_pieces = (int32_t)most;
     v.pieces = static_cast<DraftPart*>(take(sizeof(DraftPart) * (size_t)(B * most)));
     v.slot_of = static_cast<int32_t*>(take(sizeof(int32_t) * (size_t)B * (size_t)M));
-    v.list_stride = std::min(M, kListedClusters);
-    v.list = static_cast<ListedCluster*>(take(sizeof(ListedCluster) * (size_t)B * (size_t)v.list_stride));
-    v.list_len = static_cast<int32_t*>(take(sizeof(int32_t) * (size_t)B));
+    v.slot_stride = M > 0 ? std::min(V, kListedSlots) : 0;
+    v.slots = static_cast<SlotToken*>(take(sizeof(SlotToken) * (size_t)B * (size_t)v.slot_stride));
     return off;
 }
 
