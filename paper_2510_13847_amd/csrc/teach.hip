@@ -81,6 +81,7 @@ struct ListLds {
     int32_t size;  // places of the hash table, a power of two
     float tmp_f[kTT / kWave];
     double tmp_d[kTT / kWave];
+    double table[16];
 };
 
 __device__ __forceinline__ int hash_place(int x, int size) { return (int)((uint32_t)x * 2654435761u >> 16) & (size - 1); }
@@ -137,6 +138,82 @@ __device__ __forceinline__ void read_list(const DistillArgs& a, int r, const T* 
     __syncthreads();
 }
 
+// What a row's sums give: the factors of its gradient, and its loss.  Sums are
+// relative to the largest logit of their part: the rest (rm, rs) by itself, so
+// that a rest far below the list keeps its shape, and the list (lm, ls); ps is
+// the sum of the teacher's weights.  Every wave computes these, so they take the
+// short power of two and reciprocal; the logarithms are the loss's alone.
+struct RowTerms {
+    float rm, lm;
+    double rs, ps, all;   // all: sum over the row of exp((z - max(rm, lm)) / T)
+    double up;            // (max(rm, lm) - lm) / T
+    double down;          // (rm - max(rm, lm)) / T
+    double list, pr;      // the teacher's probability on the list (or NaN), and off it
+    double on_q, on_p;    // gradient at an entry: on_q exp((z - lm) / T) - on_p (its weight)
+    float factor;         // gradient off the list: factor exp((z - rm) / T)
+    bool still;           // no entry of any weight: loss and gradient 0
+
+    __device__ __forceinline__ static double reciprocal(double x) {
+        double r = __builtin_amdgcn_rcp(x);
+        r = fma(r, fma(-x, r, 1.0), r);
+        return fma(r, fma(-x, r, 1.0), r);
+    }
+    __device__ __forceinline__ RowTerms(const DistillArgs& a, const Weigher& power, int entries, float rm_, double rs_,
+                                        float lm_, double ls, double ps_, float weight)
+        : rm(rm_), lm(lm_), rs(rs_), ps(ps_) {
+        const bool has_rest = !(rs == 0.0), has_list = !(ls == 0.0);
+        const float m = !has_list ? rm : !has_rest ? lm : fmaxf(rm, lm);
+        up = has_list ? ((double)m - (double)lm) * a.inv_t : 0.0;
+        down = has_rest ? ((double)rm - (double)m) * a.inv_t : 0.0;
+        const double f_rest = power.power(down * k16Log2e), f_list = power.power(-up * k16Log2e);
+        all = rs * f_rest + ls * f_list;
+        still = !a.tail && ps == 0.0;
+        const double per_ps = a.tail ? 1.0 : reciprocal(ps);
+        list = still ? 0.0 : ps * per_ps;
+        pr = a.tail && entries < a.V ? 1.0 - list : 0.0;
+        if (pr < 0.0) pr = 0.0;
+        const double scale = (double)weight * a.inv_t, per_all = all == 0.0 ? 0.0 : reciprocal(all);
+        const double each = scale * (list + pr) * per_all;  // q_v (P ...) = e_v each
+        on_q = each * f_list;
+        on_p = scale * per_ps;
+        factor = still || !has_rest ? 0.0f : (float)(each * f_rest - (pr == 0.0 ? 0.0 : scale * pr * reciprocal(rs)));
+    }
+    // list_cost: sum over the entries of weight ((t - tm) / T - (z - lm) / T).
+    // Called by a whole wave, whose first lanes take the four logarithms.
+    __device__ __forceinline__ void results(const DistillArgs& a, double list_cost, float* loss, double* lse,
+                                            double* lse_rest) const {
+        const int lane = lane_id();
+        const double x = log(lane == 0 ? all : lane == 1 ? rs : lane == 2 ? ps : pr);
+        const double log_all = readlane_f64(x, 0), log_rs = readlane_f64(x, 1);
+        const double log_ps = a.tail ? 0.0 : readlane_f64(x, 2), log_pr = readlane_f64(x, 3);
+        double cost = list == 0.0 ? 0.0 : list_cost * (a.tail ? 1.0 : list * reciprocal(ps)) + list * (log_all + up - log_ps);
+        if (pr > 0.0 || pr != pr) cost += pr * (log_pr - (log_rs + down - log_all));
+        if (all == 0.0) cost = __builtin_inf();  // a student that allows no token
+        *loss = still ? 0.0f : (float)cost;
+        *lse = (double)lm * a.inv_t + up + log_all;
+        if (!(fabsf(lm) <= kF32Max)) *lse = (double)rm * a.inv_t - down + log_all;
+        *lse_rest = (double)rm * a.inv_t + log_rs;
+    }
+};
+
+// The teacher's weight of an entry relative to the list's largest value (tail:
+// its probability) and its part of the loss; z relative to the list's largest.
+struct EntryTerms {
+    double w, l, cost;
+    __device__ __forceinline__ EntryTerms(const DistillArgs& a, const Weigher& power, double value, float z, float tm,
+                                          float lm) {
+        const double dt = a.tail ? value : (value - (double)tm) * a.inv_t;
+        const double dz = ((double)z - (double)lm) * a.inv_t;
+        w = value == -__builtin_inf() ? 0.0 : exp_of(power, dt);
+        l = z == kNegInf ? 0.0 : exp_of(power, dz);
+        cost = w == 0.0 ? 0.0 : w * (dt - dz);
+    }
+    // exp(x) by the short power of two; NaN stays NaN
+    __device__ __forceinline__ static double exp_of(const Weigher& power, double x) {
+        return x == x ? power.power(x * k16Log2e) : x;
+    }
+};
+
 // Largest logit outside the list (0 when all are masked) and the sum of
 // exp((z - m) / T) there, from the whole row.
 template <typename T>
@@ -165,42 +242,12 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
     const float weight = a.weights ? a.weights[r] : 1.0f;
 
-    double tmax = -__builtin_inf(), p_list = 0.0, tsum = 0.0;
-    int entries = 0;
-    const bool live = weight != 0.0f;  // (NaN is live)
-    if (live) {
-        read_list(a, r, row, w);
-        float mine = kNegInf;
-        int n = 0;
-        for (int k = t; k < a.K; k += kTT) {
-            if (w.id[k] < 0) continue;
-            ++n;
-            mine = fmaxf(mine, (float)teacher_value<T>(a, r, k));
-        }
-        entries = (int)block_sum_f64<kTT>((double)n, w.tmp_d);
-        if (a.tail) {
-            double s = 0.0;
-            for (int k = t; k < a.K; k += kTT)
-                if (w.id[k] >= 0) s += exp(teacher_value<T>(a, r, k));
-            p_list = block_sum_f64<kTT>(s, w.tmp_d);
-        } else {
-            tmax = block_max_f32<kTT>(mine, w.tmp_f);
-            double s = 0.0;
-            for (int k = t; k < a.K; k += kTT)
-                if (w.id[k] >= 0) {
-                    const double x = teacher_value<T>(a, r, k);
-                    s += x == -__builtin_inf() ? 0.0 : exp((x - tmax) * a.inv_t);
-                }
-            tsum = block_sum_f64<kTT>(s, w.tmp_d);
-            p_list = tsum == 0.0 ? 0.0 : tsum / tsum;  // 1, or NaN
-        }
-    }
     auto no_gradient = [&] {
         const float zero[8] = {};
         if (grad)
             for (int v = v0 + t * 8; v < v1; v += kTT * 8) store_part(grad + v, v1 - v, zero);
     };
-    if (!live) {  // padding
+    if (weight == 0.0f) {  // padding
         if (part == 0 && t == 0) {
             if (a.out_loss) a.out_loss[r] = 0.0f;
             if (a.out_stats) a.out_stats[2 * (int64_t)r] = a.out_stats[2 * (int64_t)r + 1] = 0.0;
@@ -208,18 +255,21 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
         no_gradient();
         return;
     }
-    const bool still = !a.tail && tsum == 0.0;  // no entry of any weight
-    const double log_tsum = a.tail ? 0.0 : log(tsum);
-    auto log_p = [&](int k) {
-        const double x = teacher_value<T>(a, r, k);
-        return a.tail || x == -__builtin_inf() ? x : (x - tmax) * a.inv_t - log_tsum;
-    };
-
-    // the student's row: largest logit m and sum over all of exp((z - m) / T);
-    // the same of the rest by itself (rm, rs), so that a rest far below the
-    // list keeps its shape
-    float m, rm;
-    double all, rs;
+    fill_weight_table(w.table);
+    const Weigher power{w.table, 0.0};
+    read_list(a, r, row, w);  // with barriers
+    float tm = kNegInf, zm = kNegInf;
+    int n = 0;
+    for (int k = t; k < a.K; k += kTT) {
+        if (w.id[k] < 0) continue;
+        ++n;
+        tm = fmaxf(tm, (float)teacher_value<T>(a, r, k));
+        zm = fmaxf(zm, w.z[k]);
+    }
+    tm = block_max_f32<kTT>(tm, w.tmp_f);
+    zm = block_max_f32<kTT>(zm, w.tmp_f);
+    const int entries = (int)block_sum_f64<kTT>((double)n, w.tmp_d);
+    // the student's rest: its largest logit and sum
     double lse = 0.0, lse_rest = 0.0;
     if (a.stats != nullptr) {
         lse = a.stats[2 * (int64_t)r];
@@ -228,89 +278,464 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
     // logits of the type's lowest value: next to 10^38 a log of sums has no
     // digits left for the sums
     auto too_far = [](double x) { return fabs(x) > 0x1p28 && fabs(x) < __builtin_inf(); };
-    if (a.stats != nullptr && !too_far(lse) && !too_far(lse_rest)) {
-        m = (float)(lse / a.inv_t);
+    const bool kept = a.stats != nullptr && !too_far(lse) && !too_far(lse_rest);
+    float rm = 0.0f;
+    double rs = 0.0;
+    if (kept) {
         rm = (float)(lse_rest / a.inv_t);
-        if (!(fabsf(m) <= kF32Max)) m = 0.0f;  // every logit masked, or a NaN
-        if (!(fabsf(rm) <= kF32Max)) rm = 0.0f;
-        all = exp(lse - (double)m * a.inv_t);
+        if (!(fabsf(rm) <= kF32Max)) rm = 0.0f;  // every logit masked, or a NaN
         rs = exp(lse_rest - (double)rm * a.inv_t);
+    } else if (a.stats != nullptr) {
+        rest_of_row(a, row, w, &rm, &rs);
     } else {
-        double s = 0.0, l = 0.0;
-        if (a.stats != nullptr) {
-            rest_of_row(a, row, w, &rm, &rs);
-        } else {
-            const RestPart* p = a.parts + (int64_t)r * a.splits;
-            rm = kNegInf;
-            for (int i = t; i < a.splits; i += kTT) rm = fmaxf(rm, p[i].m);
-            rm = block_max_f32<kTT>(rm, w.tmp_f);
-            if (rm == kNegInf) rm = 0.0f;
-            for (int i = t; i < a.splits; i += kTT)
-                s += p[i].s * (p[i].m > kNegInf ? exp(((double)p[i].m - (double)rm) * a.inv_t) : 1.0);
-            rs = block_sum_f64<kTT>(s, w.tmp_d);
-        }
-        m = rs == 0.0 ? kNegInf : rm;
-        for (int k = t; k < a.K; k += kTT)
-            if (w.id[k] >= 0) m = fmaxf(m, w.z[k]);
-        m = block_max_f32<kTT>(m, w.tmp_f);
-        if (m == kNegInf) m = 0.0f;  // every logit masked: all sums are 0
-        for (int k = t; k < a.K; k += kTT)
-            if (w.id[k] >= 0) l += exp(((double)w.z[k] - (double)m) * a.inv_t);
-        l = block_sum_f64<kTT>(l, w.tmp_d);
-        all = rs == 0.0 ? l : l + rs * exp(((double)rm - (double)m) * a.inv_t);
-        if (part == 0) {
-            lse = (double)m * a.inv_t + log(all);
-            lse_rest = (double)rm * a.inv_t + log(rs);
-            const double log_all = log(all), log_rest = log(rs) + ((double)rm - (double)m) * a.inv_t;
-            if (a.out_stats && t == 0) {
-                a.out_stats[2 * (int64_t)r] = lse;
-                a.out_stats[2 * (int64_t)r + 1] = lse_rest;
-            }
-            if (a.out_loss) {
-                double cost = 0.0;
-                for (int k = t; k < a.K; k += kTT) {
-                    if (w.id[k] < 0) continue;
-                    const double lp = log_p(k);
-                    if (lp == -__builtin_inf()) continue;
-                    cost += exp(lp) * (lp - (((double)w.z[k] - (double)m) * a.inv_t - log_all));
+        const RestPart* p = a.parts + (int64_t)r * a.splits;
+        rm = kNegInf;
+        for (int i = t; i < a.splits; i += kTT) rm = fmaxf(rm, p[i].m);
+        rm = block_max_f32<kTT>(rm, w.tmp_f);
+        if (rm == kNegInf) rm = 0.0f;
+        for (int i = t; i < a.splits; i += kTT)
+            rs += p[i].s * (p[i].m > kNegInf ? power.power(((double)p[i].m - (double)rm) * a.inv_t * k16Log2e) : 1.0);
+        rs = block_sum_f64<kTT>(rs, w.tmp_d);
+    }
+    const float lm = zm == kNegInf ? rm : zm;
+    double ps = 0.0, ls = 0.0, cost = 0.0;
+    for (int k = t; k < a.K; k += kTT) {
+        if (w.id[k] < 0) continue;
+        const EntryTerms x(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
+        ps += x.w;
+        ls += x.l;
+        cost += x.cost;
+    }
+    ps = block_sum_f64<kTT>(ps, w.tmp_d);
+    ls = block_sum_f64<kTT>(ls, w.tmp_d);
+    const RowTerms q(a, power, entries, rm, rs, lm, ls, ps, weight);
+    if (part == 0 && a.stats == nullptr) {
+        cost = block_sum_f64<kTT>(cost, w.tmp_d);
+        if (t < kWave) {
+            float loss;
+            q.results(a, cost, &loss, &lse, &lse_rest);
+            if (t == 0) {
+                if (a.out_loss) a.out_loss[r] = loss;
+                if (a.out_stats) {
+                    a.out_stats[2 * (int64_t)r] = lse;
+                    a.out_stats[2 * (int64_t)r + 1] = lse_rest;
                 }
-                cost = block_sum_f64<kTT>(cost, w.tmp_d);
-                if (a.tail && entries < a.V) {
-                    const double pr = 1.0 - p_list;
-                    if (pr > 0.0) cost += pr * (log(pr) - (log_rest - log_all));
-                    else if (pr != pr) cost = pr;
-                }
-                if (all == 0.0) cost = __builtin_inf();  // a student that allows no token
-                if (still) cost = 0.0;
-                if (t == 0) a.out_loss[r] = (float)cost;
             }
         }
     }
-    if (still) no_gradient();
-    if (still || !grad) return;
-    const double scale = (double)weight * a.inv_t;
-    double pr = a.tail && entries < a.V ? 1.0 - p_list : 0.0;
-    if (pr < 0.0) pr = 0.0;
-    const double mass = p_list + pr;
-    // outside the list q_v (P - p_r / q_r) = e_v (P exp((rm - m) / T) / all - p_r / rs), e_v = exp((z_v - rm) / T)
-    const double per_all = all == 0.0 ? 0.0 : 1.0 / all;
-    const double outside =
-        rs == 0.0 ? 0.0 : mass * per_all * exp(((double)rm - (double)m) * a.inv_t) - pr / rs;
-    const float factor = (float)(scale * outside);
+    if (q.still) no_gradient();
+    if (q.still || !grad) return;
     const float c = (float)(a.inv_t * 1.4426950408889634);
     for (int v = v0 + t * 8; v < v1; v += kTT * 8) {
         float z[8];
         load_part(row + v, v1 - v, kNegInf, z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = factor * __builtin_amdgcn_exp2f((z[i] - rm) * c);
+        for (int i = 0; i < 8; ++i) z[i] = q.factor * __builtin_amdgcn_exp2f((z[i] - rm) * c);
         store_part(grad + v, v1 - v, z);
     }
     __syncthreads();  // the listed tokens' entries are written over what stands there
     for (int k = t; k < a.K; k += kTT) {
         const int x = w.id[k];
         if (x < v0 || x >= v1) continue;
-        const double q = exp(((double)w.z[k] - (double)m) * a.inv_t) * per_all;
-        store_elt(grad + x, (float)(scale * (mass * q - exp(log_p(k)))));
+        const EntryTerms y(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
+        store_elt(grad + x, (float)(q.on_q * y.l - q.on_p * y.w));
+    }
+}
+
+// ---------------------------------------------------------------- one pass
+// Rows that fit the registers of one workgroup: a thread holds NV 16-byte
+// vectors of its row, so that the row is read once, for its sums and then for
+// its gradient.  A workgroup takes several rows.  While a vector's gradient
+// leaves, the next row's vector comes into its registers, and kLag vectors later
+// it is added to that row's sums: loads, stores and both passes' arithmetic are
+// under way together, and the few reductions between rows are all that waits.
+// That code is straight: a lane past the row's end works on its own last vector
+// again (the same loads, stores of the same bytes, nothing added to the sums),
+// because a branch around a load or store would make every wait a wait for all
+// of them.  Barriers order LDS alone.
+constexpr int kLag = 4;
+
+template <typename T>
+struct Vec;  // 16 bytes of a row, `byte` from its start: a uniform base and a 32-bit offset
+template <>
+struct Vec<uint16_t> {
+    static constexpr int E = 8;
+    __device__ __forceinline__ static u32x4 load(const uint16_t* row, uint32_t byte) {
+        return *reinterpret_cast<const u32x4_h*>(reinterpret_cast<const char*>(row) + byte);
+    }
+    __device__ __forceinline__ static void get(const u32x4& w, float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = bf16_lo(w[i]);
+            x[2 * i + 1] = bf16_hi(w[i]);
+        }
+    }
+    __device__ __forceinline__ static float top(const float (&x)[8]) { return max8(x); }
+    __device__ __forceinline__ static float sum(const float (&x)[8]) {
+        return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+    }
+    __device__ __forceinline__ static void store(uint16_t* row, uint32_t byte, const float (&x)[8]) {
+        store8(reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(row) + byte), x);
+    }
+};
+template <>
+struct Vec<float> {
+    static constexpr int E = 4;
+    __device__ __forceinline__ static u32x4 load(const float* row, uint32_t byte) {
+        return *reinterpret_cast<const u32x4_w*>(reinterpret_cast<const char*>(row) + byte);
+    }
+    __device__ __forceinline__ static void get(const u32x4& w, float (&x)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+    }
+    __device__ __forceinline__ static float top(const float (&x)[4]) { return fmaxf(max3(x[0], x[1], x[2]), x[3]); }
+    __device__ __forceinline__ static float sum(const float (&x)[4]) { return (x[0] + x[1]) + (x[2] + x[3]); }
+    __device__ __forceinline__ static void store(float* row, uint32_t byte, const float (&x)[4]) {
+        u32x4_w w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+        *reinterpret_cast<u32x4_w*>(reinterpret_cast<char*>(row) + byte) = w;
+    }
+};
+
+// Three sets of tables take turns: one row's is in use while the next row's is
+// filled and the one before is cleared.
+constexpr int kSets = 3;
+struct PassTables {
+    int32_t* key;      // [kSets][size] hash table over the list
+    int32_t* first;    // [kSets][size] lowest list index of the key
+    uint32_t* listed;  // [kSets][words] bit set of the listed tokens
+    float* g;          // [NT] gradient at a list entry's token
+    int size, words;
+};
+template <int NT>
+__host__ __device__ inline size_t pass_lds_bytes(int V, int K, int* size, int* words) {
+    int n = 64;
+    while (n < 2 * K) n *= 2;
+    *size = n;
+    *words = (V + 31) / 32;
+    return 4 * ((size_t)kSets * (2 * n + *words) + NT);
+}
+
+// What the waves of a workgroup left in LDS, joined by every wave: a lane reads
+// one of them (a loop over sixteen would hold them all in registers).
+template <int kW>
+__device__ __forceinline__ float over_waves_max(const float* x) {
+    static_assert(kW <= 16, "a row of lanes");
+    const float y = lane_id() < kW ? x[lane_id()] : kNegInf;
+    const uint32_t none = __float_as_uint(kNegInf);
+    float m = fmaxf(y, __uint_as_float(dpp<kRowShr1>(none, __float_as_uint(y))));
+    m = fmaxf(m, __uint_as_float(dpp<kRowShr2>(none, __float_as_uint(m))));
+    m = fmaxf(m, __uint_as_float(dpp<kRowShr4>(none, __float_as_uint(m))));
+    m = fmaxf(m, __uint_as_float(dpp<kRowShr8>(none, __float_as_uint(m))));
+    return readlane_f32(m, 15);
+}
+template <int kW>
+__device__ __forceinline__ double over_waves_sum(const double* x) {
+    double y = lane_id() < kW ? x[lane_id()] : 0.0;
+    y += dpp_f64<kRowShr1, 0xf>(y);
+    y += dpp_f64<kRowShr2, 0xf>(y);
+    y += dpp_f64<kRowShr4, 0xf>(y);
+    y += dpp_f64<kRowShr8, 0xf>(y);
+    return readlane_f64(y, 15);
+}
+
+// A thread's share of a row's softmax pieces.
+struct RestSum {
+    float m;
+    double s;
+    __device__ __forceinline__ void rescale(float top, float c) {
+        if (top > m) {
+            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+        }
+    }
+    // Adds a vector.  A NaN or +inf logit makes s NaN and with it the row.
+    template <typename T>
+    __device__ __forceinline__ void add(float (&x)[Vec<T>::E], float c, bool counts) {
+        rescale(Vec<T>::top(x), c);
+        const float ref = m > kNegInf ? m : 0.0f;
+#pragma unroll
+        for (int k = 0; k < Vec<T>::E; ++k) x[k] = __builtin_amdgcn_exp2f((x[k] - ref) * c);
+        const float e = Vec<T>::sum(x);
+        s += counts ? (double)e : 0.0;
+    }
+};
+
+// 128 registers a thread: four waves to a SIMD, in one workgroup or several.
+template <typename T, int NT, int NV, bool GRAD>
+__global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
+    using X = Vec<T>;
+    constexpr int kW = NT / kWave;
+    constexpr int E = X::E;
+    __shared__ float tmp_f[3][kW];
+    __shared__ double tmp_d[4][kW];
+    __shared__ int tmp_n[kW];
+    __shared__ double table[16];
+    extern __shared__ int32_t lds[];
+    PassTables q;
+    pass_lds_bytes<NT>(a.V, a.K, &q.size, &q.words);
+    q.key = lds;
+    q.first = q.key + kSets * q.size;
+    q.listed = reinterpret_cast<uint32_t*>(q.first + kSets * q.size);
+    q.g = reinterpret_cast<float*>(q.listed + kSets * q.words);
+    const int t = threadIdx.x, wave = t / kWave;
+    const int V = a.V;
+    fill_weight_table(table);  // barriers follow
+    const Weigher power{table, 0.0};
+    for (int i = t; i < kSets * q.size; i += NT) {
+        q.key[i] = -1;
+        q.first[i] = INT32_MAX;
+    }
+    for (int i = t; i < kSets * q.words; i += NT) q.listed[i] = 0u;
+
+    auto row_at = [&](int r) { return static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride; };
+    auto grad_at = [&](int r) { return static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride; };
+    // the next row at or behind r with a weight; padding on the way gets its zeros
+    auto live_from = [&](int r) {
+        for (; r < a.N && !live_row(a.weights, r); r += (int)gridDim.x) {
+            if (t == 0) {
+                if (a.out_loss) a.out_loss[r] = 0.0f;
+                if (a.out_stats) a.out_stats[2 * (int64_t)r] = a.out_stats[2 * (int64_t)r + 1] = 0.0;
+            }
+            if (GRAD) {
+                const float zero[8] = {};
+                T* grad = grad_at(r);
+                for (int v = t * 8; v < V; v += NT * 8) store_part(grad + v, V - v, zero);
+            }
+        }
+        return r;
+    };
+    const float c = (float)(a.inv_t * 1.4426950408889634);
+    // whole vectors of a row; the V % E elements behind them go one to a thread
+    const int whole = V / E, v_last = whole * E + t;
+    const bool has_last = v_last < V;
+    u32x4 held[NV];
+    T last = T(0);
+    // this thread's entry of the list, in the row under way and in the next
+    struct Entry {
+        int id, place;  // id -1: none
+        float z;
+        double value;
+        bool ok;        // (with a lower list index, an equal id is the entry)
+    };
+    auto read_entry = [&](int r) {
+        Entry x{-1, 0, 0.0f, 0.0, false};
+        if (r < a.N && t < a.K) {
+            const int i = a.ids[(int64_t)r * a.K + t];
+            x.id = i >= 0 && i < V ? i : -1;
+            x.value = teacher_value<T>(a, r, t);
+        }
+        return x;
+    };
+    auto insert = [&](Entry& x, int r, int set) {
+        if (x.id < 0) return;
+        x.z = to_f32(row_at(r)[x.id]);
+        int32_t* key = q.key + set * q.size;
+        x.place = hash_place(x.id, q.size);
+        while (true) {  // at most K of the 2 K places are taken: an empty one is found
+            const int old = atomicCAS(&key[x.place], -1, x.id);
+            if (old == -1 || old == x.id) break;
+            x.place = (x.place + 1) & (q.size - 1);
+        }
+        atomicMin(&q.first[set * q.size + x.place], t);
+        atomicOr(&q.listed[set * q.words + (x.id >> 5)], 1u << (x.id & 31));
+    };
+    auto clear = [&](int id, int place, int set) {
+        if (id < 0) return;
+        q.key[set * q.size + place] = -1;
+        q.first[set * q.size + place] = INT32_MAX;
+        q.listed[set * q.words + (id >> 5)] = 0u;
+    };
+    auto bits_of = [&](const uint32_t* listed, int v) { return (listed[v >> 5] >> (v & 31)) & ((1u << E) - 1); };
+    RestSum sum;
+    // a thread's first vector and the distance to its last one: behind that one
+    // it is at that one again.  (Copies of them that are new for every vector: the
+    // addresses of all sixteen, made ahead, would not fit beside the row.)
+    struct Place {
+        int t, far, count;  // count: NT times its vectors (0: nothing counts)
+        __device__ __forceinline__ int at(int i) const { return t + min(i * NT, far); }
+        __device__ __forceinline__ void renew() { __asm__ volatile("" : "+v"(t), "+v"(far), "+v"(count)); }
+    };
+    const int far = (whole - 1 - t) / NT * NT;
+    // adds vector i of the row whose list is in `listed`.  The empty statements
+    // keep one vector's values from being unpacked while another's are in use
+    auto add_vec = [&](const uint32_t* listed, Place& p, int i) {
+        p.renew();
+        __asm__ volatile("" : "+v"(held[i]));
+        float x[E];
+        X::get(held[i], x);
+        const uint32_t out = bits_of(listed, p.at(i) * E);
+        if (out)
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if ((out >> j) & 1u) x[j] = kNegInf;
+        sum.add<T>(x, c, i * NT < p.count);
+        __asm__ volatile("" : "+v"(sum.m), "+v"(sum.s));
+    };
+    auto add_last = [&](const uint32_t* listed) {
+        if (!has_last || ((listed[v_last >> 5] >> (v_last & 31)) & 1u)) return;
+        const float x = to_f32(last);
+        sum.rescale(x, c);
+        sum.s += (double)__builtin_amdgcn_exp2f((x - (sum.m > kNegInf ? sum.m : 0.0f)) * c);
+    };
+
+    int r = live_from(blockIdx.x);
+    if (r >= a.N) return;
+    lds_barrier();
+    Entry now = read_entry(r);
+    insert(now, r, 0);
+    int next = live_from(r + (int)gridDim.x);
+    Entry then = read_entry(next);
+    {
+        const T* row = row_at(r);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) held[i] = X::load(row, (uint32_t)(t + min(i * NT, far)) * 16u);
+        if (has_last) last = row[v_last];
+    }
+    lds_barrier();
+    now.ok = now.id >= 0 && q.first[now.place] == t;
+    sum = RestSum{kNegInf, 0.0};
+    {
+        Place p{t, far, far + NT};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            add_vec(q.listed, p, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    add_last(q.listed);
+
+    int old_id = -1, old_place = 0;  // the row before
+    for (int set = 0;;) {
+        const int set1 = set == kSets - 1 ? 0 : set + 1, set2 = set == 0 ? kSets - 1 : set - 1;
+        const uint32_t* listed = q.listed + set * q.words;
+        const bool more = next < a.N;
+        if (more) insert(then, next, set1);
+        // largest logit of the rest, of the list, largest value of the list
+        {
+            const float x0 = wave_max_all(sum.m), x1 = wave_max_all(now.ok ? now.z : kNegInf);
+            const float x2 = wave_max_all(now.ok ? (float)now.value : kNegInf);
+            if (lane_id() == 0) {
+                tmp_f[0][wave] = x0;
+                tmp_f[1][wave] = x1;
+                tmp_f[2][wave] = x2;
+            }
+        }
+        lds_barrier();
+        float rm = over_waves_max<kW>(tmp_f[0]);
+        const float zm = over_waves_max<kW>(tmp_f[1]), tm = over_waves_max<kW>(tmp_f[2]);
+        clear(old_id, old_place, set2);
+        old_id = now.id;
+        old_place = now.place;
+        if (more) then.ok = then.id >= 0 && q.first[set1 * q.size + then.place] == t;
+        if (rm == kNegInf) rm = 0.0f;
+        const float lm = zm == kNegInf ? rm : zm;  // shift of the list's sum
+        // (waves without a place in the list have nothing to add to its sums)
+        const bool lists = wave * kWave < a.K;
+        double ew = 0.0, el = 0.0;
+        {
+            const double f = sum.m > kNegInf ? (double)__builtin_amdgcn_exp2f((sum.m - rm) * c) : 1.0;
+            double y0 = wave_sum_f64(sum.s * f), y1 = 0.0, y2 = 0.0, y3 = 0.0;
+            int n = 0;
+            if (lists) {
+                if (now.ok) {
+                    const EntryTerms x(a, power, now.value, now.z, tm, lm);
+                    ew = x.w;
+                    el = x.l;
+                    y3 = x.cost;
+                }
+                y1 = wave_sum_f64(el);
+                y2 = wave_sum_f64(ew);
+                y3 = wave_sum_f64(y3);
+                n = __popcll(__ballot(now.ok));
+            }
+            if (lane_id() == 0) {
+                tmp_d[0][wave] = y0;
+                tmp_d[1][wave] = y1;
+                tmp_d[2][wave] = y2;
+                tmp_d[3][wave] = y3;
+                tmp_n[wave] = n;
+            }
+        }
+        lds_barrier();
+        const double rs = over_waves_sum<kW>(tmp_d[0]), ls = over_waves_sum<kW>(tmp_d[1]);
+        const double ps = over_waves_sum<kW>(tmp_d[2]);
+        int entries = 0;
+        for (int i = 0; i * kWave < a.K; ++i) entries += tmp_n[i];
+        const RowTerms w(a, power, entries, rm, rs, lm, ls, ps, a.weights ? a.weights[r] : 1.0f);
+        if (now.ok) q.g[t] = w.still ? 0.0f : (float)(w.on_q * el - w.on_p * ew);
+        if (wave == kW - 1) {  // (the wave with the fewest entries)
+            float loss;
+            double lse, lse_rest;
+            w.results(a, over_waves_sum<kW>(tmp_d[3]), &loss, &lse, &lse_rest);
+            if (lane_id() == 0) {
+                if (a.out_loss) a.out_loss[r] = loss;
+                if (a.out_stats) {
+                    a.out_stats[2 * (int64_t)r] = lse;
+                    a.out_stats[2 * (int64_t)r + 1] = lse_rest;
+                }
+            }
+        }
+        lds_barrier();  // g
+        const int after = more ? live_from(next + (int)gridDim.x) : a.N;
+        now = then;
+        then = read_entry(after);
+
+        // the gradient of this row, the next row's vectors and their sums
+        T* grad = GRAD ? grad_at(r) : nullptr;
+        const float factor = w.factor;
+        sum = RestSum{kNegInf, 0.0};
+        const uint32_t* next_listed = q.listed + set1 * q.words;
+        auto at_entry = [&](int v) {
+            int h = hash_place(v, q.size);
+            while (q.key[set * q.size + h] != v) h = (h + 1) & (q.size - 1);
+            return q.g[q.first[set * q.size + h]];
+        };
+        auto gradient = [&](Place& p, int i) {
+            p.renew();
+            float x[E];
+            __asm__ volatile("" : "+v"(held[i]));
+            X::get(held[i], x);
+#pragma unroll
+            for (int k = 0; k < E; ++k) x[k] = factor * __builtin_amdgcn_exp2f((x[k] - rm) * c);
+            X::store(grad, (uint32_t)p.at(i) * 16u, x);
+        };
+        if (GRAD && has_last) {
+            const bool in = (listed[v_last >> 5] >> (v_last & 31)) & 1u;
+            store_elt(grad + v_last, in ? at_entry(v_last) : factor * __builtin_amdgcn_exp2f((to_f32(last) - rm) * c));
+        }
+        // behind the last row the loads all take one vector a thread, and nothing counts
+        const T* next_row = row_at(more ? next : r);
+        Place p{t, far, far + NT}, p1{t, more ? far : 0, more ? far + NT : 0};
+        if (has_last) last = next_row[v_last];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if (GRAD) gradient(p, i);
+            p1.renew();
+            held[i] = X::load(next_row, (uint32_t)p1.at(i) * 16u);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i >= kLag) add_vec(next_listed, p1, i - kLag);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // the list's entries, over what their own thread has just stored there
+        if (GRAD) {
+            for (int k = t; k < whole; k += NT)
+                for (uint32_t in = bits_of(listed, k * E); in; in &= in - 1) {
+                    const int v = k * E + __builtin_ctz(in);
+                    store_elt(grad + v, at_entry(v));
+                }
+        }
+        if (!more) return;
+#pragma unroll
+        for (int i = NV - kLag; i < NV; ++i) {
+            add_vec(next_listed, p1, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        add_last(next_listed);
+        r = next;
+        next = after;
+        set = set1;
     }
 }
 
@@ -386,10 +811,32 @@ __global__ __launch_bounds__(kTT) void router_loss_kernel(RouterLossArgs a) {
     if (t == 0 && a.out_loss) a.out_loss[r] = (float)cost;
 }
 
+constexpr int kPassCus = 256;
+
+template <typename T, int NT, int NV>
+bool run_pass(const DistillArgs& a, hipStream_t s) {
+    int size, words;
+    const size_t lds = pass_lds_bytes<NT>(a.V, a.K, &size, &words);
+    const int whole = a.V / Vec<T>::E;
+    if (whole > NV * NT || whole < NT || a.K > NT || lds > 60 * 1024) return false;
+    const int grid = std::min(a.N, kPassCus * (1024 / NT));
+    if (a.grad) distill_pass_kernel<T, NT, NV, true><<<grid, NT, (uint32_t)lds, s>>>(a);
+    else distill_pass_kernel<T, NT, NV, false><<<grid, NT, (uint32_t)lds, s>>>(a);
+    return true;
+}
+
+// Whether the row's loads fill the chip from one workgroup to a row.
+template <typename T>
+bool one_pass(const DistillArgs& a) { return true; }
+
 template <typename T>
 dyna_status run_distill(const DistillArgs& a, hipStream_t s) {
-    if (a.stats == nullptr)
+    if (a.stats == nullptr) {
+        if (one_pass<T>(a) && (run_pass<T, 256, 8>(a, s) || run_pass<T, 256, 16>(a, s) || run_pass<T, 512, 16>(a, s) ||
+                               run_pass<T, 1024, 16>(a, s)))
+            return check_launch("distill");
         rest_parts_kernel<T><<<(uint32_t)((int64_t)a.N * a.splits), kTT, 0, s>>>(a);
+    }
     const int parts = a.grad ? a.splits : 1;
     distill_finish_kernel<T><<<(uint32_t)((int64_t)a.N * parts), kTT, 0, s>>>(a, parts);
     return check_launch("distill");

@@ -20,8 +20,7 @@ namespace {
 
 constexpr int kVT = 256;  // threads of every kernel here
 constexpr int kNoSlot = INT32_MIN;
-// Chunks of all requests from which on a wave takes four of them.
-constexpr int kManyChunks = 16384;
+constexpr int kDrawWaves = 256 * 32;  // waves that the chip holds
 
 // ---------------------------------------------------------------- inputs
 __device__ __forceinline__ int chain_len(const VerifyArgs& a, int b) {
@@ -438,42 +437,43 @@ __device__ __forceinline__ int list_clusters(const VerifyArgs& a, const uint32_t
 }
 
 // Per request, workgroups g < chunk_groups: softmax pieces of the chunks of the
-// row the walk ended in, CW to a wave.  Behind them: the same of 4 chunks of the
+// row the walk ended in, per_wave to a wave.  Behind them: the same of 4 chunks of the
 // rejected draft's row, with the tokens of those slots and the target's logits
 // there; and one that maps clusters to slots for shortlists too long for that.
-template <typename T, int CW>
-__global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int n_pieces,
-                                                         int per) {
+template <typename T>
+__global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int per_wave,
+                                                         int n_pieces, int per) {
     __shared__ double table[kWaves][16];
     __shared__ uint32_t bits[kWaves][kChunk / 32];
     __shared__ unsigned long long tmp_u[kWaves];
     __shared__ int tokens;
     extern __shared__ uint32_t picked[];  // [M / 32]
-    // the longest ones first
-    const int b = blockIdx.x / per, g = per - 1 - (int)(blockIdx.x % per), t = threadIdx.x, wave = t / kWave;
+    const int b = blockIdx.x / per, g = blockIdx.x % per, t = threadIdx.x, wave = t / kWave;
     const int lane = lane_id();
     const WalkEnd e = a.ends[b];
     fill_wave_table(table[wave]);
     if (g < chunk_groups) {
         const Weigher weight{table[wave], a.inv_t * k16Log2e};
         const T* row = row_ptr<T>(a, b, e.node);
-        const int c0 = (g * kWaves + wave) * CW;
-        float z[CW][8];
+        const int c0 = (g * kWaves + wave) * per_wave, c1 = min(a.n_chunks, c0 + per_wave);
+        const int whole = min(c1, a.V / kChunk);  // chunks before it lie inside the row
+        Row8<T> next;
+        if (c0 < whole) next.load(row + c0 * kChunk + lane * 8);
+        for (int c = c0; c < c1; ++c) {
+            float z[8];
+            if (c < whole) {
+                next.get(z);
+                // the next chunk comes in while this one is summed
+                if (c + 1 < whole) next.load(row + (c + 1) * kChunk + lane * 8);
+            } else {
+                load_part(row + c * kChunk + lane * 8, a.V - c * kChunk - lane * 8, kNegInf, z);
+            }
 #pragma unroll
-        for (int k = 0; k < CW; ++k) {
-            const int v = (c0 + k) * kChunk + lane * 8;
-            load_part(row + v, a.V - v, kNegInf, z[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < CW; ++k) {
-            const int c = c0 + k;
-            if (c >= a.n_chunks) return;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[k][i] = clean(z[k][i]);
-            const float m = wave_max_all(max8(z[k]));
+            for (int i = 0; i < 8; ++i) z[i] = clean(z[i]);
+            const float m = wave_max_all(max8(z));
             double all = 0.0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) all += weight(z[k][i], m);
+            for (int i = 0; i < 8; ++i) all += weight(z[i], m);
             all = wave_sum_f64(all);
             double ex = all;
             if (e.mode == kDrawTarget) {
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable
                 if (__any(out != 0)) {
                     ex = 0.0;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) ex += (out >> i) & 1u ? 0.0 : weight(z[k][i], m);
+                    for (int i = 0; i < 8; ++i) ex += (out >> i) & 1u ? 0.0 : weight(z[i], m);
                     ex = wave_sum_f64(ex);
                 }
             }
@@ -949,13 +949,10 @@ dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hi
     const bool clusters = q.pieces > 0 && a.M > 0;
     const uint32_t set = clusters ? 8u * (uint32_t)((a.M + 63) / 64 + q.entries) : 0u;
     const int extra = (q.pieces + kWaves - 1) / kWaves + (q.mapped ? 1 : 0);
-    auto parts = [&](auto chunks_per_wave) {
-        constexpr int CW = decltype(chunks_per_wave)::value;
-        const int groups = (a.n_chunks + kWaves * CW - 1) / (kWaves * CW), per = groups + extra;
-        draw_parts_kernel<T, CW><<<(uint32_t)((int64_t)a.B * per), kVT, set, s>>>(a, st, groups, q.pieces, per);
-    };
-    if ((int64_t)a.B * a.n_chunks >= kManyChunks) parts(std::integral_constant<int, 4>{});
-    else parts(std::integral_constant<int, 1>{});
+    // enough chunks to a wave that all waves are resident at once
+    const int per_wave = (int)(((int64_t)a.B * a.n_chunks + kDrawWaves - 1) / kDrawWaves);
+    const int chunk_groups = (a.n_chunks + kWaves * per_wave - 1) / (kWaves * per_wave), per = chunk_groups + extra;
+    draw_parts_kernel<T><<<(uint32_t)((int64_t)a.B * per), kVT, set, s>>>(a, st, chunk_groups, per_wave, q.pieces, per);
     const int groups = (a.n_chunks + kWaves - 1) / kWaves;
     if (q.streamed)
         residual_kernel<T><<<(uint32_t)((int64_t)a.B * groups), kVT, 0, s>>>(a, st, groups, q.pieces);
