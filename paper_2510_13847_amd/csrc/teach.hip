@@ -20,9 +20,48 @@ namespace {
 
 constexpr int kTT = 256;            // threads
 constexpr int kMaxSplitLen = 65536; // entries of a row's part: its bit set of listed tokens is 8 KB
-constexpr int kHash = 2 * DYNA_MAX_TEACHER;
+constexpr int kFlight = 4;          // vectors a thread has in flight
 
 __device__ __forceinline__ bool live_row(const float* weights, int r) { return weights == nullptr || weights[r] != 0.0f; }
+
+// Largest and sum of a vector of logits.
+__device__ __forceinline__ float top_of(const float (&x)[8]) { return max8(x); }
+__device__ __forceinline__ float top_of(const float (&x)[4]) { return fmaxf(max3(x[0], x[1], x[2]), x[3]); }
+__device__ __forceinline__ float sum_of(const float (&x)[4]) { return (x[0] + x[1]) + (x[2] + x[3]); }
+__device__ __forceinline__ float sum_of(const float (&x)[8]) {
+    return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
+// A thread's share of a row's softmax pieces: largest logit, sum of exp2((z - m) c).
+struct RestSum {
+    float m;
+    double s;
+    __device__ __forceinline__ void rescale(float top, float c) {
+        if (top > m) {
+            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
+            m = top;
+        }
+    }
+    // Adds a vector.  A NaN or +inf logit makes s NaN and with it the row.
+    template <int E>
+    __device__ __forceinline__ void add(float (&x)[E], float c, bool counts = true) {
+        rescale(top_of(x), c);
+        const float ref = m > kNegInf ? m : 0.0f;
+#pragma unroll
+        for (int k = 0; k < E; ++k) x[k] = __builtin_amdgcn_exp2f((x[k] - ref) * c);
+        const float e = sum_of(x);
+        s += counts ? (double)e : 0.0;
+    }
+};
+
+// Takes the listed elements out of a vector.
+template <int E>
+__device__ __forceinline__ void mask_listed(float (&x)[E], uint32_t listed) {
+    if (listed)
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+            if ((listed >> k) & 1u) x[k] = kNegInf;
+}
 
 // ---------------------------------------------------------------- rest of a row
 template <typename T>
@@ -33,56 +72,58 @@ __global__ __launch_bounds__(kTT) void rest_parts_kernel(DistillArgs a) {
     const int r = blockIdx.x / a.splits, part = blockIdx.x % a.splits, t = threadIdx.x;
     if (!live_row(a.weights, r)) return;
     const int v0 = part * a.split_len, v1 = min(a.V, v0 + a.split_len);
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    constexpr int kStep = kTT * 8;
+    int v = v0 + t * 8;
+    // the first vectors come in while the list is marked
+    Row8<T> in[kFlight];
+    auto whole = [&](int at) { return at + 8 <= v1; };
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i)
+        if (whole(v + i * kStep)) in[i].load(row + v + i * kStep);
     for (int i = t; i < (a.split_len + 31) / 32; i += kTT) listed[i] = 0u;
-    __syncthreads();
+    lds_barrier();
     for (int k = t; k < a.K; k += kTT) {
         const int x = a.ids[(int64_t)r * a.K + k];
         if (x >= v0 && x < v1) atomicOr(&listed[(x - v0) >> 5], 1u << ((x - v0) & 31));
     }
-    __syncthreads();
-    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    lds_barrier();
     const float c = (float)(a.inv_t * 1.4426950408889634);
-    float m = kNegInf;
-    double s = 0.0;
-    for (int v = v0 + t * 8; v < v1; v += kTT * 8) {
-        float z[8];
-        load_part(row + v, v1 - v, kNegInf, z);
-        const uint32_t out = (listed[(v - v0) >> 5] >> ((v - v0) & 31)) & 0xffu;
-        if (out)
+    auto bits_of = [&](int v) { return (listed[(v - v0) >> 5] >> ((v - v0) & 31)) & 0xffu; };
+    RestSum sum{kNegInf, 0.0};
+    for (; v < v1; v += kFlight * kStep) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((out >> i) & 1u) z[i] = kNegInf;
-        float top = kNegInf;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, z[i]);
-        if (top > m) {
-            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
-            m = top;
+        for (int i = 0; i < kFlight; ++i) {
+            const int at = v + i * kStep, next = at + kFlight * kStep;
+            if (at >= v1) break;
+            float z[8];
+            if (whole(at)) in[i].get(z);
+            else load_part(row + at, v1 - at, kNegInf, z);
+            if (whole(next)) in[i].load(row + next);
+            mask_listed(z, bits_of(at));
+            sum.add(z, c);
         }
-        // a NaN (or +inf) logit makes s NaN and with it the whole row
-        const float ref = m > kNegInf ? m : 0.0f;
-        float e = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e += __builtin_amdgcn_exp2f((z[i] - ref) * c);
-        s += (double)e;
     }
-    const float top = block_max_f32<kTT>(m, tmp_f);
-    const double f = m > kNegInf ? (double)__builtin_amdgcn_exp2f((m - top) * c) : 1.0;
-    const double total = block_sum_f64<kTT>(s * f, tmp_d);
+    const float top = block_max_f32<kTT>(sum.m, tmp_f);
+    const double f = sum.m > kNegInf ? (double)__builtin_amdgcn_exp2f((sum.m - top) * c) : 1.0;
+    const double total = block_sum_f64<kTT>(sum.s * f, tmp_d);
     if (t == 0) a.parts[(int64_t)r * a.splits + part] = RestPart{total, top, 0.0f};
 }
 
 // ---------------------------------------------------------------- list
 struct ListLds {
-    int32_t key[kHash];
-    int32_t first[kHash];
-    int32_t id[DYNA_MAX_TEACHER];  // -1: not an entry
-    float z[DYNA_MAX_TEACHER];     // student's logit
-    int32_t size;  // places of the hash table, a power of two
-    float tmp_f[kTT / kWave];
-    double tmp_d[kTT / kWave];
-    double table[16];
+    int32_t* key;    // [size] hash table
+    int32_t* first;  // [size] lowest list index of the key
+    int32_t* id;     // [K] -1: not an entry
+    float* z;        // [K] student's logit
+    int32_t size;    // places of the hash table, a power of two
 };
+__host__ __device__ inline int list_places(int K) {
+    int n = 64;
+    while (n < 2 * K) n *= 2;
+    return n;
+}
+inline uint32_t list_lds_bytes(int K) { return 4u * (2u * (uint32_t)list_places(K) + 2u * (uint32_t)K); }
 
 __device__ __forceinline__ int hash_place(int x, int size) { return (int)((uint32_t)x * 2654435761u >> 16) & (size - 1); }
 __device__ __forceinline__ bool in_list(const ListLds& w, int x) {
@@ -101,18 +142,17 @@ __device__ __forceinline__ double teacher_value(const DistillArgs& a, int r, int
 // The row's entries: ids inside the vocabulary, the first of equal ones.  A
 // hash table over the list finds equal ids in a few steps each; the lowest
 // index wins whatever the order of arrival.
-template <typename T>
-__device__ __forceinline__ void read_list(const DistillArgs& a, int r, const T* row, ListLds& w) {
+template <typename T, int NT>
+__device__ __forceinline__ ListLds read_list(const DistillArgs& a, int r, const T* row, int32_t* lds) {
     const int t = threadIdx.x;
-    int size = 64;
-    while (size < 2 * a.K) size *= 2;
-    if (t == 0) w.size = size;
-    for (int i = t; i < size; i += kTT) {
+    const int size = list_places(a.K);
+    const ListLds w{lds, lds + size, lds + 2 * size, reinterpret_cast<float*>(lds + 2 * size + a.K), size};
+    for (int i = t; i < size; i += NT) {
         w.key[i] = -1;
         w.first[i] = INT32_MAX;
     }
-    __syncthreads();
-    for (int k = t; k < a.K; k += kTT) {
+    lds_barrier();
+    for (int k = t; k < a.K; k += NT) {
         const int x = a.ids[(int64_t)r * a.K + k];
         const bool ok = x >= 0 && x < a.V;
         w.id[k] = ok ? x : -1;
@@ -126,8 +166,8 @@ __device__ __forceinline__ void read_list(const DistillArgs& a, int r, const T* 
             atomicMin(&w.first[h], k);
         }
     }
-    __syncthreads();
-    for (int k = t; k < a.K; k += kTT) {
+    lds_barrier();
+    for (int k = t; k < a.K; k += NT) {
         const int x = w.id[k];
         if (x < 0) continue;
         int h = hash_place(x, size);
@@ -135,7 +175,8 @@ __device__ __forceinline__ void read_list(const DistillArgs& a, int r, const T* 
         if (w.first[h] != k) w.id[k] = -1;
         else w.z[k] = to_f32(row[x]);
     }
-    __syncthreads();
+    lds_barrier();
+    return w;
 }
 
 // What a row's sums give: the factors of its gradient, and its loss.  Sums are
@@ -216,25 +257,30 @@ struct EntryTerms {
 
 // Largest logit outside the list (0 when all are masked) and the sum of
 // exp((z - m) / T) there, from the whole row.
-template <typename T>
-__device__ void rest_of_row(const DistillArgs& a, const T* row, ListLds& w, float* rm, double* rs) {
+template <typename T, int NT>
+__device__ void rest_of_row(const DistillArgs& a, const T* row, const ListLds& w, float* tmp_f, double* tmp_d, float* rm,
+                            double* rs) {
     float m = kNegInf;
-    for (int v = threadIdx.x; v < a.V; v += kTT)
+    for (int v = threadIdx.x; v < a.V; v += NT)
         if (!in_list(w, v)) m = fmaxf(m, to_f32(row[v]));
-    m = block_max_f32<kTT>(m, w.tmp_f);
+    m = block_max_f32<NT>(m, tmp_f);
     *rm = m > kNegInf ? m : 0.0f;
     double s = 0.0;
-    for (int v = threadIdx.x; v < a.V; v += kTT)
+    for (int v = threadIdx.x; v < a.V; v += NT)
         if (!in_list(w, v)) s += exp(((double)to_f32(row[v]) - (double)*rm) * a.inv_t);
-    *rs = block_sum_f64<kTT>(s, w.tmp_d);
+    *rs = block_sum_f64<NT>(s, tmp_d);
 }
 
 // ---------------------------------------------------------------- finish
 // Joins the parts and the list of one row; writes its loss and statistics
 // (part 0) and its part of the gradient.
-template <typename T>
-__global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int parts) {
-    __shared__ ListLds w;
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void distill_finish_kernel(DistillArgs a, int parts) {
+    __shared__ float tmp_f[2][NT / kWave], tmp_r[NT / kWave];
+    __shared__ double tmp_d[4][NT / kWave], tmp_s[NT / kWave];
+    __shared__ int tmp_n[NT / kWave];
+    __shared__ double table[16];
+    extern __shared__ int32_t lds[];
     const int r = blockIdx.x / parts, part = blockIdx.x % parts, t = threadIdx.x;
     const int len = parts == 1 ? a.V : a.split_len;
     const int v0 = part * len, v1 = min(a.V, v0 + len);
@@ -245,7 +291,7 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
     auto no_gradient = [&] {
         const float zero[8] = {};
         if (grad)
-            for (int v = v0 + t * 8; v < v1; v += kTT * 8) store_part(grad + v, v1 - v, zero);
+            for (int v = v0 + t * 8; v < v1; v += NT * 8) store_part(grad + v, v1 - v, zero);
     };
     if (weight == 0.0f) {  // padding
         if (part == 0 && t == 0) {
@@ -255,21 +301,40 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
         no_gradient();
         return;
     }
-    fill_weight_table(w.table);
-    const Weigher power{w.table, 0.0};
-    read_list(a, r, row, w);  // with barriers
+    fill_weight_table(table);
+    const Weigher power{table, 0.0};
+    const ListLds w = read_list<T, NT>(a, r, row, lds);  // with barriers
     float tm = kNegInf, zm = kNegInf;
     int n = 0;
-    for (int k = t; k < a.K; k += kTT) {
+    for (int k = t; k < a.K; k += NT) {
         if (w.id[k] < 0) continue;
         ++n;
         tm = fmaxf(tm, (float)teacher_value<T>(a, r, k));
         zm = fmaxf(zm, w.z[k]);
     }
-    tm = block_max_f32<kTT>(tm, w.tmp_f);
-    zm = block_max_f32<kTT>(zm, w.tmp_f);
-    const int entries = (int)block_sum_f64<kTT>((double)n, w.tmp_d);
-    // the student's rest: its largest logit and sum
+    // without parts to join, the rest is known already
+    const RestPart* parts_of = a.parts + (int64_t)r * a.splits;
+    float rm = kNegInf;
+    if (a.stats == nullptr)
+        for (int i = t; i < a.splits; i += NT) rm = fmaxf(rm, parts_of[i].m);
+    const int wave = t / kWave;
+    {
+        const float x0 = wave_max_all(tm), x1 = wave_max_all(zm), x2 = wave_max_all(rm);
+        if (lane_id() == 0) {
+            tmp_f[0][wave] = x0;
+            tmp_f[1][wave] = x1;
+            tmp_r[wave] = x2;
+        }
+    }
+    lds_barrier();
+    tm = zm = rm = kNegInf;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) {
+        tm = fmaxf(tm, tmp_f[0][i]);
+        zm = fmaxf(zm, tmp_f[1][i]);
+        rm = fmaxf(rm, tmp_r[i]);
+    }
+    // the student's rest from a forward pass
     double lse = 0.0, lse_rest = 0.0;
     if (a.stats != nullptr) {
         lse = a.stats[2 * (int64_t)r];
@@ -279,38 +344,54 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
     // digits left for the sums
     auto too_far = [](double x) { return fabs(x) > 0x1p28 && fabs(x) < __builtin_inf(); };
     const bool kept = a.stats != nullptr && !too_far(lse) && !too_far(lse_rest);
-    float rm = 0.0f;
     double rs = 0.0;
     if (kept) {
         rm = (float)(lse_rest / a.inv_t);
         if (!(fabsf(rm) <= kF32Max)) rm = 0.0f;  // every logit masked, or a NaN
         rs = exp(lse_rest - (double)rm * a.inv_t);
     } else if (a.stats != nullptr) {
-        rest_of_row(a, row, w, &rm, &rs);
-    } else {
-        const RestPart* p = a.parts + (int64_t)r * a.splits;
-        rm = kNegInf;
-        for (int i = t; i < a.splits; i += kTT) rm = fmaxf(rm, p[i].m);
-        rm = block_max_f32<kTT>(rm, w.tmp_f);
-        if (rm == kNegInf) rm = 0.0f;
-        for (int i = t; i < a.splits; i += kTT)
-            rs += p[i].s * (p[i].m > kNegInf ? power.power(((double)p[i].m - (double)rm) * a.inv_t * k16Log2e) : 1.0);
-        rs = block_sum_f64<kTT>(rs, w.tmp_d);
+        rest_of_row<T, NT>(a, row, w, tmp_f[0], tmp_s, &rm, &rs);
     }
+    if (rm == kNegInf) rm = 0.0f;
     const float lm = zm == kNegInf ? rm : zm;
-    double ps = 0.0, ls = 0.0, cost = 0.0;
-    for (int k = t; k < a.K; k += kTT) {
+    double ps = 0.0, ls = 0.0, cost = 0.0, part_s = 0.0;
+    if (a.stats == nullptr)
+        for (int i = t; i < a.splits; i += NT) {
+            const RestPart x = parts_of[i];
+            part_s += x.s * (x.m > kNegInf ? power.power(((double)x.m - (double)rm) * a.inv_t * k16Log2e) : 1.0);
+        }
+    for (int k = t; k < a.K; k += NT) {
         if (w.id[k] < 0) continue;
         const EntryTerms x(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
         ps += x.w;
         ls += x.l;
         cost += x.cost;
     }
-    ps = block_sum_f64<kTT>(ps, w.tmp_d);
-    ls = block_sum_f64<kTT>(ls, w.tmp_d);
+    {
+        const double x0 = wave_sum_f64(part_s), x1 = wave_sum_f64(ps), x2 = wave_sum_f64(ls), x3 = wave_sum_f64(cost);
+        const double x4 = wave_sum_f64((double)n);
+        if (lane_id() == 0) {
+            tmp_d[0][wave] = x0;
+            tmp_d[1][wave] = x1;
+            tmp_d[2][wave] = x2;
+            tmp_d[3][wave] = x3;
+            tmp_n[wave] = (int)x4;
+        }
+    }
+    lds_barrier();
+    int entries = 0;
+    part_s = ps = ls = cost = 0.0;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) {
+        part_s += tmp_d[0][i];
+        ps += tmp_d[1][i];
+        ls += tmp_d[2][i];
+        cost += tmp_d[3][i];
+        entries += tmp_n[i];
+    }
+    if (a.stats == nullptr) rs = part_s;
     const RowTerms q(a, power, entries, rm, rs, lm, ls, ps, weight);
     if (part == 0 && a.stats == nullptr) {
-        cost = block_sum_f64<kTT>(cost, w.tmp_d);
         if (t < kWave) {
             float loss;
             q.results(a, cost, &loss, &lse, &lse_rest);
@@ -326,7 +407,7 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
     if (q.still) no_gradient();
     if (q.still || !grad) return;
     const float c = (float)(a.inv_t * 1.4426950408889634);
-    for (int v = v0 + t * 8; v < v1; v += kTT * 8) {
+    for (int v = v0 + t * 8; v < v1; v += NT * 8) {
         float z[8];
         load_part(row + v, v1 - v, kNegInf, z);
 #pragma unroll
@@ -334,7 +415,7 @@ __global__ __launch_bounds__(kTT) void distill_finish_kernel(DistillArgs a, int 
         store_part(grad + v, v1 - v, z);
     }
     __syncthreads();  // the listed tokens' entries are written over what stands there
-    for (int k = t; k < a.K; k += kTT) {
+    for (int k = t; k < a.K; k += NT) {
         const int x = w.id[k];
         if (x < v0 || x >= v1) continue;
         const EntryTerms y(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
@@ -370,10 +451,6 @@ struct Vec<uint16_t> {
             x[2 * i + 1] = bf16_hi(w[i]);
         }
     }
-    __device__ __forceinline__ static float top(const float (&x)[8]) { return max8(x); }
-    __device__ __forceinline__ static float sum(const float (&x)[8]) {
-        return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-    }
     __device__ __forceinline__ static void store(uint16_t* row, uint32_t byte, const float (&x)[8]) {
         store8(reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(row) + byte), x);
     }
@@ -388,8 +465,6 @@ struct Vec<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
     }
-    __device__ __forceinline__ static float top(const float (&x)[4]) { return fmaxf(max3(x[0], x[1], x[2]), x[3]); }
-    __device__ __forceinline__ static float sum(const float (&x)[4]) { return (x[0] + x[1]) + (x[2] + x[3]); }
     __device__ __forceinline__ static void store(float* row, uint32_t byte, const float (&x)[4]) {
         u32x4_w w;
 #pragma unroll
@@ -440,30 +515,8 @@ __device__ __forceinline__ double over_waves_sum(const double* x) {
     return readlane_f64(y, 15);
 }
 
-// A thread's share of a row's softmax pieces.
-struct RestSum {
-    float m;
-    double s;
-    __device__ __forceinline__ void rescale(float top, float c) {
-        if (top > m) {
-            s *= (double)__builtin_amdgcn_exp2f((m - top) * c);
-            m = top;
-        }
-    }
-    // Adds a vector.  A NaN or +inf logit makes s NaN and with it the row.
-    template <typename T>
-    __device__ __forceinline__ void add(float (&x)[Vec<T>::E], float c, bool counts) {
-        rescale(Vec<T>::top(x), c);
-        const float ref = m > kNegInf ? m : 0.0f;
-#pragma unroll
-        for (int k = 0; k < Vec<T>::E; ++k) x[k] = __builtin_amdgcn_exp2f((x[k] - ref) * c);
-        const float e = Vec<T>::sum(x);
-        s += counts ? (double)e : 0.0;
-    }
-};
-
 // 128 registers a thread: four waves to a SIMD, in one workgroup or several.
-template <typename T, int NT, int NV, bool GRAD>
+template <typename T, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
     using X = Vec<T>;
     constexpr int kW = NT / kWave;
@@ -498,11 +551,9 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
                 if (a.out_loss) a.out_loss[r] = 0.0f;
                 if (a.out_stats) a.out_stats[2 * (int64_t)r] = a.out_stats[2 * (int64_t)r + 1] = 0.0;
             }
-            if (GRAD) {
-                const float zero[8] = {};
-                T* grad = grad_at(r);
-                for (int v = t * 8; v < V; v += NT * 8) store_part(grad + v, V - v, zero);
-            }
+            const float zero[8] = {};
+            T* grad = grad_at(r);
+            for (int v = t * 8; v < V; v += NT * 8) store_part(grad + v, V - v, zero);
         }
         return r;
     };
@@ -565,12 +616,8 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
         __asm__ volatile("" : "+v"(held[i]));
         float x[E];
         X::get(held[i], x);
-        const uint32_t out = bits_of(listed, p.at(i) * E);
-        if (out)
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if ((out >> j) & 1u) x[j] = kNegInf;
-        sum.add<T>(x, c, i * NT < p.count);
+        mask_listed(x, bits_of(listed, p.at(i) * E));
+        sum.add(x, c, i * NT < p.count);
         __asm__ volatile("" : "+v"(sum.m), "+v"(sum.s));
     };
     auto add_last = [&](const uint32_t* listed) {
@@ -683,7 +730,7 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
         then = read_entry(after);
 
         // the gradient of this row, the next row's vectors and their sums
-        T* grad = GRAD ? grad_at(r) : nullptr;
+        T* grad = grad_at(r);
         const float factor = w.factor;
         sum = RestSum{kNegInf, 0.0};
         const uint32_t* next_listed = q.listed + set1 * q.words;
@@ -701,7 +748,7 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
             for (int k = 0; k < E; ++k) x[k] = factor * __builtin_amdgcn_exp2f((x[k] - rm) * c);
             X::store(grad, (uint32_t)p.at(i) * 16u, x);
         };
-        if (GRAD && has_last) {
+        if (has_last) {
             const bool in = (listed[v_last >> 5] >> (v_last & 31)) & 1u;
             store_elt(grad + v_last, in ? at_entry(v_last) : factor * __builtin_amdgcn_exp2f((to_f32(last) - rm) * c));
         }
@@ -711,7 +758,7 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
         if (has_last) last = next_row[v_last];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            if (GRAD) gradient(p, i);
+            gradient(p, i);
             p1.renew();
             held[i] = X::load(next_row, (uint32_t)p1.at(i) * 16u);
             __builtin_amdgcn_sched_barrier(0);
@@ -719,13 +766,11 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         }
         // the list's entries, over what their own thread has just stored there
-        if (GRAD) {
-            for (int k = t; k < whole; k += NT)
-                for (uint32_t in = bits_of(listed, k * E); in; in &= in - 1) {
-                    const int v = k * E + __builtin_ctz(in);
-                    store_elt(grad + v, at_entry(v));
-                }
-        }
+        for (int k = t; k < whole; k += NT)
+            for (uint32_t in = bits_of(listed, k * E); in; in &= in - 1) {
+                const int v = k * E + __builtin_ctz(in);
+                store_elt(grad + v, at_entry(v));
+            }
         if (!more) return;
 #pragma unroll
         for (int i = NV - kLag; i < NV; ++i) {
@@ -820,34 +865,41 @@ bool run_pass(const DistillArgs& a, hipStream_t s) {
     const int whole = a.V / Vec<T>::E;
     if (whole > NV * NT || whole < NT || a.K > NT || lds > 60 * 1024) return false;
     const int grid = std::min(a.N, kPassCus * (1024 / NT));
-    if (a.grad) distill_pass_kernel<T, NT, NV, true><<<grid, NT, (uint32_t)lds, s>>>(a);
-    else distill_pass_kernel<T, NT, NV, false><<<grid, NT, (uint32_t)lds, s>>>(a);
+    distill_pass_kernel<T, NT, NV><<<grid, NT, (uint32_t)lds, s>>>(a);
     return true;
 }
 
-// Whether the row's loads fill the chip from one workgroup to a row.
+// One pass where there are rows enough for the chip, or short ones.  Measured with
+// its gradient, one pass and two, us: bf16 rows of 32000, 64 of them 17.9 and
+// 13.7, 128 18.6 and 20.5, 1024 39.1 and 46.8; of 128256, 128 of them 35.4 and
+// 28.5, 256 40.3 and 45.0, 1024 134 and 179; rows of 32 KiB and less alike for
+// any number (64 x 8192 fp32 11.8 and 11.5), where one pass is one launch.
 template <typename T>
-bool one_pass(const DistillArgs& a) { return true; }
+bool one_pass(const DistillArgs& a) { return a.N >= 160 || a.V * sizeof(T) <= 32768; }
 
 template <typename T>
 dyna_status run_distill(const DistillArgs& a, hipStream_t s) {
     if (a.stats == nullptr) {
-        if (one_pass<T>(a) && (run_pass<T, 256, 8>(a, s) || run_pass<T, 256, 16>(a, s) || run_pass<T, 512, 16>(a, s) ||
+        if (a.grad && one_pass<T>(a) && (run_pass<T, 256, 8>(a, s) || run_pass<T, 256, 16>(a, s) || run_pass<T, 512, 16>(a, s) ||
                                run_pass<T, 1024, 16>(a, s)))
             return check_launch("distill");
         rest_parts_kernel<T><<<(uint32_t)((int64_t)a.N * a.splits), kTT, 0, s>>>(a);
     }
-    const int parts = a.grad ? a.splits : 1;
-    distill_finish_kernel<T><<<(uint32_t)((int64_t)a.N * parts), kTT, 0, s>>>(a, parts);
+    const uint32_t lds = list_lds_bytes(a.K);
+    // a loss alone needs no more than a wave to a row
+    if (a.grad) distill_finish_kernel<T, kTT><<<(uint32_t)((int64_t)a.N * a.splits), kTT, lds, s>>>(a, a.splits);
+    else distill_finish_kernel<T, kWave><<<a.N, kWave, lds, s>>>(a, 1);
     return check_launch("distill");
 }
 
 }  // namespace
 
 size_t distill_ws_bytes(int32_t N, int32_t V, DistillArgs* a, void* ws) {
+    // parts of at least one step of a workgroup, 1024 in all: twice as many take as
+    // long to launch as they save (64 x 128256 bf16 with its gradient 22.0 and 19.6 us)
     const int64_t most = (V + kPartStep - 1) / kPartStep, least = (V + kMaxSplitLen - 1) / kMaxSplitLen;
-    int64_t splits = std::min<int64_t>(most, std::max<int64_t>(least, (2048 + (int64_t)N - 1) / N));
-    const int64_t len = ((V + splits - 1) / splits + kPartStep - 1) / kPartStep * kPartStep;
+    int64_t splits = std::min<int64_t>(most, std::max<int64_t>(least, 1024 / N));
+    const int64_t len = ((V + splits - 1) / splits + 255) / 256 * 256;
     splits = (V + len - 1) / len;
     if (a) {
         a->splits = (int32_t)splits;

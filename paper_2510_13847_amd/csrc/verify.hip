@@ -162,10 +162,20 @@ __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
         for (int i = 0; i < kFlight; ++i) r[i].get(z[i]);
         run.take_any(z, v, kStep);
     }
-    for (; v < v1; v += kStep) {
-        float z[1][8];
-        load_part(x + v, v1 - v, kNegInf, z[0]);
-        run.take_any(z, v, kStep);
+    if (v < v1) {  // what is left of the part, its loads together too
+        Row8<T> r[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            if (v + i * kStep + 8 <= v1) r[i].load(x + v + i * kStep);
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int at = v + i * kStep;
+            if (at >= v1) break;
+            float z[1][8];
+            if (at + 8 <= v1) r[i].get(z[0]);
+            else load_part(x + at, v1 - at, kNegInf, z[0]);
+            run.take_any(z, at, kStep);
+        }
     }
     const float top = block_max_f32<kVT>(run.m, tmp_f);
     const double mine = run.m > kNegInf ? run.s * (double)__builtin_amdgcn_exp2f((run.m - top) * run.c) : 0.0;
