@@ -13,10 +13,10 @@ constexpr int kPartStep = 2048;  // rows are cut in steps of 256 threads of 8
 struct WalkEnd {
     int32_t node;   // its last accepted node (0: none accepted)
     int32_t depth;  // accepted drafts
-    int32_t mode;   // kDrawNone, kDrawTarget, kDrawResidual
+    int32_t mode;   // one of the values below
     int32_t pad;
 };
-enum { kDrawNone = 0, kDrawTarget = 1, kDrawResidual = 2 };
+enum { kDrawNone = 0, kDrawTarget = 1, kDrawResidual = 2, kDrawLeaf = 3 };
 
 // Softmax pieces of a row's part: largest logit (and its lowest index), sum of
 // exp((z - m) / T).
@@ -59,6 +59,7 @@ struct VerifyArgs {
     int32_t B, N;                      // N rows (nodes) per request; a chain of n drafts has n + 1
     bool chain;
     bool greedy;
+    bool late_leaves;                  // greedy trees: a leaf's row is read only if the walk ends in it
     // trees
     const int32_t* tokens;   // [B, N]
     const int32_t* parents;  // [N] or [B, N]

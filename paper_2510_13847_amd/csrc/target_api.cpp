@@ -11,6 +11,12 @@ namespace dyna {
 namespace {
 
 constexpr int32_t kMaxVocab = 1 << 20;
+// Bytes of a greedy call's rows from which on a leaf's row is left until a walk
+// ends in it.  Most rows of a tree are leaves; the price is two more launches,
+// one behind the other.  Trees of 61 nodes over 128256 bf16 entries, the whole
+// call, all rows / late leaves in us: 125 MB 33 / 39, 188 MB 41 / 44, 250 MB
+// 50 / 45, 376 MB 76 / 54, 501 MB 98 / 64.
+constexpr int64_t kLateLeafBytes = 200 << 20;
 constexpr int64_t kMaxBlocks = 1 << 23;  // workgroups of 256 threads in one launch: below 2^32 threads
 
 bool valid_dtype(int32_t t) { return t == DYNA_F32 || t == DYNA_BF16; }
@@ -214,6 +220,7 @@ DYNA_API dyna_status dyna_verify_tree(const void* target, int32_t tdtype, int32_
     a.tokens = tokens;
     a.parents = parents;
     a.parent_stride = parent_stride;
+    a.late_leaves = a.greedy && (int64_t)B * N * V * (int64_t)elt_size(tdtype) >= kLateLeafBytes;
     a.inv_t = a.greedy ? 1.0 : 1.0 / (double)temperature;
     a.uniforms = uniforms;
     a.out_len = out_len;

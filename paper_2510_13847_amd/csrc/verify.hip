@@ -128,20 +128,23 @@ struct Running {
 // then stream at 4.6 TB/s.
 constexpr int kFlight = 4;
 
-// Pieces of one part of one row, where a walk can need them.
-template <typename T>
+// Pieces of one part of one row, where a walk can need them; LEAF: of the leaves
+// that greedy walks have ended in.
+template <typename T, bool LEAF>
 __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
     __shared__ float tmp_f[kVT / kWave];
     __shared__ double tmp_d[kVT / kWave];
     __shared__ uint64_t tmp_k[kVT / kWave];
-    const int row = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
+    const int item = blockIdx.x / a.splits, part = blockIdx.x % a.splits;
+    if (LEAF && a.ends[item].mode != kDrawLeaf) return;
+    const int row = LEAF ? item * a.N + a.ends[item].node : item;
     const int b = row / a.N, j = row % a.N;
     // a row is needed if drafts hang under it (their p, and in a greedy walk
     // the token), or if a greedy walk can end there
     if (a.chain) {
         const int len = chain_len(a, b);
         if (j > len || (j == len && !a.greedy)) return;
-    } else if (!a.greedy) {
+    } else if (!LEAF && (!a.greedy || a.late_leaves)) {
         // every wave looks for itself: most rows of a tree are leaves, and their
         // workgroups leave without a barrier
         bool kid = false;
@@ -324,6 +327,12 @@ __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     __syncthreads();
     const int depth = w.depth, node = w.node;
     const int64_t o = (int64_t)b * N;
+    bool leaf = false;
+    if (a.greedy && a.late_leaves) {
+        bool kid = false;
+        for (int j = node + 1 + t; j < N; j += NT) kid |= w.parent[j] == node;
+        leaf = !__syncthreads_or(kid);
+    }
     for (int i = t; i < N; i += NT) {
         int id = -1, at = -1;
         float lp = kNegInf;
@@ -335,20 +344,51 @@ __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
             id = w.best[node];
             lp = (float)-log(w.sum[node]);
         }
-        // slot `depth` of a sampled request is the drawing kernel's
-        if (i == depth && !a.greedy) continue;
+        // slot `depth` of a sampled request is the drawing kernel's, of a leaf the
+        // joining kernel's
+        if (i == depth && (!a.greedy || leaf)) continue;
         a.out_ids[o + i] = id;
         if (a.out_logprobs) a.out_logprobs[o + i] = lp;
         if (a.out_nodes) a.out_nodes[o + i] = at;
     }
     if (t == 0) {
         a.out_len[b] = depth;
-        if (!a.greedy) {
-            if (a.out_nodes) a.out_nodes[o + depth] = -1;
+        if (a.out_nodes) a.out_nodes[o + depth] = -1;
+        if (a.greedy) {
+            a.ends[b] = WalkEnd{node, depth, leaf ? kDrawLeaf : kDrawNone, 0};
+        } else {
             int mode = kDrawTarget;
             if (a.chain && node < len && w.token[node + 1] >= 0 && st.s[node].logits != nullptr) mode = kDrawResidual;
             a.ends[b] = WalkEnd{node, depth, mode, 0};
         }
+    }
+}
+
+// The token of a leaf's row, a wave to a request.
+__global__ __launch_bounds__(kWave) void leaf_kernel(VerifyArgs a) {
+    __shared__ double table[16];
+    const int b = blockIdx.x, t = threadIdx.x;
+    const WalkEnd e = a.ends[b];
+    if (e.mode != kDrawLeaf) return;
+    fill_wave_table(table);
+    const Weigher weight{table, a.inv_t * k16Log2e};
+    const RowPart* p = a.parts + ((int64_t)b * a.N + e.node) * a.splits;
+    float m = kNegInf;
+    for (int i = t; i < a.splits; i += kWave) m = fmaxf(m, p[i].m);
+    const float top = wave_max_all(m);
+    double s = 0.0;
+    int best = INT32_MAX;
+    for (int i = t; i < a.splits; i += kWave) {
+        s += p[i].s * weight(p[i].m, top);
+        if (p[i].m == top) best = min(best, p[i].best);
+    }
+    s = wave_sum_f64(s);
+#pragma unroll
+    for (int o = kWave / 2; o > 0; o >>= 1) best = min(best, __shfl_xor(best, o, kWave));
+    if (t == 0) {
+        const int64_t o = (int64_t)b * a.N + e.depth;
+        a.out_ids[o] = top > kNegInf ? best : -1;
+        if (a.out_logprobs) a.out_logprobs[o] = top > kNegInf ? (float)-log(s) : kNegInf;
     }
 }
 
@@ -951,11 +991,17 @@ __global__ __launch_bounds__(kVT) void token_rows_kernel(const int32_t* perm, co
 
 template <typename T>
 dyna_status run(const VerifyArgs& a, const StepTable& st, const DrawNeeds& q, hipStream_t s) {
-    row_parts_kernel<T><<<(uint32_t)((int64_t)a.B * a.N * a.splits), kVT, 0, s>>>(a);
+    row_parts_kernel<T, false><<<(uint32_t)((int64_t)a.B * a.N * a.splits), kVT, 0, s>>>(a);
     // 16 lanes to a row: all rows of a tree of up to 64 nodes at once
     if (a.N > 16) walk_kernel<T, 1024><<<a.B, 1024, 0, s>>>(a, st);
     else walk_kernel<T, kVT><<<a.B, kVT, 0, s>>>(a, st);
-    if (a.greedy) return check_launch("verify");
+    if (a.greedy) {
+        if (a.late_leaves) {
+            row_parts_kernel<T, true><<<(uint32_t)((int64_t)a.B * a.splits), kVT, 0, s>>>(a);
+            leaf_kernel<<<a.B, kWave, 0, s>>>(a);
+        }
+        return check_launch("verify");
+    }
     const bool clusters = q.pieces > 0 && a.M > 0;
     const uint32_t set = clusters ? 8u * (uint32_t)((a.M + 63) / 64 + q.entries) : 0u;
     const int extra = (q.pieces + kWaves - 1) / kWaves + (q.mapped ? 1 : 0);
@@ -982,12 +1028,14 @@ dyna_status launch_token_rows(const int32_t* perm, const int32_t* offsets, int32
     return check_launch("token rows");
 }
 
-// Parts of a row: 20480 entries (ten steps of a workgroup), or fewer where the
-// rows alone would leave the chip without 2048 workgroups.
+// Parts of a row: up to 32768 entries, or fewer where the rows alone would leave
+// the chip without 2048 workgroups.  Shorter parts launch more workgroups, those
+// of a tree's leaves among them, which leave at once: 32 trees of 61 nodes over
+// 128256 take 54 us in parts of 12288, 47 of 20480, 44 of 32768, 45 of 45056.
 size_t verify_ws_bytes(int32_t B, int32_t N, int32_t V, int32_t M, VerifyArgs* a, void* ws) {
     const int64_t rows = (int64_t)B * N;
     const int64_t steps = (V + kPartStep - 1) / kPartStep, most = (V + kChunk - 1) / kChunk;
-    int64_t splits = std::min(steps, std::max<int64_t>((V + 20479) / 20480, (2048 + rows - 1) / rows));
+    int64_t splits = std::min(steps, std::max<int64_t>((V + 32767) / 32768, (2048 + rows - 1) / rows));
     const int64_t len = (steps + splits - 1) / splits * kPartStep;
     splits = (V + len - 1) / len;
     char* p = static_cast<char*>(ws);

@@ -285,6 +285,32 @@ def test_clusters_out_of_range_or_repeated_are_ignored():
         check(v, 0, want, V)
 
 
+@pytest.mark.parametrize("V,dtype", [(130003, torch.bfloat16), (65003, torch.float32)])
+def test_greedy_walks_that_end_in_leaves(V, dtype):
+    """Large greedy calls read a leaf's row only where a walk ends in it: rows of
+    all kinds behind such walks, masked ones and ones of equal logits among them."""
+    B, N = 28, 30
+    g = torch.Generator().manual_seed(2)
+    t = torch.empty((B, N, V)).normal_(0.0, 3.0, generator=g).to(dtype)
+    parents = torch.tensor([0] + [(j - 1) // 2 for j in range(1, N)], dtype=torch.int32)
+    tokens = torch.full((B, N), 3, dtype=torch.int32)
+    for b in range(B):
+        for j in range(1, N):
+            if (j + b) % 2 or b in (3, 4, 5):  # the parent's best token
+                tokens[b, j] = int(t[b, (j - 1) // 2].float().argmax())
+    t[3, 15:] = -math.inf
+    t[4, 15:] = 1.0
+    t[5, 15:] = math.nan
+    v = D.verify_tree(t.to(DEV), tokens.to(DEV), parents.to(DEV), None, 0.0)
+    leaves = set()
+    for b in range(B):
+        want = O.verify_tree(f64(t[b]), tokens[b].tolist(), parents.tolist(), [0.0] * N, 0.0)
+        check(v, b, want, V, nodes=True)
+        if want[0] == 4:
+            leaves.add(b)
+    assert {3, 4, 5} <= leaves and len(leaves) >= 5
+
+
 def random_tree(N, rng, spread):
     parents = np.zeros(N, dtype=np.int32)
     for j in range(1, N):
