@@ -380,7 +380,8 @@ int32_t dyna_static_budget(int32_t t, int32_t k_max);
 /* Rules of both calls:
  *  target   device, tdtype, logits of the target model: row j of request b is
  *           V consecutive elements at b * batch_stride + j * row_stride
- *           (strides in elements, any alignment of the element; V <= 2^20).  p_j =
+ *           (strides in elements, any alignment of the element; V <= 2^20, and
+ *           B * rows * ceil(V / 2048) <= 2^23, B <= 2^21).  p_j =
  *           softmax(row / temperature).  NaN counts as -inf (a masked token),
  *           +inf as the largest finite number.
  *  temperature  >= 0; 0 is greedy: a draft stands when it is the row's largest
@@ -434,7 +435,8 @@ size_t dyna_verify_workspace_bytes(int32_t B, int32_t rows, int32_t V, int32_t M
  * The first draft that falls ends the chain.  The token in its place is drawn
  * from max(p - q, 0), q the draft's whole distribution, (1 - beta) softmax over
  * its shortlist and beta spread over the rest; for a draft proposed outright
- * from p without its token; from p where those leave nothing.
+ * from p without its token; from p where those leave nothing (less than 2^-40
+ * of p, which is what the sums' rounding can leave of two equal distributions).
  * L and token_rows may be NULL when no step has clusters; L->V == V. */
 dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32_t V, int64_t row_stride,
                               int64_t batch_stride, int32_t B, int32_t n, const dyna_draft_step* steps,
@@ -489,7 +491,7 @@ size_t dyna_distill_workspace_bytes(int32_t N, int32_t V);
  *                 (0 for a padding row)
  *  grad           device, dtype, row r at r * grad_stride, may be NULL: weights[r] *
  *                 d loss[r] / d logits[r]; elements behind a row are left as they
- *                 were; must not overlap logits
+ *                 were; the spans of both, gaps between rows included, must not overlap
  * A row without entries (or with every value -inf, tail 0) has loss and
  * gradient 0.  A masked logit (-inf) has q = 0: the loss is +inf where the
  * teacher gives it weight, the gradient stays finite.  A NaN or +inf logit or
@@ -515,7 +517,7 @@ dyna_status dyna_distill_grad(const void* logits, int32_t dtype, int32_t V, int6
  *  pos_weight     > 0
  *  out_loss [N]   device fp32 (not weighted), may be NULL with grad
  *  grad           as above, may be NULL with out_loss.  May be `scores` itself
- *                 (same strides); otherwise the two must not overlap.
+ *                 (same strides); otherwise their spans must not overlap.
  * M <= DYNA_MAX_M. */
 dyna_status dyna_router_loss(const void* scores, int32_t dtype, int32_t M, int64_t row_stride, int32_t N,
                              const int32_t* ids, int32_t L, const int32_t* cluster_of, int32_t V,

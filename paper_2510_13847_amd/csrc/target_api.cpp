@@ -17,7 +17,8 @@ constexpr int32_t kMaxVocab = 1 << 20;
 // call, all rows / late leaves in us: 125 MB 33 / 39, 188 MB 41 / 44, 250 MB
 // 50 / 45, 376 MB 76 / 54, 501 MB 98 / 64.
 constexpr int64_t kLateLeafBytes = 200 << 20;
-constexpr int64_t kMaxBlocks = 1 << 23;  // workgroups of 256 threads in one launch: below 2^32 threads
+constexpr int64_t kMaxBlocks = 1 << 23;   // workgroups of 256 threads in one launch: below 2^32 threads
+constexpr int32_t kMaxRequests = 1 << 21; // of 1024 threads, one to a request
 
 bool valid_dtype(int32_t t) { return t == DYNA_F32 || t == DYNA_BF16; }
 size_t elt_size(int32_t t) { return t == DYNA_BF16 ? 2 : 4; }
@@ -63,7 +64,7 @@ dyna_status check_verify_sizes(int32_t tdtype, int32_t V, int32_t B, int32_t row
     if (V > kMaxVocab) return set_error(DYNA_ERR_UNSUPPORTED, "V=%d > %d", V, kMaxVocab);
     REQUIRE(B >= 0, "B=%d < 0", B);
     const int64_t steps = (V + kPartStep - 1) / kPartStep, chunks = (V + kChunk - 1) / kChunk;
-    if ((int64_t)B * rows * steps > kMaxBlocks || (int64_t)B * chunks > kMaxBlocks)
+    if ((int64_t)B * rows * steps > kMaxBlocks || (int64_t)B * chunks > kMaxBlocks || B > kMaxRequests)
         return set_error(DYNA_ERR_UNSUPPORTED, "%d requests of %d rows of %d logits in one call", B, rows, V);
     return DYNA_OK;
 }

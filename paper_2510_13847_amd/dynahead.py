@@ -641,9 +641,13 @@ class ChainVerifier(_Verifier):
 
     def __init__(self, B: int, n: int, V: int, temperature: float = 1.0, layout: Optional[Layout] = None,
                  device="cuda"):
+        import torch
         super().__init__(B, n + 1, V, temperature, layout.M if layout is not None else 0, device)
         self.n, self.layout = n, layout
         self.token_rows = token_rows(layout) if layout is not None else None
+        if layout is not None and not torch.cuda.is_current_stream_capturing():
+            # calls on other streams read it too
+            torch.cuda.current_stream(self.device).synchronize()
         self._steps = (_DraftStep * max(n, 1))()
         self._fixed = (layout.c if layout is not None else None, _ptr(self.token_rows), _ptr(self.lengths),
                        _ptr(self.ids), _ptr(self.logprobs), _ptr(self.ws), self.ws.numel())
@@ -704,14 +708,24 @@ class TreeVerifier(_Verifier):
 
 def verify_chain(target, steps, uniforms=None, lens=None, temperature=1.0, layout=None, stream=None):
     """One dyna_verify_chain call with fresh outputs (see ChainVerifier for repeated calls)."""
+    if stream is not None:  # the outputs and the workspace are that stream's too
+        import torch
+        _stream_device(stream, target.device)
+        with torch.cuda.stream(stream):
+            return verify_chain(target, steps, uniforms, lens, temperature, layout)
     v = ChainVerifier(target.shape[0], len(steps), target.shape[2], temperature, layout, target.device)
-    return v(target, steps, uniforms, lens, stream)
+    return v(target, steps, uniforms, lens)
 
 
 def verify_tree(target, tokens, parents, uniforms=None, temperature=1.0, stream=None):
     """One dyna_verify_tree call with fresh outputs (see TreeVerifier for repeated calls)."""
+    if stream is not None:  # the outputs and the workspace are that stream's too
+        import torch
+        _stream_device(stream, target.device)
+        with torch.cuda.stream(stream):
+            return verify_tree(target, tokens, parents, uniforms, temperature)
     v = TreeVerifier(target.shape[0], target.shape[1], target.shape[2], temperature, target.device)
-    return v(target, tokens, parents, uniforms, stream)
+    return v(target, tokens, parents, uniforms)
 
 
 # ---------------------------------------------------------------- learning from the target's top tokens

@@ -251,6 +251,56 @@ def test_chain_strided_target_and_untouched_neighbours():
         check(ver, b, chain_oracle(target, steps, dists, u, None, 1.0, b), V)
 
 
+def test_chain_on_a_stream_that_did_not_make_the_verifier():
+    """The verifier's own table of the layout is whole before a call on another
+    stream reads it, whatever stood before it on the stream that made it.  The
+    shortlist is too long for one workgroup, so every slot is found in the table."""
+    V, B, n = 50021, 2, 2
+    g = torch.Generator().manual_seed(31)
+    t = (3.0 * torch.randn((B, n + 1, V), generator=g)).to(torch.bfloat16).to(DEV)
+    target = f64(t)
+    of, layout, steps, dists = make_steps(B, n, V, "clusters", 8, M=20, k=16, target=target)
+    assert steps[0].logits.shape[1] > 32768
+    u = np.random.default_rng(3).random((B, n + 1)).astype(np.float32)
+    u[:, 0] = 0.9999  # most first drafts fall: the residual is drawn
+    uu = torch.from_numpy(u).to(DEV)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    busy = torch.ones((4096, 4096), device=DEV)
+    for _ in range(20):
+        busy = busy @ busy * 1e-4
+    ver = D.ChainVerifier(B, n, V, 1.0, layout)
+    ver(t, steps, uu, stream=side)
+    fresh = D.verify_chain(t, steps, uu, temperature=1.0, layout=layout, stream=side)
+    side.synchronize()
+    for b in range(B):
+        want = chain_oracle(target, steps, dists, u, None, 1.0, b)
+        check(ver, b, want, V)
+        check(fresh, b, want, V)
+
+
+def test_two_verifiers_at_once():
+    """Calls on two streams, each with its own verifier, leave each other alone."""
+    V, B, n = 32003, 4, 3
+    runs = []
+    for seed in (5, 6):
+        g = torch.Generator().manual_seed(seed)
+        t = (3.0 * torch.randn((B, n + 1, V), generator=g)).to(torch.bfloat16).to(DEV)
+        target = f64(t)
+        _, layout, steps, dists = make_steps(B, n, V, "clusters", seed, M=64, k=9, target=target)
+        u = np.random.default_rng(seed).random((B, n + 1)).astype(np.float32)
+        runs.append((t, target, steps, dists, u, torch.from_numpy(u).to(DEV), D.ChainVerifier(B, n, V, 1.0, layout),
+                     torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for t, _, steps, _, _, uu, ver, s in runs:
+            ver(t, steps, uu, stream=s)
+    torch.cuda.synchronize()
+    for t, target, steps, dists, u, _, ver, _ in runs:
+        for b in range(B):
+            check(ver, b, chain_oracle(target, steps, dists, u, None, 1.0, b), V)
+
+
 def test_chain_rows_beyond_32_bit_offsets():
     V, n = 3001, 1
     stride = (1 << 32) // 2 + 1001               # elements: the second request starts past 4 GiB

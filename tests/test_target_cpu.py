@@ -33,6 +33,7 @@ def test_chain_argument_errors():
     assert _chain(V=(1 << 22) + 1) == D.ERR_UNSUPPORTED
     assert _chain(B=-1) == D.ERR_INVALID_ARG
     assert _chain(B=1 << 23) == D.ERR_UNSUPPORTED           # more work items than one launch takes
+    assert _chain(B=(1 << 21) + 1, n=1, V=8) == D.ERR_UNSUPPORTED  # requests: one workgroup of 1024 threads each
     assert _chain(dtype=2) == D.ERR_INVALID_ARG
     assert _chain(target=None) == D.ERR_INVALID_ARG
     assert _chain(target=P + 1) == D.ERR_INVALID_ARG
