@@ -18,7 +18,7 @@
 namespace dyna {
 namespace {
 
-constexpr int kVT = 256;  // threads of every kernel here
+constexpr int kVT = 256;  // threads of a workgroup, where a kernel takes no other number
 constexpr int kNoSlot = INT32_MIN;
 constexpr int kDrawWaves = 256 * 32;  // waves that the chip holds
 
@@ -124,12 +124,19 @@ struct Running {
     }
 };
 
-// Vectors a thread has in flight.  One was measured too: the batches' rows
-// then stream at 4.6 TB/s.
+// Vectors a thread has in flight: the rows of 128 chains of 4 drafts over 262144
+// (268 MB of bf16) stream at 5.9 TB/s, with one vector at 4.6.
 constexpr int kFlight = 4;
 
 // Pieces of one part of one row, where a walk can need them; LEAF: of the leaves
-// that greedy walks have ended in.
+// that greedy walks have ended in.  One pass with a running maximum and sum per
+// thread: exponentials in 32 bits relative to it, eight to a vector and four
+// vectors to a sum in 64 bits, so that p is right to about 2^-23.  Bound by HBM:
+// 268 MB in 45.6 us (5.9 TB/s), 24.6 MB in 7.4; 1952 rows of 32 trees, of which
+// the 213 MB of rows with children are read, in 45.7.  Rows are cut in parts and
+// joined by the walk, so that one request fills the chip too (1.3 MB: 3.6 us, a
+// launch's time).  2048 or 4096 workgroups that go through the parts in a loop
+// were slower (58 and 53 us for the 268 MB).
 template <typename T, bool LEAF>
 __global__ __launch_bounds__(kVT) void row_parts_kernel(VerifyArgs a) {
     __shared__ float tmp_f[kVT / kWave];
@@ -210,7 +217,9 @@ struct WalkLds {
 
 // One workgroup per request.  Whether a draft stands, once its siblings before
 // it have fallen, does not depend on the walk, so all are tested at once; the
-// walk then only follows the drafts that stand.
+// walk then only follows the drafts that stand.  Bound by the latency of the
+// loads that wait for each other (token, its logit; parts) and by barriers: 6.9 us
+// for 1 to 128 chains of 4 to 5 drafts, 7.3 and 8.0 for 1 and 32 trees of 61 nodes.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     __shared__ WalkLds w;
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     }
 }
 
-// The token of a leaf's row, a wave to a request.
+// The token of a leaf's row, a wave to a request: the join of its few parts.
 __global__ __launch_bounds__(kWave) void leaf_kernel(VerifyArgs a) {
     __shared__ double table[16];
     const int b = blockIdx.x, t = threadIdx.x;
@@ -490,6 +499,12 @@ __device__ __forceinline__ int list_clusters(const VerifyArgs& a, const uint32_t
 // row the walk ended in, per_wave to a wave.  Behind them: the same of 4 chunks of the
 // rejected draft's row, with the tokens of those slots and the target's logits
 // there; and one that maps clusters to slots for shortlists too long for that.
+// Bound by arithmetic where there are many rows: a weight in 64 bits is 14
+// instructions (rowstat.h) and 128 rows of 262144 take 45.2 us for 67 MB, 0.74 of
+// 10^12 weights a second; 16 rows of 151936 13.9 us, one of 128256 9.1, bound by the
+// clusters' list (a scan, then a search per slot).  The number of waves that share
+// the chunks changes little (16 per compute unit 50 us, 24 46.8, 32 45.3, 40 44.5, 64
+// 45.2); a chunk is 262 instructions, 127 of them in 64 bits and 60 its two reductions.
 template <typename T>
 __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int per_wave,
                                                          int n_pieces, int per) {
@@ -700,7 +715,9 @@ __device__ __forceinline__ int streamed_slot(const VerifyArgs& a, const dyna_dra
 
 // max(p - q, 0) chunk by chunk.  Long shortlists and contiguous logits take each
 // token's q; a listed step's tokens all take the tail's constant here, and the
-// drawing kernel puts the shortlist's right.
+// drawing kernel puts the shortlist's right.  The row comes from the cache that the
+// pieces' pass left it in; every workgroup joins the pieces again, which is most
+// of its 8.9 us for 16 rows of 151936 and cheaper than a launch that joins them once.
 template <typename T>
 __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable st, int per, int n_pieces) {
     __shared__ double table[16];
@@ -758,6 +775,11 @@ constexpr double kFixOne = 0x1p62;
 // their chunks by max(p - q, 0) - max(p - q_out, 0), without a tail -min(p, q),
 // as whole multiples of 2^-62, so that the order of the additions in LDS does
 // not matter.
+//
+// One workgroup goes through joins and scans that wait for each other: 12.1 us for
+// one chain with 32 clusters of 1024 over 128256, 14.5 us for 128 over 262144; with
+// outright drafts or trees 5.8 to 7.8.  A thousand threads with listed entries,
+// for the slots; 256 without, whose barriers are shorter.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces) {
     constexpr int kW = NT / kWave;
@@ -973,6 +995,8 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
 }
 
 // ---------------------------------------------------------------- token rows
+// Once per layout: 11.9 us for 262144 tokens in 4096 clusters, a search and a
+// scattered 8-byte store per token.
 __global__ __launch_bounds__(kVT) void token_rows_kernel(const int32_t* perm, const int32_t* offsets, int V, int M,
                                                          int32_t* token_rows) {
     const int j = blockIdx.x * kVT + threadIdx.x;
