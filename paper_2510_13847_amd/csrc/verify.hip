@@ -218,8 +218,9 @@ struct WalkLds {
 // One workgroup per request.  Whether a draft stands, once its siblings before
 // it have fallen, does not depend on the walk, so all are tested at once; the
 // walk then only follows the drafts that stand.  Bound by the latency of the
-// loads that wait for each other (token, its logit; parts) and by barriers: 6.9 us
-// for 1 to 128 chains of 4 to 5 drafts, 7.3 and 8.0 for 1 and 32 trees of 61 nodes.
+// loads that wait for each other (token, then its logit) and by barriers: 5.3 us
+// for one chain of 5 drafts, 7.0 for 128 of 4, 6.9 and 8.0 for 1 and 32 trees of 61
+// nodes.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     __shared__ WalkLds w;
@@ -227,6 +228,21 @@ __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
     const int N = a.N;
     const int len = a.chain ? chain_len(a, b) : N - 1;
     const Weigher weight{w.table, a.inv_t * k16Log2e};
+    // 16 lanes join a row's parts (what stands in place of parts that were not
+    // written is not used).  A lane's first parts come in while the tokens and
+    // their logits are looked up
+    constexpr int kTeam = 16, kHold = 4;
+    const int i0 = t % kTeam;
+    RowPart held[kHold];
+    auto load_parts = [&](int j) {
+        const RowPart* p = a.parts + ((int64_t)b * N + j) * a.splits;
+#pragma unroll
+        for (int q = 0; q < kHold; ++q) {
+            held[q] = RowPart{0.0, kNegInf, -1};
+            if (j < N && i0 + q * kTeam < a.splits) held[q] = p[i0 + q * kTeam];
+        }
+    };
+    load_parts(t / kTeam);
     fill_weight_table(w.table);
     for (int j = t; j < N; j += NT) {
         const int x = j == 0 ? -1 : node_token(a, st, b, len, j), par = j == 0 ? -1 : node_parent(a, b, j);
@@ -242,29 +258,35 @@ __global__ __launch_bounds__(NT) void walk_kernel(VerifyArgs a, StepTable st) {
         w.bar[j] = bar;
     }
     __syncthreads();
-    // 16 lanes join a row's parts (what stands in place of parts that were not
-    // written is not used)
-    constexpr int kTeam = 16;
     for (int j0 = 0; j0 < N; j0 += NT / kTeam) {
-        const int j = j0 + t / kTeam, i0 = t % kTeam;
+        const int j = j0 + t / kTeam;
+        if (j0 > 0) load_parts(j);
         const bool have = j < N && (a.chain ? (j < len || (j == len && a.greedy)) : true);
         const RowPart* p = a.parts + ((int64_t)b * N + (have ? j : 0)) * a.splits;
         float m = kNegInf;
         double s = 0.0;
         int best = INT32_MAX;
-        if (have)
-#pragma unroll 4
-            for (int i = i0; i < a.splits; i += kTeam) {
+        if (have) {
+#pragma unroll
+            for (int q = 0; q < kHold; ++q) {
+                best = held[q].m > m ? held[q].best : best;
+                m = fmaxf(m, held[q].m);
+            }
+            for (int i = i0 + kHold * kTeam; i < a.splits; i += kTeam) {
                 const float x = p[i].m;
                 best = x > m ? p[i].best : best;
                 m = fmaxf(m, x);
             }
+        }
         float top = m;
 #pragma unroll
         for (int o = kTeam / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-        if (have)
-#pragma unroll 4
-            for (int i = i0; i < a.splits; i += kTeam) s += p[i].s * weight(p[i].m, top);
+        if (have) {
+#pragma unroll
+            for (int q = 0; q < kHold; ++q)
+                if (__any(held[q].m > kNegInf)) s += held[q].s * weight(held[q].m, top);
+            for (int i = i0 + kHold * kTeam; i < a.splits; i += kTeam) s += p[i].s * weight(p[i].m, top);
+        }
         best = m == top ? best : INT32_MAX;
 #pragma unroll
         for (int o = kTeam / 2; o > 0; o >>= 1) {
