@@ -111,6 +111,37 @@ def test_distill(N, V, K, dtype, T, tail):
     check_rows(logits, ids, values, T, tail, weights, None, None, back, rows)
 
 
+EDGES = [  # N, V, K, dtype: rows and lists at and just behind what a kernel's registers and threads hold
+    (200, 1020, 4, "f32"), (1100, 1024, 4, "f32"), (1100, 2055, 300, "bf16"), (170, 8192, 256, "f32"),
+    (170, 8193, 257, "f32"), (165, 16384, 256, "f32"), (165, 16388, 255, "f32"), (165, 32768, 256, "bf16"),
+    (165, 40007, 20, "bf16"), (165, 20003, 300, "f32"), (165, 65536, 512, "bf16"), (165, 65543, 513, "bf16"),
+    (260, 131072, 600, "bf16"), (165, 131080, 64, "bf16"), (161, 65539, 1024, "f32"), (40000, 5, 2, "f32"),
+]
+
+
+@pytest.mark.parametrize("N,V,K,dtype", EDGES)
+def test_distill_at_the_edges_of_its_kernels(N, V, K, dtype):
+    logits, ids, values = problem(min(N, 40), V, K, dtype, N + V + K)
+    pick = torch.arange(N) * 7 % logits.shape[0]      # rows repeat: each is held to its own place's result
+    logits, ids, values = logits[pick], ids[pick], values[pick]
+    weights = torch.where(torch.arange(N) % 5 == 1, 0.0, 0.5 + torch.arange(N) / N)
+    weights[N - 3:] = 0.0
+    dev = [x.to(DEV) for x in (logits, ids, values, weights)]
+    loss, stats, grad = D.distill(dev[0], dev[1], dev[2], 1.0, True, dev[3], want_stats=True)
+    rows = sorted({0, 1, 2, N // 3, N // 2, N - 4, N - 3, N - 1})
+    check_rows(logits, ids, values, 1.0, True, weights, loss, stats, grad, rows)
+    # the same row has the same loss wherever it stands
+    live = weights != 0
+    first = torch.full((int(pick.max()) + 1,), -1, dtype=torch.long)
+    for i in reversed(torch.nonzero(live).flatten().tolist()):
+        first[pick[i]] = i
+    assert torch.equal(loss.cpu()[live], loss.cpu()[first[pick]][live])
+    assert not loss.cpu()[~live].any() and not grad[(~live).to(DEV)].any()
+    # nothing but padding
+    loss, stats, grad = D.distill(dev[0], dev[1], dev[2], 1.0, True, torch.zeros_like(dev[3]), want_stats=True)
+    assert not loss.any() and not stats.any() and not grad.any()
+
+
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_lists_with_repeats_and_strangers(tail):
     """Ids outside the vocabulary and ids that stood earlier in the row are no

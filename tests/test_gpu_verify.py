@@ -155,6 +155,29 @@ def test_chain(V, B, n, dtype, T, kind, kw, ragged):
         check(v, b, chain_oracle(target, steps, dists, u, None if lens is None else np.clip(lens, 0, n), T, b), V)
 
 
+@pytest.mark.parametrize("V,B,n,kind,kw", [
+    (7, 5000, 1, "outright", {}), (11, 3000, 2, "clusters", dict(M=4, k=2, tail=0.2)), (40, 2000, 3, "shared", dict(M=9, k=1)),
+    (2049, 700, 2, "dense", {}), (3001, 600, 1, "clusters", dict(M=200, k=20))])
+def test_chain_many_requests(V, B, n, kind, kw):
+    """More requests than the chip holds workgroups."""
+    rng = np.random.default_rng(V)
+    t = torch.from_numpy(2.0 * rng.standard_normal((B, n + 1, V)).astype(np.float32))
+    target = f64(t)
+    _, layout, steps, dists = make_steps(B, n, V, kind, V + 1, target=target, **kw)
+    u = rng.random((B, n + 1)).astype(np.float32)
+    v = D.verify_chain(t.to(DEV), steps, torch.from_numpy(u).to(DEV), None, 1.0, layout)
+    got = (v.lengths.cpu(), v.ids.cpu(), v.logprobs.cpu())
+    fields = [(s.tokens.cpu(), s.logprobs.cpu() if s.logprobs is not None else None) for s in steps]
+    rows = range(B) if B * V < 200000 else rng.integers(0, B, 60)
+    for b in rows:
+        q = [math.exp(float(lp[b])) if lp is not None else 1.0 for _, lp in fields]
+        want = O.verify_chain(target[b], [int(x[b]) for x, _ in fields], u[b], n, 1.0, lambda i: dists[i][b], q)
+        ids = got[1][b].tolist()
+        assert (int(got[0][b]), ids) == (want[0], want[1] + [-1] * (n + 1 - len(want[1]))), b
+        for g, w in zip(got[2][b].tolist(), want[2]):
+            assert abs(g - w) <= lp_bound(V, w), (b, g, w)
+
+
 @pytest.mark.parametrize("T", [0.0, 1.0])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_chain_masked_rows(T, dtype):
