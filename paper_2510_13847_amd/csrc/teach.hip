@@ -137,7 +137,6 @@ __device__ __forceinline__ bool in_list(const ListLds& w, int x) {
     return w.key[h] == x;
 }
 
-template <typename T>
 __device__ __forceinline__ double teacher_value(const DistillArgs& a, int r, int k) {
     const int64_t i = (int64_t)r * a.K + k;
     return a.teacher_dtype == DYNA_BF16 ? (double)to_f32(static_cast<const uint16_t*>(a.teacher)[i])
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(DistillArgs a, int p
     for (int k = t; k < a.K; k += NT) {
         if (w.id[k] < 0) continue;
         ++n;
-        tm = fmaxf(tm, (float)teacher_value<T>(a, r, k));
+        tm = fmaxf(tm, (float)teacher_value(a, r, k));
         zm = fmaxf(zm, w.z[k]);
     }
     // without parts to join, the rest is known already
@@ -371,7 +370,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(DistillArgs a, int p
         }
     for (int k = t; k < a.K; k += NT) {
         if (w.id[k] < 0) continue;
-        const EntryTerms x(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
+        const EntryTerms x(a, power, teacher_value(a, r, k), w.z[k], tm, lm);
         ps += x.w;
         ls += x.l;
         cost += x.cost;
@@ -427,7 +426,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(DistillArgs a, int p
     for (int k = t; k < a.K; k += NT) {
         const int x = w.id[k];
         if (x < v0 || x >= v1) continue;
-        const EntryTerms y(a, power, teacher_value<T>(a, r, k), w.z[k], tm, lm);
+        const EntryTerms y(a, power, teacher_value(a, r, k), w.z[k], tm, lm);
         store_elt(grad + x, (float)(q.on_q * y.l - q.on_p * y.w));
     }
 }
@@ -586,7 +585,7 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
         if (r < a.N && t < a.K) {
             const int i = a.ids[(int64_t)r * a.K + t];
             x.id = i >= 0 && i < V ? i : -1;
-            x.value = teacher_value<T>(a, r, t);
+            x.value = teacher_value(a, r, t);
         }
         return x;
     };
