@@ -384,7 +384,7 @@ int32_t dyna_static_budget(int32_t t, int32_t k_max);
  *           B * rows * ceil(V / 2048) <= 2^23, B <= 2^21).  p_j =
  *           softmax(row / temperature).  NaN counts as -inf (a masked token),
  *           +inf as the largest finite number.
- *  temperature  >= 0; 0 is greedy: a draft stands when it is the row's largest
+ *  temperature  0, or FLT_MIN and above (finite); 0 is greedy: a draft stands when it is the row's largest
  *           logit (ties to the lower id), the token behind them is the largest
  *           of its row, uniforms may be NULL, and log-probabilities are those
  *           of softmax(row).
@@ -414,7 +414,7 @@ typedef struct dyna_draft_step {
                                * over the token ids [0, cap) (dyna_dense_head) */
     int32_t k, cap;
     int32_t shared;           /* 1: logits over the union of the B rows' clusters (DYNA_SEL_UNION) */
-    float temperature;        /* of the draft's softmax, > 0; with logits */
+    float temperature;        /* of the draft's softmax, FLT_MIN and above; with logits */
     float tail_beta;          /* its tail mixture weight in [0, 1); with clusters */
 } dyna_draft_step;
 
@@ -484,6 +484,7 @@ size_t dyna_distill_workspace_bytes(int32_t N, int32_t V);
  *   tail 1: p_k = exp(values) (log-probabilities of the teacher's whole row);
  *           + p_r (log p_r - log q_r), p_r = max(0, 1 - sum p_k) and q_r the
  *           student's probability outside the list.
+ *  temperature    FLT_MIN and above (finite)
  *  logits         device, dtype, row r is V <= 2^20 elements at r * row_stride, any alignment
  *  out_loss [N]   device fp32 (not weighted)
  *  out_stats [N, 2] device fp64, may be NULL: log sum exp(z / temperature) over all

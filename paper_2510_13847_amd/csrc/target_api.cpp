@@ -20,6 +20,8 @@ constexpr int64_t kLateLeafBytes = 200 << 20;
 constexpr int64_t kMaxBlocks = 1 << 23;   // workgroups of 256 threads in one launch: below 2^32 threads
 constexpr int32_t kMaxRequests = 1 << 21; // of 1024 threads, one to a request
 
+// Positive, finite, and no denormal, whose reciprocal 32 bits do not hold.
+bool valid_temperature(float t) { return t >= 1.17549435e-38f && t < 3.0e38f; }
 bool valid_dtype(int32_t t) { return t == DYNA_F32 || t == DYNA_BF16; }
 size_t elt_size(int32_t t) { return t == DYNA_BF16 ? 2 : 4; }
 bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -53,7 +55,7 @@ dyna_status check_verify(const void* target, int32_t tdtype, int32_t V, int64_t 
     REQUIRE(rows <= 1 || row_stride >= V, "target: row stride %lld < V=%d", (long long)row_stride, V);
     REQUIRE(B <= 1 || batch_stride >= V, "target: batch stride %lld < V=%d", (long long)batch_stride, V);
     REQUIRE(row_stride <= (int64_t)1 << 40 && batch_stride <= (int64_t)1 << 40, "target: stride too large");
-    REQUIRE(temperature >= 0.0f && temperature < 3.0e38f, "temperature must be finite and >= 0");
+    REQUIRE(temperature == 0.0f || valid_temperature(temperature), "temperature must be 0, or finite and at least FLT_MIN");
     REQUIRE(temperature == 0.0f || uniforms != nullptr, "uniforms is NULL with temperature > 0");
     return DYNA_OK;
 }
@@ -93,7 +95,7 @@ dyna_status check_distill_sizes(int32_t dtype, int32_t V, int32_t N, int32_t vdt
     if (K > DYNA_MAX_TEACHER) return set_error(DYNA_ERR_UNSUPPORTED, "K=%d > %d", K, DYNA_MAX_TEACHER);
     if (V > kMaxVocab) return set_error(DYNA_ERR_UNSUPPORTED, "V=%d > %d", V, kMaxVocab);
     REQUIRE(tail == 0 || tail == 1, "tail=%d", tail);
-    REQUIRE(temperature > 0.0f && temperature < 3.0e38f, "temperature must be positive and finite");
+    REQUIRE(valid_temperature(temperature), "temperature must be finite and at least FLT_MIN");
     DistillArgs a{};
     if (N > 0) distill_ws_bytes(N, V, &a, nullptr);
     if ((int64_t)N * a.splits > kMaxBlocks)
@@ -137,7 +139,7 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
         table.s[i] = d;
         if (d.logits == nullptr) continue;
         REQUIRE(d.logprobs != nullptr, "step %d: logprobs is NULL", i);
-        REQUIRE(d.temperature > 0.0f && d.temperature < 3.0e38f, "step %d: temperature must be positive and finite", i);
+        REQUIRE(valid_temperature(d.temperature), "step %d: temperature must be finite and at least FLT_MIN", i);
         REQUIRE(d.cap >= 0, "step %d: cap=%d", i, d.cap);
         needs.pieces = std::max<int32_t>(needs.pieces, std::max<int32_t>(1, (std::min(d.cap, V) + kChunk - 1) / kChunk));
         if (d.clusters == nullptr) {

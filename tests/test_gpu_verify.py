@@ -227,6 +227,26 @@ def test_greedy_ties_go_to_the_lower_id():
     assert v.ids.tolist() == [[300, 0], [0, -1], [8000, -1]]
 
 
+@pytest.mark.parametrize("T", [1.2e-38, 1e-20, 1e20, 2.9e38])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_temperatures_at_their_ends(T, dtype):
+    """One-hot and flat targets: all weight on the largest logits, equal ones
+    among them, or the same weight on every token."""
+    T = float(np.float32(T))
+    V, B, n = 2500, 6, 2
+    g = torch.Generator().manual_seed(77)
+    t = (3.0 * torch.randn((B, n + 1, V), generator=g)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    t[1, :, 40:44] = 20.0
+    t[2] = 0.0
+    t[3, :, 5] = 100.0
+    target = f64(t)
+    _, _, steps, dists = make_steps(B, n, V, "outright", 3, target=target)
+    u = np.random.default_rng(8).random((B, n + 1)).astype(np.float32)
+    v = D.verify_chain(t.to(DEV), steps, torch.from_numpy(u).to(DEV), None, T)
+    for b in range(B):
+        check(v, b, chain_oracle(target, steps, dists, u, None, T, b), V)
+
+
 def test_uniforms_at_their_ends():
     """u = 0 accepts any token of some probability and draws the first one; the
     largest u below 1 draws the last one with weight."""

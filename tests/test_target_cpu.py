@@ -39,7 +39,7 @@ def test_chain_argument_errors():
     assert _chain(target=P + 1) == D.ERR_INVALID_ARG
     assert _chain(row=999) == D.ERR_INVALID_ARG
     assert _chain(batch=10) == D.ERR_INVALID_ARG
-    for T in (-0.5, float("inf"), float("nan")):
+    for T in (-0.5, float("inf"), float("nan"), 1e-40):     # (a denormal's reciprocal is no 32-bit number)
         assert _chain(T=T) == D.ERR_INVALID_ARG
     assert _chain(u=None) == D.ERR_INVALID_ARG
     assert _chain(ids=None) == D.ERR_INVALID_ARG
@@ -59,6 +59,7 @@ def test_chain_step_errors():
     assert status(tokens=None) == D.ERR_INVALID_ARG
     assert status(logprobs=None) == D.ERR_INVALID_ARG
     assert status(temperature=0.0) == D.ERR_INVALID_ARG
+    assert status(temperature=1e-40) == D.ERR_INVALID_ARG
     assert status(tail_beta=1.0) == D.ERR_INVALID_ARG
     assert status(shared=2) == D.ERR_INVALID_ARG
     assert status(k=0) == D.ERR_INVALID_ARG
