@@ -190,6 +190,23 @@ def test_distill_masked_students(tail, dtype):
     check_rows(logits, ids, values, 1.0, tail, None, None, None, back)
 
 
+@pytest.mark.parametrize("T", [1e-20, 1e20])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("N", [5, 170])
+def test_distill_temperatures_at_their_ends(N, tail, T):
+    """One-hot and flat students and teachers, by either kernel."""
+    V, K = 9001, 12
+    logits, ids, values = problem(5, V, K, "f32", 21)
+    logits[1] = 0.0
+    pick = torch.arange(N) % 5
+    logits, ids, values = logits[pick], ids[pick], values[pick]
+    dev = [x.to(DEV) for x in (logits, ids, values)]
+    loss, stats, grad = D.distill(*dev, T, tail, want_stats=True)
+    rows = [0, 1, 2, 3, 4, N - 1]
+    check_rows(logits, ids, values, T, tail, None, loss, stats, grad, rows)
+    check_rows(logits, ids, values, T, tail, None, None, None, D.distill_grad(dev[0], stats, *dev[1:], T, tail), rows)
+
+
 def test_distill_undefined_rows_show():
     N, V, K = 5, 2500, 4
     logits, ids, values = problem(N, V, K, "f32", 7)
