@@ -783,11 +783,13 @@ __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable s
     if (lane_id() == 0 && c < a.n_chunks) a.left[(int64_t)b * a.n_chunks + c] = s;
 }
 
-// Less than this of p's mass left by the drafts counts as nothing, and less than
-// kRounding of a chunk's own mass as rounding: the chunks' sums are differences.
+// Less than this of p's mass left by the drafts counts as nothing.
 constexpr double kNothing = 0x1p-40;
-constexpr double kRounding = 0x1p-45;
 constexpr double kFixOne = 0x1p62;
+// A chunk's weight, at most, where its sum says that nothing is left of it: the sum
+// is a difference, and may be wrong about a token far below the chunk's others.
+// The draw itself finds out, where it gets there.
+constexpr double kTrace = 0x1p-100;
 
 // The draw: the chunk in which the cumulative weight passes u of the total,
 // then the token inside it.  One workgroup per request.
@@ -797,6 +799,13 @@ constexpr double kFixOne = 0x1p62;
 // their chunks by max(p - q, 0) - max(p - q_out, 0), without a tail -min(p, q),
 // as whole multiples of 2^-62, so that the order of the additions in LDS does
 // not matter.
+//
+// A chunk's sum and its tokens' own weights round differently, so a chunk can have
+// a weight and no token with p > q, masked ones or none at all.  Such a chunk is
+// passed over for the next one that holds a token (behind the last of them, for the
+// one before).  That takes a u which points into a rounding error, as u = 0 does
+// behind a first chunk that the drafts have emptied; the first wave then looks
+// alone, a chunk and all slots at a time.
 //
 // One workgroup goes through joins and scans that wait for each other: 12.1 us for
 // one chain with 32 clusters of 1024 over 128256, 14.5 us for 128 over 262144; with
@@ -876,7 +885,8 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
                     const double pv = weight(z, r.m) * r.inv_all, qv = r.q_in * wq(y, r.qm);
                     off = fmax(pv - qv, 0.0) - fmax(pv - r.q_out, 0.0);
                 }
-                if (v >= 0) atomicAdd(&change[v / kChunk], (unsigned long long)(long long)(off * kFixOne));
+                // upwards: no token's gain is lost
+                if (v >= 0) atomicAdd(&change[v / kChunk], (unsigned long long)(long long)ceil(off * kFixOne));
             }
         }
         lds_barrier();
@@ -891,7 +901,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
             x = listed && r.q_out == 0.0 ? x * r.inv_all : a.left[(int64_t)b * n + c];
             if (listed) {
                 const double kept = x + (double)(long long)change[c] / kFixOne;
-                x = kept > x * kRounding ? kept : 0.0;
+                x = kept > 0.0 ? kept : fmin(x, kTrace);
             }
             chunk_w[c] = x;
         }
@@ -939,15 +949,15 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     for (int i = kW - 1; i >= 0 && from < 0; --i)
         if (last_of[i] >= 0) from = i;
     from = max(from, 0);
-    const int chunk = past ? first_of[from] : max(last_of[from], 0);
-    const double base = before[from];
-    const int v0 = chunk * kChunk, v = v0 + t * 8;
+    int chunk = past ? first_of[from] : max(last_of[from], 0);
+    double base = before[from];
+    int v0 = chunk * kChunk, v = v0 + t * 8;
     // the chunk's tokens, eight to a lane of the first wave
     float z[8];
     if (t < kWave) load_part(row + v, a.V - v, kNegInf, z);
+    const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
     if (residual && listed) {
         // the shortlist's tokens in this chunk
-        const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
         for (int s0 = t; s0 < len; s0 += kAhead * NT) {
             if (len > kAhead * NT) load_slots(s0, x_first, y_first);
 #pragma unroll
@@ -958,28 +968,57 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
         lds_barrier();
     }
     if (t >= kWave) return;
-    // weights inside a chunk are relative to its own largest logit, as when its
-    // sum was taken: a chunk of weight holds a token of weight
     double x[8], scale = 1.0;
-    if (residual) {
-        double q[8];
-        if (listed) {
+    for (int way = 1, drawn = chunk; residual;) {
+        bool some = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                q[i] = chunk_q[t * 8 + i];
-                q[i] = q[i] < 0.0 ? r.q_out : q[i];
-            }
-        } else {
-            const Weigher wq{table, 1.0 / (double)d.temperature * k16Log2e};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 8; ++i) {
+            double q = r.q_out;
+            if (listed) {
+                const double y = chunk_q[t * 8 + i];
+                q = y < 0.0 ? q : y;
+            } else {
                 const int slot = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
-                q[i] = slot >= 0 && slot < r.len ? r.q_in * wq(clean(zq[slot]), r.qm) : r.q_out;
+                if (slot >= 0 && slot < r.len) q = r.q_in * wq(clean(zq[slot]), r.qm);
             }
+            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q, 0.0);
+            some |= x[i] > 0.0;
         }
+        if (__builtin_expect(__any(some), 1)) break;
+        int next = -1;
+        while (true) {  // the next chunk with weight, 64 at a look: behind it, then before the drawn one
+            for (int c = chunk + way; c >= 0 && c < n && next < 0; c += way * kWave) {
+                const int at = c + way * t;
+                const uint64_t hit = __ballot(at >= 0 && at < n && chunk_w[at] > 0.0);
+                if (hit) next = c + way * __builtin_ctzll(hit);
+            }
+            if (next >= 0 || way < 0) break;
+            way = -1;
+            chunk = drawn;
+        }
+        // (the sums err by less than kNothing in all, so one of the chunks holds a token)
+        if (next < 0) {
+            residual = without = false;
+            next = drawn;
+        }
+        chunk = next;
+        base = way * __builtin_inf();  // the first token there, or the last one
+        v0 = chunk * kChunk;
+        v = v0 + t * 8;
+        load_part(row + v, a.V - v, kNegInf, z);
+        if (!listed) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q[i], 0.0);
-    } else {
+        for (int i = 0; i < 8; ++i) chunk_q[t * 8 + i] = -1.0;
+        wave_lds_order();
+        for (int s0 = t; s0 < len; s0 += kWave) {
+            const int u0 = slots[s0].v - v0;
+            if (u0 >= 0 && u0 < kChunk) chunk_q[u0] = r.q_in * wq(clean(zq[s0]), r.qm);
+        }
+        wave_lds_order();
+    }
+    if (!residual) {
+        // weights inside a chunk are relative to its own largest logit, as when its
+        // sum was taken: a chunk of weight holds a token of weight
         if (without) mark_rejected(a, st, b, e, v0, bits);
         const uint32_t out = without ? marks8(bits, t * 8) : 0u;
         const float top = p[chunk].m;

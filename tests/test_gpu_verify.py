@@ -543,3 +543,87 @@ def test_verifier_refuses_what_does_not_fit():
     with pytest.raises(D.DynaError) as err:
         D.verify_chain(t, [short, short], u, None, 1.0, layout)
     assert err.value.status == D.ERR_CAPACITY
+
+
+def masked_problem(kind, dtype, B, V, M=0, k=0, td=1.0, tail=0.0, allowed=40, seed=0):
+    """Rows that allow a few tokens, all of them on the draft's shortlist; the draft
+    proposed a token that the target forbids.  -> (target, steps, layout, q of each row)."""
+    rng = np.random.default_rng(seed)
+    td, tail = float(np.float32(td)), float(np.float32(tail))
+    clusters = layout = None
+    if kind == "dense":
+        ids = [np.arange(V - V // 5)] * B
+        cap = V - V // 5
+    else:
+        of, layout = layout_of(V, M, seed)
+        clusters = np.stack([rng.permutation(M)[:k] for _ in range(B)]).astype(np.int32)
+        shared = kind == "shared"
+        union = shortlist(of, clusters.reshape(-1)) if shared else None
+        ids = [union if shared else shortlist(of, c) for c in clusters]
+        cap = D.union_cap(layout, B, k) if shared else layout.cap(k)
+    target = torch.full((B, 2, V), -math.inf)
+    logits = np.full((B, cap), np.nan, dtype=np.float32)
+    tokens = np.zeros(B, dtype=np.int32)
+    for b in range(B):
+        at = rng.permutation(len(ids[b]))[:allowed]
+        z = (3.0 * rng.standard_normal(len(at))).astype(np.float32)
+        target[b, 0, torch.from_numpy(ids[b][at])] = torch.from_numpy(z)
+        # every other draft is masked as the target is
+        logits[b, :len(ids[b])] = -np.inf if b % 2 else rng.standard_normal(len(ids[b])) - 4.0
+        logits[b, at] = 0.8 * z + rng.standard_normal(len(at))
+        tokens[b] = next(v for v in rng.integers(0, V, V) if v not in ids[b][at])
+    target[:, 1] = 0.0
+    target = target.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q = [O.draft_distribution(V, logits[b].astype(np.float64), td, ids[b], tail) for b in range(B)]
+    step = D.DraftStep(torch.from_numpy(tokens).to(DEV), torch.zeros(B, device=DEV), torch.from_numpy(logits).to(DEV),
+                       None if clusters is None else torch.from_numpy(clusters).to(DEV), td, tail, kind == "shared")
+    return target, step, layout, q, tokens
+
+
+MASKED = [  # kind, dtype, T, V, kwargs
+    ("clusters", "f32", 1.0, 8192, dict(M=16, k=4)), ("clusters", "f32", 1.0, 8192, dict(M=8, k=8)),
+    ("clusters", "bf16", 0.75, 8191, dict(M=16, k=4, td=0.9, tail=0.25)),
+    ("clusters", "f32", 1.0, 8192, dict(M=8, k=8, tail=0.25)),                       # no token for the tail
+    ("shared", "bf16", 1.0, 8192, dict(M=200, k=1)), ("shared", "f32", 1.25, 9001, dict(M=300, k=1, tail=0.125)),
+    ("dense", "bf16", 1.0, 8192, {}), ("clusters", "f32", 1.0, 20011, dict(M=2500, k=2100)),
+]
+
+
+@pytest.mark.parametrize("kind,dtype,T,V,kw", MASKED)
+@pytest.mark.parametrize("u", [0.0, 2.0 ** -24, 1.0 - 2.0 ** -24])
+def test_draws_behind_a_shortlist_hold_to_the_residual(kind, dtype, T, V, kw, u):
+    """Whole stretches of the row are emptied by the drafts or masked: the token
+    drawn has p > q wherever u points, at its ends too."""
+    B = 200
+    target, step, layout, q, tokens = masked_problem(kind, dtype, B, V, **kw)
+    us = torch.tensor([[0.75, u]]).repeat(B, 1)
+    v = D.verify_chain(target.to(DEV), [step], us.to(DEV), None, T, layout)
+    for b in range(B):
+        row = f64(target[b])
+        p = O.softmax(row[0], T)
+        some = p > 0
+        # sums of 200 terms and of differences are right to 1e-13 of the total: no border is near
+        assert (np.abs(p - q[b])[some] > 1e-9 * p[some]).all()
+        F = np.cumsum(np.maximum(p - q[b], 0.0))
+        assert u == 0.0 or np.abs(F / F[-1] - u).min() > 1e-11
+        check(v, b, O.verify_chain(row, [int(tokens[b])], [0.75, u], 1, T, lambda i: q[b], [1.0]), V)
+        x = int(v.ids[b, 0])
+        assert p[x] > q[b][x] and math.isfinite(float(v.logprobs[b, 0]))
+
+
+@pytest.mark.parametrize("M,k", [(16, 16), (2500, 2500)])
+def test_equal_distributions_over_a_shortlist_leave_the_target(M, k):
+    """p = q over a shortlist of the whole vocabulary: nothing is left, whatever u."""
+    V = 20000
+    of, layout = layout_of(V, M, 4)
+    z = torch.randn((4, V), generator=torch.Generator().manual_seed(6)) * 3.0
+    ids = torch.from_numpy(shortlist(of, range(M)))
+    clusters = torch.arange(M, dtype=torch.int32).repeat(4, 1)
+    step = D.DraftStep(torch.full((4,), 9, dtype=torch.int32, device=DEV), torch.zeros(4, device=DEV),
+                       z[:, ids].contiguous().to(DEV), clusters.to(DEV))
+    t = torch.stack([z, z], 1)
+    for u in (0.0, 0.25, 0.75, 1.0 - 2.0 ** -24):
+        us = torch.tensor([[0.999, u]]).repeat(4, 1)
+        v = D.verify_chain(t.to(DEV), [step], us.to(DEV), None, 1.0, layout)
+        for b in range(4):
+            assert int(v.lengths[b]) == 0 and int(v.ids[b, 0]) == O.place(O.softmax(f64(z[b]), 1.0), u)
