@@ -627,3 +627,22 @@ def test_equal_distributions_over_a_shortlist_leave_the_target(M, k):
         v = D.verify_chain(t.to(DEV), [step], us.to(DEV), None, 1.0, layout)
         for b in range(4):
             assert int(v.lengths[b]) == 0 and int(v.ids[b, 0]) == O.place(O.softmax(f64(z[b]), 1.0), u)
+
+
+@pytest.mark.parametrize("d,u", [(0.45257025957107544, 0.3887498378753662), (1.6673763990402222, 0.15877428650856018),
+                                 (6.1758198738098145, 0.002074786927551031)])
+@pytest.mark.parametrize("first,second,V", [(0, 1, 2), (3, 4097, 5000)])
+def test_draws_next_to_a_border(d, u, first, second, V):
+    """Two tokens d apart, u below p of the first by 3 to 7 parts in 10^14 of it:
+    weights in 64 bits draw the first, ones right to 43 bits the second."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 40
+    w = (-Decimal(d)).exp()
+    assert Decimal("2e-14") < (w - Decimal(u) * (1 + w)) / w < Decimal("8e-14")
+    t = torch.full((2, 1, V), -math.inf)
+    t[:, :, first], t[:, :, second] = -d, 0.0
+    us = torch.tensor([[u], [float(np.nextafter(np.float32(u), np.float32(1.0)))]])
+    for v in (D.verify_chain(t.to(DEV), [], us.to(DEV)),
+              D.verify_tree(t.to(DEV), torch.zeros((2, 1), dtype=torch.int32, device=DEV),
+                            torch.zeros(1, dtype=torch.int32, device=DEV), us.to(DEV))):
+        assert v.ids.tolist() == [[first], [second]]
