@@ -970,18 +970,24 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     if (t >= kWave) return;
     double x[8], scale = 1.0;
     for (int way = 1, drawn = chunk; residual;) {
+        double q[8];
+        if (listed) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q[i] = chunk_q[t * 8 + i];
+                q[i] = q[i] < 0.0 ? r.q_out : q[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int slot = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
+                q[i] = slot >= 0 && slot < r.len ? r.q_in * wq(clean(zq[slot]), r.qm) : r.q_out;
+            }
+        }
         bool some = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            double q = r.q_out;
-            if (listed) {
-                const double y = chunk_q[t * 8 + i];
-                q = y < 0.0 ? q : y;
-            } else {
-                const int slot = v + i < a.V ? streamed_slot(a, d, b, v + i) : -1;
-                if (slot >= 0 && slot < r.len) q = r.q_in * wq(clean(zq[slot]), r.qm);
-            }
-            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q, 0.0);
+            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q[i], 0.0);
             some |= x[i] > 0.0;
         }
         if (__builtin_expect(__any(some), 1)) break;
