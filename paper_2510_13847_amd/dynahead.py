@@ -346,6 +346,7 @@ class DraftHead:
         self.logits = torch.full((B, self.cap), float("nan"), dtype=torch.float32,
                                  device=device) if keep_logits else None
         self.ws = workspace(layout, router, B, k, self.cap, device)
+        self.ran = False  # the outputs hold a step
 
     def __call__(self, x, h, uniforms=None, stream=None, route_stream=None, x_ready=None,
                  layout: Optional[Layout] = None, router: Optional[Router] = None):
@@ -359,6 +360,7 @@ class DraftHead:
                                      _ptr(self.sample_logprob), _ptr(self.clusters),
                                      _ptr(self.logits), self.cap, _ptr(self.ws), self.ws.numel(),
                                      _stream(stream), rs, ev))
+        self.ran = True
         return self
 
 
@@ -376,6 +378,7 @@ def draft_head_noalloc(head: "DraftHead", x, h, uniforms=None, stream=None,
                                          _ptr(uniforms), _ptr(head.ids), _ptr(head.logprobs),
                                          _ptr(head.sample), _ptr(head.sample_logprob), _ptr(head.clusters),
                                          _ptr(head.logits), head.cap, _stream(stream)))
+    head.ran = True
     return head
 
 
@@ -405,6 +408,7 @@ class DenseHead:
         self.logits = torch.empty((B, n_rows), dtype=torch.float32, device=device) if keep_logits else None
         n = dense_workspace_bytes(n_rows, B)
         self.ws = torch.empty(max(n, 1), dtype=torch.uint8, device=device)
+        self.ran = False  # the outputs hold a step
 
     def __call__(self, h, uniforms=None, stream=None, W=None):
         W = self.W if W is None else W
@@ -413,6 +417,7 @@ class DenseHead:
                                      _ptr(uniforms), _ptr(self.ids), _ptr(self.logprobs),
                                      _ptr(self.sample), _ptr(self.sample_logprob), _ptr(self.logits),
                                      _ptr(self.ws), self.ws.numel(), _stream(stream)))
+        self.ran = True
         return self
 
 
@@ -572,17 +577,30 @@ class DraftStep:
                              int(self.shared), self.temperature, self.tail_beta)
 
     @classmethod
-    def of(cls, head) -> "DraftStep":
-        """The step a DraftHead (keep_logits, keep_clusters) or DenseHead
-        (keep_logits) holds: its sample and the distribution it came from, or
-        its best tokens, proposed outright, when it does not sample."""
+    def of(cls, head, stream=None) -> "DraftStep":
+        """The step that the last run of a DraftHead (keep_logits, keep_clusters)
+        or DenseHead (keep_logits) wrote: its sample and the distribution it came
+        from, or its best tokens, proposed outright, when it does not sample.
+
+        The step is a copy, made on `stream` (the head's): the head may run again,
+        for the next position.  A head that runs once a cycle needs no copy:
+        DraftStep(head.sample, head.sample_logprob, head.logits, head.clusters, ...)
+        stands for whatever its buffers hold when the chain is judged."""
+        if not head.ran:
+            raise ValueError("the head has not run: its step is taken behind the run")
+        if stream is not None:
+            import torch
+            _stream_device(stream, (head.ids if head.sample is None else head.sample).device)
+            with torch.cuda.stream(stream):
+                return cls.of(head)
         if head.sample is None:
-            return cls(head.ids[:, 0].contiguous())
+            return cls(head.ids[:, 0].clone())
         if head.logits is None or (isinstance(head, DraftHead) and head.clusters is None):
             raise ValueError("a sampled step needs a head that keeps its logits and clusters")
+        sampled = head.sample.clone(), head.sample_logprob.clone(), head.logits.clone()
         if isinstance(head, DenseHead):
-            return cls(head.sample, head.sample_logprob, head.logits, temperature=head.temperature)
-        return cls(head.sample, head.sample_logprob, head.logits, head.clusters, head.temperature, head.tail_beta,
+            return cls(*sampled, temperature=head.temperature)
+        return cls(*sampled, head.clusters.clone(), head.temperature, head.tail_beta,
                    bool(head.mode & SEL_UNION) and head.B > 1)
 
 

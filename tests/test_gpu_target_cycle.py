@@ -171,3 +171,69 @@ def test_target_teaches_drafter_and_router():
     (cost.sum(1) * weights).sum().backward()
     for got, exp in ((W1.grad, a1.grad), (W2.grad, a2.grad)):
         assert (got - exp).abs().max() <= 1e-5 * exp.abs().max()
+
+
+def head_of(kind, w, layout, router, W_lm, B, T):
+    sampled = dict(temperature=T, keep_logits=True)
+    if kind == "dense":
+        return D.DenseHead(W_lm, V, B, D.SEL_SAMPLE, **sampled)
+    if kind == "union":
+        return D.DraftHead(router, layout, B, 3, D.SEL_SAMPLE | D.SEL_UNION, **sampled)
+    if kind == "argmax":
+        return D.DraftHead(router, layout, B, 8, D.SEL_ARGMAX)
+    if kind == "best of 4":
+        return D.DraftHead(router, layout, B, 8, D.SEL_TOPK, 4)
+    return D.DraftHead(router, layout, B, 8, D.SEL_SAMPLE, tail_beta=0.125 if kind == "tail" else 0.0, **sampled)
+
+
+KINDS = ["shortlist", "tail", "union", "dense", "argmax", "best of 4"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_one_head_drafts_position_after_position(kind):
+    """A step is what its head wrote at that position, though the head ran again:
+    the chain is judged as one drafted by a head for each position, also where the
+    steps are taken on a side stream and inside a captured graph."""
+    B, n, T = 6, 4, 0.75
+    w, of, W_lm, layout, router = model(B)
+    hidden = [W.contexts(w, DEV, batch=B, salt=i) for i in range(n + 1)]
+    us = [W.uniforms(w, DEV, batch=B, salt=i) for i in range(n)]
+    rows = torch.stack([rows_like(h, i) for i, h in enumerate(hidden)], 1).reshape(B * (n + 1), DIM).contiguous()
+    target = D.DenseHead(W_lm, V, B * (n + 1), D.SEL_ARGMAX, keep_logits=True)(rows).logits.view(B, n + 1, V)
+    u = 0.2 * torch.rand((B, n + 1), generator=torch.Generator().manual_seed(4)).to(DEV)
+
+    def run(head, i, **kw):
+        return head(hidden[i], us[i], **kw) if kind == "dense" else head(hidden[i], hidden[i], us[i], **kw)
+
+    def results(v):
+        return [x.clone() for x in (v.lengths, v.ids, v.logprobs)]
+    heads = [run(head_of(kind, w, layout, router, W_lm, B, T), i) for i in range(n)]
+    ver = D.ChainVerifier(B, n, V, T, layout)
+    want = results(ver(target, [D.DraftStep.of(h) for h in heads], u))
+    assert int(want[0].max()) > 0
+    one = head_of(kind, w, layout, router, W_lm, B, T)
+    got = results(ver(target, [D.DraftStep.of(run(one, i)) for i in range(n)], u))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    steps = [D.DraftStep.of(run(one, i, stream=side), stream=side) for i in range(n)]
+    ver(target, steps, u, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(results(ver), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps = [D.DraftStep.of(run(one, i)) for i in range(n)]
+        ver(target, steps, u)
+    for again in range(3):
+        ver.ids.fill_(-7)
+        run(one, again)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(results(ver), want))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_head_that_has_not_run_has_no_step(kind):
+    w, of, W_lm, layout, router = model(2)
+    with pytest.raises(ValueError, match="has not run"):
+        D.DraftStep.of(head_of(kind, w, layout, router, W_lm, 2, 1.0))
