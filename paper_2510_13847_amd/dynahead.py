@@ -626,6 +626,8 @@ class _Verifier:
     def __init__(self, B, rows, V, temperature, M, device):
         import torch
         self.B, self.rows, self.V, self.temperature = B, rows, V, float(temperature)
+        if self.temperature != 0.0 and _F(self.temperature).value == 0.0:
+            raise ValueError(f"temperature {temperature} is 0 in 32 bits, which would ask for greedy verification")
         dev = torch.empty(0, device=device).device
         self.device = dev
         self.lengths = torch.empty(B, dtype=torch.int32, device=dev)

@@ -203,3 +203,14 @@ def test_a_mistaken_oracle_is_seen():
     a = O.distill_row(row, [0], [LN(0.25)], 1.0, True)[1]
     b = O.distill_row(row, [0], [LN(0.25)], 1.0, False)[1]
     assert np.abs(a - b).max() > 0.1
+
+
+@pytest.mark.parametrize("T", [1e-46, -1e-46, 5e-324])
+def test_a_temperature_that_32_bits_round_to_zero_is_refused(T):
+    """The library takes 0 as greedy verification; only 0 itself asks for it."""
+    assert ctypes.c_float(T).value == 0.0
+    for make in (lambda: D.ChainVerifier(1, 1, 8, T, device="cpu"), lambda: D.TreeVerifier(1, 2, 8, T, device="cpu")):
+        with pytest.raises(ValueError, match="32 bits"):
+            make()
+    for ok in (0.0, 1.0, float(np.float32(1.2e-38))):
+        assert D.ChainVerifier(1, 1, 8, ok, device="cpu").temperature == ok
