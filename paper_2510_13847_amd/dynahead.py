@@ -662,6 +662,10 @@ class ChainVerifier(_Verifier):
     def __init__(self, B: int, n: int, V: int, temperature: float = 1.0, layout: Optional[Layout] = None,
                  device="cuda"):
         import torch
+        if layout is not None:
+            at = torch.empty(0, device=device).device
+            if layout.perm.device != at:
+                raise ValueError(f"layout is on {layout.perm.device}, not on {at}")
         super().__init__(B, n + 1, V, temperature, layout.M if layout is not None else 0, device)
         self.n, self.layout = n, layout
         self.token_rows = token_rows(layout) if layout is not None else None

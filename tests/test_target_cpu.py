@@ -214,3 +214,13 @@ def test_a_temperature_that_32_bits_round_to_zero_is_refused(T):
             make()
     for ok in (0.0, 1.0, float(np.float32(1.2e-38))):
         assert D.ChainVerifier(1, 1, 8, ok, device="cpu").temperature == ok
+
+
+def test_a_layout_on_another_device_is_refused():
+    """Its tables would be read by kernels on the verifier's device."""
+    import types
+
+    import torch
+    layout = types.SimpleNamespace(M=4, V=8, perm=torch.empty(8, dtype=torch.int32, device="meta"))
+    with pytest.raises(ValueError, match="layout is on meta"):
+        D.ChainVerifier(1, 1, 8, layout=layout, device="cpu")
