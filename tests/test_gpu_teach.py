@@ -408,3 +408,20 @@ def test_learning_refusals():
     assert err.value.status == D.ERR_WORKSPACE
     empty = D.distill(z[:0], ids[:0], val[:0])
     assert empty[0].numel() == 0 and empty[2].shape == (0, V)
+
+
+@pytest.mark.parametrize("N,dtype,K", [(2, "f32", 1024), (65, "bf16", 200), (1030, "bf16", 7)])
+def test_distill_over_the_largest_vocabulary(N, dtype, K):
+    """Parts of every length, up to 65536 entries with a bit for each."""
+    V = 1 << 20
+    logits, ids, values = problem(2, V, K, dtype, 3)
+    pick = torch.arange(N) % 2
+    z = logits.to(DEV)[pick.to(DEV)]
+    dev = [x[pick].to(DEV) for x in (ids, values)]
+    loss, stats, grad = D.distill(z, *dev, 1.0, True, want_stats=True)
+    back = D.distill_grad(z, stats, *dev, 1.0, True)
+    for r in (0, N - 1):
+        one = [x[r:r + 1].cpu() for x in (z, *dev)]
+        check_rows(*one, 1.0, True, None, loss[r:r + 1], stats[r:r + 1], grad[r:r + 1])
+        check_rows(*one, 1.0, True, None, None, None, back[r:r + 1])
+    assert torch.equal(loss, loss[pick.to(DEV)]) and torch.equal(grad[N - 1], grad[(N - 1) % 2])

@@ -646,3 +646,64 @@ def test_draws_next_to_a_border(d, u, first, second, V):
               D.verify_tree(t.to(DEV), torch.zeros((2, 1), dtype=torch.int32, device=DEV),
                             torch.zeros(1, dtype=torch.int32, device=DEV), us.to(DEV))):
         assert v.ids.tolist() == [[first], [second]]
+
+
+LARGEST = [  # V, B, n, dtype, T, kind, kwargs: more chunks than the drawing kernel's threads, up to the limit
+    (524801, 2, 2, "bf16", 1.0, "clusters", dict(M=2048, k=10)),
+    (1 << 20, 2, 2, "bf16", 1.0, "clusters", dict(M=4096, k=8)),
+    (1 << 20, 1, 2, "f32", 0.75, "clusters", dict(M=4096, k=64, tail=0.125)),
+    ((1 << 20) - 1, 3, 1, "bf16", 1.0, "shared", dict(M=4096, k=8)),
+    (1 << 20, 1, 1, "f32", 1.0, "clusters", dict(M=100, k=5)),              # a shortlist longer than 32768
+    (1 << 20, 2, 1, "bf16", 1.0, "dense", {}), (1 << 20, 2, 3, "bf16", 1.0, "outright", {}),
+    (1 << 20, 2, 3, "f32", 0.0, "outright", {}),
+]
+
+
+@pytest.mark.parametrize("V,B,n,dtype,T,kind,kw", LARGEST)
+def test_chain_over_the_largest_vocabularies(V, B, n, dtype, T, kind, kw):
+    rng = np.random.default_rng(V + n)
+    t = torch.from_numpy(3.0 * rng.standard_normal((B, n + 1, V), dtype=np.float32))
+    t = t.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    target = f64(t)
+    _, layout, steps, dists = make_steps(B, n, V, kind, V + 1, target=target, **kw)
+    td = t.to(DEV)
+    ver = D.ChainVerifier(B, n, V, T, layout)
+    for last in (0.0, 0.37, 0.999, 1.0 - 2.0 ** -24):
+        u = rng.random((B, n + 1)).astype(np.float32)
+        u[:, 0] = 0.999 if last < 0.5 else 0.001  # most first drafts fall, most stand
+        u[:, n] = last
+        ver(td, steps, torch.from_numpy(u).to(DEV))
+        for b in range(B):
+            check(ver, b, chain_oracle(target, steps, dists, u, None, T, b), V)
+
+
+@pytest.mark.parametrize("kind,V,kw", [("clusters", 1 << 20, dict(M=4096, k=8)), ("dense", 600011, {}),
+                                       ("clusters", 600011, dict(M=4096, k=8, tail=0.25))])
+@pytest.mark.parametrize("u", [0.0, 1.0 - 2.0 ** -24])
+def test_draws_over_the_largest_vocabularies_hold_to_the_residual(kind, V, kw, u):
+    B = 12
+    target, step, layout, q, tokens = masked_problem(kind, "f32", B, V, allowed=150, **kw)
+    us = torch.tensor([[0.75, u]]).repeat(B, 1)
+    v = D.verify_chain(target.to(DEV), [step], us.to(DEV), None, 1.0, layout)
+    for b in range(B):
+        check(v, b, O.verify_chain(f64(target[b]), [int(tokens[b])], [0.75, u], 1, 1.0, lambda i: q[b], [1.0]), V)
+
+
+@pytest.mark.parametrize("T", [0.0, 1.0])
+def test_tree_over_the_largest_vocabulary(T):
+    V, B, N = 1 << 20, 2, 6
+    rng = np.random.default_rng(12)
+    t = torch.from_numpy(3.0 * rng.standard_normal((B, N, V), dtype=np.float32)).to(torch.bfloat16)
+    target = f64(t)
+    parents = np.array([0, 0, 0, 1, 2, 3], dtype=np.int32)
+    tokens = np.zeros((B, N), dtype=np.int32)
+    for b in range(B):
+        for j in range(1, N):
+            tokens[b, j] = np.argsort(-target[b, parents[j]])[rng.integers(0, 2)]
+    for last in (0.0, 0.5, 1.0 - 2.0 ** -24):
+        u = (rng.random((B, N)) * 0.01).astype(np.float32)
+        u[:, 0] = last
+        v = D.verify_tree(t.to(DEV), torch.from_numpy(tokens).to(DEV), torch.from_numpy(parents).to(DEV),
+                          torch.from_numpy(u).to(DEV), T)
+        for b in range(B):
+            check(v, b, O.verify_tree(target[b], tokens[b], parents, u[b], T), V, nodes=True)
