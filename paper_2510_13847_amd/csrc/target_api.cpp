@@ -72,8 +72,8 @@ dyna_status check_verify_sizes(int32_t tdtype, int32_t V, int32_t B, int32_t row
 }
 
 dyna_status check_distill(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
-                          const int32_t* ids, const void* values, int32_t vdtype, int32_t K, float temperature,
-                          const void* grad, int64_t grad_stride) {
+                          const int32_t* ids, const void* values, int32_t vdtype, const void* grad,
+                          int64_t grad_stride) {
     TRY(check_rows("logits", logits, dtype, N, row_stride, V));
     REQUIRE(ids != nullptr, "ids is NULL");
     REQUIRE(values != nullptr && aligned_to(values, elt_size(vdtype)), "values NULL or misaligned");
@@ -245,7 +245,7 @@ DYNA_API dyna_status dyna_distill(const void* logits, int32_t dtype, int32_t V, 
                                   void* grad, int64_t grad_stride, void* ws, size_t ws_bytes, hipStream_t stream) {
     TRY(check_distill_sizes(dtype, V, N, vdtype, K, tail, temperature));
     if (N == 0) return DYNA_OK;
-    TRY(check_distill(logits, dtype, V, row_stride, N, ids, values, vdtype, K, temperature, grad, grad_stride));
+    TRY(check_distill(logits, dtype, V, row_stride, N, ids, values, vdtype, grad, grad_stride));
     REQUIRE(out_loss && ws && aligned_to(ws, 16), "NULL argument or ws not 16-byte aligned");
     DistillArgs a{};
     const size_t need = distill_ws_bytes(N, V, &a, ws);
@@ -276,7 +276,7 @@ DYNA_API dyna_status dyna_distill_grad(const void* logits, int32_t dtype, int32_
     TRY(check_distill_sizes(dtype, V, N, vdtype, K, tail, temperature));
     if (N == 0) return DYNA_OK;
     REQUIRE(grad != nullptr && stats != nullptr, "NULL argument");
-    TRY(check_distill(logits, dtype, V, row_stride, N, ids, values, vdtype, K, temperature, grad, grad_stride));
+    TRY(check_distill(logits, dtype, V, row_stride, N, ids, values, vdtype, grad, grad_stride));
     DistillArgs a{};
     distill_ws_bytes(N, V, &a, nullptr);
     a.logits = logits;
