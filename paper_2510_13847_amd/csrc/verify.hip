@@ -819,7 +819,7 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     __shared__ double sums[kW], before[kW];
     __shared__ int first_of[kW], last_of[kW];  // each wave's first chunk past the goal and last one of weight
     __shared__ uint32_t bits[kChunk / 32];
-    extern __shared__ char lds[];
+    extern __shared__ __align__(16) char lds[];
     const int b = blockIdx.x, t = threadIdx.x, n = a.n_chunks, wave = t / kWave;
     double* chunk_w = reinterpret_cast<double*>(lds);                             // [n]
     // and, for listed steps: [n] changes, [kChunk] the drawn chunk's q
