@@ -804,8 +804,9 @@ constexpr double kTrace = 0x1p-100;
 // a weight and no token with p > q, masked ones or none at all.  Such a chunk is
 // passed over for the next one that holds a token (behind the last of them, for the
 // one before).  That takes a u which points into a rounding error, as u = 0 does
-// behind a first chunk that the drafts have emptied; the first wave then looks
-// alone, a chunk and all slots at a time.
+// behind a first chunk that the drafts have emptied.  The first wave then looks
+// alone: it counts how many tokens each chunk loses to the shortlist, and goes
+// through the chunks until one has more.
 //
 // One workgroup goes through joins and scans that wait for each other: 12.1 us for
 // one chain with 32 clusters of 1024 over 128256, 14.5 us for 128 over 262144; with
@@ -969,6 +970,8 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
     }
     if (t >= kWave) return;
     double x[8], scale = 1.0;
+    auto over = [&](float y, double q) { return fma(weight(clean(y), r.m), r.inv_all, -q); };  // p - q
+    bool counted = false;
     for (int way = 1, drawn = chunk; residual;) {
         double q[8];
         if (listed) {
@@ -987,38 +990,52 @@ __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, in
         bool some = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = fmax(weight(clean(z[i]), r.m) * r.inv_all - q[i], 0.0);
+            x[i] = fmax(over(z[i], q[i]), 0.0);
             some |= x[i] > 0.0;
         }
         if (__builtin_expect(__any(some), 1)) break;
-        int next = -1;
+        if (listed && !counted) {
+            counted = true;
+            for (int c = t; c < n; c += kWave) change[c] = 0;
+            wave_lds_order();
+            for (int s = t; s < len; s += kWave) {
+                const SlotToken k = slots[s];
+                const int loss = (over(k.z, r.q_out) > 0.0) - (over(k.z, r.q_in * wq(clean(zq[s]), r.qm)) > 0.0);
+                if (k.v >= 0 && loss) atomicAdd(&change[k.v / kChunk], (unsigned long long)(long long)loss);
+            }
+            wave_lds_order();
+        }
         while (true) {  // the next chunk with weight, 64 at a look: behind it, then before the drawn one
+            int next = -1;
             for (int c = chunk + way; c >= 0 && c < n && next < 0; c += way * kWave) {
                 const int at = c + way * t;
                 const uint64_t hit = __ballot(at >= 0 && at < n && chunk_w[at] > 0.0);
                 if (hit) next = c + way * __builtin_ctzll(hit);
             }
-            if (next >= 0 || way < 0) break;
-            way = -1;
-            chunk = drawn;
+            chunk = next >= 0 ? next : drawn;
+            if (next < 0 && way > 0) {
+                way = -1;
+                continue;
+            }
+            // (the sums err by less than kNothing in all, so one of the chunks holds a token)
+            if (next < 0) residual = without = false;
+            v0 = chunk * kChunk;
+            v = v0 + t * 8;
+            load_part(row + v, a.V - v, kNegInf, z);
+            if (!listed || !residual) break;
+            int with = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) with += __popcll(__ballot(over(z[i], r.q_out) > 0.0));
+            if (with > (int)change[chunk]) break;
         }
-        // (the sums err by less than kNothing in all, so one of the chunks holds a token)
-        if (next < 0) {
-            residual = without = false;
-            next = drawn;
-        }
-        chunk = next;
         base = way * __builtin_inf();  // the first token there, or the last one
-        v0 = chunk * kChunk;
-        v = v0 + t * 8;
-        load_part(row + v, a.V - v, kNegInf, z);
         if (!listed) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) chunk_q[t * 8 + i] = -1.0;
         wave_lds_order();
-        for (int s0 = t; s0 < len; s0 += kWave) {
-            const int u0 = slots[s0].v - v0;
-            if (u0 >= 0 && u0 < kChunk) chunk_q[u0] = r.q_in * wq(clean(zq[s0]), r.qm);
+        for (int s = t; s < len; s += kWave) {
+            const int at = slots[s].v - v0;
+            if (at >= 0 && at < kChunk) chunk_q[at] = r.q_in * wq(clean(zq[s]), r.qm);
         }
         wave_lds_order();
     }

@@ -707,3 +707,48 @@ def test_tree_over_the_largest_vocabulary(T):
                           torch.from_numpy(u).to(DEV), T)
         for b in range(B):
             check(v, b, O.verify_tree(target[b], tokens[b], parents, u[b], T), V, nodes=True)
+
+
+@pytest.mark.parametrize("kind,V,kw", [("clusters", 50021, dict(M=64, k=8)), ("clusters", 50021, dict(M=64, k=64)),
+                                       ("shared", 50021, dict(M=64, k=4)), ("dense", 50021, {}),
+                                       ("clusters", 1 << 20, dict(M=4096, k=64))])
+@pytest.mark.parametrize("where", [0.0, 0.5, 1.0])
+def test_one_token_is_left_among_emptied_chunks(kind, V, kw, where):
+    """The draft gives nothing to one token of p = 10^-11 and its share to all
+    others, which are left nothing: whatever u, wherever it stands, that token is
+    drawn, though rounding weighs the emptied chunks too."""
+    B, allowed = 3, 400
+    rng = np.random.default_rng(19)
+    clusters = layout = None
+    if kind == "dense":
+        ids, cap = [np.arange(V)] * B, V
+    else:
+        of, layout = layout_of(V, kw["M"], 19)
+        clusters = np.stack([rng.permutation(kw["M"])[:kw["k"]] for _ in range(B)]).astype(np.int32)
+        shared = kind == "shared"
+        ids = [shortlist(of, clusters.reshape(-1) if shared else c) for c in clusters]
+        cap = D.union_cap(layout, B, kw["k"]) if shared else layout.cap(kw["k"])
+    target = torch.full((B, 2, V), -math.inf)
+    target[:, 1] = 0.0
+    logits = np.full((B, cap), np.nan, dtype=np.float32)
+    left = []
+    for b in range(B):
+        at = rng.permutation(len(ids[b]))[:allowed]
+        at = at[np.argsort(ids[b][at])]
+        z = rng.standard_normal(allowed).astype(np.float32)
+        k = int(where * (allowed - 1))
+        z[k] = -np.inf
+        logits[b, :len(ids[b])] = -np.inf
+        logits[b, at] = z
+        z[k] = np.log(np.exp(z.astype(np.float64)).sum()) + math.log(1e-11)
+        target[b, 0, torch.from_numpy(ids[b][at])] = torch.from_numpy(z)
+        left.append(int(ids[b][at[k]]))
+    tokens = torch.tensor([int(np.nonzero(np.isinf(f64(target[b, 0])))[0][0]) for b in range(B)], dtype=torch.int32)
+    step = D.DraftStep(tokens.to(DEV), torch.zeros(B, device=DEV), torch.from_numpy(logits).to(DEV),
+                       None if clusters is None else torch.from_numpy(clusters).to(DEV), shared=kind == "shared")
+    for u in (0.0, 0.3, 1.0 - 2.0 ** -24):
+        v = D.verify_chain(target.to(DEV), [step], torch.tensor([[0.75, u]]).repeat(B, 1).to(DEV), None, 1.0, layout)
+        assert v.lengths.tolist() == [0] * B and v.ids[:, 0].tolist() == left
+        for b in range(B):
+            q = O.draft_distribution(V, logits[b].astype(np.float64), 1.0, ids[b])
+            check(v, b, O.verify_chain(f64(target[b]), [int(tokens[b])], [0.75, u], 1, 1.0, lambda i: q, [1.0]), V)
