@@ -253,9 +253,10 @@ struct EntryTerms {
         l = z == kNegInf ? 0.0 : exp_of(power, dz);
         cost = w == 0.0 ? 0.0 : w * (dt - dz);
     }
-    // exp(x) by the short power of two; NaN stays NaN
+    // exp(x) by the short power of two, which takes no x above its own range; NaN
+    // stays NaN, and what no 64 bits hold is +inf
     __device__ __forceinline__ static double exp_of(const Weigher& power, double x) {
-        return x == x ? power.power(x * k16Log2e) : x;
+        return x < 1000.0 ? power.power(x * k16Log2e) : x == x ? __builtin_inf() : x;
     }
 };
 

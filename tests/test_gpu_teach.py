@@ -425,3 +425,20 @@ def test_distill_over_the_largest_vocabulary(N, dtype, K):
         check_rows(*one, 1.0, True, None, loss[r:r + 1], stats[r:r + 1], grad[r:r + 1])
         check_rows(*one, 1.0, True, None, None, None, back[r:r + 1])
     assert torch.equal(loss, loss[pick.to(DEV)]) and torch.equal(grad[N - 1], grad[(N - 1) % 2])
+
+
+@pytest.mark.parametrize("N", [5, 170])
+@pytest.mark.parametrize("value", [800.0, 1e10, 1e30, 3e38])
+def test_values_that_are_no_log_probabilities_show(N, value):
+    """exp(value) is above every number: such a row's loss is not finite, by either
+    kernel, and the rows beside it keep theirs."""
+    V, K = 3000, 8
+    logits, ids, values = problem(5, V, K, "f32", 33)
+    pick = torch.arange(N) % 5
+    logits, ids, values = logits[pick], ids[pick], values[pick]
+    values[1, 3] = value
+    dev = [x.to(DEV) for x in (logits, ids, values)]
+    loss, _, grad = D.distill(*dev, 1.0, True)
+    only, _, _ = D.distill(*dev, 1.0, True, want_grad=False)
+    assert not math.isfinite(float(loss[1])) and not math.isfinite(float(only[1]))
+    check_rows(logits, ids, values, 1.0, True, None, loss, None, grad, [0, 2, 3, 4])
