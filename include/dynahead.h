@@ -401,7 +401,8 @@ int32_t dyna_static_budget(int32_t t, int32_t k_max);
  *                    nothing between calls.  Calls that may overlap (two
  *                    streams, two captured graphs) need one each.
  * The rows are summed in 32 bits with 64-bit partial sums; the row a token is
- * drawn from is read again in 64 bits. */
+ * drawn from is read again in 64 bits (weights right to 2^-51).  A token that a
+ * draw's distribution gives nothing is never emitted, whatever u in [0, 1]. */
 
 /* One drafted position of every chain.  As a draft head writes it (SAMPLE),
  * or tokens alone (logits NULL) for drafts proposed outright: argmax drafts,
@@ -424,7 +425,8 @@ typedef struct dyna_draft_step {
 dyna_status dyna_token_rows(const dyna_layout* L, int32_t* token_rows, hipStream_t stream);
 
 /* rows: n + 1 of a chain of n drafts, N of a tree; M: clusters of the layout
- * (0 without one). */
+ * (0 without one; with one, 8 min(V, 32768) bytes a request are for the tokens
+ * of a shortlist, whatever the steps' cap). */
 size_t dyna_verify_workspace_bytes(int32_t B, int32_t rows, int32_t V, int32_t M);
 
 /* Chains of up to n drafts.  Row i of `target` judges draft i (0-based), the
@@ -493,6 +495,11 @@ size_t dyna_distill_workspace_bytes(int32_t N, int32_t V);
  *  grad           device, dtype, row r at r * grad_stride, may be NULL: weights[r] *
  *                 d loss[r] / d logits[r]; elements behind a row are left as they
  *                 were; the spans of both, gaps between rows included, must not overlap
+ *  ws             dyna_distill_workspace_bytes of the same sizes; it holds
+ *                 nothing between calls.  Calls that may overlap need one each
+ * Loss and gradient together read a row of up to 131072 bf16 or 65536 fp32 logits
+ * once where there are 160 rows or more and the list is short (K up to 128 at
+ * 128256 tokens, 512 up to 65536), other rows twice.
  * A row without entries (or with every value -inf, tail 0) has loss and
  * gradient 0.  A masked logit (-inf) has q = 0: the loss is +inf where the
  * teacher gives it weight, the gradient stays finite.  A NaN or +inf logit or

@@ -443,8 +443,16 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(DistillArgs a, int p
 // again (the same loads, stores of the same bytes, nothing added to the sums),
 // because a branch around a load or store would make every wait a wait for all
 // of them.  Barriers order LDS alone.  4000 rows of 128256 bf16 with their gradient
-// and 96 of padding (2.08 GB) take 446-485 us, 4.3-4.7 TB/s; two passes, which read
-// the rows twice, 633.
+// and 96 of padding (2.08 GB) take 460 us, 4.5 TB/s (445-500 under a trace); two
+// passes, which read the rows twice, 650.
+//
+// Its limits: rows of at most 131072 bf16 or 65536 fp32 entries, sixteen vectors for
+// each of 1024 threads; lists of at most 256, 512 or 1024 entries, one to a thread;
+// and 60 KiB of LDS for the three sets of tables, 3 (V / 8 + 8 places) bytes and the
+// list's gradients, which 128256 entries leave for K of 128.  What is beyond takes two
+// passes, whose second read comes from memory again where there are many rows: 1024
+// rows of 128256 bf16 142 us at K 128 and 186 at 129, of 151936 212 (129 at a copy's
+// rate), of 262144 342 (222), of 128256 fp32 343 (217).
 constexpr int kLag = 4;
 
 template <typename T>
@@ -800,8 +808,9 @@ __global__ __launch_bounds__(NT, 4) void distill_pass_kernel(DistillArgs a) {
 //   cost = y pw softplus(-s) + (1 - y) softplus(s),
 //   ds   = w ((1 - y) sigma(s) - y pw (1 - sigma(s))),
 // both from e = exp(-|s|): softplus(s) = max(s, 0) + log1p(e), sigma of -|s|
-// is e / (1 + e).  In 32 bits, a vector's eight costs summed there and the row's
-// in 64.  A workgroup to a row: its labels are a bit set in LDS, from the listed
+// is e / (1 + e).  In 32 bits, with the hardware's reciprocals as they are (2^-23 of
+// terms that the exponential has rounded by as much), a vector's eight costs summed
+// there and the row's in 64.  A workgroup to a row: its labels are a bit set in LDS, from the listed
 // tokens' clusters, so the scores are read once.  Bound by HBM: 16384 x 4096 fp32
 // with the gradient (533 MB) 98.6-101.5 us, 5.3 TB/s; 64 x 64 3.8 us, a launch's time.
 __device__ __forceinline__ float log1p_unit(float e) {
@@ -883,11 +892,20 @@ bool run_pass(const DistillArgs& a, hipStream_t s) {
     return true;
 }
 
-// One pass where there are rows enough for the chip, or short ones.  Measured with
-// its gradient, one pass and two, us: bf16 rows of 32000, 64 of them 17.9 and
-// 13.7, 128 18.6 and 20.5, 1024 39.1 and 46.8; of 128256, 128 of them 35.4 and
-// 28.5, 256 40.3 and 45.0, 1024 134 and 179; rows of 32 KiB and less alike for
-// any number (64 x 8192 fp32 11.8 and 11.5), where one pass is one launch.
+// One pass where there are rows enough for the chip, or short ones.  It works in
+// rounds of 256 rows at 1024 threads (512 at 512, 1024 at 256), and a round that a
+// few rows begin costs as much as a full one; two passes read the rows twice, which
+// costs most where the rows and the gradient pass the 256 MB of the last cache.  One
+// pass and two, us, K 64 with the tail:
+//   128256 bf16: 160 rows 38 and 32, 200 39 and 36, 256 41 and 42, 257 59 and 45,
+//     384 63 and 57, 512 70 and 73, 513 86 and 77, 640 100 and 94, 768 107 and 123,
+//     1024 137 and 178, 4096 461 and 650
+//   50021 fp32: 160 28 and 25, 256 32 and 35, 257 43 and 35, 512 53 and 57, 513 61
+//     and 58, 1024 115 and 141
+//   32000 bf16: 160 22 and 18, 256 22 and 20, 512 28 and 28, 1024 41 and 43
+// So the line is right for the training batches it is meant for, and costs up to 30%
+// just behind one full round.  Rows of 32 KiB and less are alike for any number
+// (64 x 8192 fp32 11.8 and 11.5), where one pass is one launch.
 template <typename T>
 bool one_pass(const DistillArgs& a) { return a.N >= 160 || a.V * sizeof(T) <= 32768; }
 

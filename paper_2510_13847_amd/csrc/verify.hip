@@ -521,12 +521,12 @@ __device__ __forceinline__ int list_clusters(const VerifyArgs& a, const uint32_t
 // row the walk ended in, per_wave to a wave.  Behind them: the same of 4 chunks of the
 // rejected draft's row, with the tokens of those slots and the target's logits
 // there; and one that maps clusters to slots for shortlists too long for that.
-// Bound by arithmetic where there are many rows: a weight in 64 bits is 14
-// instructions (rowstat.h) and 128 rows of 262144 take 45.2 us for 67 MB, 0.74 of
-// 10^12 weights a second; 16 rows of 151936 13.9 us, one of 128256 9.1, bound by the
+// Bound by arithmetic where there are many rows: a weight in 64 bits is 15
+// instructions (rowstat.h) and 128 rows of 262144 take 45.9-47 us for 67 MB, 0.72 of
+// 10^12 weights a second; 16 rows of 151936 14.1 us, one of 128256 9.2, bound by the
 // clusters' list (a scan, then a search per slot).  The number of waves that share
-// the chunks changes little (16 per compute unit 50 us, 24 46.8, 32 45.3, 40 44.5, 64
-// 45.2); a chunk is 262 instructions, 127 of them in 64 bits and 60 its two reductions.
+// the chunks changes little (16 per compute unit 52.5 us, 24 49.8, 32 45.9, 40 46.7, 64
+// 47.8); a chunk is 271 instructions, 135 of them in 64 bits and 60 its two reductions.
 template <typename T>
 __global__ __launch_bounds__(kVT) void draw_parts_kernel(VerifyArgs a, StepTable st, int chunk_groups, int per_wave,
                                                          int n_pieces, int per) {
@@ -739,7 +739,10 @@ __device__ __forceinline__ int streamed_slot(const VerifyArgs& a, const dyna_dra
 // token's q; a listed step's tokens all take the tail's constant here, and the
 // drawing kernel puts the shortlist's right.  The row comes from the cache that the
 // pieces' pass left it in; every workgroup joins the pieces again, which is most
-// of its 8.9 us for 16 rows of 151936 and cheaper than a launch that joins them once.
+// of its 8.6 us for 16 rows of 151936 and cheaper than a launch that joins them once.
+// Whole calls that take each token's q: 5 drafts with logits over all 128256 tokens
+// 25 us, 16 chains of 4 over 151936 48; with shortlists of 50000, which are looked up
+// token by token, 34 and 58.
 template <typename T>
 __global__ __launch_bounds__(kVT) void residual_kernel(VerifyArgs a, StepTable st, int per, int n_pieces) {
     __shared__ double table[16];
@@ -808,10 +811,12 @@ constexpr double kTrace = 0x1p-100;
 // alone: it counts how many tokens each chunk loses to the shortlist, and goes
 // through the chunks until one has more.
 //
-// One workgroup goes through joins and scans that wait for each other: 12.1 us for
-// one chain with 32 clusters of 1024 over 128256, 14.5 us for 128 over 262144; with
-// outright drafts or trees 5.8 to 7.8.  A thousand threads with listed entries,
-// for the slots; 256 without, whose barriers are shorter.
+// One workgroup goes through joins and scans that wait for each other: 12.8 us for
+// one chain with 32 clusters of 1024 over 128256, 15.0-15.6 us for 128 over 262144;
+// with outright drafts or trees 6.2 to 7.9.  Behind 40 emptied chunks a call with u = 0
+// takes 101 us instead of 34, behind 2000 of 2^20 tokens, near the most there can be,
+// 1.5 ms.  A thousand threads with listed entries, for the slots; 256 without, whose
+// barriers are shorter.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void draw_kernel(VerifyArgs a, StepTable st, int n_pieces) {
     constexpr int kW = NT / kWave;

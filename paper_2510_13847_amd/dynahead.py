@@ -657,7 +657,8 @@ class _Verifier:
 class ChainVerifier(_Verifier):
     """Preallocated outputs + workspace for repeated dyna_verify_chain calls:
     lengths [B], ids and logprobs [B, n + 1].  temperature 0 is greedy; layout
-    is that of the draft heads whose logits span clusters."""
+    is that of the draft heads whose logits span clusters: its token rows are
+    made here, and waited for (verify_chain does so in every call)."""
 
     def __init__(self, B: int, n: int, V: int, temperature: float = 1.0, layout: Optional[Layout] = None,
                  device="cuda"):
