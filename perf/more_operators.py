@@ -1,0 +1,546 @@
+"""Performance cases of four-bit heads and of the log-probabilities of their tokens: inputs, one pass, cost, 64-bit result.
+
+A case is one call of one operator at one size:
+
+* ``quantize``   rows to microscaled four-bit form (blocks of 32 columns, e2m1 values, one power-of-two scale each) and
+                 back to the values they stand for (``quantize_rows``, ``dequantize_rows``);
+* ``product``    contexts with every four-bit row: the dense head; the contexts in bf16, in fp32 or, quantised within
+                 the call, four-bit themselves (``quant_product``);
+* ``shortlist``  contexts with the four-bit rows of the clusters that each selected (``quant_shortlist_logits``);
+* ``logprobs``   log-probabilities of given tokens, the row's entropy and its best alternatives, over whole rows or over
+                 the shortlists of a draft head (``token_logprobs``);
+* ``grad``       the gradient of those log-probabilities and entropies with respect to the logits, from the statistics
+                 that a forward pass kept (``token_logprobs_grad``).
+
+With ``own`` false, ``run`` computes the operators with elementary tensor operations; with ``own`` true it makes the
+package's calls.  Vocabularies, widths, cluster counts and batches are those of the package's workloads (Llama-3-8B,
+Qwen-2.5 and Gemma-3 shaped heads) and generic odd ones.
+
+Weights are normal with variance 1/d.  Contexts are normal with a scale of its own for every column, as a language
+model's hidden states have.  Logits are normal with a standard deviation of 3, which at these vocabularies puts most of
+a row's probability on a few tens of tokens.
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda"
+SPREAD = 3.0             # standard deviation of a model's logits
+BLOCK = 32               # columns that share a scale
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+# ---------------------------------------------------------------- cases
+def _quantize(name=None, **kw):
+    c = dict(dict(kind="quantize", dtype="bf16"), **kw)
+    return dict(c, name=name) if name else c
+
+
+def _product(name=None, **kw):
+    """a: the contexts' type, "f32", "bf16" or "four" (bf16 quantised within the call); out: the products' type."""
+    c = dict(dict(kind="product", a="bf16", out="f32"), **kw)
+    return dict(c, name=name) if name else c
+
+
+def _shortlist(name=None, **kw):
+    c = dict(dict(kind="shortlist", a="bf16"), **kw)
+    return dict(c, name=name) if name else c
+
+
+def _logprobs(name=None, **kw):
+    """M, k: the rows are shortlists of k of M clusters (0: whole rows); T: tokens a row; top: alternatives a row."""
+    c = dict(dict(kind="logprobs", dtype="bf16", temperature=1.0, T=1, top=0, M=0, k=0, pad=0), **kw)
+    return dict(c, name=name) if name else c
+
+
+def _grad(name=None, **kw):
+    c = dict(dict(kind="grad", dtype="bf16", temperature=1.0, T=1, entropy=True, pad=0), **kw)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one serving batch's hidden states before a four-bit product: the smallest call, where launches count
+        _quantize("quantize_contexts", N=16, d=3584),
+        # a whole LM head, once when it is loaded
+        _quantize("quantize_head", N=128256, d=4096),
+        # a small fp32 model's step
+        _product("product_small_fp32", B=4, V=8192, d=256, a="f32"),
+        # one user's dense head: every row streamed for one context
+        _product("product_b1", B=1, V=128256, d=4096),
+        # a tree's batch of contexts over every row
+        _product("product_tree_b64", B=64, V=128256, d=4096),
+        # a training batch's logits, contexts quantised too, kept in bf16 for the loss that reads them: the largest work
+        _product("product_train_four", B=2048, V=128256, d=4096, a="four", out="bf16"),
+        # one user's draft step behind the router
+        _shortlist("shortlist_b1", B=1, V=128256, d=4096, M=1024, k=32),
+        # the largest vocabulary and batch of draft steps
+        _shortlist("shortlist_large_b128", B=128, V=262144, d=5376, M=4096, k=64),
+        # the drafter's confidence in its tokens over its shortlists, with alternatives: whether to draft on
+        _logprobs("logprobs_draft_b16", N=16, V=151936, dtype="f32", M=2048, k=64, top=10),
+        # the target's log-probabilities of a training batch, with entropy and alternatives, padding rows behind
+        _logprobs("logprobs_train", N=4096, V=128256, top=20, pad=96),
+        # a short fp32 batch's gradient, four tokens a row
+        _grad("grad_small", N=64, V=8191, dtype="f32", T=4),
+        # the backward pass of a training batch
+        _grad("grad_train", N=4096, V=128256, pad=96),
+    ]
+
+
+def draw(rng):
+    def between(lo, hi):
+        return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+    kind = rng.choice(["quantize", "product", "product", "shortlist", "shortlist", "logprobs", "logprobs", "grad"])
+    V = between(8191, 262144)
+    if kind == "quantize":
+        d = between(64, 8192)
+        return _quantize(N=between(1, min(131072, (1 << 29) // d)), d=d, dtype=rng.choice(["bf16", "bf16", "f32"]))
+    if kind == "product":
+        d = rng.choice([between(64, 8192), 256 * between(1, 32)])
+        V = min(V, (1 << 29) // d)
+        a = rng.choice(["bf16", "bf16", "f32", "four"])
+        return _product(B=between(1, 1024 if a == "four" else 256), V=V, d=d, a=a, out=rng.choice(["f32", "f32", "bf16"]))
+    if kind == "shortlist":
+        # a cluster layout takes widths of a multiple of 8
+        d = 8 * between(8, 672)
+        M = between(64, min(4096, V // 32))
+        return _shortlist(B=between(1, 128), V=V, d=d, M=M, k=between(2, min(64, M // 4)),
+                          a=rng.choice(["bf16", "bf16", "f32"]))
+    T, temperature, dtype = rng.choice([1, 1, between(1, 16)]), rng.choice([0.625, 1.0, 1.0]), rng.choice(["bf16", "bf16", "f32"])
+    N = between(1, max(1, min(4096, (1 << 28) // V)))
+    pad = rng.choice([0, N // 8])
+    if kind == "grad":
+        return _grad(N=N, V=V, dtype=dtype, temperature=temperature, T=T, entropy=rng.random() < 0.5, pad=pad)
+    top = rng.choice([0, 1, between(2, 64)])
+    if rng.random() < 0.3:
+        M = between(64, min(4096, V // 32))
+        return _logprobs(N=min(N, 128), V=V, dtype="f32", temperature=temperature, T=T, top=top, M=M,
+                         k=between(2, min(64, M // 4)))
+    return _logprobs(N=N, V=V, dtype=dtype, temperature=temperature, T=T, top=top, pad=pad)
+
+
+# ---------------------------------------------------------------- inputs
+def _gen(seed, stream):
+    return torch.Generator(device=DEV).manual_seed(7919 * int(seed) + stream)
+
+
+def _normal(gen, rows, cols, dtype, scale=1.0):
+    """Normal values; scale: one number, or one of every column."""
+    out = torch.empty((rows, cols), dtype=DTYPES[dtype], device=DEV)
+    step = max(1, (1 << 26) // cols)
+    for r in range(0, rows, step):
+        out[r:r + step] = torch.randn((min(rows, r + step) - r, cols), generator=gen, device=DEV) * scale
+    return out
+
+
+def _contexts(gen, rows, d, dtype):
+    return _normal(gen, rows, d, dtype, torch.exp(0.5 * torch.randn(d, generator=gen, device=DEV)))
+
+
+def _partition(c, seed):
+    """cluster_of [V]: lognormal cluster sizes, each at least one (the same for every seed, so that shapes are),
+    tokens at random."""
+    V, M = c["V"], c["M"]
+    rng = random.Random(V * 8209 + M)
+    w = [math.exp(0.5 * rng.gauss(0.0, 1.0)) for _ in range(M)]
+    total = sum(w)
+    size = [1 + int(x / total * (V - M)) for x in w]
+    for i in range(V - sum(size)):
+        size[i % M] += 1
+    of = torch.empty(V, dtype=torch.int32, device=DEV)
+    runs = torch.repeat_interleave(torch.arange(M, dtype=torch.int32, device=DEV), torch.tensor(size, device=DEV))
+    of[torch.randperm(V, generator=_gen(seed, 90), device=DEV)] = runs
+    return of, size
+
+
+def _selection(c, rows, seed):
+    """The clusters of every row, some more popular than others, and the tokens of its shortlist: slot j of a row is
+    token tokens[row, j] (ascending cluster, ascending token inside it), and -1 past the row's length."""
+    V, M, k = c["V"], c["M"], c["k"]
+    of, size = _partition(c, seed)
+    gen = _gen(seed, 91)
+    score = torch.randn((rows, M), generator=gen, device=DEV) + torch.randn(M, generator=gen, device=DEV)
+    clusters = score.topk(k, dim=1).indices.to(torch.int32)
+    perm = torch.argsort(of.long(), stable=True)
+    chosen = torch.zeros((rows, M), dtype=torch.bool, device=DEV).scatter_(1, clusters.long(), True)
+    cap = sum(sorted(size, reverse=True)[:k])
+    tokens = torch.full((rows, cap), -1, dtype=torch.int64, device=DEV)
+    for b in range(rows):
+        mine = perm[chosen[b][of.long()[perm]]]
+        tokens[b, :mine.numel()] = mine
+    return dict(of=of, clusters=clusters, cap=cap, tokens=tokens)
+
+
+def _product_inputs(c, seed):
+    h = _contexts(_gen(seed, 1), c["B"], c["d"], "f32" if c["a"] == "f32" else "bf16")
+    return dict(h=h, W=_normal(_gen(seed, 2), c["V"], c["d"], "bf16", c["d"] ** -0.5))
+
+
+def _shortlist_inputs(c, seed):
+    return dict(_product_inputs(c, seed), **_selection(c, c["B"], seed))
+
+
+def _logprob_inputs(c, seed):
+    N, V, T, pad = c["N"], c["V"], c["T"], c["pad"]
+    gen = _gen(seed, 3)
+    s = {}
+    if c.get("M"):
+        s = _selection(c, N, seed)
+        V = s["cap"]
+        logits = _normal(gen, N, V, c["dtype"], SPREAD)
+        logits[s["tokens"] < 0] = float("nan")  # nothing is read behind a row
+    else:
+        logits = _normal(gen, N, V, c["dtype"], SPREAD)
+    # what such a model says itself: its rows' tokens by their probability
+    at = torch.empty((N, T), dtype=torch.int64, device=DEV)
+    step = max(1, (1 << 25) // V)
+    for r in range(0, N, step):
+        z = logits[r:r + step].float() / c["temperature"]
+        z = torch.where(torch.isnan(z), -math.inf, z)
+        noise = -torch.log(-torch.log(torch.rand(z.shape, generator=gen, device=DEV).clamp(1e-9, 1.0 - 1e-7)))
+        at[r:r + step] = (z + noise).topk(T, dim=1).indices
+    ids = s["tokens"].gather(1, at) if s else at
+    ids[N - pad:] = -1
+    return dict(s, logits=logits, ids=ids.to(torch.int32))
+
+
+def _grad_inputs(c, seed):
+    s = _logprob_inputs(c, seed)
+    N, T, pad = c["N"], c["T"], c["pad"]
+    gen = _gen(seed, 4)
+    # a policy's advantages over the batch, and the weight of its entropy; padding rows have none
+    g = torch.randn((N, T), generator=gen, device=DEV) / (N * T)
+    ge = torch.full((N,), 0.01 / N, device=DEV) if c["entropy"] else None
+    g[N - pad:] = 0.0
+    if ge is not None:
+        ge[N - pad:] = 0.0
+    stats = torch.empty((N, 2), dtype=torch.float64, device=DEV)
+    step = max(1, (1 << 25) // c["V"])
+    for r in range(0, N, step):
+        logp = torch.log_softmax(s["logits"][r:r + step].double() / c["temperature"], 1)
+        stats[r:r + step, 0] = torch.logsumexp(s["logits"][r:r + step].double() / c["temperature"], 1)
+        stats[r:r + step, 1] = -(logp.exp() * logp).sum(1)
+    return dict(s, g=g, ge=ge, stats=stats)
+
+
+def _values(x):
+    """What the four-bit form of x stands for, in fp32: every block of 32 columns over its power of two, rounded to the
+    nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (ties to the even code)."""
+    rows, d = x.shape
+    x = x.float()
+    tail = -d % BLOCK
+    if tail:
+        x = torch.cat([x, x.new_zeros((rows, tail))], 1)
+    x = x.view(rows, -1, BLOCK)
+    exponent = torch.frexp(x.abs().amax(2, keepdim=True))[1] - 3  # floor(log2) - 2
+    exponent = exponent.clamp_min(-127)
+    inverse = ((127 - exponent) << 23).to(torch.int32).view(torch.float32)
+    v = x * inverse
+    a = v.abs()
+    step = torch.where(a < 2.0, 0.5, torch.where(a < 4.0, 1.0, 2.0))
+    a = (torch.round(a / step) * step).clamp_max(6.0)
+    return (torch.copysign(a, v) / inverse).view(rows, -1)[:, :d]
+
+
+def _all_values(x):
+    out = torch.empty(x.shape, device=DEV)
+    step = max(1, (1 << 26) // x.shape[1])
+    for r in range(0, x.shape[0], step):
+        out[r:r + step] = _values(x[r:r + step])
+    return out
+
+
+def prepare(case, seed):
+    c = case
+    if own:
+        from paper_2510_13847_amd import dynahead as D
+    if c["kind"] == "quantize":
+        s = dict(x=_contexts(_gen(seed, 1), c["N"], c["d"], c["dtype"]))
+        if own:
+            s["q"] = D.quantize_rows(s["x"])
+        return dict(s, case=c)
+    if c["kind"] in ("product", "shortlist"):
+        s = (_product_inputs if c["kind"] == "product" else _shortlist_inputs)(c, seed)
+        W = s.pop("W")
+        if c["kind"] == "product":
+            s["out"] = torch.empty((c["B"], c["V"]), dtype=DTYPES[c["out"]], device=DEV)
+            if own:
+                # the head's four-bit rows, made once; the contexts' form and the call's scratch are kept too
+                s["W4"] = D.quantize_rows(W)
+                s["a4"] = D.quantize_rows(s["h"]) if c["a"] == "four" else None
+                s["ws"] = D.quant_product_workspace(c["B"], c["d"])
+            else:
+                s["W"] = _all_values(W)
+        else:
+            s["out"] = torch.zeros((c["B"], s["cap"]), device=DEV)
+            if own:
+                layout = D.build_layout(s["of"], W, c["M"])
+                s["layout"], s["W4"] = layout, D.quantize_rows(layout.W_perm)
+                s["sel"] = D.shortlist(layout, s["clusters"], with_ids=False)[:3]
+                s["ws"] = D.workspace(layout, None, c["B"], c["k"], s["cap"])
+            else:
+                s["W"] = _all_values(W)
+        return dict(s, case=c)
+    s = _logprob_inputs(c, seed) if c["kind"] == "logprobs" else _grad_inputs(c, seed)
+    if own and c["kind"] == "logprobs":
+        s["rows"] = None
+        if c["M"]:
+            layout = D.build_layout(s["of"], torch.zeros((c["V"], 8), dtype=torch.bfloat16, device=DEV), c["M"])
+            s["rows"] = D.ShortlistRows(layout, *D.shortlist(layout, s["clusters"], with_ids=False)[:3])
+        s["ws"] = D.token_logprobs_workspace(c["N"], s["logits"].shape[1], c["T"], c["top"])
+    return dict(s, case=c)
+
+
+# ---------------------------------------------------------------- one pass
+def run(state):
+    c = state["case"]
+    return (_OWN if own else _PLAIN)[c["kind"]](c, state)
+
+
+def _own_quantize(c, s):
+    from paper_2510_13847_amd import dynahead as D
+    return dict(values=D.dequantize_rows(D.quantize_rows(s["x"], out=s["q"]), dtype=s["x"].dtype))
+
+
+def _own_product(c, s):
+    from paper_2510_13847_amd import dynahead as D
+    a = D.quantize_rows(s["h"], out=s["a4"]) if c["a"] == "four" else s["h"]
+    return dict(logits=D.quant_product(a, s["W4"], out=s["out"], ws=s["ws"]))
+
+
+def _own_shortlist(c, s):
+    from paper_2510_13847_amd import dynahead as D
+    return dict(logits=D.quant_shortlist_logits(s["layout"], s["W4"], s["h"], *s["sel"], ws=s["ws"], out=s["out"]))
+
+
+def _own_logprobs(c, s):
+    from paper_2510_13847_amd import dynahead as D
+    r = D.token_logprobs(s["logits"], s["ids"], temperature=c["temperature"], top=c["top"], rows=s["rows"], ws=s["ws"])
+    out = dict(logprobs=r.logprobs, entropy=r.entropy)
+    return dict(out, top_ids=r.top_ids, top_logprobs=r.top_logprobs) if c["top"] else out
+
+
+def _own_grad(c, s):
+    from paper_2510_13847_amd import dynahead as D
+    return dict(grad=D.token_logprobs_grad(s["logits"], s["stats"], s["ids"], s["g"], s["ge"],
+                                           temperature=c["temperature"]))
+
+
+def _plain_quantize(c, s):
+    x = s["x"]
+    out = torch.empty_like(x)
+    step = max(1, (1 << 26) // c["d"])
+    for r in range(0, c["N"], step):
+        out[r:r + step] = _values(x[r:r + step])
+    return dict(values=out)
+
+
+def _plain_product(c, s):
+    h = _values(s["h"]) if c["a"] == "four" else s["h"].float()
+    return dict(logits=(h @ s["W"].t()).to(DTYPES[c["out"]]))
+
+
+def _plain_shortlist(c, s):
+    out = s["out"]
+    for b in range(c["B"]):
+        tokens = s["tokens"][b]
+        z = s["W"][tokens.clamp_min(0)] @ s["h"][b].float()
+        out[b] = torch.where(tokens >= 0, z, out[b])
+    return dict(logits=out)
+
+
+def _slots(s):
+    """Slot of every given token in its row, and whether it is there."""
+    if "tokens" not in s:
+        return s["ids"].long().clamp_min(0), s["ids"] >= 0
+    same = s["ids"].long()[:, :, None] == s["tokens"][:, None, :]
+    return same.int().argmax(2), same.any(2)
+
+
+def _plain_logprobs(c, s):
+    N, V, top = c["N"], s["logits"].shape[1], c["top"]
+    at, there = _slots(s)
+    inside = s["tokens"] >= 0 if "tokens" in s else None
+    out = dict(logprobs=torch.empty((N, c["T"]), device=DEV), entropy=torch.empty(N, device=DEV))
+    if top:
+        out["top_ids"] = torch.empty((N, top), dtype=torch.int32, device=DEV)
+        out["top_logprobs"] = torch.empty((N, top), device=DEV)
+    step = max(1, (1 << 27) // V)
+    for r in range(0, N, step):
+        e = min(N, r + step)
+        raw = s["logits"][r:e].float()
+        if inside is not None:
+            raw = torch.where(inside[r:e], raw, -math.inf)
+        z = raw / c["temperature"]
+        z = z - z.amax(1, keepdim=True)
+        w = torch.exp(z)
+        total = w.sum(1, keepdim=True)
+        logp = z - torch.log(total)
+        out["entropy"][r:e] = -torch.where(w > 0, w / total * logp, 0.0).sum(1)
+        out["logprobs"][r:e] = torch.where(there[r:e], logp.gather(1, at[r:e]), -math.inf)
+        if top:
+            # one whole number to a slot: larger logits first, then lower tokens
+            bits = (raw + 0.0).view(torch.int32).long()
+            order = torch.where(bits < 0, -2147483648 - bits, bits)
+            ids = s["tokens"][r:e] if inside is not None else torch.arange(V, device=DEV)
+            best = (order * (1 << 20) - ids).topk(top, dim=1).indices
+            lp = logp.gather(1, best)
+            names = ids.gather(1, best) if inside is not None else best
+            out["top_ids"][r:e] = torch.where(lp > -math.inf, names, -1).to(torch.int32)
+            out["top_logprobs"][r:e] = lp
+    return out
+
+
+def _plain_grad(c, s):
+    z = s["logits"].float() / c["temperature"]
+    logp = z - s["stats"][:, :1].float()
+    p = torch.exp(logp)
+    g = torch.where(s["ids"] >= 0, s["g"], 0.0) / c["temperature"]
+    out = -g.sum(1, keepdim=True) * p
+    if s["ge"] is not None:
+        out -= s["ge"][:, None] / c["temperature"] * torch.where(p > 0, p * (logp + s["stats"][:, 1:].float()), 0.0)
+    out.scatter_add_(1, s["ids"].long().clamp_min(0), g)
+    return dict(grad=out.to(s["logits"].dtype))
+
+
+_OWN = dict(quantize=_own_quantize, product=_own_product, shortlist=_own_shortlist, logprobs=_own_logprobs, grad=_own_grad)
+_PLAIN = dict(quantize=_plain_quantize, product=_plain_product, shortlist=_plain_shortlist, logprobs=_plain_logprobs,
+              grad=_plain_grad)
+
+
+# ---------------------------------------------------------------- what a pass costs at least
+def _row_bytes(d):
+    """Bytes of a row's four-bit form: half a byte to a column and one to a block."""
+    blocks = -(-d // BLOCK)
+    return blocks * (BLOCK // 2 + 1)
+
+
+def work(case):
+    c = case
+    size = {"f32": 4, "bf16": 2}
+    if c["kind"] == "quantize":
+        e = size[c["dtype"]]
+        return dict(bytes=2 * c["N"] * c["d"] * e, flops=3 * c["N"] * c["d"])
+    if c["kind"] in ("product", "shortlist"):
+        B, V, d = c["B"], c["V"], c["d"]
+        contexts = B * d * (4 if c["a"] == "f32" else 2)
+        if c["kind"] == "product":
+            return dict(bytes=V * _row_bytes(d) + contexts + B * V * size[c["out"]], flops=2 * B * V * d)
+        # about as many clusters as the contexts choose at random, and each one's rows once
+        M, k = c["M"], c["k"]
+        slots = B * k * V // M
+        rows = int(V * (1.0 - (1.0 - k / M) ** B))
+        return dict(bytes=rows * _row_bytes(d) + contexts + 4 * slots, flops=2 * slots * d)
+    N, real, V, T = c["N"], c["N"] - c["pad"], c["V"], c["T"]
+    e = size[c["dtype"]]
+    if c["kind"] == "logprobs":
+        slots = N * (c["k"] * V // c["M"] if c["M"] else V)
+        return dict(bytes=slots * e + 8 * N * T + 4 * N + 8 * N * c["top"], flops=5 * slots)
+    return dict(bytes=(real + N) * V * e + 12 * N * T + 16 * N, flops=6 * real * V)
+
+
+# ---------------------------------------------------------------- the same pass in 64 bits
+def exact(case, seed):
+    """From the definitions, row by row or in blocks of rows."""
+    return _EXACT[case["kind"]](case, seed)
+
+
+# halfway points between neighbouring values, and on which side a tie falls: to the value with the even code
+_HALF = ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False), (3.5, True), (5.0, False))
+
+
+def _exact_values(x):
+    level = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=DEV)
+    out = torch.zeros(x.shape, dtype=torch.float64, device=DEV)
+    for k in range(0, x.shape[1], BLOCK):
+        b = x[:, k:k + BLOCK].double()
+        largest = b.abs().max(1, keepdim=True).values
+        power = torch.exp2(torch.floor(torch.log2(largest.clamp_min(1e-300))).clamp_min(-125.0) - 2.0)
+        a = b.abs() / power
+        code = torch.zeros(b.shape, dtype=torch.int64, device=DEV)
+        for half, up in _HALF:
+            code += (a >= half) if up else (a > half)
+        out[:, k:k + BLOCK] = torch.sign(b) * level[code] * power
+    return out
+
+
+def _exact_quantize(c, seed):
+    return dict(values=_exact_values(_contexts(_gen(seed, 1), c["N"], c["d"], c["dtype"])))
+
+
+def _exact_product(c, seed):
+    s = _product_inputs(c, seed)
+    h = _exact_values(s["h"]) if c["a"] == "four" else s["h"].double()
+    out = torch.empty((c["B"], c["V"]), dtype=torch.float64, device=DEV)
+    for r in range(0, c["V"], 8192):
+        out[:, r:r + 8192] = torch.mm(h, _exact_values(s["W"][r:r + 8192]).t().contiguous())
+    return dict(logits=out)
+
+
+def _exact_shortlist(c, seed):
+    s = _shortlist_inputs(c, seed)
+    W, h = _exact_values(s["W"]), s["h"].double()
+    out = torch.zeros((c["B"], s["cap"]), dtype=torch.float64, device=DEV)
+    for b in range(c["B"]):
+        n = int((s["tokens"][b] >= 0).sum())
+        out[b, :n] = (W[s["tokens"][b, :n]] * h[b]).sum(1)
+    return dict(logits=out)
+
+
+def _exact_logprobs(c, seed):
+    s = _logprob_inputs(c, seed)
+    N, T, top = c["N"], c["T"], c["top"]
+    out = dict(logprobs=torch.full((N, T), -math.inf, dtype=torch.float64, device=DEV),
+               entropy=torch.zeros(N, dtype=torch.float64, device=DEV))
+    if top:
+        out["top_ids"] = torch.full((N, top), -1, dtype=torch.int32, device=DEV)
+        out["top_logprobs"] = torch.full((N, top), -math.inf, dtype=torch.float64, device=DEV)
+    for r in range(N):
+        z = s["logits"][r].double()
+        names = torch.arange(z.numel(), device=DEV)
+        if c["M"]:
+            names = s["tokens"][r][s["tokens"][r] >= 0]
+            z = z[:names.numel()]
+        logp = torch.log_softmax(z / c["temperature"], 0)
+        out["entropy"][r] = -(logp.exp() * logp).sum()
+        if r < N - c["pad"]:
+            for t, token in enumerate(s["ids"][r].tolist()):
+                if token >= 0:
+                    out["logprobs"][r, t] = logp[names == token][0] if c["M"] else logp[token]
+        if top:
+            # by token first, so that a stable sort by logit leaves the lower one in front
+            by_name = torch.argsort(names)
+            best = by_name[torch.argsort(z[by_name], descending=True, stable=True)[:top]]
+            out["top_ids"][r, :best.numel()] = names[best].to(torch.int32)
+            out["top_logprobs"][r, :best.numel()] = logp[best]
+    return out
+
+
+def _exact_grad(c, seed):
+    s = _grad_inputs(c, seed)
+    T = c["temperature"]
+    out = torch.zeros((c["N"], c["V"]), dtype=torch.float64, device=DEV)
+    step = max(1, (1 << 25) // c["V"])
+    for r in range(0, c["N"] - c["pad"], step):
+        e = min(c["N"] - c["pad"], r + step)
+        logp = torch.log_softmax(s["logits"][r:e].double() / T, 1)
+        p = logp.exp()
+        d = torch.zeros_like(p)
+        for t in range(c["T"]):
+            one = torch.zeros_like(p).scatter_(1, s["ids"][r:e, t:t + 1].long(), 1.0)
+            d += s["g"][r:e, t:t + 1].double() * (one - p)
+        if s["ge"] is not None:
+            entropy = -(p * logp).sum(1, keepdim=True)
+            d -= s["ge"][r:e].double()[:, None] * p * (logp + entropy)
+        out[r:e] = d / T
+    return dict(grad=out)
+
+
+_EXACT = dict(quantize=_exact_quantize, product=_exact_product, shortlist=_exact_shortlist, logprobs=_exact_logprobs,
+              grad=_exact_grad)
