@@ -220,12 +220,16 @@ def _grad_inputs(c, seed):
     g[N - pad:] = 0.0
     if ge is not None:
         ge[N - pad:] = 0.0
-    stats = torch.empty((N, 2), dtype=torch.float64, device=DEV)
+    # what the forward pass keeps of a row: its largest logit, the log of the sum of exponentials over it, its entropy
+    stats = torch.empty((N, 3), dtype=torch.float64, device=DEV)
     step = max(1, (1 << 25) // c["V"])
     for r in range(0, N, step):
-        logp = torch.log_softmax(s["logits"][r:r + step].double() / c["temperature"], 1)
-        stats[r:r + step, 0] = torch.logsumexp(s["logits"][r:r + step].double() / c["temperature"], 1)
-        stats[r:r + step, 1] = -(logp.exp() * logp).sum(1)
+        z = s["logits"][r:r + step].double()
+        stats[r:r + step, 0] = z.amax(1)
+        z = (z - stats[r:r + step, :1]) / c["temperature"]
+        stats[r:r + step, 1] = torch.logsumexp(z, 1)
+        logp = z - stats[r:r + step, 1:2]
+        stats[r:r + step, 2] = -(logp.exp() * logp).sum(1)
     return dict(s, g=g, ge=ge, stats=stats)
 
 
@@ -398,13 +402,13 @@ def _plain_logprobs(c, s):
 
 
 def _plain_grad(c, s):
-    z = s["logits"].float() / c["temperature"]
-    logp = z - s["stats"][:, :1].float()
+    top, log_sum, entropy = s["stats"].float().split(1, 1)
+    logp = (s["logits"].float() - top) / c["temperature"] - log_sum
     p = torch.exp(logp)
     g = torch.where(s["ids"] >= 0, s["g"], 0.0) / c["temperature"]
     out = -g.sum(1, keepdim=True) * p
     if s["ge"] is not None:
-        out -= s["ge"][:, None] / c["temperature"] * torch.where(p > 0, p * (logp + s["stats"][:, 1:].float()), 0.0)
+        out -= s["ge"][:, None] / c["temperature"] * torch.where(p > 0, p * (logp + entropy), 0.0)
     out.scatter_add_(1, s["ids"].long().clamp_min(0), g)
     return dict(grad=out.to(s["logits"].dtype))
 
@@ -442,7 +446,7 @@ def work(case):
     if c["kind"] == "logprobs":
         slots = N * (c["k"] * V // c["M"] if c["M"] else V)
         return dict(bytes=slots * e + 8 * N * T + 4 * N + 8 * N * c["top"], flops=5 * slots)
-    return dict(bytes=(real + N) * V * e + 12 * N * T + 16 * N, flops=6 * real * V)
+    return dict(bytes=(real + N) * V * e + 12 * N * T + 24 * N, flops=6 * real * V)
 
 
 # ---------------------------------------------------------------- the same pass in 64 bits
