@@ -533,6 +533,121 @@ dyna_status dyna_router_loss(const void* scores, int32_t dtype, int32_t M, int64
                              int64_t grad_stride, hipStream_t stream);
 
 /* ------------------------------------------------------------------ */
+/* Four-bit rows (OCP microscaling, MXFP4): the head at a quarter of    */
+/* bf16's bytes.                                                       */
+/* ------------------------------------------------------------------ */
+
+/* A matrix of rows whose blocks of 32 columns are e2m1 values (0, 1/2, 1, 3/2,
+ * 2, 3, 4, 6 and their negatives) over one power of two each (e8m0).  Of a
+ * block with largest magnitude a the scale is 2^(floor(log2 a) - 2), 2^-127 at
+ * least; a value is the nearest one to x / scale, ties to the even code, 6 at
+ * most.  A block with a NaN or an infinity is NaN throughout.
+ * data: dyna_quant_bytes(rows, d) bytes of device memory, 256-byte aligned, as
+ * dyna_quantize_rows writes them: an order of the library's own, in which 16
+ * rows by 128 columns are the 1 KiB that a wave loads for a matrix instruction
+ * (rows filled up to 16 and columns to 128 with zeros).
+ * 1 <= rows <= 2^24, 1 <= d <= 8192 (any d). */
+typedef struct dyna_quant {
+    int32_t rows, d;
+    const void* data;
+} dyna_quant;
+
+size_t dyna_quant_bytes(int32_t rows, int32_t d);
+
+/* Rows to four-bit form and back.
+ *  x, out   device, dtype, row r is d elements at r * row_stride, any alignment
+ *           of the element; elements of `out` behind a row are left as they were
+ *  data     device output, dyna_quant_bytes(rows, d)
+ * Values come back exactly, in bf16 too.  Asynchronous on `stream`. */
+dyna_status dyna_quantize_rows(const void* x, int32_t dtype, int32_t rows, int32_t d, int64_t row_stride, void* data,
+                               hipStream_t stream);
+dyna_status dyna_dequantize_rows(const dyna_quant* q, void* out, int32_t dtype, int64_t row_stride,
+                                 hipStream_t stream);
+
+/* Workspace of dyna_quant_product for B contexts.  It holds nothing between
+ * calls; calls that may overlap (two streams, two captured graphs) need one each. */
+size_t dyna_quant_product_workspace_bytes(int32_t B, int32_t d);
+
+/* out[b, r] = a_b . W_r for r < n_rows (<= W->rows): the dense head over
+ * four-bit rows, and the static head over their first ones.
+ *  a [B, d]  device, dtype adtype, row b at b * a_stride, any alignment; or NULL
+ *            with a4
+ *  a4        four-bit contexts (rows = B, d = W->d), or NULL with a
+ *  out       device, dtype odtype, row b is n_rows elements at b * out_stride;
+ *            elements behind a row are left as they were
+ * The products of the values are exact and summed in 32 bits: fp32 contexts are
+ * taken as three bf16 terms each, which hold all 24 bits.  B = 0 is a no-op. */
+dyna_status dyna_quant_product(const dyna_quant* W, int32_t n_rows, const void* a, int32_t adtype, int64_t a_stride,
+                               const dyna_quant* a4, int32_t B, void* out, int32_t odtype, int64_t out_stride,
+                               void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* dyna_shortlist_logits over four-bit rows: W holds the layout's rows in layout
+ * order (dyna_quantize_rows of W_perm; rows = V, the same d).  L->W_perm is not
+ * read.  Other arguments, results and workspace as there. */
+dyna_status dyna_quant_shortlist_logits(const dyna_layout* L, const dyna_quant* W, const void* h, int32_t hdtype,
+                                        int32_t B, int32_t k, const int32_t* sel_sorted, const int32_t* sel_rowoff,
+                                        const int32_t* row_len, float* logits, int32_t cap, void* ws,
+                                        size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------ */
+/* Log-probabilities of given tokens.                                   */
+/* ------------------------------------------------------------------ */
+
+/* The shortlists that rows of draft logits span, as dyna_shortlist wrote them
+ * (k entries a row; shared: one row of them for every row of logits).  */
+typedef struct dyna_shortlist_rows {
+    const dyna_layout* L;        /* perm and offsets are read */
+    const int32_t* token_rows;   /* device [V, 2], dyna_token_rows of L */
+    const int32_t* sel_sorted;   /* device [N, k] or [1, k] */
+    const int32_t* sel_rowoff;   /* device [N, k + 1] or [1, k + 1] */
+    const int32_t* row_len;      /* device [N] or [1], clamped to the logits' columns */
+    int32_t k;
+    int32_t shared;              /* 0 or 1 */
+} dyna_shortlist_rows;
+
+/* workspace of dyna_token_logprobs for N rows of V columns; 256-byte aligned,
+ * holds nothing between calls, and calls that may overlap need one each */
+size_t dyna_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t T, int32_t top);
+
+/* N rows of logits, p = softmax(z / temperature) of each:
+ *  logits       device, dtype, row r is V <= 2^20 columns at r * row_stride, any
+ *               alignment.  rows NULL: column v is token v.  Otherwise the row is
+ *               its shortlist (slots past row_len are not read, whatever they hold).
+ *  tokens [N, T]  device: the given tokens, T <= DYNA_MAX_KT (0: none)
+ *  temperature  FLT_MIN and above (finite)
+ *  out_logprobs [N, T]  log p of each; -inf for a token that is not in the row (an
+ *               id outside the vocabulary or the shortlist: padding)
+ *  out_entropy [N]      -sum p log p; may be NULL
+ *  out_top_ids, out_top_logprobs [N, top]  the row's best tokens, (z desc, id
+ *               asc), top <= DYNA_MAX_KT (0: none; then both may be NULL); -1 and
+ *               -inf where the row has no more (NaN and -inf are no alternatives)
+ *  out_stats [N, 3]     fp64, may be NULL: the row's largest logit m, log sum
+ *               exp((z - m) / temperature) and the entropy, for dyna_token_logprobs_grad
+ * A masked logit (-inf) has p = 0.  A row that allows no token (empty, or masked
+ * throughout) has every log-probability -inf and entropy 0.  A NaN or +inf logit
+ * makes its row's log-probabilities and entropy NaN. */
+dyna_status dyna_token_logprobs(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
+                                const dyna_shortlist_rows* rows, const int32_t* tokens, int32_t T, float temperature,
+                                int32_t top, float* out_logprobs, float* out_entropy, int32_t* out_top_ids,
+                                float* out_top_logprobs, double* out_stats, void* ws, size_t ws_bytes,
+                                hipStream_t stream);
+
+/* The gradient with respect to the logits, from a forward call's out_stats and
+ * the same other arguments:
+ *   dz_v = 1 / temperature (sum_t g_t ([v = t] - p_v) - e p_v (log p_v + H))
+ *  grad_logprobs [N, T]  device fp32: g; what stands at a token that is not in its row is not used
+ *  grad_entropy [N]      device fp32: e; may be NULL (zeros)
+ *  grad         device, dtype, row r at r * grad_stride; elements behind a row (or
+ *               its shortlist) are left as they were; the spans of both, gaps between rows
+ *               included, must not overlap
+ * A row whose g (at its tokens) and e are all 0 is padding: nothing of its logits
+ * is read, its gradient is 0.  So is the gradient of a row that allows no token. */
+dyna_status dyna_token_logprobs_grad(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
+                                     const dyna_shortlist_rows* rows, const int32_t* tokens, int32_t T,
+                                     float temperature, const double* stats, const float* grad_logprobs,
+                                     const float* grad_entropy, void* grad, int64_t grad_stride, hipStream_t stream);
+
+/* ------------------------------------------------------------------ */
 /* Diagnostics.                                                        */
 /* ------------------------------------------------------------------ */
 

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "dyna_internal.h"
+#include "quant.h"
 
 #define DYNA_API extern "C" __attribute__((visibility("default")))
 
@@ -634,6 +635,38 @@ DYNA_API dyna_status dyna_shortlist_logits(const dyna_layout* L, const void* h, 
     if (ws_bytes < c0.bytes) return set_error(DYNA_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, c0.bytes);
     const Carve c = carve(L, nullptr, B, k, cap, ws);
     return run_logits(L, h, hdtype, B, k, sel_sorted, sel_rowoff, logits, cap, c.plan, stream);
+}
+
+DYNA_API dyna_status dyna_quant_shortlist_logits(const dyna_layout* L, const dyna_quant* W, const void* h,
+                                                 int32_t hdtype, int32_t B, int32_t k, const int32_t* sel_sorted,
+                                                 const int32_t* sel_rowoff, const int32_t* row_len, float* logits,
+                                                 int32_t cap, void* ws, size_t ws_bytes, hipStream_t stream) {
+    TRY(check_layout(L));
+    TRY(check_quant(W, "W"));
+    REQUIRE(W->rows == L->V && W->d == L->d, "W: rows=%d d=%d, not the layout's V=%d d=%d", W->rows, W->d, L->V, L->d);
+    TRY(check_k(L, k));
+    REQUIRE(B >= 0, "B=%d < 0", B);
+    REQUIRE(valid_dtype(hdtype), "bad hdtype %d", hdtype);
+    TRY(check_cap(L, k, cap));
+    if (B == 0) return DYNA_OK;
+    REQUIRE(h && aligned16(h) && sel_sorted && sel_rowoff && row_len && logits && ws,
+            "NULL argument or h misaligned");
+    const Carve c0 = carve(L, nullptr, B, k, cap, nullptr);
+    if (ws_bytes < c0.bytes) return set_error(DYNA_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, c0.bytes);
+    const Carve c = carve(L, nullptr, B, k, cap, ws);
+    TRY(launch_plan(L->offsets, L->M, sel_sorted, sel_rowoff, B, k, c.plan, stream));
+    QuantProductArgs a{};
+    a.W = quant_view(W->data, W->rows, W->d);
+    a.a = h;
+    a.adtype = hdtype;
+    a.a_stride = L->d;
+    a.B = B;
+    a.out = logits;
+    a.odtype = DYNA_F32;
+    a.ld = cap;
+    a.plan = c.plan;
+    a.max_chunks_bound = chunk_bound(L, B, k);
+    return timed([&] { return launch_quant_rows(a, stream); }, stream);
 }
 
 DYNA_API dyna_status dyna_draft_select(const dyna_layout* L, const float* logits, const int32_t* sel_sorted,

@@ -1,0 +1,299 @@
+// Streamed four-bit rows times a few contexts: the dense head of up to 16
+// contexts, and the gathered head over the chunks of a plan.
+//
+// The work is an HBM stream of the rows: 17/32 byte per weight, converted to bf16
+// in registers (exactly: an e2m1 value over a power of two) and multiplied on the
+// matrix cores.  A workgroup has a wave for each unit of 512 columns and takes
+// tiles of 16 rows one after the other, so its waves together request a tile's
+// consecutive bytes.  A wave's context columns stay in registers; its partial
+// products are added through LDS in wave order (bit-identical from run to run).
+//
+// An fp32 context is three columns of bf16: its 24 bits cut in three terms of
+// eight, whose products with a four-bit value are exact.
+#include "quant.h"
+#include "rowstat.h"
+
+namespace dyna {
+namespace {
+
+template <typename T>
+using sptr = const __attribute__((address_space(4))) T*;  // read through the scalar unit
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+enum { kActFour = 0, kActBf16 = 1, kActF32 = 3 };  // the contexts' type; columns of the product for each
+
+__host__ __device__ constexpr int contexts_per_pass(int act) { return act == kActF32 ? 5 : 16; }
+
+// Eight bf16 of a four-bit code word.
+__device__ __forceinline__ bf16x8 row_operand(uint32_t code, float scale) {
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3));
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+// Term t of three of an fp32 value, each cut off behind eight bits (so the sum is
+// the value, and no term overflows); an infinity or NaN is its own first term.
+__device__ __forceinline__ float term_of(float x, int t) {
+    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    if (t == 0) return x == x ? a : x;
+    const float b = fabsf(x) <= kF32Max ? x - a : 0.0f;
+    const float c = __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    return t == 1 ? c : b - c;
+}
+
+// One tile and the contexts that it is multiplied with.
+struct QuantTile {
+    int r0, nrows;   // first row and number of rows (0: no tile left)
+    int list, cnt;   // its contexts: list entries, or [0, cnt) where there is no plan
+    int first;       // first of them in this pass
+};
+
+template <int ACT, bool PLAN, int MAXW, typename OT>
+__global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProductArgs a) {
+    constexpr int CPP = contexts_per_pass(ACT);
+    constexpr int kOut = CPP * kMfmaRows;
+    __shared__ __attribute__((aligned(16))) f32x4 red[2][MAXW][kWave];
+    const int lane = lane_id();
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int NW = a.W.units, NT = NW * kWave;
+    const int col = lane & 15, g = lane >> 4;
+    const int steps = min(kQuantUnitSteps, a.W.steps - wv * kQuantUnitSteps);  // of this wave's unit
+    const int d = a.W.d;
+
+    // this workgroup's tiles: plans, a run of consecutive chunks; else every
+    // gridDim.x-th group
+    int c1 = 0, run0 = 0;  // plans: end of the run; first chunk of those with the same contexts
+    int at = 0;
+    sptr<int32_t> chunks = (sptr<int32_t>)a.plan.chunks;
+    auto read_tile = [&](int i, int first) {
+        QuantTile t{0, 0, 0, 0, 0};
+        if constexpr (PLAN) {
+            t.r0 = chunks[4 * i];
+            t.nrows = min(kMfmaRows, chunks[4 * i + 1]);
+            t.list = chunks[4 * i + 2];
+            t.cnt = chunks[4 * i + 3];
+        } else {
+            t.r0 = i * kMfmaRows;
+            t.nrows = min(kMfmaRows, a.n_rows - t.r0);
+            t.cnt = a.B;
+        }
+        t.first = first;
+        return t;
+    };
+    QuantTile cur{0, 0, 0, 0, 0};
+    if constexpr (PLAN) {
+        const int64_t n = ((sptr<int32_t>)a.plan.hdr)[0];
+        at = run0 = (int)(n * blockIdx.x / gridDim.x);
+        c1 = (int)(n * (blockIdx.x + 1) / gridDim.x);
+        if (at < c1) cur = read_tile(at, 0);
+    } else {
+        at = blockIdx.x;
+        if ((int64_t)at * kMfmaRows < a.n_rows) cur = read_tile(at, blockIdx.y * CPP);
+    }
+    // The tile behind cur: plans walk the chunks of one context list once for each
+    // CPP of its contexts.
+    auto next_tile = [&]() -> QuantTile {
+        if constexpr (PLAN) {
+            const int i = at + 1;
+            if (i < c1) {
+                const QuantTile t = read_tile(i, cur.first);
+                if (t.list == cur.list) {
+                    at = i;
+                    return t;
+                }
+            }
+            if (cur.first + CPP < cur.cnt) {
+                at = run0;
+                return read_tile(at, cur.first + CPP);
+            }
+            at = run0 = i;
+            return i < c1 ? read_tile(i, 0) : QuantTile{0, 0, 0, 0, 0};
+        } else {
+            const int64_t i = (int64_t)at + gridDim.x;
+            if (i * kMfmaRows >= a.n_rows) return QuantTile{0, 0, 0, 0, 0};
+            at = (int)i;
+            return read_tile(at, cur.first);
+        }
+    };
+
+    // ---- rows
+    u32x4 w[2][kQuantUnitSteps];
+    uint32_t ws[2];
+    auto load_rows = [&](int set, const QuantTile& t) {
+        const int r = t.r0 + (PLAN ? min(col, t.nrows - 1) : col);
+        const uint8_t* p = a.W.data + (int64_t)(r / kMfmaRows) * a.W.group_bytes + wv * kQuantUnitBytes;
+        const int at = (r % kMfmaRows) * 64 + g * 16;
+        // steps that the unit lacks repeat its last one; their contexts are zero
+#pragma unroll
+        for (int j = 0; j < kQuantUnitSteps; ++j)
+            w[set][j] = *reinterpret_cast<const u32x4*>(p + min(j, steps - 1) * kQuantStepBytes + at);
+        ws[set] = *reinterpret_cast<const uint32_t*>(p + steps * kQuantStepBytes + at / 4);
+    };
+
+    // ---- contexts, in the operand layout
+    constexpr int NS = ACT == kActFour ? 1 : 4;
+    u32x4 b[kQuantUnitSteps][NS];
+    uint32_t bs = 0;
+    constexpr int NE = 4;        // results of a thread at most: 256 of 64 threads
+    constexpr int64_t kNowhere = INT64_MIN;
+    int64_t out_at[NE];          // where result i of this thread's context would go for layout row 0
+    auto load_contexts = [&](const QuantTile& t) {
+        auto context = [&](int c, int* slot) -> int {  // context c of this pass, -1 past the last
+            const int i = t.first + c;
+            *slot = 0;
+            if (c >= CPP || i >= t.cnt) return -1;
+            if constexpr (PLAN) {
+                const ListEntry e = a.plan.list[t.list + i];
+                *slot = e.slot_base;
+                return e.b;
+            }
+            return i;
+        };
+        int slot;
+        const int c = context(ACT == kActF32 ? col / 3 : col, &slot);
+#pragma unroll
+        for (int j = 0; j < kQuantUnitSteps; ++j)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) b[j][s] = u32x4{0u, 0u, 0u, 0u};
+        if (c >= 0) {
+            if constexpr (ACT == kActFour) {
+                const uint8_t* p = a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes + wv * kQuantUnitBytes;
+                const int at = (c % kMfmaRows) * 64 + g * 16;
+#pragma unroll
+                for (int j = 0; j < kQuantUnitSteps; ++j)
+                    if (j < steps) b[j][0] = *reinterpret_cast<const u32x4*>(p + j * kQuantStepBytes + at);
+                bs = *reinterpret_cast<const uint32_t*>(p + steps * kQuantStepBytes + at / 4);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kQuantUnitSteps; ++j)
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const int k = wv * kQuantUnit + j * kQuantStep + g * kQuantBlock + s * 8;
+                        if (k >= d) continue;
+                        float x[8];
+                        if constexpr (ACT == kActBf16) {
+                            load_part(static_cast<const uint16_t*>(a.a) + (int64_t)c * a.a_stride + k, d - k, 0.0f, x);
+                        } else {
+                            load_part(static_cast<const float*>(a.a) + (int64_t)c * a.a_stride + k, d - k, 0.0f, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = term_of(x[e], col % 3);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) b[j][s][e] = bf16_pair(x[2 * e], x[2 * e + 1]);
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            const int o = (int)threadIdx.x + i * NT;
+            out_at[i] = kNowhere;
+            if (o >= kOut) break;
+            int base;
+            const int x = context(o >> 4, &base);
+            if (x >= 0) out_at[i] = (int64_t)x * a.ld + base;
+        }
+    };
+
+    if (cur.nrows == 0) return;  // whole workgroup
+    load_rows(0, cur);
+    load_contexts(cur);
+    OT* out = static_cast<OT*>(a.out);
+    int set = 0;
+    auto tile = [&](auto set_tag) {
+        constexpr int S = decltype(set_tag)::value;
+        const QuantTile nxt = next_tile();
+        load_rows(1 - S, nxt.nrows > 0 ? nxt : cur);
+        f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        if constexpr (ACT == kActFour) {
+            auto product = [&](auto j_tag) {
+                constexpr int j = decltype(j_tag)::value;
+                i32x8 x{}, y{};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = (int)b[j][0][e];
+                    y[e] = (int)w[S][j][e];
+                }
+                acc[j & 1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc[j & 1], 4, 4, j, (int)bs, j,
+                                                                            (int)ws[S]);
+            };
+            product(std::integral_constant<int, 0>{});
+            product(std::integral_constant<int, 1>{});
+            product(std::integral_constant<int, 2>{});
+            product(std::integral_constant<int, 3>{});
+        } else {
+#pragma unroll
+            for (int j = 0; j < kQuantUnitSteps; ++j) {
+                const float scale = __uint_as_float(((ws[S] >> (8 * j)) & 0xffu) << 23);
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[j][s % NS]),
+                                                                         row_operand(w[S][j][s], scale), acc[s & 1], 0, 0, 0);
+            }
+        }
+        // lane: columns 4 g .. 4 g + 3 of the product with row lane % 16
+        red[S][wv][lane] = acc[0] + acc[1];
+        lds_barrier();  // the other buffer's readers have passed the barrier before
+        const float* sums = reinterpret_cast<const float*>(red[S][0]);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            const int o = (int)threadIdx.x + i * NT;
+            if (o >= kOut || out_at[i] == kNowhere) continue;
+            const int row = o & 15, ctx = o >> 4;
+            float x = 0.0f;
+#pragma unroll
+            for (int q = 0; q < (ACT == kActF32 ? 3 : 1); ++q) {
+                const int c = ACT == kActF32 ? 3 * ctx + q : ctx;
+                const int p = (((c >> 2) * 16 + row) << 2) + (c & 3);
+                for (int v = 0; v < NW; ++v) x += sums[v * kWave * 4 + p];
+            }
+            if (row < cur.nrows) store_elt(out + out_at[i] + cur.r0 + row, x);
+        }
+        const bool other = PLAN && nxt.nrows > 0 && (nxt.list != cur.list || nxt.first != cur.first);
+        cur = nxt;
+        if (other) load_contexts(cur);
+    };
+    while (true) {
+        tile(std::integral_constant<int, 0>{});
+        if (cur.nrows == 0) break;
+        tile(std::integral_constant<int, 1>{});
+        if (cur.nrows == 0) break;
+    }
+}
+
+template <int ACT, bool PLAN, int MAXW, typename OT>
+dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
+    const int NW = a.W.units;
+    const int64_t tiles = PLAN ? a.max_chunks_bound : ((int64_t)a.n_rows + kMfmaRows - 1) / kMfmaRows;
+    const int passes = PLAN ? 1 : (a.B + contexts_per_pass(ACT) - 1) / contexts_per_pass(ACT);
+    const int64_t resident = 256 * (int64_t)std::max(1, 16 / NW);
+    const int64_t blocks = std::max<int64_t>(1, std::min(tiles, resident));
+    launch_timed_kernel(quant_rows_kernel<ACT, PLAN, MAXW, OT>, dim3((unsigned)blocks, (unsigned)passes), dim3(NW * kWave),
+                        0, stream, a);
+    return check_launch("quant_rows_kernel");
+}
+template <int ACT, bool PLAN, typename OT>
+dyna_status launch_w(const QuantProductArgs& a, hipStream_t stream) {
+    return a.W.units <= 8 ? launch_t<ACT, PLAN, 8, OT>(a, stream) : launch_t<ACT, PLAN, 16, OT>(a, stream);
+}
+
+}  // namespace
+
+size_t quant_product_ws_bytes(int32_t B, int32_t d) { return 256; }
+dyna_status launch_quant_product(const QuantProductArgs& a, hipStream_t stream) { return launch_quant_rows(a, stream); }
+
+dyna_status launch_quant_rows(const QuantProductArgs& a, hipStream_t stream) {
+    if (a.plan.hdr != nullptr)
+        return a.adtype == DYNA_BF16 ? launch_w<kActBf16, true, float>(a, stream)
+                                     : launch_w<kActF32, true, float>(a, stream);
+    const bool f32 = a.odtype == DYNA_F32;
+    if (a.a == nullptr)
+        return f32 ? launch_w<kActFour, false, float>(a, stream) : launch_w<kActFour, false, uint16_t>(a, stream);
+    if (a.adtype == DYNA_BF16)
+        return f32 ? launch_w<kActBf16, false, float>(a, stream) : launch_w<kActBf16, false, uint16_t>(a, stream);
+    return f32 ? launch_w<kActF32, false, float>(a, stream) : launch_w<kActF32, false, uint16_t>(a, stream);
+}
+
+}  // namespace dyna

@@ -51,6 +51,16 @@ class _DraftStep(ctypes.Structure):
                 ("shared", ctypes.c_int32), ("temperature", ctypes.c_float), ("tail_beta", ctypes.c_float)]
 
 
+class _Quant(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("d", ctypes.c_int32), ("data", ctypes.c_void_p)]
+
+
+class _ShortlistRows(ctypes.Structure):
+    _fields_ = [("L", ctypes.c_void_p), ("token_rows", ctypes.c_void_p), ("sel_sorted", ctypes.c_void_p),
+                ("sel_rowoff", ctypes.c_void_p), ("row_len", ctypes.c_void_p), ("k", ctypes.c_int32),
+                ("shared", ctypes.c_int32)]
+
+
 _lib = None
 ABI_VERSION = 2  # DYNA_ABI_VERSION of include/dynahead.h
 
@@ -94,6 +104,15 @@ _SIGNATURES = {
     "dyna_distill": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _I, _I, _F, _P, _P, _P, _P, _L, _P, _Z, _P]),
     "dyna_distill_grad": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _I, _I, _F, _P, _P, _P, _L, _P]),
     "dyna_router_loss": (_I, [_P, _I, _I, _L, _I, _P, _I, _P, _I, _F, _P, _P, _P, _L, _P]),
+    "dyna_quant_bytes": (_Z, [_I, _I]),
+    "dyna_quantize_rows": (_I, [_P, _I, _I, _I, _L, _P, _P]),
+    "dyna_dequantize_rows": (_I, [_P, _P, _I, _L, _P]),
+    "dyna_quant_product_workspace_bytes": (_Z, [_I, _I]),
+    "dyna_quant_product": (_I, [_P, _I, _P, _I, _L, _P, _I, _P, _I, _L, _P, _Z, _P]),
+    "dyna_quant_shortlist_logits": (_I, [_P, _P, _P, _I, _I, _I, _P, _P, _P, _P, _I, _P, _Z, _P]),
+    "dyna_token_logprobs_workspace_bytes": (_Z, [_I, _I, _I, _I]),
+    "dyna_token_logprobs": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _F, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "dyna_token_logprobs_grad": (_I, [_P, _I, _I, _L, _I, _P, _P, _I, _F, _P, _P, _P, _P, _L, _P]),
     "dyna_dense_head": (_I, [_P, _I, _I, _I, _P, _I, _I, _I, _I, _F, _P, _P, _P, _P, _P, _P, _P,
                              _Z, _P]),
 }
@@ -865,3 +884,281 @@ def router_loss(scores, ids, cluster_of, pos_weight=1.0, weights=None, want_grad
     _launch(dev, lib().dyna_router_loss, _ptr(scores), code, M, stride, N, _ptr(ids), L, _ptr(cluster_of), V,
             pos_weight, _ptr(weights), _ptr(loss), _ptr(grad), gstride)
     return loss, grad
+
+
+# ---------------------------------------------------------------- four-bit rows
+_EMPTY_WS = 256  # bytes of a workspace that nothing reads
+
+
+@dataclass
+class QuantRows:
+    """Four-bit rows (quantize_rows; the tensor is kept alive here): 17 bytes to 32 columns, in the library's
+    own order."""
+    rows: int
+    d: int
+    data: object
+
+    def __post_init__(self):
+        self._c = _Quant(self.rows, self.d, _ptr(self.data))
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+    @property
+    def device(self):
+        return self.data.device
+
+
+def quant_bytes(rows: int, d: int) -> int:
+    return int(lib().dyna_quant_bytes(rows, d))
+
+
+def _on(stream, device):
+    """The context of a call on `stream`, checked against the tensors' device."""
+    import torch
+    _stream_device(stream, device)
+    return torch.cuda.stream(stream)
+
+
+def _quant(q, name, device):
+    if not isinstance(q, QuantRows):
+        raise TypeError(f"{name} must be QuantRows, not {type(q).__name__}")
+    if q.device != device:
+        raise ValueError(f"{name} is on {q.device}, not on {device}")
+
+
+def quantize_rows(x, out: Optional[QuantRows] = None, stream=None) -> QuantRows:
+    """dyna_quantize_rows: x [rows, d] (fp32 or bf16, contiguous rows) in four-bit form; out: rows of the same
+    shape to write again."""
+    import torch
+    code, stride = _matrix(x, "x")
+    if stream is not None:
+        with _on(stream, x.device):
+            return quantize_rows(x, out)
+    rows, d = x.shape
+    if out is None:
+        n = quant_bytes(rows, d)
+        out = QuantRows(rows, d, torch.empty(max(n, 1), dtype=torch.uint8, device=x.device))
+    else:
+        _quant(out, "out", x.device)
+        if (out.rows, out.d) != (rows, d):
+            raise ValueError(f"out has shape {(out.rows, out.d)}, not {(rows, d)}")
+    _launch(x.device, lib().dyna_quantize_rows, _ptr(x), code, rows, d, stride, _ptr(out.data))
+    return out
+
+
+def dequantize_rows(q: QuantRows, dtype=None, out=None, stream=None):
+    """dyna_dequantize_rows -> the values that q stands for, [rows, d] in dtype (fp32 or bf16, fp32 by default)
+    or in `out`."""
+    import torch
+    _quant(q, "q", q.device)
+    if stream is not None:
+        with _on(stream, q.device):
+            return dequantize_rows(q, dtype, out)
+    if out is None:
+        out = torch.empty((q.rows, q.d), dtype=torch.float32 if dtype is None else dtype, device=q.device)
+    elif out.shape != (q.rows, q.d) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must have shape {(q.rows, q.d)}" + (f" and be {dtype}" if dtype is not None else ""))
+    code, stride = _matrix(out, "out")
+    if out.device != q.device:
+        raise ValueError(f"out is on {out.device}, not on {q.device}")
+    _launch(q.device, lib().dyna_dequantize_rows, q.c, _ptr(out), code, stride)
+    return out
+
+
+def quant_product_workspace(B: int, d: int, device="cuda"):
+    import torch
+    n = int(lib().dyna_quant_product_workspace_bytes(B, d))
+    return torch.empty(max(n, _EMPTY_WS), dtype=torch.uint8, device=device)
+
+
+def quant_product(a, W: QuantRows, n_rows: Optional[int] = None, out=None, out_dtype=None, ws=None, stream=None):
+    """dyna_quant_product -> [B, n_rows]: contexts a ([B, d] fp32 or bf16, or QuantRows) times the first n_rows
+    four-bit rows (all of them by default); the result is fp32, out_dtype or `out`."""
+    import torch
+    _quant(W, "W", W.device)
+    dev = W.device
+    if stream is not None:
+        with _on(stream, dev):
+            return quant_product(a, W, n_rows, out, out_dtype, ws)
+    four = isinstance(a, QuantRows)
+    if four:
+        _quant(a, "a", dev)
+        B, d, code, stride = a.rows, a.d, 0, 0
+    else:
+        code, stride = _matrix(a, "a")
+        B, d = a.shape
+        if a.device != dev:
+            raise ValueError(f"a is on {a.device}, not on {dev}")
+    if d != W.d:
+        raise ValueError(f"a has {d} columns, W {W.d}")
+    n_rows = W.rows if n_rows is None else n_rows
+    if out is None:
+        out = torch.empty((B, n_rows), dtype=torch.float32 if out_dtype is None else out_dtype, device=dev)
+    elif out.shape != (B, n_rows) or (out_dtype is not None and out.dtype != out_dtype):
+        raise ValueError(f"out must have shape {(B, n_rows)}" + (f" and be {out_dtype}" if out_dtype is not None else ""))
+    ocode, ostride = _matrix(out, "out")
+    if out.device != dev:
+        raise ValueError(f"out is on {out.device}, not on {dev}")
+    if ws is None:
+        ws = quant_product_workspace(B, d, dev)
+    elif ws.device != dev:
+        raise ValueError(f"ws is on {ws.device}, not on {dev}")
+    _launch(dev, lib().dyna_quant_product, W.c, n_rows, None if four else _ptr(a), code, stride, a.c if four else None,
+            B, _ptr(out), ocode, ostride, _ptr(ws), ws.numel())
+    return out
+
+
+def quant_shortlist_logits(layout: Layout, W: QuantRows, h, sel_sorted, sel_rowoff, row_len, cap=None, ws=None,
+                           out=None, stream=None):
+    """dyna_quant_shortlist_logits -> logits [B, cap] fp32 (slots past row_len untouched): shortlist_logits over
+    four-bit rows, W = quantize_rows(layout.W_perm); ws = workspace(layout, None, B, k, cap)."""
+    import torch
+    _quant(W, "W", W.device)
+    dev = W.device
+    if stream is not None:
+        with _on(stream, dev):
+            return quant_shortlist_logits(layout, W, h, sel_sorted, sel_rowoff, row_len, cap, ws, out)
+    B, k = _dims(sel_sorted, "sel_sorted", 2)
+    _typed(sel_sorted, "sel_sorted", torch.int32, (B, k), dev)
+    _typed(sel_rowoff, "sel_rowoff", torch.int32, (B, k + 1), dev)
+    _typed(row_len, "row_len", torch.int32, (B,), dev)
+    _typed(h, "h", torch.bfloat16 if h.dtype is torch.bfloat16 else torch.float32, (B, layout.d), dev)
+    if out is None:
+        cap = layout.cap(k) if cap is None else cap
+        out = torch.full((B, cap), float("nan"), dtype=torch.float32, device=dev)
+    else:
+        cap = out.shape[1] if cap is None else cap
+        _typed(out, "out", torch.float32, (B, cap), dev)
+    if ws is None:
+        ws = workspace(layout, None, B, k, cap, dev)
+    elif ws.device != dev:
+        raise ValueError(f"ws is on {ws.device}, not on {dev}")
+    _launch(dev, lib().dyna_quant_shortlist_logits, layout.c, W.c, _ptr(h), _dtype_code(h), B, k, _ptr(sel_sorted),
+            _ptr(sel_rowoff), _ptr(row_len), _ptr(out), cap, _ptr(ws), ws.numel())
+    return out
+
+
+# ---------------------------------------------------------------- log-probabilities of given tokens
+@dataclass
+class ShortlistRows:
+    """The shortlists that rows of draft logits span, as shortlist() wrote them for each row; one row of them
+    stands for every row of logits (a step whose rows share their union: shortlist(layout, clusters.view(1, -1))).
+    token_rows: token_rows(layout), made here (and waited for) when not given."""
+    layout: Layout
+    sel_sorted: object
+    sel_rowoff: object
+    row_len: object
+    token_rows: Optional[object] = None
+
+    def __post_init__(self):
+        import torch
+        dev = self.layout.perm.device
+        N, k = _dims(self.sel_sorted, "sel_sorted", 2)
+        _typed(self.sel_sorted, "sel_sorted", torch.int32, (N, k), dev)
+        _typed(self.sel_rowoff, "sel_rowoff", torch.int32, (N, k + 1), dev)
+        _typed(self.row_len, "row_len", torch.int32, (N,), dev)
+        if self.token_rows is None:
+            self.token_rows = token_rows(self.layout)
+            if not torch.cuda.is_current_stream_capturing():
+                # calls on other streams read it too
+                torch.cuda.current_stream(dev).synchronize()
+        _typed(self.token_rows, "token_rows", torch.int32, (self.layout.V, 2), dev)
+        self.N, self.device = N, dev
+        self._c = _ShortlistRows(ctypes.addressof(self.layout._c), _ptr(self.token_rows), _ptr(self.sel_sorted),
+                                 _ptr(self.sel_rowoff), _ptr(self.row_len), k, int(N == 1))
+
+
+def _shortlist_arg(rows, N, device):
+    """The C argument for rows of logits (None without shortlists)."""
+    if rows is None:
+        return None
+    if rows.device != device:
+        raise ValueError(f"rows are on {rows.device}, the logits on {device}")
+    if rows.N not in (1, N):
+        raise ValueError(f"rows holds {rows.N} shortlists for {N} rows of logits")
+    return ctypes.byref(rows._c)
+
+
+@dataclass
+class TokenLogprobs:
+    """logprobs [N, T], entropy [N]; top_ids and top_logprobs [N, top] or None; stats [N, 3] for
+    token_logprobs_grad or None."""
+    logprobs: object
+    entropy: object
+    top_ids: Optional[object] = None
+    top_logprobs: Optional[object] = None
+    stats: Optional[object] = None
+
+
+def token_logprobs_workspace(N: int, V: int, T: int = 1, top: int = 0, device="cuda"):
+    import torch
+    n = int(lib().dyna_token_logprobs_workspace_bytes(N, V, T, top))
+    return torch.empty(max(n, _EMPTY_WS), dtype=torch.uint8, device=device)
+
+
+def token_logprobs(logits, tokens, temperature=1.0, top=0, rows: Optional[ShortlistRows] = None, want_stats=False,
+                   ws=None, stream=None) -> TokenLogprobs:
+    """dyna_token_logprobs: log-probabilities of tokens [N, T] (or [N]) in softmax(logits / temperature), the rows'
+    entropy and their `top` best tokens.  rows: the shortlists that the logits span (tokens are vocabulary ids all
+    the same); want_stats: keep what token_logprobs_grad needs."""
+    import torch
+    code, stride = _matrix(logits, "logits")
+    dev = logits.device
+    if stream is not None:
+        with _on(stream, dev):
+            return token_logprobs(logits, tokens, temperature, top, rows, want_stats, ws)
+    N, V = logits.shape
+    shape = _token_shape(tokens, N, dev)
+    T = shape[1] if len(shape) == 2 else 1
+    out = TokenLogprobs(torch.empty(shape, dtype=torch.float32, device=dev),
+                        torch.empty(N, dtype=torch.float32, device=dev))
+    if top > 0:
+        out.top_ids = torch.empty((N, top), dtype=torch.int32, device=dev)
+        out.top_logprobs = torch.empty((N, top), dtype=torch.float32, device=dev)
+    if want_stats:
+        out.stats = torch.empty((N, 3), dtype=torch.float64, device=dev)
+    if ws is None:
+        ws = token_logprobs_workspace(N, V, T, top, dev)
+    elif ws.device != dev:
+        raise ValueError(f"ws is on {ws.device}, not on {dev}")
+    _launch(dev, lib().dyna_token_logprobs, _ptr(logits), code, V, stride, N, _shortlist_arg(rows, N, dev), _ptr(tokens),
+            T, temperature, top, _ptr(out.logprobs), _ptr(out.entropy), _ptr(out.top_ids), _ptr(out.top_logprobs),
+            _ptr(out.stats), _ptr(ws), ws.numel())
+    return out
+
+
+def _token_shape(tokens, N, device):
+    import torch
+    if tokens.dim() not in (1, 2):
+        raise ValueError("tokens must have one or two dimensions")
+    shape = (N,) if tokens.dim() == 1 else (N, tokens.shape[1])
+    _typed(tokens, "tokens", torch.int32, shape, device)
+    return shape
+
+
+def token_logprobs_grad(logits, stats, tokens, grad_logprobs, grad_entropy=None, temperature=1.0,
+                        rows: Optional[ShortlistRows] = None, out=None, stream=None):
+    """dyna_token_logprobs_grad -> the gradient [N, V] of sum(grad_logprobs * logprobs) + sum(grad_entropy * entropy)
+    with respect to the logits, from the stats of a token_logprobs call: the training loop passes it on with
+    ``logits.backward(grad)``.  out: an existing gradient to write."""
+    import torch
+    code, stride = _matrix(logits, "logits")
+    dev = logits.device
+    if stream is not None:
+        with _on(stream, dev):
+            return token_logprobs_grad(logits, stats, tokens, grad_logprobs, grad_entropy, temperature, rows, out)
+    N, V = logits.shape
+    shape = _token_shape(tokens, N, dev)
+    T = shape[1] if len(shape) == 2 else 1
+    _typed(stats, "stats", torch.float64, (N, 3), dev)
+    _typed(grad_logprobs, "grad_logprobs", torch.float32, shape, dev)
+    if grad_entropy is not None:
+        _typed(grad_entropy, "grad_entropy", torch.float32, (N,), dev)
+    if out is None and rows is not None:
+        out = torch.zeros(logits.shape, dtype=logits.dtype, device=dev)  # nothing is written behind a shortlist
+    grad, gstride = _gradient(out, logits)
+    _launch(dev, lib().dyna_token_logprobs_grad, _ptr(logits), code, V, stride, N, _shortlist_arg(rows, N, dev),
+            _ptr(tokens), T, temperature, _ptr(stats), _ptr(grad_logprobs), _ptr(grad_entropy), _ptr(grad), gstride)
+    return grad

@@ -1,0 +1,239 @@
+"""Four-bit rows and token log-probabilities without a GPU: the oracle's pins, sizes and refusals."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import quant_oracle as O
+from paper_2510_13847_amd import dynahead as D
+
+P = 0x100000  # a 256-byte aligned address that no refused call reads
+
+
+# ---------------------------------------------------------------- oracle
+def test_every_value_of_a_scale_stands_for_itself():
+    block = [s * v for v in O.VALUES for s in (1.0, -1.0)]
+    assert O.block_scale(block) == 1.0
+    np.testing.assert_array_equal(O.quantized_rows([block]), [block])
+    np.testing.assert_array_equal(O.quantized_rows([[v * 2.0 ** 20 for v in block]]), [[v * 2.0 ** 20 for v in block]])
+
+
+@pytest.mark.parametrize("x,want", [(0.25, 0.0), (0.75, 1.0), (1.25, 1.0), (1.75, 2.0), (2.5, 2.0), (3.5, 4.0), (5.0, 4.0),
+                                    (0.26, 0.5), (0.74, 0.5), (5.01, 6.0), (7.9, 6.0)])
+def test_rounding_by_hand(x, want):
+    # the scale is 1 with a magnitude of [4, 8) in the block
+    assert O.quantized_rows([[x, 4.0]])[0, 0] == want
+    assert O.quantized_rows([[-x, 4.0]])[0, 0] == -want
+
+
+def test_scale_by_hand():
+    assert O.block_scale([4.0]) == 1.0 and O.block_scale([7.99]) == 1.0 and O.block_scale([8.0]) == 2.0
+    assert O.block_scale([3.99]) == 0.5 and O.block_scale([2.0 ** -126]) == 2.0 ** -127
+    assert np.isnan(O.quantized_rows([[1.0, np.inf] + [1.0] * 40])[0, :32]).all()
+    assert not np.isnan(O.quantized_rows([[1.0, np.inf] + [1.0] * 40])[0, 32:]).any()
+
+
+def test_error_is_at_most_a_quarter_of_a_block():
+    """The widest gap below a block's power of two 2^e is half of 2^(e - 2) * 2; what is cut off at 6 / 4 of 2^e at
+    most a quarter of the value."""
+    x = np.random.default_rng(1).standard_normal((8, 256))
+    y = O.quantized_rows(x)
+    for r in range(8):
+        for k in range(0, 256, 32):
+            power = 4.0 * O.block_scale(x[r, k:k + 32])
+            assert (np.abs(x - y)[r, k:k + 32] <= np.maximum(power / 4, np.abs(x[r, k:k + 32]) / 4)).all()
+
+
+def test_logprobs_against_torch():
+    z = np.random.default_rng(2).standard_normal(50) * 3
+    want = torch.log_softmax(torch.tensor(z) / 0.7, 0)
+    given, entropy, best, logp = O.token_logprobs(z, range(50), [3, 49, 50, -1], 0.7, 3)
+    np.testing.assert_allclose(logp, want.numpy(), atol=1e-13)
+    assert given[0] == logp[3] and given[1] == logp[49] and (given[2:] == -np.inf).all()
+    assert abs(entropy - float(torch.distributions.Categorical(logits=torch.tensor(z) / 0.7).entropy())) < 1e-12
+    assert [b[0] for b in best] == torch.topk(torch.tensor(z), 3).indices.tolist()
+
+
+def test_rows_without_tokens_and_ties():
+    assert O.token_logprobs([-np.inf, -np.inf], [4, 7], [4], 1.0, 1)[:3] == (np.array([-np.inf]), 0.0, [(-1, -np.inf)])
+    assert [b[0] for b in O.token_logprobs([1.0, 1.0, 0.0], [9, 2, 5], [], 1.0, 2)[2]] == [2, 9]
+    given, entropy, best, _ = O.token_logprobs([0.0, np.nan], [0, 1], [0], 1.0, 2)
+    assert np.isnan(given[0]) and np.isnan(entropy) and best[0][0] == 0 and best[1] == (-1, -np.inf)
+
+
+def test_gradient_against_differences_and_autograd():
+    rng = np.random.default_rng(3)
+    z = rng.standard_normal(12)
+    tokens, g, e, T = [3, 3, 7, 40], [0.5, -0.25, 1.5, 9.0], -0.75, 0.6
+    grad = O.token_logprobs_grad(z, range(12), tokens, g, e, T)
+
+    def objective(z):
+        given, entropy, _, _ = O.token_logprobs(z, range(12), tokens, T)
+        return sum(a * b for a, b in zip(g[:3], given[:3])) + e * entropy
+
+    for i in range(12):
+        h = np.zeros(12)
+        h[i] = 1e-5
+        # central differences: h^2 / 6 of a third derivative below 100, and 2^-52 * 10 / h of rounding
+        assert abs((objective(z + h) - objective(z - h)) / 2e-5 - grad[i]) < 2e-9 + 5e-10
+    x = torch.tensor(z, requires_grad=True)
+    logp = torch.log_softmax(x / T, 0)
+    (0.5 * logp[3] - 0.25 * logp[3] + 1.5 * logp[7] + 0.75 * (logp.exp() * logp).sum()).backward()
+    np.testing.assert_allclose(grad, x.grad.numpy(), atol=1e-14)
+
+
+def test_a_planted_mistake_shows():
+    """Entropy's gradient without H is another gradient."""
+    z = np.array([0.3, -1.0, 2.0])
+    right = O.token_logprobs_grad(z, range(3), [], [], 1.0)
+    _, H, _, logp = O.token_logprobs(z, range(3), [])
+    wrong = -np.exp(logp) * logp
+    assert np.abs(right.sum()) < 1e-15 and np.abs(wrong.sum()) > 0.1 and np.abs(right - wrong).max() > 0.1
+
+
+# ---------------------------------------------------------------- sizes
+def test_quant_bytes():
+    assert D.quant_bytes(16, 512) == 16 * 512 // 2 + 256
+    assert D.quant_bytes(1, 1) == 1024 + 256
+    assert D.quant_bytes(17, 640) == 2 * (5 * 1024 + 2 * 256)
+    assert D.quant_bytes(128256, 4096) == 128256 * 4096 * 17 // 32
+    for rows, d in ((0, 8), (8, 0), (1 << 25, 8), (8, 8193)):
+        assert D.quant_bytes(rows, d) == 0
+    assert D.lib().dyna_quant_product_workspace_bytes(0, 8) == 0
+    assert D.lib().dyna_token_logprobs_workspace_bytes(4, 100, 65, 0) == 0
+    assert D.lib().dyna_token_logprobs_workspace_bytes(4, 100, 1, 65) == 0
+    assert D.lib().dyna_token_logprobs_workspace_bytes(4, (1 << 20) + 1, 1, 1) == 0
+
+
+# ---------------------------------------------------------------- refusals
+def _quant(rows=64, d=128, data=P):
+    return ctypes.byref(D._Quant(rows, d, data))
+
+
+def test_quantize_refuses():
+    f, g = D.lib().dyna_quantize_rows, D.lib().dyna_dequantize_rows
+    far = P + (1 << 30)
+    ok = dict(x=far, dtype=D.BF16, rows=64, d=128, stride=128, data=P)
+    for change, status in ((dict(x=None), D.ERR_INVALID_ARG), (dict(x=far + 1), D.ERR_INVALID_ARG),
+                           (dict(dtype=2), D.ERR_INVALID_ARG), (dict(rows=0), D.ERR_INVALID_ARG),
+                           (dict(d=0), D.ERR_INVALID_ARG), (dict(d=8193, stride=8193), D.ERR_UNSUPPORTED),
+                           (dict(rows=(1 << 24) + 1), D.ERR_UNSUPPORTED), (dict(stride=127), D.ERR_INVALID_ARG),
+                           (dict(stride=1 << 41), D.ERR_INVALID_ARG), (dict(data=None), D.ERR_INVALID_ARG),
+                           (dict(data=P + 16), D.ERR_INVALID_ARG), (dict(x=P + 64), D.ERR_INVALID_ARG)):
+        a = dict(ok, **change)
+        assert f(a["x"], a["dtype"], a["rows"], a["d"], a["stride"], a["data"], None) == status, change
+    assert g(None, far, D.F32, 128, None) == D.ERR_INVALID_ARG
+    assert g(_quant(), None, D.F32, 128, None) == D.ERR_INVALID_ARG
+    assert g(_quant(), far, 5, 128, None) == D.ERR_INVALID_ARG
+    assert g(_quant(), far, D.F32, 100, None) == D.ERR_INVALID_ARG
+    assert g(_quant(), P + 4, D.F32, 128, None) == D.ERR_INVALID_ARG
+    assert g(_quant(data=P + 8), far, D.F32, 128, None) == D.ERR_INVALID_ARG
+
+
+def test_product_refuses():
+    f = D.lib().dyna_quant_product
+    far, out = P + (1 << 30), P + (1 << 31)
+    ok = dict(W=_quant(), n=64, a=far, adtype=D.BF16, stride=128, a4=None, B=4, out=out, odtype=D.F32, ostride=64,
+              ws=P + (1 << 32), bytes=1 << 30)
+
+    def call(**change):
+        a = dict(ok, **change)
+        return f(a["W"], a["n"], a["a"], a["adtype"], a["stride"], a["a4"], a["B"], a["out"], a["odtype"], a["ostride"],
+                 a["ws"], a["bytes"], None)
+
+    assert call(B=0) == D.OK
+    for change in (dict(W=None), dict(n=0), dict(n=65), dict(a=None), dict(a4=_quant(4)), dict(adtype=3), dict(odtype=3),
+                   dict(stride=127), dict(a=far + 1), dict(out=None), dict(ostride=63), dict(out=P), dict(out=far),
+                   dict(B=-1), dict(ws=None), dict(ws=P + 3), dict(a=None, a4=_quant(5)), dict(a=None, a4=_quant(4, 256)),
+                   dict(a=None, a4=_quant(4, 128, out))):
+        assert call(**change) == D.ERR_INVALID_ARG, change
+    assert call(bytes=0) == D.ERR_WORKSPACE
+    assert call(B=(1 << 24) + 1) == D.ERR_UNSUPPORTED
+
+
+def _layout(V=1000, d=64, M=10):
+    cap = (ctypes.c_int32 * (M + 1))(*[100 * i for i in range(M + 1)])
+    L = D._Layout(V, d, M, D.BF16, 0x1000, 0x2000, 0x3000, ctypes.addressof(cap), 100)
+    return L, cap
+
+
+def test_shortlist_logits_refuses():
+    f = D.lib().dyna_quant_shortlist_logits
+    L, keep = _layout()
+    ok = dict(L=ctypes.byref(L), W=_quant(1000, 64), h=P, dtype=D.BF16, B=2, k=3, s=P, cap=300, ws=P, bytes=1 << 30)
+
+    def call(**change):
+        a = dict(ok, **change)
+        return f(a["L"], a["W"], a["h"], a["dtype"], a["B"], a["k"], a["s"], a["s"], a["s"], a["s"], a["cap"], a["ws"],
+                 a["bytes"], None)
+
+    assert call(B=0) == D.OK
+    for change in (dict(L=None), dict(W=None), dict(W=_quant(999, 64)), dict(W=_quant(1000, 128)), dict(h=None),
+                   dict(h=P + 2), dict(dtype=2), dict(B=-1), dict(k=0), dict(k=11), dict(s=None), dict(ws=None)):
+        assert call(**change) == D.ERR_INVALID_ARG, change
+    assert call(cap=299) == D.ERR_CAPACITY
+    assert call(bytes=16) == D.ERR_WORKSPACE
+
+
+def _rows(layout, **change):
+    a = dict(dict(L=ctypes.addressof(layout), token_rows=P, s=P, off=P, len=P, k=3, shared=0), **change)
+    return ctypes.byref(D._ShortlistRows(a["L"], a["token_rows"], a["s"], a["off"], a["len"], a["k"], a["shared"]))
+
+
+def test_logprobs_refuse():
+    f = D.lib().dyna_token_logprobs
+    L, keep = _layout()
+    ok = dict(z=P, dtype=D.F32, V=100, stride=100, N=4, rows=None, tokens=P, T=1, t=1.0, top=2, lp=P, ids=P, tlp=P, ws=P,
+              bytes=1 << 30)
+
+    def call(**change):
+        a = dict(ok, **change)
+        return f(a["z"], a["dtype"], a["V"], a["stride"], a["N"], a["rows"], a["tokens"], a["T"], a["t"], a["top"],
+                 a["lp"], P, a["ids"], a["tlp"], P, a["ws"], a["bytes"], None)
+
+    assert call(N=0) == D.OK
+    for change in (dict(z=None), dict(z=P + 2), dict(dtype=2), dict(V=0), dict(stride=99), dict(N=-1), dict(tokens=None),
+                   dict(T=-1), dict(t=0.0), dict(t=-1.0), dict(t=math.inf), dict(t=math.nan), dict(t=1e-39),
+                   dict(top=-1), dict(lp=None), dict(ids=None), dict(tlp=None), dict(ws=None), dict(ws=P + 8),
+                   dict(rows=_rows(L, L=None)), dict(rows=_rows(L, token_rows=P + 4)), dict(rows=_rows(L, s=None)),
+                   dict(rows=_rows(L, off=None)), dict(rows=_rows(L, len=None)), dict(rows=_rows(L, k=0)),
+                   dict(rows=_rows(L, shared=2))):
+        assert call(**change) == D.ERR_INVALID_ARG, change
+    for change in (dict(V=(1 << 20) + 1, stride=1 << 21), dict(T=65), dict(top=65), dict(N=(1 << 23) + 1)):
+        assert call(**change) == D.ERR_UNSUPPORTED, change
+    assert call(bytes=0) == D.ERR_WORKSPACE
+
+
+def test_logprobs_grad_refuses():
+    f = D.lib().dyna_token_logprobs_grad
+    far = P + (1 << 30)
+    ok = dict(z=P, dtype=D.F32, V=100, stride=100, N=4, tokens=P, T=1, t=1.0, stats=P, g=P, grad=far, gstride=100)
+
+    def call(**change):
+        a = dict(ok, **change)
+        return f(a["z"], a["dtype"], a["V"], a["stride"], a["N"], None, a["tokens"], a["T"], a["t"], a["stats"], a["g"],
+                 None, a["grad"], a["gstride"], None)
+
+    assert call(N=0) == D.OK
+    for change in (dict(z=None), dict(dtype=9), dict(stats=None), dict(g=None), dict(grad=None), dict(grad=far + 2),
+                   dict(gstride=99), dict(grad=P), dict(grad=P + 400), dict(grad=P + 100, gstride=200), dict(t=0.0)):
+        assert call(**change) == D.ERR_INVALID_ARG, change
+    assert call(T=65) == D.ERR_UNSUPPORTED
+
+
+def test_binding_refuses_host_tensors_and_shapes():
+    x = torch.zeros(4, 64)
+    with pytest.raises(ValueError):
+        D.quantize_rows(x)
+    with pytest.raises(TypeError):
+        D.dequantize_rows(x)
+    with pytest.raises(TypeError):
+        D.quant_product(x, x)
+    with pytest.raises(ValueError):
+        D.token_logprobs(x, torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        D.token_logprobs_grad(x, None, None, None)
