@@ -5,6 +5,13 @@
 
 namespace dyna {
 
+// Sums of a part of a row relative to its largest logit m: w = exp((z - m) / T),
+// and w times (z - m) / T in powers of two.
+struct ScorePart {
+    double s, u;
+    float m, pad;
+};
+
 struct ScoreArgs {
     const void* logits;
     int32_t dtype;
@@ -38,8 +45,12 @@ struct ScoreArgs {
     int64_t grad_stride;
     // workspace
     void* ws;
+    int32_t splits, split_len;
+    ScorePart* parts;        // [N, splits]
+    uint64_t* lists;         // [N, splits, top] selection keys, 0 behind them
 };
 
+int32_t grad_parts(int32_t V);  // work items of a row's gradient
 size_t token_logprobs_ws_bytes(int32_t N, int32_t V, int32_t T, int32_t top);
 dyna_status launch_token_logprobs(const ScoreArgs& a, hipStream_t stream);
 dyna_status launch_token_logprobs_grad(const ScoreArgs& a, hipStream_t stream);

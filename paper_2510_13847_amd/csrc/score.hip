@@ -4,6 +4,8 @@
 //   s = sum exp((z - m) / T)           u = sum exp((z - m) / T) (z - m) / T
 //   log p_v = (z_v - m) / T - log s    H = log s - u / s
 //   dz_v = 1 / T (sum_t g_t ([v = t] - p_v) - e p_v (log p_v + H))
+#include <algorithm>
+
 #include "rowstat.h"
 #include "score.h"
 
@@ -11,7 +13,15 @@ namespace dyna {
 namespace {
 
 constexpr int kST = 256;  // threads
-constexpr double kNan = __builtin_nan("");
+constexpr int kFlight = 4;                  // vectors of 8 a thread has in flight
+constexpr int kVecStep = kST * 8;
+constexpr int kSweep = kFlight * kVecStep;  // columns that a workgroup goes through between two looks at its list
+// The list of candidates: at most kSoft stay in it, and a sweep adds at most what
+// 63 groups of a thread's columns hold and 64 equal ones (see add_sweep).
+constexpr int kSoft = 512;
+constexpr int kCap = kSoft + (DYNA_MAX_KT - 1) * 8 * kFlight + DYNA_MAX_KT;
+constexpr int kMaxParts = 64;
+constexpr int kGradLen = 32768;             // columns of a gradient's work item
 
 // ---------------------------------------------------------------- rows
 struct RowSlots {
@@ -52,112 +62,498 @@ __device__ __forceinline__ int token_of_slot(const ScoreArgs& a, const RowSlots&
     return a.perm[a.offsets[row.sel[lo]] + (slot - row.off[lo])];
 }
 
-template <typename T>
-__global__ __launch_bounds__(kST) void score_kernel(ScoreArgs a) {
-    __shared__ float tmp_f[kST / kWave];
-    __shared__ double tmp_d[kST / kWave];
-    __shared__ uint64_t tmp_k[kST / kWave];
-    const int r = blockIdx.x, t = threadIdx.x;
-    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
-    const RowSlots w = slots_of(a, r);
+// ---------------------------------------------------------------- sums
+// A thread's share of a row: largest logit m, sum of w = exp2((z - m) c), c =
+// log2(e) / T, and of w (z - m) c.  Weights are 32 bits; sums of eight go on in 64.
+struct RowSum {
     float m = kNegInf;
-    for (int v = t; v < w.len; v += kST) m = fmaxf(m, to_f32(row[v]));
-    m = block_max_f32<kST>(m, tmp_f);
-    const float ref = m > kNegInf ? m : 0.0f;
-    const float c = (float)(a.inv_t * 1.4426950408889634);
     double s = 0.0, u = 0.0;
-    for (int v = t; v < w.len; v += kST) {
-        const float y = (to_f32(row[v]) - ref) * c, e = __builtin_amdgcn_exp2f(y);
-        s += (double)e;
-        u += (double)(e * fmaxf(y, -1000.0f));
+    __device__ __forceinline__ void rescale(float top, float c) {
+        if (top > m) {
+            const float y = (m - top) * c;
+            if (m > kNegInf) {
+                const double f = (double)__builtin_amdgcn_exp2f(y);
+                u = f * (u + s * (double)fmaxf(y, -1000.0f));
+                s *= f;
+            }
+            m = top;
+        }
     }
-    s = block_sum_f64<kST>(s, tmp_d);
-    u = block_sum_f64<kST>(u, tmp_d) * 0.69314718055994530942;
-    const bool none = s == 0.0;  // no token is allowed
-    const double log_s = none ? 0.0 : log(s), entropy = none ? 0.0 : log_s - u / s;
-    auto logprob = [&](float z) { return none ? -__builtin_inf() : ((double)z - (double)ref) * a.inv_t - log_s; };
-    if (t == 0) {
+    // A NaN or +inf logit makes s NaN and with it the row.
+    __device__ __forceinline__ void add(const float (&z)[8], float top, float c) {
+        rescale(top, c);
+        const float ref = m > kNegInf ? m : 0.0f;
+        float e[8], x = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float y = (z[k] - ref) * c;
+            e[k] = __builtin_amdgcn_exp2f(y);
+            x = fmaf(e[k], fmaxf(y, -1000.0f), x);  // 0 for a masked logit, not 0 times infinity
+        }
+        s += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
+        u += (double)x;
+    }
+};
+
+// Sums of a part seen from another largest logit.
+__device__ __forceinline__ void seen_from(float m, double c, double& s, double& u, float from) {
+    if (from > kNegInf && from < m) {
+        const double y = ((double)from - (double)m) * c, f = exp2(y);
+        u = f == 0.0 ? 0.0 : f * (u + s * y);
+        s *= f;
+    }
+}
+
+// ---------------------------------------------------------------- best tokens
+struct TopLds {
+    uint64_t keys[kCap];
+    uint32_t groups[kST];
+    int counts[2][kST / kWave];
+    int n;
+    float floor;
+};
+
+// A value that at least k of the workgroup's threads' values `mine` reach: the
+// k-th largest of them, or with BITS < 32 one that is not above it.  -inf where
+// fewer than k threads have one.  The first wave finds it bit by bit.
+template <int BITS>
+__device__ __forceinline__ float kth_of_threads(TopLds& w, float mine, int k) {
+    w.groups[threadIdx.x] = ord_f32(mine);
+    lds_barrier();
+    if (threadIdx.x < kWave) {
+        uint32_t x[kST / kWave];
+#pragma unroll
+        for (int i = 0; i < kST / kWave; ++i) x[i] = w.groups[i * kWave + threadIdx.x];
+        uint32_t found = 0;
+        for (int b = 31; b >= 32 - BITS; --b) {
+            const uint32_t want = found | (1u << b);
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < kST / kWave; ++i) n += __popcll(__ballot(x[i] >= want));
+            if (n >= k) found = want;
+        }
+        if (threadIdx.x == 0) w.floor = found > ord_f32(kNegInf) ? ord_to_f32(found) : kNegInf;
+    }
+    lds_barrier();
+    return w.floor;
+}
+
+// Number of keys that hold, over the workgroup.
+__device__ __forceinline__ int block_count(TopLds& w, int mine, int turn) {
+    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
+    if (lane_id() == 0) w.counts[turn & 1][threadIdx.x / kWave] = mine;
+    lds_barrier();
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kST / kWave; ++i) n += w.counts[turn & 1][i];
+    return n;
+}
+
+// The k-th largest of n > k keys, E to a thread (0: none); keys differ.
+template <int E>
+__device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], int k) {
+    uint64_t found = 0;
+    for (int b = 63; b >= 0; --b) {
+        const uint64_t want = found | (1ull << b);
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) mine += x[i] >= want;
+        if (block_count(w, mine, b) >= k) found = want;
+    }
+    return found;
+}
+
+// Leaves the k largest of the keys in the list (in any order): all of its n <= k,
+// or those not below the k-th, which becomes the floor.
+template <int E>
+__device__ __forceinline__ void keep_best(TopLds& w, const uint64_t (&x)[E], int k) {
+    const uint64_t last = kth_key<E>(w, x, k);
+    if (threadIdx.x == 0) {
+        w.n = 0;
+        w.floor = key_val(last);
+    }
+    lds_barrier();  // everyone has its keys in registers
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (x[i] >= last) w.keys[atomicAdd(&w.n, 1)] = x[i];
+    lds_barrier();
+}
+__device__ __forceinline__ void shorten_list(TopLds& w, int n, int k) {
+    constexpr int E = (kCap + kST - 1) / kST;
+    uint64_t x[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int at = i * kST + (int)threadIdx.x;
+        x[i] = at < n ? w.keys[at] : 0;
+    }
+    keep_best<E>(w, x, k);
+}
+
+// Key of rank `threadIdx.x` ... of the list's n <= kST keys: the thread's own key
+// and how many are larger (n where the thread has none).
+__device__ __forceinline__ int rank_in_list(const TopLds& w, int n, uint64_t* key) {
+    *key = (int)threadIdx.x < n ? w.keys[threadIdx.x] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; ++i) rank += w.keys[i] > *key;
+    return (int)threadIdx.x < n ? rank : INT32_MAX;
+}
+
+// Adds a sweep's candidates to the list: the logits that reach `floor`, which at
+// least k of those before do (or of this sweep, the row's first).  Most sweeps
+// behind the first add a few and some none.  Where they are too many (rising or
+// equal logits), the sweep starts again behind a floor of its own: at most k - 1
+// threads have a logit above the k-th largest of the threads' maxima, and of those
+// equal to it the k lowest tokens are enough.
+template <int F>
+__device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& row, TopLds& w, const float (&z)[F][8],
+                                          int at, float most, bool first, int k) {
+    float floor = first ? kth_of_threads<16>(w, most, k) : w.floor;
+    const int before = w.n;
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f(z[i][e], at + i * kVecStep + e);
+    };
+    auto push = [&](float x, int slot) {
+        const int p = atomicAdd(&w.n, 1);
+        if (p < kCap) w.keys[p] = sel_key(x, (uint32_t)token_of_slot(a, row, slot));
+    };
+    lds_barrier();  // `before` and the floor have been read
+    if (most >= floor && most > kNegInf)
+        each([&](float x, int slot) {
+            if (x >= floor && x > kNegInf) push(x, slot);
+        });
+    lds_barrier();
+    int n = w.n;
+    if (n > kCap) {
+        lds_barrier();
+        if (threadIdx.x == 0) w.n = before;
+        floor = fmaxf(floor, kth_of_threads<32>(w, most, k));  // with barriers
+        if (most > floor)
+            each([&](float x, int slot) {
+                if (x > floor) push(x, slot);
+            });
+        // the tokens of equal logits up to `last`, k of them or all
+        int equal = 0;
+        each([&](float x, int) { equal += x == floor; });
+        int last = INT32_MAX;
+        if (block_count(w, equal, 0) > k) {
+            last = 0;
+            for (int b = 20; b >= 0; --b) {  // the largest number with fewer than k tokens below it
+                int below = 0;
+                if (equal)
+                    each([&](float x, int slot) { below += x == floor && token_of_slot(a, row, slot) < (last | (1 << b)); });
+                if (block_count(w, below, b + 1) < k) last |= 1 << b;
+            }
+        }
+        if (equal)
+            each([&](float x, int slot) {
+                if (x == floor && token_of_slot(a, row, slot) <= last) push(x, slot);
+            });
+        lds_barrier();
+        n = w.n;
+    }
+    if (n > kSoft) shorten_list(w, n, k);
+    else if (threadIdx.x == 0) w.floor = floor;
+    lds_barrier();
+}
+
+// ---------------------------------------------------------------- results
+struct RowResult {
+    float m;
+    double log_s, entropy;
+    bool none;  // no token is allowed
+    __device__ __forceinline__ RowResult(float m_, double s, double u) : m(m_), none(s == 0.0) {
+        log_s = none ? 0.0 : log(s);
+        entropy = none ? 0.0 : log_s - 0.69314718055994530942 * (u / s);
+    }
+    __device__ __forceinline__ float logprob(float z, double inv_t) const {
+        return none ? kNegInf : (float)(((double)z - (double)m) * inv_t - log_s);
+    }
+    __device__ __forceinline__ void write(const ScoreArgs& a, int r) const {
         if (a.out_entropy) a.out_entropy[r] = (float)entropy;
         if (a.out_stats) {
-            a.out_stats[3 * (int64_t)r] = none ? -__builtin_inf() : (double)m;
+            // a row that is NaN is so in all three
+            a.out_stats[3 * (int64_t)r] = none ? -__builtin_inf() : log_s == log_s ? (double)m : log_s;
             a.out_stats[3 * (int64_t)r + 1] = log_s;
             a.out_stats[3 * (int64_t)r + 2] = entropy;
         }
     }
-    for (int i = t; i < a.T; i += kST) {
-        const int slot = slot_of_token(a, w, a.tokens[(int64_t)r * a.T + i]);
-        a.out_logprobs[(int64_t)r * a.T + i] = slot < 0 ? kNegInf : (float)logprob(to_f32(row[slot]));
+};
+
+// The list's n keys, ranked, as the row's best tokens.
+__device__ __forceinline__ void write_best(const ScoreArgs& a, int r, TopLds& w, int n, const RowResult& q) {
+    uint64_t key;
+    const int rank = rank_in_list(w, n, &key);
+    const int64_t base = (int64_t)r * a.top;
+    if (rank < a.top) {
+        a.out_top_ids[base + rank] = (int)key_id(key);
+        a.out_top_logprobs[base + rank] = q.logprob(key_val(key), a.inv_t);
     }
-    uint64_t before = ~0ull;
-    for (int i = 0; i < a.top; ++i) {
-        uint64_t best = 0;
-        for (int v = t; v < w.len; v += kST) {
-            const float z = to_f32(row[v]);
-            if (!(z > kNegInf)) continue;
-            const uint64_t key = sel_key(z, (uint32_t)token_of_slot(a, w, v));
-            if (key < before && key > best) best = key;
-        }
-        best = wave_max_u64(best);
-        __syncthreads();
-        if (lane_id() == 0) tmp_k[t / kWave] = best;
-        __syncthreads();
-        best = tmp_k[0];
-        for (int q = 1; q < kST / kWave; ++q) best = max(best, tmp_k[q]);
-        if (t == 0) {
-            a.out_top_ids[(int64_t)r * a.top + i] = best ? (int)key_id(best) : -1;
-            a.out_top_logprobs[(int64_t)r * a.top + i] = best ? (float)logprob(key_val(best)) : kNegInf;
-        }
-        before = best;
+    if ((int)threadIdx.x >= n && (int)threadIdx.x < a.top) {
+        a.out_top_ids[base + threadIdx.x] = -1;
+        a.out_top_logprobs[base + threadIdx.x] = kNegInf;
     }
 }
 
+// The logit of given token threadIdx.x, and whether it is in the row.
 template <typename T>
-__global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
-    __shared__ int slots[DYNA_MAX_KT];
+__device__ __forceinline__ float given_logit(const ScoreArgs& a, int r, const T* row, const RowSlots& w, bool* there) {
+    *there = false;
+    if ((int)threadIdx.x >= a.T) return 0.0f;
+    const int slot = slot_of_token(a, w, a.tokens[(int64_t)r * a.T + threadIdx.x]);
+    if (slot < 0) return 0.0f;
+    *there = true;
+    return to_f32(row[slot]);
+}
+
+// ---------------------------------------------------------------- kernels
+// One pass over a row, or over a part of it where there are few rows.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
+    __shared__ float tmp_f[kST / kWave];
+    __shared__ double tmp_d[2][kST / kWave];
+    __shared__ typename std::conditional<TOP, TopLds, int>::type best;
+    const int r = blockIdx.x / a.splits, part = blockIdx.x % a.splits, t = threadIdx.x;
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    const RowSlots w = slots_of(a, r);
+    const int v0 = part * a.split_len, v1 = min(w.len, v0 + a.split_len);
+    const bool whole = a.splits == 1;
+    bool there = false;
+    const float given = whole ? given_logit(a, r, row, w, &there) : 0.0f;
+    const float c = (float)(a.inv_t * 1.4426950408889634);
+    if constexpr (TOP) {
+        if (t == 0) {
+            best.n = 0;
+            best.floor = kNegInf;
+        }
+        lds_barrier();
+    }
+    Row8<T> in[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+        const int at = v0 + i * kVecStep + t * 8;
+        if (at + 8 <= v1) in[i].load(row + at);
+    }
+    RowSum sum;
+    for (int base = v0; base < v1; base += kSweep) {
+        float z[kFlight][8], most = kNegInf;
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int at = base + i * kVecStep + t * 8, next = at + kSweep;
+            if (at + 8 <= v1) in[i].get(z[i]);
+            else load_part(row + at, v1 - at, kNegInf, z[i]);
+            if (next + 8 <= v1) in[i].load(row + next);
+            const float top = max8(z[i]);
+            sum.add(z[i], top, c);
+            most = fmaxf(most, top);
+        }
+        if constexpr (TOP) add_sweep<kFlight>(a, w, best, z, base + t * 8, most, base == v0, a.top);
+    }
+    const float m = block_max_f32<kST>(sum.m, tmp_f);
+    double s = sum.s, u = sum.u;
+    seen_from(m, (double)c, s, u, sum.m);
+    s = block_sum_f64<kST>(s, tmp_d[0]);
+    u = block_sum_f64<kST>(u, tmp_d[1]);
+    int n = 0;
+    if constexpr (TOP) {
+        n = best.n;
+        if (n > kST) {
+            shorten_list(best, n, a.top);
+            n = a.top;
+        }
+    }
+    if (whole) {
+        const RowResult q(m, s, u);
+        if (t == 0) q.write(a, r);
+        if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
+        if constexpr (TOP) write_best(a, r, best, n, q);
+        return;
+    }
+    const int64_t at = (int64_t)r * a.splits + part;
+    if (t == 0) a.parts[at] = ScorePart{s, u, m, 0.0f};
+    if constexpr (TOP) {
+        uint64_t key;
+        const int rank = rank_in_list(best, n, &key);
+        if (rank < a.top) a.lists[at * a.top + rank] = key;
+        if (t >= n && t < a.top) a.lists[at * a.top + t] = 0;
+    }
+}
+
+// Joins the parts of a row.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
+    __shared__ float tmp_f[kST / kWave];
+    __shared__ double tmp_d[2][kST / kWave];
+    __shared__ typename std::conditional<TOP, TopLds, int>::type best;
     const int r = blockIdx.x, t = threadIdx.x;
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
-    T* grad = static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride;
     const RowSlots w = slots_of(a, r);
-    if (t < a.T) slots[t] = slot_of_token(a, w, a.tokens[(int64_t)r * a.T + t]);
-    __syncthreads();
-    double gsum = 0.0;
-    bool live = false;
-    for (int i = 0; i < a.T; ++i)
-        if (slots[i] >= 0) {
-            const float g = a.g[(int64_t)r * a.T + i];
-            gsum += (double)g;
-            live |= g != 0.0f;
+    bool there;
+    const float given = given_logit(a, r, row, w, &there);
+    ScorePart p{0.0, 0.0, kNegInf, 0.0f};
+    if (t < a.splits) p = a.parts[(int64_t)r * a.splits + t];
+    constexpr int E = kMaxParts * DYNA_MAX_KT / kST;
+    uint64_t x[E];
+    int n = 0;
+    if constexpr (TOP) {
+        const int all = a.splits * a.top;
+        const uint64_t* lists = a.lists + (int64_t)r * all;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            x[i] = i * kST + t < all ? lists[i * kST + t] : 0;
+            n += x[i] != 0;
         }
-    const float e = a.ge ? a.ge[r] : 0.0f;
-    live |= e != 0.0f;
-    const double m = a.stats[3 * (int64_t)r], log_s = a.stats[3 * (int64_t)r + 1], entropy = a.stats[3 * (int64_t)r + 2];
-    live &= m > -__builtin_inf() || m != m;
-    for (int v = t; v < w.len; v += kST) {
-        double x = 0.0;
-        if (live) {
-            const double lp = ((double)to_f32(row[v]) - m) * a.inv_t - log_s;
-            const double p = exp(lp);
-            x = -p * gsum - (p == 0.0 ? 0.0 : (double)e * p * (lp + entropy));
-            for (int i = 0; i < a.T; ++i)
-                if (slots[i] == v) x += (double)a.g[(int64_t)r * a.T + i];
-        }
-        store_elt(grad + v, (float)(x * a.inv_t));
+        if (t == 0) best.n = 0;
     }
+    const float m = block_max_f32<kST>(p.m, tmp_f);
+    const float c = (float)(a.inv_t * 1.4426950408889634);
+    seen_from(m, (double)c, p.s, p.u, p.m);
+    const double s = block_sum_f64<kST>(p.s, tmp_d[0]), u = block_sum_f64<kST>(p.u, tmp_d[1]);
+    const RowResult q(m, s, u);
+    if (t == 0) q.write(a, r);
+    if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
+    if constexpr (TOP) {
+        n = block_count(best, n, 0);
+        if (n > a.top) {
+            keep_best<E>(best, x, a.top);
+            n = a.top;
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (x[i] != 0) best.keys[atomicAdd(&best.n, 1)] = x[i];
+            lds_barrier();
+        }
+        write_best(a, r, best, n, q);
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+// A vector's listed tokens are bits in LDS, so that one read tells a thread that it
+// has none.
+template <typename T>
+__global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
+    __shared__ uint32_t listed[kGradLen / 32];
+    __shared__ int slots[DYNA_MAX_KT];
+    __shared__ float gs[DYNA_MAX_KT];
+    const int r = blockIdx.x / a.splits, part = blockIdx.x % a.splits, t = threadIdx.x;
+    const RowSlots w = slots_of(a, r);
+    const int v0 = part * kGradLen, v1 = min(w.len, v0 + kGradLen);
+    if (v0 >= v1) return;  // whole workgroup
+    const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
+    T* grad = static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride;
+    const float e = a.ge ? a.ge[r] : 0.0f;
+    const double m = a.stats[3 * (int64_t)r], log_s = a.stats[3 * (int64_t)r + 1], entropy = a.stats[3 * (int64_t)r + 2];
+    for (int i = t; i < (v1 - v0 + 31) / 32; i += kST) listed[i] = 0u;
+    lds_barrier();
+    if (t < a.T) {
+        const int slot = slot_of_token(a, w, a.tokens[(int64_t)r * a.T + t]);
+        slots[t] = slot;
+        gs[t] = slot < 0 ? 0.0f : a.g[(int64_t)r * a.T + t];
+        if (slot >= v0 && slot < v1) atomicOr(&listed[(slot - v0) >> 5], 1u << ((slot - v0) & 31));
+    }
+    lds_barrier();
+    double all = 0.0;
+    bool live = e != 0.0f;
+    for (int i = 0; i < a.T; ++i) {
+        all += (double)gs[i];
+        live |= gs[i] != 0.0f;
+    }
+    live &= !(m == -__builtin_inf());
+    if (!live) {
+        const float zero[8] = {};
+        for (int v = v0 + t * 8; v < v1; v += kVecStep) store_part(grad + v, v1 - v, zero);
+        return;
+    }
+    const float inv_t = (float)a.inv_t, top = (float)m, lg = (float)log_s, h = (float)entropy;
+    const float on_p = (float)(-a.inv_t * all), on_h = (float)(-a.inv_t * (double)e);
+    Row8<T> in[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+        const int at = v0 + i * kVecStep + t * 8;
+        if (at + 8 <= v1) in[i].load(row + at);
+    }
+    for (int base = v0; base < v1; base += kSweep) {
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int at = base + i * kVecStep + t * 8, next = at + kSweep;
+            if (at >= v1) break;
+            float z[8];
+            if (at + 8 <= v1) in[i].get(z);
+            else load_part(row + at, v1 - at, kNegInf, z);
+            if (next + 8 <= v1) in[i].load(row + next);
+            const uint32_t mine = (listed[(at - v0) >> 5] >> ((at - v0) & 31)) & 0xffu;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float lp = (z[k] - top) * inv_t - lg;
+                const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+                z[k] = p * fmaf(on_h, fmaxf(lp, -10000.0f) + h, on_p);  // 0 where p is
+            }
+            if (mine)
+                for (int j = 0; j < a.T; ++j) {
+                    const int k = slots[j] - at;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (k == q) z[q] = fmaf(gs[j], inv_t, z[q]);
+                }
+            store_part(grad + at, v1 - at, z);
+        }
+    }
+}
+
+// Parts of a row: whole rows where there are enough of them for the device's
+// compute units.
+void split_rows(int32_t N, int32_t V, int32_t* splits, int32_t* len) {
+    int64_t parts = 1;
+    if (V > 2 * kSweep && N < 1024) {
+        parts = std::min<int64_t>(kMaxParts, std::max<int64_t>(1, 2048 / N));
+        parts = std::min<int64_t>(parts, (V + 2 * kVecStep - 1) / (2 * kVecStep));
+    }
+    int64_t each = (V + parts - 1) / parts;
+    each = (each + kVecStep - 1) / kVecStep * kVecStep;
+    *len = (int32_t)each;
+    *splits = (int32_t)((V + each - 1) / each);
+}
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+template <typename T>
+dyna_status launch_pass(const ScoreArgs& a, hipStream_t stream) {
+    const unsigned blocks = (unsigned)((int64_t)a.N * a.splits);
+    if (a.top > 0) score_pass_kernel<T, true><<<blocks, kST, 0, stream>>>(a);
+    else score_pass_kernel<T, false><<<blocks, kST, 0, stream>>>(a);
+    dyna_status st = check_launch("score_pass_kernel");
+    if (st != DYNA_OK || a.splits == 1) return st;
+    if (a.top > 0) score_finish_kernel<T, true><<<a.N, kST, 0, stream>>>(a);
+    else score_finish_kernel<T, false><<<a.N, kST, 0, stream>>>(a);
+    return check_launch("score_finish_kernel");
 }
 
 }  // namespace
 
-size_t token_logprobs_ws_bytes(int32_t N, int32_t V, int32_t T, int32_t top) { return 256; }
+int32_t grad_parts(int32_t V) { return (V + kGradLen - 1) / kGradLen; }
 
-dyna_status launch_token_logprobs(const ScoreArgs& a, hipStream_t stream) {
-    if (a.dtype == DYNA_BF16) score_kernel<uint16_t><<<a.N, kST, 0, stream>>>(a);
-    else score_kernel<float><<<a.N, kST, 0, stream>>>(a);
-    return check_launch("score_kernel");
+size_t token_logprobs_ws_bytes(int32_t N, int32_t V, int32_t T, int32_t top) {
+    int32_t splits, len;
+    split_rows(N, V, &splits, &len);
+    if (splits == 1) return 256;
+    return align256(sizeof(ScorePart) * (size_t)N * splits) + align256(sizeof(uint64_t) * (size_t)N * splits * top);
 }
 
-dyna_status launch_token_logprobs_grad(const ScoreArgs& a, hipStream_t stream) {
-    if (a.dtype == DYNA_BF16) score_grad_kernel<uint16_t><<<a.N, kST, 0, stream>>>(a);
-    else score_grad_kernel<float><<<a.N, kST, 0, stream>>>(a);
+dyna_status launch_token_logprobs(const ScoreArgs& args, hipStream_t stream) {
+    ScoreArgs a = args;
+    split_rows(a.N, a.V, &a.splits, &a.split_len);
+    a.parts = static_cast<ScorePart*>(a.ws);
+    a.lists = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + align256(sizeof(ScorePart) * (size_t)a.N * a.splits));
+    return a.dtype == DYNA_BF16 ? launch_pass<uint16_t>(a, stream) : launch_pass<float>(a, stream);
+}
+
+dyna_status launch_token_logprobs_grad(const ScoreArgs& args, hipStream_t stream) {
+    ScoreArgs a = args;
+    a.splits = grad_parts(a.V);
+    const unsigned blocks = (unsigned)((int64_t)a.N * a.splits);
+    if (a.dtype == DYNA_BF16) score_grad_kernel<uint16_t><<<blocks, kST, 0, stream>>>(a);
+    else score_grad_kernel<float><<<blocks, kST, 0, stream>>>(a);
     return check_launch("score_grad_kernel");
 }
 

@@ -253,7 +253,8 @@ def test_gradients(N, V, T, pad, lead, temperature, dtype):
 def test_gradients_of_masked_rows(dtype):
     inf, V = float("inf"), 3000
     low = torch.finfo(DT[dtype]).min
-    z = rows(8, V, dtype, 1)
+    z = rows(9, V, dtype, 1)
+    z[8] = float("nan")
     z[0] = -inf
     z[1] = low
     z[2, torch.rand(V, generator=gen(1)) < 0.9] = -inf
@@ -264,15 +265,15 @@ def test_gradients_of_masked_rows(dtype):
     z[5, 9] = float("nan")
     z[6, 9] = inf
     z[7, 11] = float("nan")            # in a padding row, which nothing reads
-    t = torch.tensor([[5, 7, 5, -1]], dtype=torch.int32).expand(8, 4).contiguous().cuda()
-    g, e = torch.randn((8, 4), generator=gen(3)).cuda(), torch.randn(8, generator=gen(4)).cuda()
+    t = torch.tensor([[5, 7, 5, -1]], dtype=torch.int32).expand(9, 4).contiguous().cuda()
+    g, e = torch.randn((9, 4), generator=gen(3)).cuda(), torch.randn(9, generator=gen(4)).cuda()
     g[7], e[7] = 0.0, 0.0
     g[7, 3] = 5.0                      # at a token that is not there: not used
     g[:, 3] = float("nan")
     stats = D.token_logprobs(z, t, want_stats=True).stats
     grad = D.token_logprobs_grad(z, stats, t, g, e)
     assert (grad[0] == 0).all() and (grad[7] == 0).all()
-    assert torch.isnan(grad[5]).all() and torch.isnan(grad[6]).all()
+    assert torch.isnan(grad[5]).all() and torch.isnan(grad[6]).all() and torch.isnan(grad[8]).all()
     keep = [0, 1, 2, 3, 4, 7]
     gradient_check(z[keep], t[keep], g[keep], e[keep], 1.0, stats[keep], grad[keep])
 

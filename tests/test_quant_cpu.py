@@ -223,6 +223,8 @@ def test_logprobs_grad_refuses():
                    dict(gstride=99), dict(grad=P), dict(grad=P + 400), dict(grad=P + 100, gstride=200), dict(t=0.0)):
         assert call(**change) == D.ERR_INVALID_ARG, change
     assert call(T=65) == D.ERR_UNSUPPORTED
+    # 32 work items to a row of 2^20, 2^23 in a launch
+    assert call(V=1 << 20, stride=1 << 20, gstride=1 << 20, N=(1 << 18) + 1) == D.ERR_UNSUPPORTED
 
 
 def test_binding_refuses_host_tensors_and_shapes():
