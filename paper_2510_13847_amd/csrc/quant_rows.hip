@@ -52,7 +52,7 @@ struct QuantTile {
 };
 
 template <int ACT, bool PLAN, int MAXW, typename OT>
-__global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProductArgs a) {
+__global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_rows_kernel(QuantProductArgs a) {
     constexpr int CPP = contexts_per_pass(ACT);
     constexpr int kOut = CPP * kMfmaRows;
     __shared__ __attribute__((aligned(16))) f32x4 red[2][MAXW][kWave];
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProduct
     }
     // The tile behind cur: plans walk the chunks of one context list once for each
     // CPP of its contexts.
-    auto next_tile = [&]() -> QuantTile {
+    auto next_tile = [&]() __attribute__((always_inline)) -> QuantTile {
         if constexpr (PLAN) {
             const int i = at + 1;
             if (i < c1) {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProduct
     // ---- rows
     u32x4 w[2][kQuantUnitSteps];
     uint32_t ws[2];
-    auto load_rows = [&](int set, const QuantTile& t) {
+    auto load_rows = [&](int set, const QuantTile& t) __attribute__((always_inline)) {
         const int r = t.r0 + (PLAN ? min(col, t.nrows - 1) : col);
         const uint8_t* p = a.W.data + (int64_t)(r / kMfmaRows) * a.W.group_bytes + wv * kQuantUnitBytes;
         const int at = (r % kMfmaRows) * 64 + g * 16;
@@ -137,10 +137,10 @@ __global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProduct
     constexpr int NS = ACT == kActFour ? 1 : 4;
     u32x4 b[kQuantUnitSteps][NS];
     uint32_t bs = 0;
-    constexpr int NE = 4;        // results of a thread at most: 256 of 64 threads
+    constexpr int NE = MAXW < 4 ? 4 : 1;  // results of a thread at most: 256 of 64 threads, or of 256 and more
     constexpr int64_t kNowhere = INT64_MIN;
     int64_t out_at[NE];          // where result i of this thread's context would go for layout row 0
-    auto load_contexts = [&](const QuantTile& t) {
+    auto load_contexts = [&](const QuantTile& t) __attribute__((always_inline)) {
         auto context = [&](int c, int* slot) -> int {  // context c of this pass, -1 past the last
             const int i = t.first + c;
             *slot = 0;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(MAXW* kWave, 2) void quant_rows_kernel(QuantProduct
     load_contexts(cur);
     OT* out = static_cast<OT*>(a.out);
     int set = 0;
-    auto tile = [&](auto set_tag) {
+    auto tile = [&](auto set_tag) __attribute__((always_inline)) {
         constexpr int S = decltype(set_tag)::value;
         const QuantTile nxt = next_tile();
         load_rows(1 - S, nxt.nrows > 0 ? nxt : cur);
@@ -276,7 +276,10 @@ dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
 }
 template <int ACT, bool PLAN, typename OT>
 dyna_status launch_w(const QuantProductArgs& a, hipStream_t stream) {
-    return a.W.units <= 8 ? launch_t<ACT, PLAN, 8, OT>(a, stream) : launch_t<ACT, PLAN, 16, OT>(a, stream);
+    const int units = a.W.units;
+    if (units <= 3) return launch_t<ACT, PLAN, 3, OT>(a, stream);
+    if (units <= 8) return launch_t<ACT, PLAN, 8, OT>(a, stream);
+    return units <= 12 ? launch_t<ACT, PLAN, 12, OT>(a, stream) : launch_t<ACT, PLAN, 16, OT>(a, stream);
 }
 
 }  // namespace
