@@ -11,38 +11,14 @@
 // An fp32 context is three columns of bf16: its 24 bits cut in three terms of
 // eight, whose products with a four-bit value are exact.
 #include "quant.h"
-#include "rowstat.h"
+#include "quant_operand.h"
 
 namespace dyna {
 namespace {
 
 template <typename T>
 using sptr = const __attribute__((address_space(4))) T*;  // read through the scalar unit
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-enum { kActFour = 0, kActBf16 = 1, kActF32 = 3 };  // the contexts' type; columns of the product for each
-
-__host__ __device__ constexpr int contexts_per_pass(int act) { return act == kActF32 ? 5 : 16; }
-
-// Eight bf16 of a four-bit code word.
-__device__ __forceinline__ bf16x8 row_operand(uint32_t code, float scale) {
-    u32x4 r;
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3));
-    return __builtin_bit_cast(bf16x8, r);
-}
-
-// Term t of three of an fp32 value, each cut off behind eight bits (so the sum is
-// the value, and no term overflows); an infinity or NaN is its own first term.
-__device__ __forceinline__ float term_of(float x, int t) {
-    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    if (t == 0) return x == x ? a : x;
-    const float b = fabsf(x) <= kF32Max ? x - a : 0.0f;
-    const float c = __uint_as_float(__float_as_uint(b) & 0xffff0000u);
-    return t == 1 ? c : b - c;
-}
+__host__ __device__ constexpr int contexts_per_pass(int act) { return act == kActF32 ? kRowsMostF32 : kRowsMost; }
 
 // One tile and the contexts that it is multiplied with.
 struct QuantTile {
@@ -226,7 +202,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
         } else {
 #pragma unroll
             for (int j = 0; j < kQuantUnitSteps; ++j) {
-                const float scale = __uint_as_float(((ws[S] >> (8 * j)) & 0xffu) << 23);
+                const float scale = scale_value(ws[S] >> (8 * j));
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
                     acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[j][s % NS]),
@@ -283,9 +259,6 @@ dyna_status launch_w(const QuantProductArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
-
-size_t quant_product_ws_bytes(int32_t B, int32_t d) { return 256; }
-dyna_status launch_quant_product(const QuantProductArgs& a, hipStream_t stream) { return launch_quant_rows(a, stream); }
 
 dyna_status launch_quant_rows(const QuantProductArgs& a, hipStream_t stream) {
     if (a.plan.hdr != nullptr)
