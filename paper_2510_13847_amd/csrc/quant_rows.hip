@@ -186,14 +186,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
         if constexpr (ACT == kActFour) {
             auto product = [&](auto j_tag) {
                 constexpr int j = decltype(j_tag)::value;
-                i32x8 x{}, y{};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = (int)b[j][0][e];
-                    y[e] = (int)w[S][j][e];
-                }
-                acc[j & 1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc[j & 1], 4, 4, j, (int)bs, j,
-                                                                            (int)ws[S]);
+                acc[j & 1] = four_bit_product<j>(b[j][0], bs, w[S][j], ws[S], acc[j & 1]);
             };
             product(std::integral_constant<int, 0>{});
             product(std::integral_constant<int, 1>{});

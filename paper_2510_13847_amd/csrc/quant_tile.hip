@@ -1,11 +1,11 @@
 // Four-bit rows times many contexts: LDS-staged tiles on the matrix cores.
 //
-// A workgroup's tile is 16 WR NRG rows by 16 WC NCG contexts, a wave's 16 NRG rows
-// by 16 NCG contexts, and a stage 128 columns.  Rows go from memory to registers in
-// the operand layout that they are stored in, and are converted there; contexts go
-// straight to LDS, which the tile's waves share.  fp32 and bf16 contexts are put
-// into operand order first (context_operand_kernel: each 1 KiB piece is one wave's
-// operand of one instruction); four-bit ones are stored in it.
+// A workgroup's tile is 32 WR NR rows by 32 WC NC contexts, a wave's 32 NR rows by
+// 32 NC contexts, and a stage 128 columns.  Rows go from memory to registers as
+// operands of 32 rows by 64 columns, and are converted there; contexts go straight
+// to LDS, which the tile's waves share.  fp32 and bf16 contexts are put
+// into operand order first (context_operand_kernel: each 1 KiB piece is 32
+// columns of 16 contexts); four-bit ones are stored in it.
 //
 // Rows are the left operand, so that a lane ends with four consecutive rows of one
 // context and stores them together.
@@ -19,7 +19,6 @@ namespace dyna {
 namespace {
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
-typedef const __attribute__((address_space(1))) void* glb_ptr;
 constexpr int kTileXcds = 8;  // workgroups go to the XCDs in turn
 constexpr int kPiece = 1024;  // bytes of 16 contexts' operand of one instruction
 
@@ -55,42 +54,63 @@ __global__ __launch_bounds__(256) void context_operand_kernel(const T* __restric
 }
 
 // ---------------------------------------------------------------- tiles
-template <int ACT, int NRG, int NCG, int WR, int WC>
+template <int ACT, int NR, int NC, int WR, int WC, typename OT>
 struct TileShape {
-    static constexpr int ROWS = 16 * WR * NRG, CTX = 16 * WC * NCG, GROUPS = WC * NCG, WAVES = WR * WC;
+    static constexpr int ROWS = 32 * WR * NR, CTX = 32 * WC * NC, GROUPS = CTX / 16, WAVES = WR * WC;
     static constexpr int TERMS = ACT == kActF32 ? 3 : 1;
-    // pieces of a stage, and four-bit contexts' scales behind them
-    static constexpr int PIECES = ACT == kActFour ? GROUPS : TERMS * 4 * GROUPS;
+    static constexpr int PIECES = ACT == kActFour ? GROUPS : TERMS * 4 * GROUPS;  // of a stage
+    static constexpr int STAGE = PIECES * kPiece;
+    // stages in LDS: a unit's four where a compute unit holds two workgroups of them
+    static constexpr int RING = 4 * STAGE <= 80 * 1024 ? 4 : 2, AHEAD = RING - 1;
+    // four-bit contexts' scales, of a unit at a time
     static constexpr int SCALES = ACT == kActFour ? GROUPS * kQuantScaleBytes : 0;
-    static constexpr int STAGE = PIECES * kPiece + SCALES;
-    static constexpr int AHEAD = 3 * STAGE <= 80 * 1024 ? 2 : 1;  // stages under way beside the one in use
-    static constexpr int RING = AHEAD + 1;
-    static constexpr int LDS = RING * STAGE;
     static_assert(PIECES % WAVES == 0, "each wave loads as many pieces");
     static_assert(ACT != kActFour || GROUPS % WAVES == 0, "and scales");
-    static constexpr int NI = PIECES / WAVES + (ACT == kActFour ? GROUPS / WAVES : 0);
-    // loads of a wave and stage: contexts, rows and their scales
-    static constexpr int LOADS = NI + 2 * NRG;
+    static constexpr int NI = PIECES / WAVES;
+    static constexpr int LOADS = NI + 2 * NR;  // of a wave and stage, scales left out
+    // products on their way out: 32 contexts of a wave's rows, and a piece to spare so
+    // that contexts start in different banks
+    static constexpr int OUT_ROW = 32 * NR * (int)sizeof(OT) + 16;
+    static constexpr int LDS_IN = RING * STAGE + 2 * SCALES, LDS_OUT = WAVES * 32 * OUT_ROW;
+    static constexpr int LDS = LDS_IN > LDS_OUT ? LDS_IN : LDS_OUT;
+    static_assert(LDS <= 160 * 1024, "LDS per block");
 };
 
-// The loads of all stages but the last N loads' have arrived, for every wave.
+// 16 or 4 bytes per lane of a piece, or of a unit's scales, straight to LDS at dst +
+// 16 (4) * lane.  (Behind the buffer form the compiler lets LDS be read without
+// waiting for all loads.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_at(const uint8_t* p, int n) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), (short)0, n, 0x00027000);
+}
+__device__ __forceinline__ void load_piece(const uint8_t* from, int at, char* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(bytes_at(from, kPiece), (lds_ptr)dst, 16, at, 0, 0, 0);
+}
+__device__ __forceinline__ void load_scales(const uint8_t* from, int at, char* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(bytes_at(from, kQuantScaleBytes), (lds_ptr)dst, 4, at, 0, 0, 0);
+}
+
+// Every load of this wave but the last N has arrived, and every wave is here.
 template <int N>
 __device__ __forceinline__ void loads_barrier() {
     static_assert(N < 64, "vmcnt");
     __asm__ __volatile__("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ void store4(float* p, const f32x4& x, int n) {
-    if (n >= 4) *reinterpret_cast<f32x4_w*>(p) = x;
-    else
-        for (int i = 0; i < n; ++i) p[i] = x[i];
+// Four products, and 16 bytes of n products left of a context's row.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put4(float* p, const f32x4& x) { *reinterpret_cast<f32x4*>(p) = x; }
+__device__ __forceinline__ void put4(uint16_t* p, const f32x4& x) {
+    *reinterpret_cast<u32x2*>(p) = u32x2{bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
 }
-typedef uint32_t u32x2_h __attribute__((ext_vector_type(2), aligned(2)));
-__device__ __forceinline__ void store4(uint16_t* p, const f32x4& x, int n) {
-    const u32x2_h w = {bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3])};
-    if (n >= 4) *reinterpret_cast<u32x2_h*>(p) = w;
+__device__ __forceinline__ void store16(float* p, const float* from, int n) {
+    if (n >= 4) *reinterpret_cast<u32x4_w*>(p) = *reinterpret_cast<const u32x4*>(from);
     else
-        for (int i = 0; i < n; ++i) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        for (int i = 0; i < n; ++i) p[i] = from[i];
+}
+__device__ __forceinline__ void store16(uint16_t* p, const uint16_t* from, int n) {
+    if (n >= 8) *reinterpret_cast<u32x4_h*>(p) = *reinterpret_cast<const u32x4*>(from);
+    else
+        for (int i = 0; i < n; ++i) p[i] = from[i];
 }
 
 struct TileGrid {
@@ -99,150 +119,210 @@ struct TileGrid {
     int row_tiles, ctx_tiles;
 };
 
-template <int ACT, int NRG, int NCG, int WR, int WC, typename OT>
-__global__ __launch_bounds__(kWave* WR* WC, WR* WC <= 4 ? 1 : 2) void quant_tile_kernel(QuantProductArgs a, TileGrid grid) {
-    using Sh = TileShape<ACT, NRG, NCG, WR, WC>;
+template <int ACT, int NR, int NC, int WR, int WC, typename OT>
+__global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProductArgs a, TileGrid grid) {
+    using Sh = TileShape<ACT, NR, NC, WR, WC, OT>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int lane = lane_id();
+    const int lane = lane_id(), half = lane >> 5;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wr = wv % WR, wc = wv / WR;
     // the tiles of one block of rows run side by side on one XCD
     const int xcd = blockIdx.x % kTileXcds, j = blockIdx.x / kTileXcds;
     const int rt = j / grid.ctx_tiles * kTileXcds + xcd, ct = j % grid.ctx_tiles;
     if (rt >= grid.row_tiles) return;  // whole workgroup
-    const int steps = a.W.steps;
+    const int steps = a.W.steps, units = a.W.units;
 
-    // this lane's place in the row groups of its wave; groups past the last repeat it
+    // this lane's row of each block of 32 (groups past the last repeat it)
     const int last_group = (a.W.rows - 1) / kMfmaRows;
-    const uint8_t* wp[NRG];
+    const uint8_t* wp[NR];
 #pragma unroll
-    for (int r = 0; r < NRG; ++r) {
-        const int group = min((rt * WR + wr) * NRG + r, last_group);
+    for (int r = 0; r < NR; ++r) {
+        const int group = min(((rt * WR + wr) * NR + r) * 2 + ((lane >> 4) & 1), last_group);
         wp[r] = a.W.data + (int64_t)group * a.W.group_bytes;
     }
-    const int lane_at = (lane & 15) * 64 + (lane >> 4) * 16;  // in a step's 1 KiB
-    u32x4 w[Sh::RING][NRG];
-    uint32_t ws[Sh::RING][NRG];
+    const int row_at = (lane & 15) * 64 + half * 16;         // columns 0 .. 63 of a step; 64 .. are 32 bytes on
+    const int ctx_at = (lane & 15) * 64 + (lane >> 4) * 16;  // four-bit contexts: a whole step of 16
+    // this lane's operand in a stage: blocks 0 and 1 of a step; 2 and 3 are 512 bytes on
+    const int lds_at = wc * NC * 2 * kPiece + ((lane >> 4) & 1) * kPiece + half * 256 + (lane & 15) * 16;
+    char* scales = smem + Sh::RING * Sh::STAGE;
+    u32x4 w[Sh::RING][NR][2];
+    uint32_t ws[NR][2], ws_next[NR][2];
 
-    // stage `step` into ring place p: contexts to LDS, rows to registers.  Stages
-    // past the last one repeat it.
-    auto load = [&](int step, auto place) __attribute__((always_inline)) {
-        constexpr int p = decltype(place)::value;
-        step = min(step, steps - 1);
-        const int unit = step / kQuantUnitSteps, in = step % kQuantUnitSteps;
-        const int unit_steps = min(kQuantUnitSteps, steps - unit * kQuantUnitSteps);
-        char* stage = smem + p * Sh::STAGE;
+    auto unit_steps = [&](int unit) { return min(kQuantUnitSteps, steps - unit * kQuantUnitSteps); };
+    // the scales of a unit: rows' to registers, contexts' to LDS.  A unit past the
+    // last one repeats it.
+    auto load_unit = [&](int unit) __attribute__((always_inline)) {
+        unit = min(unit, units - 1);
+        const int64_t at = (int64_t)unit * kQuantUnitBytes + unit_steps(unit) * kQuantStepBytes;
         if constexpr (ACT == kActFour) {
             const int last = (a.B - 1) / kMfmaRows;
 #pragma unroll
             for (int i = 0; i < Sh::GROUPS / Sh::WAVES; ++i) {
                 const int g = wv * (Sh::GROUPS / Sh::WAVES) + i;
-                const uint8_t* from = a.a4.data + (int64_t)min(ct * Sh::GROUPS + g, last) * a.a4.group_bytes +
-                                      (int64_t)unit * kQuantUnitBytes;
-                __builtin_amdgcn_global_load_lds((glb_ptr)(from + in * kQuantStepBytes + lane_at),
-                                                 (lds_ptr)(stage + g * kPiece), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((glb_ptr)(from + unit_steps * kQuantStepBytes + lane_at / 4),
-                                                 (lds_ptr)(stage + Sh::PIECES * kPiece + g * kQuantScaleBytes), 4, 0, 0);
+                load_scales(a.a4.data + (int64_t)min(ct * Sh::GROUPS + g, last) * a.a4.group_bytes + at, ctx_at / 4,
+                            scales + (unit & 1) * Sh::SCALES + g * kQuantScaleBytes);
             }
-        } else {
+        }
 #pragma unroll
-            for (int i = 0; i < Sh::NI; ++i) {
-                const int piece = wv * Sh::NI + i;  // (term, s) major, group minor
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                ws_next[r][h] = *reinterpret_cast<const uint32_t*>(wp[r] + at + row_at / 4 + h * 8);
+    };
+    // stage `step` into ring place p: contexts to LDS, rows to registers.  Stages
+    // past the last one repeat it.
+    auto load = [&](int step, auto place) __attribute__((always_inline)) {
+        constexpr int p = decltype(place)::value;
+        step = min(step, steps - 1);
+        const int64_t at = (int64_t)(step / kQuantUnitSteps) * kQuantUnitBytes + step % kQuantUnitSteps * kQuantStepBytes;
+        char* stage = smem + p * Sh::STAGE;
+#pragma unroll
+        for (int i = 0; i < Sh::NI; ++i) {
+            const int piece = wv * Sh::NI + i;  // (term, s) major, group minor
+            if constexpr (ACT == kActFour) {
+                const int group = min(ct * Sh::GROUPS + piece, (a.B - 1) / kMfmaRows);
+                load_piece(a.a4.data + (int64_t)group * a.a4.group_bytes + at, ctx_at, stage + piece * kPiece);
+            } else {
                 const int64_t from = ((int64_t)step * Sh::TERMS * 4 + piece / Sh::GROUPS) * grid.groups +
                                      ct * Sh::GROUPS + piece % Sh::GROUPS;
-                __builtin_amdgcn_global_load_lds((glb_ptr)(grid.operand + from * kPiece + lane * 16),
-                                                 (lds_ptr)(stage + piece * kPiece), 16, 0, 0);
+                load_piece(grid.operand + from * kPiece, lane * 16, stage + piece * kPiece);
             }
         }
 #pragma unroll
-        for (int r = 0; r < NRG; ++r) {
-            const uint8_t* from = wp[r] + (int64_t)unit * kQuantUnitBytes;
-            w[p][r] = *reinterpret_cast<const u32x4*>(from + in * kQuantStepBytes + lane_at);
-            ws[p][r] = *reinterpret_cast<const uint32_t*>(from + unit_steps * kQuantStepBytes + lane_at / 4);
-        }
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[p][r][h] = *reinterpret_cast<const u32x4*>(wp[r] + at + row_at + h * 32);
     };
 
-    f32x4 acc[NRG][NCG];
+    f32x16 acc[NR][NC];
 #pragma unroll
-    for (int r = 0; r < NRG; ++r)
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
-        for (int c = 0; c < NCG; ++c) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
 
-    auto stage = [&](int step, auto place) __attribute__((always_inline)) {
-        constexpr int p = decltype(place)::value;
-        // this stage has arrived, and everyone has read the one whose place is next
-        loads_barrier<(Sh::AHEAD - 1) * Sh::LOADS>();
-        load(step + Sh::AHEAD, std::integral_constant<int, (p + Sh::AHEAD) % Sh::RING>{});
-        const char* at = smem + p * Sh::STAGE;
-        const int shift = 8 * (step % kQuantUnitSteps);
-        if constexpr (ACT == kActFour) {
-            u32x4 b[NCG];
-            uint32_t bs[NCG];
-#pragma unroll
-            for (int c = 0; c < NCG; ++c) {
-                const int g = wc * NCG + c;
-                b[c] = *reinterpret_cast<const u32x4*>(at + g * kPiece + lane * 16);
-                bs[c] = *reinterpret_cast<const uint32_t*>(at + Sh::PIECES * kPiece + g * kQuantScaleBytes + lane * 4) >> shift;
-            }
-#pragma unroll
-            for (int r = 0; r < NRG; ++r)
-#pragma unroll
-                for (int c = 0; c < NCG; ++c)
-                    acc[r][c] = four_bit_product(w[p][r], ws[p][r] >> shift, b[c], bs[c], acc[r][c]);
+    // step j of a unit.  `more`: loads go on AHEAD stages before their use.
+    auto stage = [&](int unit, auto in_unit, auto more) __attribute__((always_inline)) {
+        constexpr int j = decltype(in_unit)::value, p = j % Sh::RING;
+        // This stage has arrived, and everyone has read the one whose place is next.
+        // At least LOADS loads were issued in each of the AHEAD - 1 stages since its own;
+        // where those may be fewer, all are waited for.
+        if constexpr (decltype(more)::value) {
+            loads_barrier<(Sh::AHEAD - 1) * Sh::LOADS>();
+            load(unit * kQuantUnitSteps + j + Sh::AHEAD, std::integral_constant<int, (p + Sh::AHEAD) % Sh::RING>{});
+            if constexpr (j == 0) load_unit(unit + 1);
         } else {
+            loads_barrier<0>();
+        }
+        const char* at = smem + p * Sh::STAGE + lds_at;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                bf16x8 x[NRG];
+        for (int h = 0; h < 2; ++h) {
+            if constexpr (ACT == kActFour) {
+                u32x4 b[NC];
+                uint32_t bs[NC];
+                const char* sc = scales + (unit & 1) * Sh::SCALES + lds_at / 4 + h * 128;
 #pragma unroll
-                for (int r = 0; r < NRG; ++r)
-                    x[r] = row_operand(w[p][r][s], scale_value(ws[p][r] >> shift));
+                for (int c = 0; c < NC; ++c) {
+                    b[c] = *reinterpret_cast<const u32x4*>(at + c * 2 * kPiece + h * 512);
+                    bs[c] = *reinterpret_cast<const uint32_t*>(sc + c * 2 * kQuantScaleBytes);
+                }
 #pragma unroll
-                for (int t = 0; t < Sh::TERMS; ++t)
+                for (int r = 0; r < NR; ++r)
 #pragma unroll
-                    for (int c = 0; c < NCG; ++c) {
-                        const u32x4 b = *reinterpret_cast<const u32x4*>(
-                            at + ((t * 4 + s) * Sh::GROUPS + wc * NCG + c) * kPiece + lane * 16);
+                    for (int c = 0; c < NC; ++c)
+                        acc[r][c] = four_bit_product<j>(w[p][r][h], ws[r][h], b[c], bs[c], acc[r][c]);
+            } else {
 #pragma unroll
-                        for (int r = 0; r < NRG; ++r)
-                            acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[r], __builtin_bit_cast(bf16x8, b),
-                                                                               acc[r][c], 0, 0, 0);
-                    }
+                for (int s = 0; s < 4; ++s) {
+                    bf16x8 x[NR];
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) x[r] = row_operand(w[p][r][h][s], scale_value(ws[r][h] >> (8 * j)));
+#pragma unroll
+                    for (int t = 0; t < Sh::TERMS; ++t)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const u32x4 b = *reinterpret_cast<const u32x4*>(
+                                at + (t * 4 + s) * Sh::GROUPS * kPiece + c * 2 * kPiece + h * 512);
+#pragma unroll
+                            for (int r = 0; r < NR; ++r)
+                                acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                    x[r], __builtin_bit_cast(bf16x8, b), acc[r][c], 0, 0, 0);
+                        }
+                }
             }
         }
     };
-    load(0, std::integral_constant<int, 0>{});
-    if constexpr (Sh::AHEAD == 2) load(1, std::integral_constant<int, 1>{});
-    for (int step = 0; step < steps; step += Sh::RING) {
-        stage(step, std::integral_constant<int, 0>{});
-        if (step + 1 < steps) stage(step + 1, std::integral_constant<int, 1>{});
-        if constexpr (Sh::RING == 3)
-            if (step + 2 < steps) stage(step + 2, std::integral_constant<int, 2>{});
+    auto next_unit = [&]() {
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) ws[r][h] = ws_next[r][h];
+    };
+    using J0 = std::integral_constant<int, 0>;
+    using J1 = std::integral_constant<int, 1>;
+    using J2 = std::integral_constant<int, 2>;
+    using J3 = std::integral_constant<int, 3>;
+    load_unit(0);
+    load(0, J0{});
+    if constexpr (Sh::AHEAD == 3) {
+        load(1, J1{});
+        load(2, J2{});
     }
-    // nothing may land in LDS behind the workgroup's end
-    __asm__ __volatile__("s_waitcnt vmcnt(0)" ::: "memory");
+    next_unit();
+    // (whole units without a branch inside, so that the compiler counts the loads in
+    // flight exactly)
+    int unit = 0;
+    for (; (unit + 1) * kQuantUnitSteps <= steps; ++unit) {
+        stage(unit, J0{}, std::true_type{});
+        stage(unit, J1{}, std::true_type{});
+        stage(unit, J2{}, std::true_type{});
+        stage(unit, J3{}, std::true_type{});
+        next_unit();
+    }
+    // the last unit's steps are in the ring already, or come one by one
+    using More = std::integral_constant<bool, Sh::AHEAD == 1>;
+    const int left = steps - unit * kQuantUnitSteps;
+    if (left > 0) stage(unit, J0{}, More{});
+    if (left > 1) stage(unit, J1{}, More{});
+    if (left > 2) stage(unit, J2{}, More{});
+    loads_barrier<0>();  // nothing lands in LDS any more, and everyone has read it
 
+    // A lane holds context l % 32 of a block, rows 8 q + 4 (l / 32) .. + 3: they leave
+    // through LDS, as whole pieces of a context's row.
     OT* out = static_cast<OT*>(a.out);
+    char* mine = smem + wv * 32 * Sh::OUT_ROW;
+    constexpr int LANES = 32 * NR * (int)sizeof(OT) / 16, PER = 16 / (int)sizeof(OT);  // lanes to a context's rows
+    const int row0 = (rt * WR + wr) * NR * 32;
 #pragma unroll
-    for (int c = 0; c < NCG; ++c) {
-        const int ctx = ct * Sh::CTX + (wc * NCG + c) * 16 + (lane & 15);
-        if (ctx >= a.B) continue;
+    for (int c = 0; c < NC; ++c) {
+        wave_lds_order();
 #pragma unroll
-        for (int r = 0; r < NRG; ++r) {
-            const int row = ((rt * WR + wr) * NRG + r) * kMfmaRows + 4 * (lane >> 4);
-            store4(out + (int64_t)ctx * a.ld + row, acc[r][c], a.n_rows - row);
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                put4(reinterpret_cast<OT*>(mine + (lane & 31) * Sh::OUT_ROW) + r * 32 + 8 * q + 4 * half,
+                     f32x4{acc[r][c][4 * q], acc[r][c][4 * q + 1], acc[r][c][4 * q + 2], acc[r][c][4 * q + 3]});
+        wave_lds_order();
+#pragma unroll
+        for (int i = 0; i < 32 * LANES / kWave; ++i) {
+            const int k = i * (kWave / LANES) + lane / LANES, row = lane % LANES * PER;
+            const int ctx = ct * Sh::CTX + (wc * NC + c) * 32 + k;
+            if (ctx < a.B)
+                store16(out + (int64_t)ctx * a.ld + row0 + row, reinterpret_cast<const OT*>(mine + k * Sh::OUT_ROW) + row,
+                        a.n_rows - row0 - row);
         }
     }
 }
 
-template <int ACT, int NRG, int NCG, int WR, int WC, typename OT>
+template <int ACT, int NR, int NC, int WR, int WC, typename OT>
 dyna_status launch_tile(const QuantProductArgs& a, TileGrid g, hipStream_t stream) {
-    using Sh = TileShape<ACT, NRG, NCG, WR, WC>;
-    static_assert(Sh::LDS <= 160 * 1024, "LDS per block");
+    using Sh = TileShape<ACT, NR, NC, WR, WC, OT>;
     static std::atomic<uint64_t> allowed{0};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return set_error(DYNA_ERR_HIP, "tile: device");
     if (!(allowed.load() & (1ull << dev))) {
-        if (hipFuncSetAttribute((const void*)quant_tile_kernel<ACT, NRG, NCG, WR, WC, OT>,
+        if (hipFuncSetAttribute((const void*)quant_tile_kernel<ACT, NR, NC, WR, WC, OT>,
                                 hipFuncAttributeMaxDynamicSharedMemorySize, Sh::LDS) != hipSuccess)
             return set_error(DYNA_ERR_HIP, "tile: LDS attribute");
         allowed.fetch_or(1ull << dev);
@@ -252,7 +332,7 @@ dyna_status launch_tile(const QuantProductArgs& a, TileGrid g, hipStream_t strea
     const int64_t blocks = (int64_t)((g.row_tiles + kTileXcds - 1) / kTileXcds) * kTileXcds * g.ctx_tiles;
     if (blocks * kWave * Sh::WAVES > 0xffffffffll)
         return set_error(DYNA_ERR_UNSUPPORTED, "%d contexts by %d rows in one call", a.B, a.n_rows);
-    quant_tile_kernel<ACT, NRG, NCG, WR, WC, OT><<<(unsigned)blocks, kWave * Sh::WAVES, Sh::LDS, stream>>>(a, g);
+    quant_tile_kernel<ACT, NR, NC, WR, WC, OT><<<(unsigned)blocks, kWave * Sh::WAVES, Sh::LDS, stream>>>(a, g);
     return check_launch("quant_tile_kernel");
 }
 
@@ -265,15 +345,17 @@ int operand_groups(int32_t B) {
 template <int ACT, typename OT>
 dyna_status launch_shape(const QuantProductArgs& a, const TileGrid& g, hipStream_t stream) {
     const int64_t tiles = ((int64_t)a.n_rows + 255) / 256;
-    if (tiles * ((a.B + 63) / 64) < 256) return launch_tile<ACT, 1, 4, 4, 1, OT>(a, g, stream);
+    if (tiles * ((a.B + 63) / 64) < 256) return launch_tile<ACT, 1, 1, 2, 2, OT>(a, g, stream);
     if constexpr (ACT != kActF32) {
-        if (tiles * ((a.B + 255) / 256) >= 256 && a.B > 128) return launch_tile<ACT, 4, 8, 4, 2, OT>(a, g, stream);
-        if (a.B > 64 && tiles * ((a.B + 127) / 128) >= 256) {
-            if constexpr (ACT == kActFour) return launch_tile<ACT, 4, 8, 4, 1, OT>(a, g, stream);
-            else return launch_tile<ACT, 4, 4, 4, 2, OT>(a, g, stream);
-        }
+#ifdef SHAPE_A
+        if (a.B > 64) return launch_tile<ACT, 2, 4, 4, 1, OT>(a, g, stream);
+#else
+        if (a.B > 64) return launch_tile<ACT, 2, 4, 4, 2, OT>(a, g, stream);
+#endif
     }
-    return launch_tile<ACT, 4, 4, 4, 1, OT>(a, g, stream);
+    if constexpr (ACT != kActFour)
+        if (a.B <= 32) return launch_tile<ACT, 2, 1, 4, 1, OT>(a, g, stream);
+    return launch_tile<ACT, 2, 2, 4, 1, OT>(a, g, stream);
 }
 
 template <typename T, int TERMS>
