@@ -4,12 +4,17 @@
 // 16 rows are a group, 128 columns a step and four steps a unit.  A group is its
 // units one after the other: a unit's steps of 1 KiB, then 256 bytes of scales.
 // In a step, row i of the group and block g (32 columns) are 16 bytes at
-// i * 64 + g * 16, the even column in the low half of each byte; in the scales,
-// the word at (i * 4 + g) * 4 holds the e8m0 bytes of block g in the unit's four
+// (g * 16 + i) * 16, the even column in the low half of each byte; in the scales,
+// the word at (g * 16 + i) * 4 holds the e8m0 bytes of block g in the unit's four
 // steps.  So lane i + 16 g of a wave loads the 32 values that a matrix
-// instruction of 16 rows by 128 columns takes from it with one instruction, a
-// wave's load is 1 KiB of consecutive bytes, and a group of whole rows is
-// consecutive too.  Rows past the last one and columns past d are zeros.
+// instruction of 16 rows by 128 columns takes from it with one instruction, lane
+// after lane, and a group of whole rows is consecutive too.  (With a row's four
+// blocks side by side, 64 bytes, a wave's load was the same 1 KiB in another order
+// of lanes, and the loads alone took longer than the products: 2048 four-bit
+// contexts over 128256 x 4096 675 us, with or without the products.)  Rows past the last one and columns past d are zeros.
+// A group is an odd number of 256-byte pieces (256 bytes of zeros behind it where need
+// be): the same columns of all groups would otherwise lie in a part of the memory
+// channels, where every compute unit works on the same columns at a time.
 #pragma once
 
 #include "dyna_internal.h"
@@ -33,6 +38,10 @@ struct QuantView {
     int64_t group_bytes;
 };
 
+// Bytes of a group that hold something.
+__host__ __device__ inline int64_t quant_group_used(int32_t steps, int32_t units) {
+    return (int64_t)steps * kQuantStepBytes + (int64_t)units * kQuantScaleBytes;
+}
 __host__ __device__ inline QuantView quant_view(const void* data, int32_t rows, int32_t d) {
     QuantView q;
     q.data = static_cast<const uint8_t*>(data);
@@ -40,7 +49,8 @@ __host__ __device__ inline QuantView quant_view(const void* data, int32_t rows, 
     q.d = d;
     q.steps = (d + kQuantStep - 1) / kQuantStep;
     q.units = (q.steps + kQuantUnitSteps - 1) / kQuantUnitSteps;
-    q.group_bytes = (int64_t)q.steps * kQuantStepBytes + (int64_t)q.units * kQuantScaleBytes;
+    const int64_t bytes = quant_group_used(q.steps, q.units);
+    q.group_bytes = bytes + (bytes / 256 % 2 == 0 ? 256 : 0);
     return q;
 }
 inline size_t quant_bytes(int32_t rows, int32_t d) {

@@ -23,7 +23,10 @@ template <typename T>
 __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* __restrict__ x, int64_t row_stride,
                                                                        QuantView q, uint8_t* __restrict__ data,
                                                                        int64_t n_items) {
-    __shared__ __attribute__((aligned(16))) uint32_t codes[kQuantWaves][kQuantUnitSteps * kQuantStepBytes / 4];
+    // 16 blocks of a unit, rows one after the other; a piece to spare between blocks, so
+    // that a row's codes go to different banks
+    constexpr int kBlock = kMfmaRows * 4 + 4;
+    __shared__ __attribute__((aligned(16))) uint32_t codes[kQuantWaves][kQuantUnit / kQuantBlock * kBlock];
     __shared__ __attribute__((aligned(16))) uint8_t scales[kQuantWaves][kQuantScaleBytes];
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t item = (int64_t)blockIdx.x * kQuantWaves + wv;
@@ -32,8 +35,8 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
     const int steps = min(kQuantUnitSteps, q.steps - u * kQuantUnitSteps);
     const int col = u * kQuantUnit + lane * 8, left = q.d - col;
     const int step = lane >> 4, g = (lane >> 2) & 3;
-    uint32_t* cw = codes[wv] + step * (kQuantStepBytes / 4) + (lane & 15);
-    uint8_t* sw = scales[wv] + g * 4 + step;
+    uint32_t* cw = codes[wv] + (lane >> 2) * kBlock + (lane & 3);
+    uint8_t* sw = scales[wv] + g * 64 + step;
 #pragma unroll
     for (int h = 0; h < kMfmaRows; h += kQuantHalf) {
         Row8<T> in[kQuantHalf];
@@ -63,8 +66,8 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
             code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2] * inverse, v[3] * inverse, 1.0f, 1);
             code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4] * inverse, v[5] * inverse, 1.0f, 2);
             code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6] * inverse, v[7] * inverse, 1.0f, 3);
-            cw[(h + i) * 16] = bad ? 0u : code;
-            if ((lane & 3) == 0) sw[(h + i) * 16] = bad ? 255 : (uint8_t)scale;
+            cw[(h + i) * 4] = bad ? 0u : code;
+            if ((lane & 3) == 0) sw[(h + i) * 4] = bad ? 255 : (uint8_t)scale;
         }
     }
     wave_lds_order();
@@ -73,9 +76,12 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
     for (int j = 0; j < kQuantUnitSteps; ++j)
         if (j < steps)
             *reinterpret_cast<u32x4*>(out + j * kQuantStepBytes + lane * 16) =
-                *reinterpret_cast<const u32x4*>(codes[wv] + j * (kQuantStepBytes / 4) + lane * 4);
+                *reinterpret_cast<const u32x4*>(codes[wv] + (j * 4 + (lane >> 4)) * kBlock + (lane & 15) * 4);
     *reinterpret_cast<uint32_t*>(out + steps * kQuantStepBytes + lane * 4) =
         *reinterpret_cast<const uint32_t*>(scales[wv] + lane * 4);
+    const int64_t used = quant_group_used(q.steps, q.units);
+    if (u == q.units - 1 && q.group_bytes > used)
+        *reinterpret_cast<uint32_t*>(data + group * q.group_bytes + used + lane * 4) = 0u;
 }
 
 // Eight values of a row from its code word and scale.
@@ -101,13 +107,13 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void dequantize_kernel(QuantVie
     const int step = lane >> 4, g = (lane >> 2) & 3;
     if (left <= 0) return;  // the lane's step is one of the unit's then: steps cover d
     const uint8_t* in = q.data + group * q.group_bytes + (int64_t)u * kQuantUnitBytes;
-    const uint8_t* cr = in + step * kQuantStepBytes + (lane & 15) * 4;
-    const uint8_t* sr = in + steps * kQuantStepBytes + g * 16 / 4 + step;
+    const uint8_t* cr = in + step * kQuantStepBytes + g * 256 + (lane & 3) * 4;
+    const uint8_t* sr = in + steps * kQuantStepBytes + g * 64 + step;
     uint32_t code[kMfmaRows], scale[kMfmaRows];
 #pragma unroll
     for (int i = 0; i < kMfmaRows; ++i) {
-        code[i] = *reinterpret_cast<const uint32_t*>(cr + i * 64);
-        scale[i] = sr[i * 16];
+        code[i] = *reinterpret_cast<const uint32_t*>(cr + i * 16);
+        scale[i] = sr[i * 4];
     }
 #pragma unroll
     for (int i = 0; i < kMfmaRows; ++i) {

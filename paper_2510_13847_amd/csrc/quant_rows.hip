@@ -101,7 +101,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
     auto load_rows = [&](int set, const QuantTile& t) __attribute__((always_inline)) {
         const int r = t.r0 + (PLAN ? min(col, t.nrows - 1) : col);
         const uint8_t* p = a.W.data + (int64_t)(r / kMfmaRows) * a.W.group_bytes + wv * kQuantUnitBytes;
-        const int at = (r % kMfmaRows) * 64 + g * 16;
+        const int at = (r % kMfmaRows) * 16 + g * 256;
         // steps that the unit lacks repeat its last one; their contexts are zero
 #pragma unroll
         for (int j = 0; j < kQuantUnitSteps; ++j)
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
         if (c >= 0) {
             if constexpr (ACT == kActFour) {
                 const uint8_t* p = a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes + wv * kQuantUnitBytes;
-                const int at = (c % kMfmaRows) * 64 + g * 16;
+                const int at = (c % kMfmaRows) * 16 + g * 256;
 #pragma unroll
                 for (int j = 0; j < kQuantUnitSteps; ++j)
                     if (j < steps) b[j][0] = *reinterpret_cast<const u32x4*>(p + j * kQuantStepBytes + at);

@@ -58,16 +58,18 @@ template <int ACT, int NR, int NC, int WR, int WC, typename OT>
 struct TileShape {
     static constexpr int ROWS = 32 * WR * NR, CTX = 32 * WC * NC, GROUPS = CTX / 16, WAVES = WR * WC;
     static constexpr int TERMS = ACT == kActF32 ? 3 : 1;
-    static constexpr int PIECES = ACT == kActFour ? GROUPS : TERMS * 4 * GROUPS;  // of a stage
+    // four-bit tiles that several columns of waves share have their rows in LDS too
+    static constexpr bool ROWS_LDS = ACT == kActFour && WC > 1 && NR > 1;
+    static constexpr int ROW_PIECES = ROWS_LDS ? ROWS / 16 : 0;
+    static constexpr int PIECES = (ACT == kActFour ? GROUPS : TERMS * 4 * GROUPS) + ROW_PIECES;  // of a stage
     static constexpr int STAGE = PIECES * kPiece;
     // stages in LDS: a unit's four where a compute unit holds two workgroups of them
-    static constexpr int RING = 4 * STAGE <= 80 * 1024 ? 4 : 2, AHEAD = RING - 1;
-    // four-bit contexts' scales, of a unit at a time
-    static constexpr int SCALES = ACT == kActFour ? GROUPS * kQuantScaleBytes : 0;
+    static constexpr int RING = ROWS_LDS || 4 * STAGE <= 80 * 1024 ? 4 : 2, AHEAD = RING - 1;
+    // scales of four-bit pieces, of a unit at a time
+    static constexpr int SCALES = ACT == kActFour ? PIECES * kQuantScaleBytes : 0;
     static_assert(PIECES % WAVES == 0, "each wave loads as many pieces");
-    static_assert(ACT != kActFour || GROUPS % WAVES == 0, "and scales");
     static constexpr int NI = PIECES / WAVES;
-    static constexpr int LOADS = NI + 2 * NR;  // of a wave and stage, scales left out
+    static constexpr int LOADS = NI + (ROWS_LDS ? 0 : 2 * NR);  // of a wave and stage, scales left out
     // products on their way out: 32 contexts of a wave's rows, and a piece to spare so
     // that contexts start in different banks
     static constexpr int OUT_ROW = 32 * NR * (int)sizeof(OT) + 16;
@@ -140,14 +142,21 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
         const int group = min(((rt * WR + wr) * NR + r) * 2 + ((lane >> 4) & 1), last_group);
         wp[r] = a.W.data + (int64_t)group * a.W.group_bytes;
     }
-    const int row_at = (lane & 15) * 64 + half * 16;         // columns 0 .. 63 of a step; 64 .. are 32 bytes on
-    const int ctx_at = (lane & 15) * 64 + (lane >> 4) * 16;  // four-bit contexts: a whole step of 16
+    const int row_at = (lane & 15) * 16 + half * 256;  // columns 0 .. 63 of a step; 64 .. are 512 bytes on
     // this lane's operand in a stage: blocks 0 and 1 of a step; 2 and 3 are 512 bytes on
     const int lds_at = wc * NC * 2 * kPiece + ((lane >> 4) & 1) * kPiece + half * 256 + (lane & 15) * 16;
     char* scales = smem + Sh::RING * Sh::STAGE;
-    u32x4 w[Sh::RING][NR][2];
+    // rows: a stage's operands (those in LDS: of the one in use) and their scales
+    u32x4 w[Sh::ROWS_LDS ? 1 : Sh::RING][NR][2];
     uint32_t ws[NR][2], ws_next[NR][2];
 
+    // a stage's four-bit pieces: its contexts' groups of 16, then its rows'
+    auto four_bits = [&](int piece) {
+        const bool row = piece >= Sh::GROUPS;
+        const int group = row ? min(rt * (Sh::ROWS / 16) + piece - Sh::GROUPS, last_group)
+                              : min(ct * Sh::GROUPS + piece, (a.B - 1) / kMfmaRows);
+        return (row ? a.W.data : a.a4.data) + (int64_t)group * a.W.group_bytes;  // (both have d columns)
+    };
     auto unit_steps = [&](int unit) { return min(kQuantUnitSteps, steps - unit * kQuantUnitSteps); };
     // the scales of a unit: rows' to registers, contexts' to LDS.  A unit past the
     // last one repeats it.
@@ -155,43 +164,49 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
         unit = min(unit, units - 1);
         const int64_t at = (int64_t)unit * kQuantUnitBytes + unit_steps(unit) * kQuantStepBytes;
         if constexpr (ACT == kActFour) {
-            const int last = (a.B - 1) / kMfmaRows;
 #pragma unroll
-            for (int i = 0; i < Sh::GROUPS / Sh::WAVES; ++i) {
-                const int g = wv * (Sh::GROUPS / Sh::WAVES) + i;
-                load_scales(a.a4.data + (int64_t)min(ct * Sh::GROUPS + g, last) * a.a4.group_bytes + at, ctx_at / 4,
-                            scales + (unit & 1) * Sh::SCALES + g * kQuantScaleBytes);
+            for (int i = 0; i < Sh::NI; ++i) {
+                const int piece = wv * Sh::NI + i;
+                load_scales(four_bits(piece) + at, lane * 4, scales + (unit & 1) * Sh::SCALES + piece * kQuantScaleBytes);
             }
         }
+        if constexpr (!Sh::ROWS_LDS)
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                ws_next[r][h] = *reinterpret_cast<const uint32_t*>(wp[r] + at + row_at / 4 + h * 8);
+                ws_next[r][h] = *reinterpret_cast<const uint32_t*>(wp[r] + at + row_at / 4 + h * 128);
     };
     // stage `step` into ring place p: contexts to LDS, rows to registers.  Stages
     // past the last one repeat it.
-    auto load = [&](int step, auto place) __attribute__((always_inline)) {
+    auto step_at = [&](int step) {
+        return (int64_t)(step / kQuantUnitSteps) * kQuantUnitBytes + step % kQuantUnitSteps * kQuantStepBytes;
+    };
+    auto load_contexts = [&](int step, auto place) __attribute__((always_inline)) {
         constexpr int p = decltype(place)::value;
         step = min(step, steps - 1);
-        const int64_t at = (int64_t)(step / kQuantUnitSteps) * kQuantUnitBytes + step % kQuantUnitSteps * kQuantStepBytes;
+        const int64_t at = step_at(step);
         char* stage = smem + p * Sh::STAGE;
 #pragma unroll
         for (int i = 0; i < Sh::NI; ++i) {
             const int piece = wv * Sh::NI + i;  // (term, s) major, group minor
             if constexpr (ACT == kActFour) {
-                const int group = min(ct * Sh::GROUPS + piece, (a.B - 1) / kMfmaRows);
-                load_piece(a.a4.data + (int64_t)group * a.a4.group_bytes + at, ctx_at, stage + piece * kPiece);
+                load_piece(four_bits(piece) + at, lane * 16, stage + piece * kPiece);
             } else {
                 const int64_t from = ((int64_t)step * Sh::TERMS * 4 + piece / Sh::GROUPS) * grid.groups +
                                      ct * Sh::GROUPS + piece % Sh::GROUPS;
                 load_piece(grid.operand + from * kPiece, lane * 16, stage + piece * kPiece);
             }
         }
+    };
+    auto load_rows = [&](int step, auto place) __attribute__((always_inline)) {
+        constexpr int p = decltype(place)::value;
+        const int64_t at = step_at(min(step, steps - 1));
+        if constexpr (!Sh::ROWS_LDS)
 #pragma unroll
         for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w[p][r][h] = *reinterpret_cast<const u32x4*>(wp[r] + at + row_at + h * 32);
+            for (int h = 0; h < 2; ++h) w[p][r][h] = *reinterpret_cast<const u32x4*>(wp[r] + at + row_at + h * 512);
     };
 
     f32x16 acc[NR][NC];
@@ -202,37 +217,95 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[r][c][i] = 0.0f;
 
+    // Four-bit products run in quarters of a stage (half the columns, half the
+    // contexts).  A quarter's operands are read while the one before runs, and a
+    // stage's last quarter runs behind the barrier that starts the next stage, so that
+    // its products cover that stage's first reads.  (The order is pinned; left alone,
+    // the compiler sinks the reads to their uses.)
+    constexpr int HC = ACT == kActFour && NC > 1 ? NC / 2 : 1;  // contexts' blocks of a quarter
+    constexpr int QUARTERS = 2 * NC / HC;
+    u32x4 b[2][HC];
+    uint32_t bs[2][HC];
+    auto fetch = [&](int unit, auto place, auto quarter) __attribute__((always_inline)) {
+        constexpr int p = decltype(place)::value, k = decltype(quarter)::value, set = k & 1;
+        constexpr int h = k * HC / NC, c0 = k * HC % NC;
+        const char* at = smem + p * Sh::STAGE + lds_at + h * 512;
+        const char* sc = scales + (unit & 1) * Sh::SCALES + lds_at / 4 + h * 128;
+#pragma unroll
+        for (int c = 0; c < HC; ++c) {
+            b[set][c] = *reinterpret_cast<const u32x4*>(at + (c0 + c) * 2 * kPiece);
+            bs[set][c] = *reinterpret_cast<const uint32_t*>(sc + (c0 + c) * 2 * kQuantScaleBytes);
+        }
+        if constexpr (Sh::ROWS_LDS && c0 == 0) {
+            const int row_pieces = (Sh::GROUPS + (wr * NR - wc * NC) * 2) * kPiece;  // from this wave's contexts on
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                w[0][r][h] = *reinterpret_cast<const u32x4*>(at + row_pieces + r * 2 * kPiece);
+                ws[r][h] = *reinterpret_cast<const uint32_t*>(sc + row_pieces / 4 + r * 2 * kQuantScaleBytes);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](auto in_unit, auto quarter) __attribute__((always_inline)) {
+        constexpr int j = decltype(in_unit)::value, p = j % Sh::RING, k = decltype(quarter)::value, set = k & 1;
+        constexpr int h = k * HC / NC, c0 = k * HC % NC;
+#pragma unroll
+        for (int c = 0; c < HC; ++c)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                acc[r][c0 + c] = four_bit_product<j>(w[Sh::ROWS_LDS ? 0 : p][r][h], ws[r][h], b[set][c], bs[set][c], acc[r][c0 + c]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
     // step j of a unit.  `more`: loads go on AHEAD stages before their use.
     auto stage = [&](int unit, auto in_unit, auto more) __attribute__((always_inline)) {
         constexpr int j = decltype(in_unit)::value, p = j % Sh::RING;
+        constexpr bool ahead = decltype(more)::value;
+        using Next = std::integral_constant<int, (p + Sh::AHEAD) % Sh::RING>;
+        const int next = unit * kQuantUnitSteps + j + Sh::AHEAD;
         // This stage has arrived, and everyone has read the one whose place is next.
         // At least LOADS loads were issued in each of the AHEAD - 1 stages since its own;
         // where those may be fewer, all are waited for.
-        if constexpr (decltype(more)::value) {
-            loads_barrier<(Sh::AHEAD - 1) * Sh::LOADS>();
-            load(unit * kQuantUnitSteps + j + Sh::AHEAD, std::integral_constant<int, (p + Sh::AHEAD) % Sh::RING>{});
-            if constexpr (j == 0) load_unit(unit + 1);
-        } else {
-            loads_barrier<0>();
-        }
-        const char* at = smem + p * Sh::STAGE + lds_at;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (ACT == kActFour) {
-                u32x4 b[NC];
-                uint32_t bs[NC];
-                const char* sc = scales + (unit & 1) * Sh::SCALES + lds_at / 4 + h * 128;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    b[c] = *reinterpret_cast<const u32x4*>(at + c * 2 * kPiece + h * 512);
-                    bs[c] = *reinterpret_cast<const uint32_t*>(sc + c * 2 * kQuantScaleBytes);
-                }
+        loads_barrier<ahead ? (Sh::AHEAD - 1) * Sh::LOADS : 0>();
+        if constexpr (ahead) load_contexts(next, Next{});
+        if constexpr (ACT == kActFour) {
+            using Place = std::integral_constant<int, p>;
+            fetch(unit, Place{}, std::integral_constant<int, 0>{});
+            // the last quarter of the step before (of zeros in the first one)
+            multiply(std::integral_constant<int, (j + 3) % 4>{}, std::integral_constant<int, QUARTERS - 1>{});
+            if constexpr (j == 0 && !Sh::ROWS_LDS)
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
 #pragma unroll
-                    for (int c = 0; c < NC; ++c)
-                        acc[r][c] = four_bit_product<j>(w[p][r][h], ws[r][h], b[c], bs[c], acc[r][c]);
+                    for (int h = 0; h < 2; ++h) ws[r][h] = ws_next[r][h];
+            if constexpr (ahead) {
+                load_rows(next, Next{});
+                if constexpr (j == 0) load_unit(unit + 1);
+            }
+            if constexpr (QUARTERS == 4) {
+                fetch(unit, Place{}, std::integral_constant<int, 1>{});
+                multiply(in_unit, std::integral_constant<int, 0>{});
+                fetch(unit, Place{}, std::integral_constant<int, 2>{});
+                multiply(in_unit, std::integral_constant<int, 1>{});
+                fetch(unit, Place{}, std::integral_constant<int, 3>{});
+                multiply(in_unit, std::integral_constant<int, 2>{});
             } else {
+                fetch(unit, Place{}, std::integral_constant<int, 1>{});
+                multiply(in_unit, std::integral_constant<int, 0>{});
+            }
+        } else {
+            if constexpr (j == 0)
+#pragma unroll
+                for (int r = 0; r < NR; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) ws[r][h] = ws_next[r][h];
+            if constexpr (ahead) {
+                load_rows(next, Next{});
+                if constexpr (j == 0) load_unit(unit + 1);
+            }
+            const char* at = smem + p * Sh::STAGE + lds_at;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     bf16x8 x[NR];
@@ -242,34 +315,42 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
                     for (int t = 0; t < Sh::TERMS; ++t)
 #pragma unroll
                         for (int c = 0; c < NC; ++c) {
-                            const u32x4 b = *reinterpret_cast<const u32x4*>(
+                            const u32x4 y = *reinterpret_cast<const u32x4*>(
                                 at + (t * 4 + s) * Sh::GROUPS * kPiece + c * 2 * kPiece + h * 512);
 #pragma unroll
                             for (int r = 0; r < NR; ++r)
                                 acc[r][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                                    x[r], __builtin_bit_cast(bf16x8, b), acc[r][c], 0, 0, 0);
+                                    x[r], __builtin_bit_cast(bf16x8, y), acc[r][c], 0, 0, 0);
                         }
                 }
-            }
         }
-    };
-    auto next_unit = [&]() {
-#pragma unroll
-        for (int r = 0; r < NR; ++r)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) ws[r][h] = ws_next[r][h];
     };
     using J0 = std::integral_constant<int, 0>;
     using J1 = std::integral_constant<int, 1>;
     using J2 = std::integral_constant<int, 2>;
     using J3 = std::integral_constant<int, 3>;
-    load_unit(0);
-    load(0, J0{});
-    if constexpr (Sh::AHEAD == 3) {
-        load(1, J1{});
-        load(2, J2{});
+    if constexpr (ACT == kActFour) {
+        const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            w[Sh::ROWS_LDS ? 0 : Sh::RING - 1][r][1] = zero;
+            ws[r][1] = 0;
+        }
+#pragma unroll
+        for (int c = 0; c < HC; ++c) {
+            b[1][c] = zero;
+            bs[1][c] = 0;
+        }
     }
-    next_unit();
+    load_unit(0);
+    load_contexts(0, J0{});
+    load_rows(0, J0{});
+    if constexpr (Sh::AHEAD == 3) {
+        load_contexts(1, J1{});
+        load_rows(1, J1{});
+        load_contexts(2, J2{});
+        load_rows(2, J2{});
+    }
     // (whole units without a branch inside, so that the compiler counts the loads in
     // flight exactly)
     int unit = 0;
@@ -278,7 +359,6 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
         stage(unit, J1{}, std::true_type{});
         stage(unit, J2{}, std::true_type{});
         stage(unit, J3{}, std::true_type{});
-        next_unit();
     }
     // the last unit's steps are in the ring already, or come one by one
     using More = std::integral_constant<bool, Sh::AHEAD == 1>;
@@ -286,6 +366,13 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
     if (left > 0) stage(unit, J0{}, More{});
     if (left > 1) stage(unit, J1{}, More{});
     if (left > 2) stage(unit, J2{}, More{});
+    if constexpr (ACT == kActFour) {
+        using Last = std::integral_constant<int, QUARTERS - 1>;
+        if (left == 0) multiply(J3{}, Last{});
+        else if (left == 1) multiply(J0{}, Last{});
+        else if (left == 2) multiply(J1{}, Last{});
+        else multiply(J2{}, Last{});
+    }
     loads_barrier<0>();  // nothing lands in LDS any more, and everyone has read it
 
     // A lane holds context l % 32 of a block, rows 8 q + 4 (l / 32) .. + 3: they leave
