@@ -63,45 +63,71 @@ __device__ __forceinline__ int token_of_slot(const ScoreArgs& a, const RowSlots&
 }
 
 // ---------------------------------------------------------------- sums
-// A thread's share of a row: largest logit m, sum of w = exp2((z - m) c), c =
-// log2(e) / T, and of w (z - m) c.  Weights are 32 bits; sums of eight go on in 64.
+// A thread's share of a row, in powers of two with c = log2(e) / T: its largest logit
+// m, and relative to `base`, which is m c, the sums of w = 2^(z c - base) and of w (z c
+// - base).  z c - base is one fused multiply-add with base rounded to 32 bits, and the
+// sums' base is that rounded number; past 2^20, where its rounding would move the
+// weights by more than 2^(1/32), it is (z - m) c, relative to m c itself.  Weights are 32 bits, summed 32 at a time by pairs, or in runs
+// of four, and from there on in 64.
 struct RowSum {
-    float m = kNegInf;
+    float m = kNegInf, ref = 0.0f;
+    bool wide = false;
     double s = 0.0, u = 0.0;
-    __device__ __forceinline__ void rescale(float top, float c) {
+    __device__ __forceinline__ double base(float c) const { return wide ? (double)m * (double)c : (double)ref; }
+    __device__ __forceinline__ void raise(float top, float c) {
         if (top > m) {
-            const float y = (m - top) * c;
-            if (m > kNegInf) {
-                const double f = (double)__builtin_amdgcn_exp2f(y);
-                u = f * (u + s * (double)fmaxf(y, -1000.0f));
-                s *= f;
-            }
+            const double before = base(c);
+            const bool some = m > kNegInf;
             m = top;
+            ref = m * c;
+            wide = !(fabsf(ref) <= 0x1p20f);
+            if (some) {
+                const float y = (float)(before - base(c)), f = __builtin_amdgcn_exp2f(y);
+                u = (double)f * (u + s * (double)fmaxf(y, -1000.0f));
+                s *= (double)f;
+            }
         }
     }
     // A NaN or +inf logit makes s NaN and with it the row.
-    __device__ __forceinline__ void add(const float (&z)[8], float top, float c) {
-        rescale(top, c);
-        const float ref = m > kNegInf ? m : 0.0f;
-        float e[8], x = 0.0f;
+    template <int F>
+    __device__ __forceinline__ void add(const float (&z)[F][8], float c) {
+        if (wide) add_from<F, true>(z, c);
+        else add_from<F, false>(z, c);
+    }
+    template <int F, bool WIDE>
+    __device__ __forceinline__ void add_from(const float (&z)[F][8], float c) {
+        float part[F], dot[F];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float y = (z[k] - ref) * c;
-            e[k] = __builtin_amdgcn_exp2f(y);
-            x = fmaf(e[k], fmaxf(y, -1000.0f), x);  // 0 for a masked logit, not 0 times infinity
+        for (int i = 0; i < F; ++i) {
+            float e[8], y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                y[k] = WIDE ? (z[i][k] - m) * c : fmaf(z[i][k], c, -ref);
+                e[k] = __builtin_amdgcn_exp2f(y[k]);
+                y[k] = fmaxf(y[k], -1000.0f);  // a masked logit adds 0, not 0 times infinity
+            }
+            part[i] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+            dot[i] = fmaf(e[3], y[3], fmaf(e[2], y[2], fmaf(e[1], y[1], e[0] * y[0]))) +
+                     fmaf(e[7], y[7], fmaf(e[6], y[6], fmaf(e[5], y[5], e[4] * y[4])));
         }
-        s += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
-        u += (double)x;
+#pragma unroll
+        for (int n = F / 2; n > 0; n /= 2)
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                part[i] += part[i + n];
+                dot[i] += dot[i + n];
+            }
+        s += (double)part[0];
+        u += (double)dot[0];
     }
 };
 
-// Sums of a part seen from another largest logit.
-__device__ __forceinline__ void seen_from(float m, double c, double& s, double& u, float from) {
-    if (from > kNegInf && from < m) {
-        const double y = ((double)from - (double)m) * c, f = exp2(y);
-        u = f == 0.0 ? 0.0 : f * (u + s * y);
-        s *= f;
-    }
+// Sums relative to `from` (a power of two's exponent) seen from `to`.
+__device__ __forceinline__ void seen_from(double to, double& s, double& u, double from) {
+    if (s == 0.0) return;
+    const double y = from - to, f = exp2(y);
+    u = f == 0.0 ? 0.0 : f * (u + s * y);
+    s *= f;
 }
 
 // ---------------------------------------------------------------- best tokens
@@ -198,35 +224,45 @@ __device__ __forceinline__ int rank_in_list(const TopLds& w, int n, uint64_t* ke
     return (int)threadIdx.x < n ? rank : INT32_MAX;
 }
 
-// Adds a sweep's candidates to the list: the logits that reach `floor`, which at
-// least k of those before do (or of this sweep, the row's first).  Most sweeps
-// behind the first add a few and some none.  Where they are too many (rising or
-// equal logits), the sweep starts again behind a floor of its own: at most k - 1
-// threads have a logit above the k-th largest of the threads' maxima, and of those
-// equal to it the k lowest tokens are enough.
-template <int F>
+template <typename T>
+__device__ __forceinline__ float logit_at(const T* row, int v, int v1) { return v < v1 ? to_f32(row[v]) : kNegInf; }
+
+// Adds a sweep's candidates to the list: the logits that reach `floor`, which at least
+// k of this sweep and those before do.  The floor is the k-th largest of the threads'
+// largest logits so far (`highest`), found again after 1, 2, 4, .. sweeps (`look`), so
+// that a row adds about k candidates each time it doubles.  Where a sweep's are too
+// many for the list (equal logits), it starts again behind a floor of its own: at most
+// k - 1 threads have a logit above the k-th largest of the threads' maxima, and of
+// those equal to it the k lowest tokens are enough.  Those logits are read again.
+template <typename T, int F>
 __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& row, TopLds& w, const float (&z)[F][8],
-                                          int at, float most, bool first, int k) {
-    float floor = first ? kth_of_threads<16>(w, most, k) : w.floor;
+                                          const float (&tops)[F], float most, float highest, bool look, const T* logits,
+                                          int at, int v1, int k) {
+    float floor = w.floor;
     const int before = w.n;
-    auto each = [&](auto&& f) {
-#pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f(z[i][e], at + i * kVecStep + e);
-    };
+    if (look) floor = fmaxf(floor, kth_of_threads<16>(w, highest, k));
     auto push = [&](float x, int slot) {
         const int p = atomicAdd(&w.n, 1);
         if (p < kCap) w.keys[p] = sel_key(x, (uint32_t)token_of_slot(a, row, slot));
     };
     lds_barrier();  // `before` and the floor have been read
     if (most >= floor && most > kNegInf)
-        each([&](float x, int slot) {
-            if (x >= floor && x > kNegInf) push(x, slot);
-        });
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+            if (tops[i] >= floor)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (z[i][e] >= floor && z[i][e] > kNegInf) push(z[i][e], at + i * kVecStep + e);
     lds_barrier();
     int n = w.n;
     if (n > kCap) {
+        auto each = [&](auto&& f) {
+#pragma unroll 1
+            for (int i = 0; i < F * 8; ++i) {
+                const int slot = at + (i >> 3) * kVecStep + (i & 7);
+                f(logit_at(logits, slot, v1), slot);
+            }
+        };
         lds_barrier();
         if (threadIdx.x == 0) w.n = before;
         floor = fmaxf(floor, kth_of_threads<32>(w, most, k));  // with barriers
@@ -236,7 +272,7 @@ __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& ro
             });
         // the tokens of equal logits up to `last`, k of them or all
         int equal = 0;
-        each([&](float x, int) { equal += x == floor; });
+        each([&](float x, int) { equal += x == floor && x > kNegInf; });
         int last = INT32_MAX;
         if (block_count(w, equal, 0) > k) {
             last = 0;
@@ -337,23 +373,26 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
         if (at + 8 <= v1) in[i].load(row + at);
     }
     RowSum sum;
-    for (int base = v0; base < v1; base += kSweep) {
-        float z[kFlight][8], most = kNegInf;
+    int sweep = 0;
+    for (int base = v0; base < v1; base += kSweep, ++sweep) {
+        float z[kFlight][8], tops[kFlight], most = kNegInf;
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
             const int at = base + i * kVecStep + t * 8, next = at + kSweep;
             if (at + 8 <= v1) in[i].get(z[i]);
             else load_part(row + at, v1 - at, kNegInf, z[i]);
             if (next + 8 <= v1) in[i].load(row + next);
-            const float top = max8(z[i]);
-            sum.add(z[i], top, c);
-            most = fmaxf(most, top);
+            tops[i] = max8(z[i]);
+            most = fmaxf(most, tops[i]);
         }
-        if constexpr (TOP) add_sweep<kFlight>(a, w, best, z, base + t * 8, most, base == v0, a.top);
+        sum.raise(most, c);
+        sum.add(z, c);
+        if constexpr (TOP)
+            add_sweep(a, w, best, z, tops, most, sum.m, (sweep & (sweep + 1)) == 0, row, base + t * 8, v1, a.top);
     }
     const float m = block_max_f32<kST>(sum.m, tmp_f);
     double s = sum.s, u = sum.u;
-    seen_from(m, (double)c, s, u, sum.m);
+    if (sum.m > kNegInf) seen_from((double)m * (double)c, s, u, sum.base(c));
     s = block_sum_f64<kST>(s, tmp_d[0]);
     u = block_sum_f64<kST>(u, tmp_d[1]);
     int n = 0;
@@ -395,35 +434,43 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     ScorePart p{0.0, 0.0, kNegInf, 0.0f};
     if (t < a.splits) p = a.parts[(int64_t)r * a.splits + t];
     constexpr int E = kMaxParts * DYNA_MAX_KT / kST;
-    uint64_t x[E];
-    int n = 0;
+    uint64_t x[E], most = 0;
+    const int all = a.splits * a.top;
     if constexpr (TOP) {
-        const int all = a.splits * a.top;
         const uint64_t* lists = a.lists + (int64_t)r * all;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            x[i] = i * kST + t < all ? lists[i * kST + t] : 0;
-            n += x[i] != 0;
+            // parts are sorted: turned against each other, so that no thread has the best of many
+            const int at = i * kST + ((t + 37 * i) & (kST - 1));
+            x[i] = at < all ? lists[at] : 0;
+            most = max(most, x[i]);
         }
         if (t == 0) best.n = 0;
     }
     const float m = block_max_f32<kST>(p.m, tmp_f);
-    const float c = (float)(a.inv_t * 1.4426950408889634);
-    seen_from(m, (double)c, p.s, p.u, p.m);
+    const double c = (double)(float)(a.inv_t * 1.4426950408889634);
+    if (p.m > kNegInf) seen_from((double)m * c, p.s, p.u, (double)p.m * c);
     const double s = block_sum_f64<kST>(p.s, tmp_d[0]), u = block_sum_f64<kST>(p.u, tmp_d[1]);
     const RowResult q(m, s, u);
     if (t == 0) q.write(a, r);
     if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
     if constexpr (TOP) {
-        n = block_count(best, n, 0);
-        if (n > a.top) {
+        // the keys that reach the k-th largest of the threads' best, all where there are few
+        const float floor = all <= kST ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (x[i] != 0 && key_val(x[i]) >= floor) {
+                const int at = atomicAdd(&best.n, 1);
+                if (at < kCap) best.keys[at] = x[i];
+            }
+        lds_barrier();
+        int n = best.n;
+        if (n > kCap) {  // equal logits
             keep_best<E>(best, x, a.top);
             n = a.top;
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (x[i] != 0) best.keys[atomicAdd(&best.n, 1)] = x[i];
-            lds_barrier();
+        } else if (n > kST) {
+            shorten_list(best, n, a.top);
+            n = a.top;
         }
         write_best(a, r, best, n, q);
     }
