@@ -79,9 +79,6 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
                 *reinterpret_cast<const u32x4*>(codes[wv] + (j * 4 + (lane >> 4)) * kBlock + (lane & 15) * 4);
     *reinterpret_cast<uint32_t*>(out + steps * kQuantStepBytes + lane * 4) =
         *reinterpret_cast<const uint32_t*>(scales[wv] + lane * 4);
-    const int64_t used = quant_group_used(q.steps, q.units);
-    if (u == q.units - 1 && q.group_bytes > used)
-        *reinterpret_cast<uint32_t*>(data + group * q.group_bytes + used + lane * 4) = 0u;
 }
 
 // Eight values of a row from its code word and scale.

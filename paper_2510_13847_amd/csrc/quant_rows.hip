@@ -39,13 +39,12 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
     const int steps = min(kQuantUnitSteps, a.W.steps - wv * kQuantUnitSteps);  // of this wave's unit
     const int d = a.W.d;
 
-    // this workgroup's tiles: plans, a run of consecutive chunks; else every
-    // gridDim.x-th group
-    int c1 = 0, run0 = 0;  // plans: end of the run; first chunk of those with the same contexts
-    int at = 0;
+    // this workgroup's tiles: of a plan, a run of consecutive chunks; else every
+    // gridDim.x-th group of 16 rows
     sptr<int32_t> chunks = (sptr<int32_t>)a.plan.chunks;
-    auto read_tile = [&](int i, int first) {
-        QuantTile t{0, 0, 0, 0, 0};
+    int at = 0, c1 = 0, run0 = 0;  // plans: end of the run; first chunk of those with the same contexts
+    auto read_tile = [&](int i, int first) __attribute__((always_inline)) {
+        QuantTile t{0, 0, 0, 0, first};
         if constexpr (PLAN) {
             t.r0 = chunks[4 * i];
             t.nrows = min(kMfmaRows, chunks[4 * i + 1]);
@@ -56,10 +55,10 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
             t.nrows = min(kMfmaRows, a.n_rows - t.r0);
             t.cnt = a.B;
         }
-        t.first = first;
         return t;
     };
-    QuantTile cur{0, 0, 0, 0, 0};
+    constexpr QuantTile kNone{0, 0, 0, 0, 0};
+    QuantTile cur = kNone;
     if constexpr (PLAN) {
         const int64_t n = ((sptr<int32_t>)a.plan.hdr)[0];
         at = run0 = (int)(n * blockIdx.x / gridDim.x);
@@ -72,12 +71,12 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
     // The tile behind cur: plans walk the chunks of one context list once for each
     // CPP of its contexts.
     auto next_tile = [&]() __attribute__((always_inline)) -> QuantTile {
+        const int64_t i = at + (PLAN ? 1 : (int64_t)gridDim.x);
         if constexpr (PLAN) {
-            const int i = at + 1;
             if (i < c1) {
-                const QuantTile t = read_tile(i, cur.first);
+                const QuantTile t = read_tile((int)i, cur.first);
                 if (t.list == cur.list) {
-                    at = i;
+                    at = (int)i;
                     return t;
                 }
             }
@@ -85,11 +84,10 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
                 at = run0;
                 return read_tile(at, cur.first + CPP);
             }
-            at = run0 = i;
-            return i < c1 ? read_tile(i, 0) : QuantTile{0, 0, 0, 0, 0};
+            at = run0 = (int)i;
+            return i < c1 ? read_tile(at, 0) : kNone;
         } else {
-            const int64_t i = (int64_t)at + gridDim.x;
-            if (i * kMfmaRows >= a.n_rows) return QuantTile{0, 0, 0, 0, 0};
+            if (i * kMfmaRows >= a.n_rows) return kNone;
             at = (int)i;
             return read_tile(at, cur.first);
         }
@@ -111,77 +109,110 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
 
     // ---- contexts, in the operand layout
     constexpr int NS = ACT == kActFour ? 1 : 4;
+    constexpr int NE = MAXW < 4 ? 4 : 1;  // results of a thread at most: 256 of 64 threads, or of 256 and more
     u32x4 b[kQuantUnitSteps][NS];
     uint32_t bs = 0;
-    constexpr int NE = MAXW < 4 ? 4 : 1;  // results of a thread at most: 256 of 64 threads, or of 256 and more
-    constexpr int64_t kNowhere = INT64_MIN;
-    int64_t out_at[NE];          // where result i of this thread's context would go for layout row 0
-    auto load_contexts = [&](const QuantTile& t) __attribute__((always_inline)) {
-        auto context = [&](int c, int* slot) -> int {  // context c of this pass, -1 past the last
-            const int i = t.first + c;
-            *slot = 0;
-            if (c >= CPP || i >= t.cnt) return -1;
-            if constexpr (PLAN) {
-                const ListEntry e = a.plan.list[t.list + i];
-                *slot = e.slot_base;
-                return e.b;
+    // context c of a pass, and its slot of layout row 0; b < 0: none
+    auto context_of = [&](const QuantTile& t, int c) __attribute__((always_inline)) {
+        ListEntry e{-1, 0};
+        const int i = t.first + c;
+        if (c < CPP && i < t.cnt) {
+            if constexpr (PLAN) e = a.plan.list[t.list + i];
+            else e.b = i;
+        }
+        return e;
+    };
+    struct Seats {           // the contexts that a lane's column and a thread's results belong to
+        int column;
+        ListEntry result[NE];
+    };
+    auto seats_of = [&](const QuantTile& t) __attribute__((always_inline)) {
+        Seats s;
+        s.column = context_of(t, ACT == kActF32 ? col / 3 : col).b;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) s.result[i] = context_of(t, ((int)threadIdx.x + i * NT) >> 4);
+        return s;
+    };
+    // (a lane without a context takes context 0: its column goes nowhere)
+    const bool inside = (wv + 1) * kQuantUnit <= d;  // the whole unit holds columns
+    auto load_contexts = [&](int c) __attribute__((always_inline)) {
+        c = max(c, 0);
+        if constexpr (ACT == kActFour) {
+            const uint8_t* p = a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes + wv * kQuantUnitBytes +
+                               (c % kMfmaRows) * 16 + g * 256;
+#pragma unroll
+            for (int j = 0; j < kQuantUnitSteps; ++j) {
+                b[j][0] = u32x4{0u, 0u, 0u, 0u};
+                if (j < steps) b[j][0] = *reinterpret_cast<const u32x4*>(p + j * kQuantStepBytes);
             }
-            return i;
-        };
-        int slot;
-        const int c = context(ACT == kActF32 ? col / 3 : col, &slot);
+            bs = *reinterpret_cast<const uint32_t*>(a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes +
+                                                    wv * kQuantUnitBytes + steps * kQuantStepBytes +
+                                                    (c % kMfmaRows) * 4 + g * 64);
+        } else {
+            using T = typename std::conditional<ACT == kActBf16, uint16_t, float>::type;
+            const int k0 = wv * kQuantUnit + g * kQuantBlock;
+            const T* p = static_cast<const T*>(a.a) + (int64_t)c * a.a_stride + k0;
+            auto packed = [&](float (&x)[8]) {
+                u32x4 r;
+                if constexpr (ACT == kActF32)
 #pragma unroll
-        for (int j = 0; j < kQuantUnitSteps; ++j)
+                    for (int e = 0; e < 8; ++e) x[e] = term_of(x[e], col % 3);
 #pragma unroll
-            for (int s = 0; s < NS; ++s) b[j][s] = u32x4{0u, 0u, 0u, 0u};
-        if (c >= 0) {
-            if constexpr (ACT == kActFour) {
-                const uint8_t* p = a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes + wv * kQuantUnitBytes;
-                const int at = (c % kMfmaRows) * 16 + g * 256;
+                for (int e = 0; e < 4; ++e) r[e] = bf16_pair(x[2 * e], x[2 * e + 1]);
+                return r;
+            };
+            auto whole = [&](int k) {
+                if constexpr (ACT == kActBf16) return (u32x4)*reinterpret_cast<const u32x4_h*>(p + k);
+                Row8<T> r;
+                float x[8];
+                r.load(p + k);
+                r.get(x);
+                return packed(x);
+            };
 #pragma unroll
-                for (int j = 0; j < kQuantUnitSteps; ++j)
-                    if (j < steps) b[j][0] = *reinterpret_cast<const u32x4*>(p + j * kQuantStepBytes + at);
-                bs = *reinterpret_cast<const uint32_t*>(p + steps * kQuantStepBytes + at / 4);
-            } else {
+            for (int j = 0; j < kQuantUnitSteps; ++j)
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const int k = j * kQuantStep + s * 8;
+                    // (fp32 values become terms a few at a time where all do not fit)
+                    if constexpr (ACT == kActF32 && MAXW > 3)
+                        if (s % 2 == 0 && (MAXW > 8 || s == 0)) __builtin_amdgcn_sched_barrier(0);
+                    if (inside) {
+                        b[j][s] = whole(k);
+                    } else {
+                        b[j][s] = u32x4{0u, 0u, 0u, 0u};
+                        if (k0 + k + 8 <= d) b[j][s] = whole(k);
+                    }
+                }
+            if (!PLAN && !inside && d % 8 != 0) {  // a row's last, shorter piece (a layout's rows have none)
+                const int at = d / 8 * 8 - k0;
+                const bool mine = at >= 0 && at < kQuantUnit && at % kQuantStep < kQuantBlock;
+                float x[8];
+                load_part(p + (mine ? at : 0), mine ? d % 8 : 0, 0.0f, x);
+                const u32x4 r = packed(x);
 #pragma unroll
                 for (int j = 0; j < kQuantUnitSteps; ++j)
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
-                        const int k = wv * kQuantUnit + j * kQuantStep + g * kQuantBlock + s * 8;
-                        if (k >= d) continue;
-                        float x[8];
-                        if constexpr (ACT == kActBf16) {
-                            load_part(static_cast<const uint16_t*>(a.a) + (int64_t)c * a.a_stride + k, d - k, 0.0f, x);
-                        } else {
-                            load_part(static_cast<const float*>(a.a) + (int64_t)c * a.a_stride + k, d - k, 0.0f, x);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = term_of(x[e], col % 3);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) b[j][s][e] = bf16_pair(x[2 * e], x[2 * e + 1]);
+                        const uint32_t here = mine && at == j * kQuantStep + s * 8 ? ~0u : 0u;
+                        b[j][s] |= r & here;  // zeros so far
                     }
             }
-        }
-#pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            const int o = (int)threadIdx.x + i * NT;
-            out_at[i] = kNowhere;
-            if (o >= kOut) break;
-            int base;
-            const int x = context(o >> 4, &base);
-            if (x >= 0) out_at[i] = (int64_t)x * a.ld + base;
         }
     };
 
     if (cur.nrows == 0) return;  // whole workgroup
     load_rows(0, cur);
-    load_contexts(cur);
+    Seats seats = seats_of(cur);
+    load_contexts(seats.column);
     OT* out = static_cast<OT*>(a.out);
-    int set = 0;
     auto tile = [&](auto set_tag) __attribute__((always_inline)) {
         constexpr int S = decltype(set_tag)::value;
         const QuantTile nxt = next_tile();
         load_rows(1 - S, nxt.nrows > 0 ? nxt : cur);
+        const bool other = PLAN && nxt.nrows > 0 && (nxt.list != cur.list || nxt.first != cur.first);
+        Seats later = seats;
+        if (other) later = seats_of(nxt);
         f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         if constexpr (ACT == kActFour) {
             auto product = [&](auto j_tag) {
@@ -202,6 +233,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
                                                                          row_operand(w[S][j][s], scale), acc[s & 1], 0, 0, 0);
             }
         }
+        if (other) load_contexts(later.column);  // under way while the sums are joined
         // lane: columns 4 g .. 4 g + 3 of the product with row lane % 16
         red[S][wv][lane] = acc[0] + acc[1];
         lds_barrier();  // the other buffer's readers have passed the barrier before
@@ -209,7 +241,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
             const int o = (int)threadIdx.x + i * NT;
-            if (o >= kOut || out_at[i] == kNowhere) continue;
+            if (o >= kOut || seats.result[i].b < 0) continue;
             const int row = o & 15, ctx = o >> 4;
             float x = 0.0f;
 #pragma unroll
@@ -218,11 +250,11 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
                 const int p = (((c >> 2) * 16 + row) << 2) + (c & 3);
                 for (int v = 0; v < NW; ++v) x += sums[v * kWave * 4 + p];
             }
-            if (row < cur.nrows) store_elt(out + out_at[i] + cur.r0 + row, x);
+            if (row < cur.nrows)
+                store_elt(out + (int64_t)seats.result[i].b * a.ld + seats.result[i].slot_base + cur.r0 + row, x);
         }
-        const bool other = PLAN && nxt.nrows > 0 && (nxt.list != cur.list || nxt.first != cur.first);
         cur = nxt;
-        if (other) load_contexts(cur);
+        seats = later;
     };
     while (true) {
         tile(std::integral_constant<int, 0>{});

@@ -429,16 +429,18 @@ int operand_groups(int32_t B) {
     return (groups + kMostGroups - 1) / kMostGroups * kMostGroups;
 }
 
+// Tiles by the contexts, so that few columns of the products are computed for nothing
+// and rows are read few times, with the most rows that still leave every compute unit a
+// tile.  bf16 contexts over 128256 x 4096, us: 32 contexts 53 (tiles of 32); 64 73 (64);
+// 70 121 (128; 134 with two of 64, or eight waves of 64 by 64); 128 133 (138, 142; 187
+// with one of 256); 192 207 (256).  fp32 contexts' three terms fill LDS with 64.
 template <int ACT, typename OT>
 dyna_status launch_shape(const QuantProductArgs& a, const TileGrid& g, hipStream_t stream) {
     const int64_t tiles = ((int64_t)a.n_rows + 255) / 256;
     if (tiles * ((a.B + 63) / 64) < 256) return launch_tile<ACT, 1, 1, 2, 2, OT>(a, g, stream);
     if constexpr (ACT != kActF32) {
-#ifdef SHAPE_A
+        if (a.B > 128) return launch_tile<ACT, 2, 4, 4, 2, OT>(a, g, stream);
         if (a.B > 64) return launch_tile<ACT, 2, 4, 4, 1, OT>(a, g, stream);
-#else
-        if (a.B > 64) return launch_tile<ACT, 2, 4, 4, 2, OT>(a, g, stream);
-#endif
     }
     if constexpr (ACT != kActFour)
         if (a.B <= 32) return launch_tile<ACT, 2, 1, 4, 1, OT>(a, g, stream);

@@ -99,9 +99,8 @@ def test_a_planted_mistake_shows():
 def test_quant_bytes():
     assert D.quant_bytes(16, 512) == 16 * 512 // 2 + 256
     assert D.quant_bytes(1, 1) == 1024 + 256
-    # 16 rows are an odd number of 256-byte pieces
-    assert D.quant_bytes(17, 640) == 2 * (5 * 1024 + 2 * 256 + 256)
-    assert D.quant_bytes(128256, 4096) == 128256 * 4096 * 17 // 32 + 128256 // 16 * 256
+    assert D.quant_bytes(17, 640) == 2 * (5 * 1024 + 2 * 256)
+    assert D.quant_bytes(128256, 4096) == 128256 * 4096 * 17 // 32
     for rows, d in ((0, 8), (8, 0), (1 << 25, 8), (8, 8193)):
         assert D.quant_bytes(rows, d) == 0
     assert D.lib().dyna_quant_product_workspace_bytes(0, 8) == 0
