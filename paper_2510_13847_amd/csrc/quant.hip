@@ -8,7 +8,6 @@ namespace dyna {
 namespace {
 
 constexpr int kQuantWaves = 4;
-constexpr int kQuantHalf = 8;  // rows whose loads are in flight at once
 
 // Largest of the four lanes that hold a block, on each of them.
 __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
@@ -28,6 +27,7 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
     constexpr int kBlock = kMfmaRows * 4 + 4;
     __shared__ __attribute__((aligned(16))) uint32_t codes[kQuantWaves][kQuantUnit / kQuantBlock * kBlock];
     __shared__ __attribute__((aligned(16))) uint8_t scales[kQuantWaves][kQuantScaleBytes];
+    constexpr int kFlight = sizeof(T) == 2 ? 16 : 8;  // rows whose loads are in flight at once: 64 registers
     const int lane = lane_id(), wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t item = (int64_t)blockIdx.x * kQuantWaves + wv;
     if (item >= n_items) return;  // whole wave; the kernel has no barrier
@@ -38,15 +38,15 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* _
     uint32_t* cw = codes[wv] + (lane >> 2) * kBlock + (lane & 3);
     uint8_t* sw = scales[wv] + g * 64 + step;
 #pragma unroll
-    for (int h = 0; h < kMfmaRows; h += kQuantHalf) {
-        Row8<T> in[kQuantHalf];
+    for (int h = 0; h < kMfmaRows; h += kFlight) {
+        Row8<T> in[kFlight];
 #pragma unroll
-        for (int i = 0; i < kQuantHalf; ++i) {
+        for (int i = 0; i < kFlight; ++i) {
             const int r = min(group * kMfmaRows + h + i, q.rows - 1);
             if (left >= 8) in[i].load(x + (int64_t)r * row_stride + col);
         }
 #pragma unroll
-        for (int i = 0; i < kQuantHalf; ++i) {
+        for (int i = 0; i < kFlight; ++i) {
             const int r = group * kMfmaRows + h + i;
             float v[8] = {};
             if (r < q.rows && left > 0) {

@@ -187,7 +187,7 @@ DYNA_API dyna_status dyna_token_logprobs_grad(const void* logits, int32_t dtype,
                                               const float* grad_logprobs, const float* grad_entropy, void* grad,
                                               int64_t grad_stride, hipStream_t stream) {
     TRY(check_score_sizes(dtype, V, N, T, temperature, 0));
-    if ((int64_t)N * grad_parts(V) > kMaxBlocks)
+    if ((int64_t)N * grad_parts(N, V) > kMaxBlocks)
         return set_error(DYNA_ERR_UNSUPPORTED, "%d rows of %d logits in one call", N, V);
     if (N == 0) return DYNA_OK;
     ScoreArgs a{};

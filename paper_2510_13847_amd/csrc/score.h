@@ -50,7 +50,7 @@ struct ScoreArgs {
     uint64_t* lists;         // [N, splits, top] selection keys, 0 behind them
 };
 
-int32_t grad_parts(int32_t V);  // work items of a row's gradient
+int32_t grad_parts(int32_t N, int32_t V);  // work items of a row's gradient
 size_t token_logprobs_ws_bytes(int32_t N, int32_t V, int32_t T, int32_t top);
 dyna_status launch_token_logprobs(const ScoreArgs& a, hipStream_t stream);
 dyna_status launch_token_logprobs_grad(const ScoreArgs& a, hipStream_t stream);

@@ -24,41 +24,79 @@ constexpr int kMaxParts = 64;
 constexpr int kGradLen = 32768;             // columns of a gradient's work item
 
 // ---------------------------------------------------------------- rows
+// A row's shortlist: its clusters ascending (-1 behind them), the first slot of each
+// with the row's length behind them, and the clusters' first layout rows.  Up to
+// kTableLen clusters stand in LDS, where a search costs no round trips to memory.
+constexpr int kTableLen = 512;
+struct SlotTable {
+    int32_t sel[kTableLen], off[kTableLen], first[kTableLen];
+};
 struct RowSlots {
     int len;               // columns that hold a logit
-    const int32_t* sel;    // shortlists: clusters of the row ascending, -1 behind them
-    const int32_t* off;    // first slot of each, and the row's length behind them
+    const int32_t* sel;    // nullptr: column v is token v
+    const int32_t* off;
+    const SlotTable* table;  // in LDS, or nullptr
 };
 __device__ __forceinline__ RowSlots slots_of(const ScoreArgs& a, int r) {
-    if (a.row_len == nullptr) return RowSlots{a.V, nullptr, nullptr};
+    if (a.row_len == nullptr) return RowSlots{a.V, nullptr, nullptr, nullptr};
     const int64_t at = a.shared ? 0 : r;
-    return RowSlots{min(max(a.row_len[at], 0), a.V), a.sel_sorted + at * a.k, a.sel_rowoff + at * (a.k + 1)};
+    return RowSlots{min(max(a.row_len[at], 0), a.V), a.sel_sorted + at * a.k, a.sel_rowoff + at * (a.k + 1), nullptr};
+}
+// Fills the table, which a barrier of the workgroup has to follow.
+template <int NT>
+__device__ __forceinline__ void fill_table(const ScoreArgs& a, RowSlots& row, SlotTable& table) {
+    if (row.sel == nullptr || a.k > kTableLen) return;
+    for (int i = threadIdx.x; i < a.k; i += NT) {
+        const int m = row.sel[i];
+        table.sel[i] = m;
+        table.off[i] = row.off[i];
+        table.first[i] = m >= 0 ? a.offsets[m] : 0;
+    }
+    row.table = &table;
 }
 // Slot of a token in its row, -1 where it has none.
 __device__ __forceinline__ int slot_of_token(const ScoreArgs& a, const RowSlots& row, int x) {
     if (row.sel == nullptr) return x >= 0 && x < row.len ? x : -1;
     if (x < 0 || x >= a.vocab) return -1;
     const int cluster = a.token_rows[2 * (int64_t)x], at = a.token_rows[2 * (int64_t)x + 1];
-    int lo = 0, hi = a.k;  // the first entry that is not below the cluster (-1 counts as behind all)
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if ((uint32_t)row.sel[mid] < (uint32_t)cluster) lo = mid + 1;
-        else hi = mid;
+    // the first entry that is not below the cluster (-1 counts as behind all)
+    int lo = 0, hi = a.k, slot = -1;
+    if (row.table != nullptr) {
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if ((uint32_t)row.table->sel[mid] < (uint32_t)cluster) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo < a.k && row.table->sel[lo] == cluster) slot = row.table->off[lo] + (at - row.table->first[lo]);
+    } else {
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if ((uint32_t)row.sel[mid] < (uint32_t)cluster) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo < a.k && row.sel[lo] == cluster) slot = row.off[lo] + (at - a.offsets[cluster]);
     }
-    if (lo == a.k || row.sel[lo] != cluster) return -1;
-    const int slot = row.off[lo] + (at - a.offsets[cluster]);
     return slot >= 0 && slot < row.len ? slot : -1;
 }
 // Token of a slot of the row.
 __device__ __forceinline__ int token_of_slot(const ScoreArgs& a, const RowSlots& row, int slot) {
     if (row.sel == nullptr) return slot;
-    int lo = 0, hi = a.k - 1;  // the last entry that starts at the slot or before (of empty clusters, the last)
+    // the last entry that starts at the slot or before: of empty clusters the last, and
+    // entries behind the row's clusters start at its end, so it is a cluster
+    int lo = 0, hi = a.k - 1;
+    if (row.table != nullptr) {
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (row.table->off[mid] <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        return a.perm[row.table->first[lo] + (slot - row.table->off[lo])];
+    }
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (row.off[mid] <= slot) lo = mid;
         else hi = mid - 1;
     }
-    // entries behind the row's clusters start at its end, so lo is a cluster
     return a.perm[a.offsets[row.sel[lo]] + (slot - row.off[lo])];
 }
 
@@ -128,6 +166,23 @@ __device__ __forceinline__ void seen_from(double to, double& s, double& u, doubl
     const double y = from - to, f = exp2(y);
     u = f == 0.0 ? 0.0 : f * (u + s * y);
     s *= f;
+}
+
+// Both sums over the workgroup, on every thread; tmp has no earlier readers.
+__device__ __forceinline__ void block_sums(double& s, double& u, double (&tmp)[2][kST / kWave]) {
+    s = wave_sum_f64(s);
+    u = wave_sum_f64(u);
+    if (lane_id() == 0) {
+        tmp[0][threadIdx.x / kWave] = s;
+        tmp[1][threadIdx.x / kWave] = u;
+    }
+    lds_barrier();
+    s = u = 0.0;
+#pragma unroll
+    for (int i = 0; i < kST / kWave; ++i) {
+        s += tmp[0][i];
+        u += tmp[1][i];
+    }
 }
 
 // ---------------------------------------------------------------- best tokens
@@ -351,27 +406,29 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     __shared__ float tmp_f[kST / kWave];
     __shared__ double tmp_d[2][kST / kWave];
     __shared__ typename std::conditional<TOP, TopLds, int>::type best;
+    __shared__ SlotTable table;
     const int r = blockIdx.x / a.splits, part = blockIdx.x % a.splits, t = threadIdx.x;
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
-    const RowSlots w = slots_of(a, r);
+    RowSlots w = slots_of(a, r);
     const int v0 = part * a.split_len, v1 = min(w.len, v0 + a.split_len);
     const bool whole = a.splits == 1;
-    bool there = false;
-    const float given = whole ? given_logit(a, r, row, w, &there) : 0.0f;
     const float c = (float)(a.inv_t * 1.4426950408889634);
-    if constexpr (TOP) {
-        if (t == 0) {
-            best.n = 0;
-            best.floor = kNegInf;
-        }
-        lds_barrier();
-    }
     Row8<T> in[kFlight];
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
         const int at = v0 + i * kVecStep + t * 8;
         if (at + 8 <= v1) in[i].load(row + at);
     }
+    fill_table<kST>(a, w, table);
+    if constexpr (TOP) {
+        if (t == 0) {
+            best.n = 0;
+            best.floor = kNegInf;
+        }
+    }
+    lds_barrier();
+    bool there = false;
+    const float given = whole ? given_logit(a, r, row, w, &there) : 0.0f;
     RowSum sum;
     int sweep = 0;
     for (int base = v0; base < v1; base += kSweep, ++sweep) {
@@ -393,8 +450,7 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     const float m = block_max_f32<kST>(sum.m, tmp_f);
     double s = sum.s, u = sum.u;
     if (sum.m > kNegInf) seen_from((double)m * (double)c, s, u, sum.base(c));
-    s = block_sum_f64<kST>(s, tmp_d[0]);
-    u = block_sum_f64<kST>(u, tmp_d[1]);
+    block_sums(s, u, tmp_d);
     int n = 0;
     if constexpr (TOP) {
         n = best.n;
@@ -428,7 +484,7 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     __shared__ typename std::conditional<TOP, TopLds, int>::type best;
     const int r = blockIdx.x, t = threadIdx.x;
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
-    const RowSlots w = slots_of(a, r);
+    const RowSlots w = slots_of(a, r);  // (one search a token: no table)
     bool there;
     const float given = given_logit(a, r, row, w, &there);
     ScorePart p{0.0, 0.0, kNegInf, 0.0f};
@@ -450,8 +506,8 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     const float m = block_max_f32<kST>(p.m, tmp_f);
     const double c = (double)(float)(a.inv_t * 1.4426950408889634);
     if (p.m > kNegInf) seen_from((double)m * c, p.s, p.u, (double)p.m * c);
-    const double s = block_sum_f64<kST>(p.s, tmp_d[0]), u = block_sum_f64<kST>(p.u, tmp_d[1]);
-    const RowResult q(m, s, u);
+    block_sums(p.s, p.u, tmp_d);
+    const RowResult q(m, p.s, p.u);
     if (t == 0) q.write(a, r);
     if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
     if constexpr (TOP) {
@@ -482,17 +538,19 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
 template <typename T>
 __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
     __shared__ uint32_t listed[kGradLen / 32];
+    __shared__ SlotTable table;
     __shared__ int slots[DYNA_MAX_KT];
     __shared__ float gs[DYNA_MAX_KT];
     const int r = blockIdx.x / a.splits, part = blockIdx.x % a.splits, t = threadIdx.x;
-    const RowSlots w = slots_of(a, r);
-    const int v0 = part * kGradLen, v1 = min(w.len, v0 + kGradLen);
+    RowSlots w = slots_of(a, r);
+    const int v0 = part * a.split_len, v1 = min(w.len, v0 + a.split_len);
     if (v0 >= v1) return;  // whole workgroup
     const T* row = static_cast<const T*>(a.logits) + (int64_t)r * a.row_stride;
     T* grad = static_cast<T*>(a.grad) + (int64_t)r * a.grad_stride;
     const float e = a.ge ? a.ge[r] : 0.0f;
     const double m = a.stats[3 * (int64_t)r], log_s = a.stats[3 * (int64_t)r + 1], entropy = a.stats[3 * (int64_t)r + 2];
     for (int i = t; i < (v1 - v0 + 31) / 32; i += kST) listed[i] = 0u;
+    fill_table<kST>(a, w, table);
     lds_barrier();
     if (t < a.T) {
         const int slot = slot_of_token(a, w, a.tokens[(int64_t)r * a.T + t]);
@@ -578,7 +636,12 @@ dyna_status launch_pass(const ScoreArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-int32_t grad_parts(int32_t V) { return (V + kGradLen - 1) / kGradLen; }
+// Work items of a row's gradient: kGradLen columns each, fewer where there are few rows
+// (64 rows of 8191 fp32, four items a row 6.6 us, one 8.2).
+int32_t grad_parts(int32_t N, int32_t V) {
+    const int64_t most = (V + kVecStep - 1) / kVecStep, least = (V + kGradLen - 1) / kGradLen;
+    return (int32_t)std::max<int64_t>(least, std::min<int64_t>(most, N > 0 ? 1024 / N : 1));
+}
 
 size_t token_logprobs_ws_bytes(int32_t N, int32_t V, int32_t T, int32_t top) {
     int32_t splits, len;
@@ -597,7 +660,9 @@ dyna_status launch_token_logprobs(const ScoreArgs& args, hipStream_t stream) {
 
 dyna_status launch_token_logprobs_grad(const ScoreArgs& args, hipStream_t stream) {
     ScoreArgs a = args;
-    a.splits = grad_parts(a.V);
+    const int64_t parts = grad_parts(a.N, a.V);
+    a.split_len = (int32_t)(((a.V + parts - 1) / parts + kVecStep - 1) / kVecStep * kVecStep);
+    a.splits = (a.V + a.split_len - 1) / a.split_len;
     const unsigned blocks = (unsigned)((int64_t)a.N * a.splits);
     if (a.dtype == DYNA_BF16) score_grad_kernel<uint16_t><<<blocks, kST, 0, stream>>>(a);
     else score_grad_kernel<float><<<blocks, kST, 0, stream>>>(a);
