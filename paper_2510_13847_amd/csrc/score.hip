@@ -219,9 +219,9 @@ __device__ __forceinline__ float kth_of_threads(TopLds& w, float mine, int k) {
     return w.floor;
 }
 
-// Number of keys that hold, over the workgroup.
+// A count over the workgroup.
 __device__ __forceinline__ int block_count(TopLds& w, int mine, int turn) {
-    for (int d = 32; d > 0; d >>= 1) mine += __shfl_xor(mine, d);
+    mine = __builtin_amdgcn_readlane(wave_inclusive_scan(mine), kWave - 1);
     if (lane_id() == 0) w.counts[turn & 1][threadIdx.x / kWave] = mine;
     lds_barrier();
     int n = 0;
@@ -230,16 +230,28 @@ __device__ __forceinline__ int block_count(TopLds& w, int mine, int turn) {
     return n;
 }
 
-// The k-th largest of n > k keys, E to a thread (0: none); keys differ.
+// The k-th largest of n > k keys, E to a thread (0: none); keys differ.  Bit by bit:
+// the logits' 32, then, where equal ones are too many, those of the tokens (below 2^20:
+// the first 11 of their complement are ones).
 template <int E>
 __device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], int k) {
     uint64_t found = 0;
+    int reach = 0;  // keys that reach `found`
     for (int b = 63; b >= 0; --b) {
+        if (b == 31) {
+            if (reach == k) break;
+            found |= 0xffe00000ull;
+            b = 20;
+        }
         const uint64_t want = found | (1ull << b);
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < E; ++i) mine += x[i] >= want;
-        if (block_count(w, mine, b) >= k) found = want;
+        const int n = block_count(w, mine, b);
+        if (n >= k) {
+            found = want;
+            reach = n;
+        }
     }
     return found;
 }
@@ -270,13 +282,15 @@ __device__ __forceinline__ void shorten_list(TopLds& w, int n, int k) {
     keep_best<E>(w, x, k);
 }
 
-// Key of rank `threadIdx.x` ... of the list's n <= kST keys: the thread's own key
-// and how many are larger (n where the thread has none).
-__device__ __forceinline__ int rank_in_list(const TopLds& w, int n, uint64_t* key) {
-    *key = (int)threadIdx.x < n ? w.keys[threadIdx.x] : 0;
-    int rank = 0;
-    for (int i = 0; i < n; ++i) rank += w.keys[i] > *key;
-    return (int)threadIdx.x < n ? rank : INT32_MAX;
+// f(rank, key) of the `top` largest of the list's n <= kSoft keys.
+template <typename F>
+__device__ __forceinline__ void each_ranked(const TopLds& w, int n, int top, F&& f) {
+    for (int own = threadIdx.x; own < n; own += kST) {
+        const uint64_t key = w.keys[own];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) rank += w.keys[i] > key;
+        if (rank < top) f(rank, key);
+    }
 }
 
 template <typename T>
@@ -375,13 +389,11 @@ struct RowResult {
 
 // The list's n keys, ranked, as the row's best tokens.
 __device__ __forceinline__ void write_best(const ScoreArgs& a, int r, TopLds& w, int n, const RowResult& q) {
-    uint64_t key;
-    const int rank = rank_in_list(w, n, &key);
     const int64_t base = (int64_t)r * a.top;
-    if (rank < a.top) {
+    each_ranked(w, n, a.top, [&](int rank, uint64_t key) {
         a.out_top_ids[base + rank] = (int)key_id(key);
         a.out_top_logprobs[base + rank] = q.logprob(key_val(key), a.inv_t);
-    }
+    });
     if ((int)threadIdx.x >= n && (int)threadIdx.x < a.top) {
         a.out_top_ids[base + threadIdx.x] = -1;
         a.out_top_logprobs[base + threadIdx.x] = kNegInf;
@@ -452,13 +464,7 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     if (sum.m > kNegInf) seen_from((double)m * (double)c, s, u, sum.base(c));
     block_sums(s, u, tmp_d);
     int n = 0;
-    if constexpr (TOP) {
-        n = best.n;
-        if (n > kST) {
-            shorten_list(best, n, a.top);
-            n = a.top;
-        }
-    }
+    if constexpr (TOP) n = best.n;
     if (whole) {
         const RowResult q(m, s, u);
         if (t == 0) q.write(a, r);
@@ -469,9 +475,7 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     const int64_t at = (int64_t)r * a.splits + part;
     if (t == 0) a.parts[at] = ScorePart{s, u, m, 0.0f};
     if constexpr (TOP) {
-        uint64_t key;
-        const int rank = rank_in_list(best, n, &key);
-        if (rank < a.top) a.lists[at * a.top + rank] = key;
+        each_ranked(best, n, a.top, [&](int rank, uint64_t key) { a.lists[at * a.top + rank] = key; });
         if (t >= n && t < a.top) a.lists[at * a.top + t] = 0;
     }
 }
@@ -512,7 +516,7 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
     if constexpr (TOP) {
         // the keys that reach the k-th largest of the threads' best, all where there are few
-        const float floor = all <= kST ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
+        const float floor = all <= kSoft ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (x[i] != 0 && key_val(x[i]) >= floor) {
@@ -524,7 +528,7 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
         if (n > kCap) {  // equal logits
             keep_best<E>(best, x, a.top);
             n = a.top;
-        } else if (n > kST) {
+        } else if (n > kSoft) {
             shorten_list(best, n, a.top);
             n = a.top;
         }
