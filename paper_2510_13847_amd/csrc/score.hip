@@ -576,7 +576,7 @@ __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
         return;
     }
     const float inv_t = (float)a.inv_t, top = (float)m, lg = (float)log_s, h = (float)entropy;
-    const float on_p = (float)(-a.inv_t * all), on_h = (float)(-a.inv_t * (double)e);
+    const float on_p = (float)-all, on_h = -e;
     Row8<T> in[kFlight];
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
@@ -604,8 +604,11 @@ __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
                     const int k = slots[j] - at;
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        if (k == q) z[q] = fmaf(gs[j], inv_t, z[q]);
+                        if (k == q) z[q] += gs[j];
                 }
+            // last, so that an element of no weight is 0 under any temperature
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] *= inv_t;
             store_part(grad + at, v1 - at, z);
         }
     }

@@ -154,6 +154,24 @@ def test_alternatives_of_rows_with_many_equal_or_sorted_logits(kind, V, dtype):
         check(z, t, 1.0, top, D.token_logprobs(z, t, top=top))
 
 
+@pytest.mark.parametrize("kind", ["equal", "rising", "two", "late"])
+def test_many_rows_with_many_equal_or_sorted_logits(kind):
+    """Rows that one workgroup goes through in several sweeps, the list not empty when a sweep overflows it."""
+    V = 30000
+    i = torch.arange(V)
+    z = {"equal": torch.ones(V), "rising": i / 8.0, "two": (i % 2).float(),
+         "late": torch.where(i < 20000, torch.randn(V, generator=gen(1)), torch.full((V,), 9.0))}[kind]
+    z = z.float()[None].expand(1030, V).contiguous().cuda()
+    t = torch.full((1030, 1), 5, dtype=torch.int32).cuda()
+    for top in (1, 20, 64):
+        got = D.token_logprobs(z, t, top=top)
+        for x in (got.logprobs, got.entropy, got.top_ids, got.top_logprobs):
+            assert torch.equal(x, x[:1].expand_as(x))
+        for name in ("logprobs", "entropy", "top_ids", "top_logprobs"):
+            setattr(got, name, getattr(got, name)[:1])
+        check(z[:1], t[:1], 1.0, top, got)
+
+
 # ---------------------------------------------------------------- shortlists
 def shortlists(V, M, k, N, seed, dtype="f32"):
     g = gen(seed)
@@ -247,6 +265,31 @@ def test_gradients(N, V, T, pad, lead, temperature, dtype):
         assert int(torch.isnan(base).sum()) == base.numel() - N * V
     fresh = D.token_logprobs_grad(z, stats, t, g, None, temperature=temperature)
     assert torch.equal(fresh, out)
+
+
+@pytest.mark.parametrize("temperature", [1.2e-38, 1e-20, 1e20, 2.9e38])
+def test_gradients_at_the_ends_of_temperatures(temperature):
+    """All weight on the largest logit, or evenly spread: the gradient is the given tokens' own, or that less a share."""
+    temperature = float(np.float32(temperature))
+    z = rows(2, 500, "f32", 4)
+    best = z.argmax(1).to(torch.int32)
+    t = torch.stack([best, (best + 1) % 500], 1).contiguous()
+    g = torch.tensor([[0.5, 0.0], [0.25, 0.25]]).cuda()
+    e = torch.tensor([3.0, 0.0]).cuda()
+    stats = D.token_logprobs(z, t, temperature=temperature, want_stats=True).stats
+    grad = D.token_logprobs_grad(z, stats, t, g, e, temperature=temperature).double().cpu()
+    want = torch.zeros((2, 500), dtype=torch.float64)
+    share = 0.0 if temperature < 1.0 else 1.0 / 500
+    for r in range(2):
+        want[r] -= share * 0.5
+        if temperature < 1.0:
+            want[r, int(best[r])] -= 0.5
+        want[r, int(t[r, 0])] += float(g[r, 0])
+        want[r, int(t[r, 1])] += float(g[r, 1])
+    want /= temperature
+    # past 32 bits nothing is left of it; a share is off by a few steps and by exp(z / T) - 1 < 1e-18
+    assert torch.isfinite(grad).all()
+    assert ((grad - want).abs() <= 2.0 ** -20 * 0.5 / temperature + 2.0 ** -126).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
