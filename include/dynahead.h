@@ -564,8 +564,9 @@ dyna_status dyna_quantize_rows(const void* x, int32_t dtype, int32_t rows, int32
 dyna_status dyna_dequantize_rows(const dyna_quant* q, void* out, int32_t dtype, int64_t row_stride,
                                  hipStream_t stream);
 
-/* Workspace of dyna_quant_product for B contexts.  It holds nothing between
- * calls; calls that may overlap (two streams, two captured graphs) need one each. */
+/* Workspace of dyna_quant_product for B contexts of any type (bf16 ones take a third
+ * of it, four-bit ones 256 bytes).  It holds nothing between calls; calls that may
+ * overlap (two streams, two captured graphs) need one each. */
 size_t dyna_quant_product_workspace_bytes(int32_t B, int32_t d);
 
 /* out[b, r] = a_b . W_r for r < n_rows (<= W->rows): the dense head over

@@ -72,7 +72,9 @@ struct QuantProductArgs {
     void* ws;
 };
 dyna_status launch_quant_rows(const QuantProductArgs& a, hipStream_t stream);
-size_t quant_product_ws_bytes(int32_t B, int32_t d);
+// terms: bf16 terms of a context's values (0: four-bit contexts)
+size_t quant_product_ws_bytes(int32_t B, int32_t d, int32_t terms);
+bool quant_product_fits(int32_t n_rows, int32_t B, int32_t d);  // its launches' sizes
 dyna_status launch_quant_product(const QuantProductArgs& a, hipStream_t stream);
 
 }  // namespace dyna

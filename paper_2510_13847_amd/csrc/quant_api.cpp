@@ -107,7 +107,7 @@ DYNA_API dyna_status dyna_dequantize_rows(const dyna_quant* q, void* out, int32_
 
 DYNA_API size_t dyna_quant_product_workspace_bytes(int32_t B, int32_t d) {
     if (B < 1 || d < 1 || B > kQuantMaxRows || d > kQuantMaxD) return 0;
-    return quant_product_ws_bytes(B, d);
+    return quant_product_ws_bytes(B, d, 3);
 }
 
 DYNA_API dyna_status dyna_quant_product(const dyna_quant* W, int32_t n_rows, const void* a, int32_t adtype,
@@ -135,8 +135,10 @@ DYNA_API dyna_status dyna_quant_product(const dyna_quant* W, int32_t n_rows, con
         row_range(a, B, a_stride, W->d, elt_size(adtype), &lo, &hi);
         REQUIRE(!rows_touch(out, odtype, B, out_stride, n_rows, a, hi - lo), "out overlaps a");
     }
+    if (!quant_product_fits(n_rows, B, W->d))
+        return set_error(DYNA_ERR_UNSUPPORTED, "%d contexts by %d rows in one call", B, n_rows);
     REQUIRE(ws != nullptr && aligned_to(ws, 256), "ws NULL or not 256-byte aligned");
-    const size_t need = quant_product_ws_bytes(B, W->d);
+    const size_t need = quant_product_ws_bytes(B, W->d, a4 != nullptr ? 0 : adtype == DYNA_F32 ? 3 : 1);
     if (ws_bytes < need) return set_error(DYNA_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, need);
     q.W = quant_view(W->data, W->rows, W->d);
     q.n_rows = n_rows;

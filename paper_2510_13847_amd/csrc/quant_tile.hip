@@ -417,8 +417,6 @@ dyna_status launch_tile(const QuantProductArgs& a, TileGrid g, hipStream_t strea
     g.row_tiles = (a.n_rows + Sh::ROWS - 1) / Sh::ROWS;
     g.ctx_tiles = (a.B + Sh::CTX - 1) / Sh::CTX;
     const int64_t blocks = (int64_t)((g.row_tiles + kTileXcds - 1) / kTileXcds) * kTileXcds * g.ctx_tiles;
-    if (blocks * kWave * Sh::WAVES > 0xffffffffll)
-        return set_error(DYNA_ERR_UNSUPPORTED, "%d contexts by %d rows in one call", a.B, a.n_rows);
     quant_tile_kernel<ACT, NR, NC, WR, WC, OT><<<(unsigned)blocks, kWave * Sh::WAVES, Sh::LDS, stream>>>(a, g);
     return check_launch("quant_tile_kernel");
 }
@@ -450,7 +448,6 @@ dyna_status launch_shape(const QuantProductArgs& a, const TileGrid& g, hipStream
 template <typename T, int TERMS>
 dyna_status launch_operand(const QuantProductArgs& a, int groups, hipStream_t stream) {
     const int64_t items = (int64_t)a.W.steps * groups, blocks = (items + 3) / 4;
-    if (blocks > 1 << 23) return set_error(DYNA_ERR_UNSUPPORTED, "%d contexts in one call", a.B);
     context_operand_kernel<T, TERMS><<<(unsigned)blocks, 256, 0, stream>>>(static_cast<const T*>(a.a), a.a_stride, a.B,
                                                                           a.W.d, a.W.steps, groups,
                                                                           static_cast<uint8_t*>(a.ws));
@@ -459,10 +456,16 @@ dyna_status launch_operand(const QuantProductArgs& a, int groups, hipStream_t st
 
 }  // namespace
 
-size_t quant_product_ws_bytes(int32_t B, int32_t d) {
-    // fp32 contexts' three terms
-    return B <= kRowsMostF32 ? 256
-                             : (size_t)quant_view(nullptr, 1, d).steps * 3 * 4 * (size_t)operand_groups(B) * kPiece;
+size_t quant_product_ws_bytes(int32_t B, int32_t d, int32_t terms) {
+    if (terms == 0 || B <= (terms == 3 ? kRowsMostF32 : kRowsMost)) return 256;
+    return (size_t)quant_view(nullptr, 1, d).steps * terms * 4 * (size_t)operand_groups(B) * kPiece;
+}
+
+bool quant_product_fits(int32_t n_rows, int32_t B, int32_t d) {
+    // threads of the tiles' launch (at most 512 to 256 rows by 64 contexts) and of the operands'
+    const int64_t threads = ((int64_t)n_rows / 256 + 9) * ((int64_t)B / 64 + 1) * 512;
+    const int64_t items = (int64_t)quant_view(nullptr, 1, d).steps * operand_groups(B);
+    return threads <= 0xffffffffll && items * kWave <= 0xffffffffll;
 }
 
 dyna_status launch_quant_product(const QuantProductArgs& a, hipStream_t stream) {

@@ -899,6 +899,12 @@ class QuantRows:
     data: object
 
     def __post_init__(self):
+        import torch
+        n = quant_bytes(self.rows, self.d)
+        if n == 0:
+            raise ValueError(f"four-bit rows of shape {(self.rows, self.d)} are not supported")
+        if self.data.dtype is not torch.uint8 or not self.data.is_contiguous() or self.data.numel() < n:
+            raise ValueError(f"data must be {n} contiguous bytes")
         self._c = _Quant(self.rows, self.d, _ptr(self.data))
 
     @property
@@ -924,6 +930,8 @@ def _on(stream, device):
 def _quant(q, name, device):
     if not isinstance(q, QuantRows):
         raise TypeError(f"{name} must be QuantRows, not {type(q).__name__}")
+    if not q.data.is_cuda:
+        raise ValueError(f"{name} must be on a device")
     if q.device != device:
         raise ValueError(f"{name} is on {q.device}, not on {device}")
 
@@ -938,8 +946,7 @@ def quantize_rows(x, out: Optional[QuantRows] = None, stream=None) -> QuantRows:
             return quantize_rows(x, out)
     rows, d = x.shape
     if out is None:
-        n = quant_bytes(rows, d)
-        out = QuantRows(rows, d, torch.empty(max(n, 1), dtype=torch.uint8, device=x.device))
+        out = QuantRows(rows, d, torch.empty(quant_bytes(rows, d), dtype=torch.uint8, device=x.device))
     else:
         _quant(out, "out", x.device)
         if (out.rows, out.d) != (rows, d):
@@ -952,7 +959,7 @@ def dequantize_rows(q: QuantRows, dtype=None, out=None, stream=None):
     """dyna_dequantize_rows -> the values that q stands for, [rows, d] in dtype (fp32 or bf16, fp32 by default)
     or in `out`."""
     import torch
-    _quant(q, "q", q.device)
+    _quant(q, "q", getattr(q, "device", None))
     if stream is not None:
         with _on(stream, q.device):
             return dequantize_rows(q, dtype, out)
@@ -977,7 +984,7 @@ def quant_product(a, W: QuantRows, n_rows: Optional[int] = None, out=None, out_d
     """dyna_quant_product -> [B, n_rows]: contexts a ([B, d] fp32 or bf16, or QuantRows) times the first n_rows
     four-bit rows (all of them by default); the result is fp32, out_dtype or `out`."""
     import torch
-    _quant(W, "W", W.device)
+    _quant(W, "W", getattr(W, "device", None))
     dev = W.device
     if stream is not None:
         with _on(stream, dev):
@@ -1002,7 +1009,7 @@ def quant_product(a, W: QuantRows, n_rows: Optional[int] = None, out=None, out_d
     if out.device != dev:
         raise ValueError(f"out is on {out.device}, not on {dev}")
     if ws is None:
-        ws = quant_product_workspace(B, d, dev)
+        ws = quant_product_workspace(1 if four else B, d, dev)
     elif ws.device != dev:
         raise ValueError(f"ws is on {ws.device}, not on {dev}")
     _launch(dev, lib().dyna_quant_product, W.c, n_rows, None if four else _ptr(a), code, stride, a.c if four else None,
@@ -1015,7 +1022,7 @@ def quant_shortlist_logits(layout: Layout, W: QuantRows, h, sel_sorted, sel_rowo
     """dyna_quant_shortlist_logits -> logits [B, cap] fp32 (slots past row_len untouched): shortlist_logits over
     four-bit rows, W = quantize_rows(layout.W_perm); ws = workspace(layout, None, B, k, cap)."""
     import torch
-    _quant(W, "W", W.device)
+    _quant(W, "W", getattr(W, "device", None))
     dev = W.device
     if stream is not None:
         with _on(stream, dev):

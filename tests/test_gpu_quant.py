@@ -154,6 +154,27 @@ def test_whole_numbers_are_exact(B, n, d, kind):
     assert int(torch.isnan(base).sum()) == base.numel() - B * n
 
 
+# tables of rows long enough for the large tiles: of 32, 64, 128 and 256 contexts by 256 rows, ends inside a tile and
+# inside every place of a unit of four steps
+TALL = [(20, 66000, 130), (31, 65537, 384), (33, 65600, 513), (64, 65537, 256), (65, 66001, 640), (128, 65600, 96),
+        (129, 33000, 385), (200, 33100, 700), (257, 33000, 1000), (300, 65793, 60)]
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "four"])
+@pytest.mark.parametrize("B,n,d", TALL)
+def test_whole_numbers_are_exact_over_tall_tables(B, n, d, kind):
+    W = scaled_whole(n, d, n + d)
+    a, exact = contexts(kind, B, d, B, (1, 3))
+    # |terms| <= 54 * 24 in units of 2^-4: no rounding in 64 bits or in 32
+    want = (exact.cuda() @ W.double().cuda().t().contiguous()).float()
+    q = D.quantize_rows(W.cuda())
+    assert torch.equal(D.quant_product(a, q), want)
+    out, base = framed((B, n), torch.bfloat16, (3, 5))
+    D.quant_product(a, q, out=out)
+    assert torch.equal(out, want.to(torch.bfloat16))
+    assert int(torch.isnan(base).sum()) == base.numel() - B * n
+
+
 @pytest.mark.parametrize("B,n,d", [(1, 40, 300), (3, 100, 4096), (16, 37, 1000), (70, 200, 520), (150, 300, 256)])
 def test_fp32_contexts_keep_all_their_bits(B, n, d):
     """One column of every row is not zero: the product is the context's value times it, exactly."""
@@ -217,6 +238,23 @@ def test_undefined_values_stay_in_their_row_and_context(B, kind):
     for r in range(100):
         if r != 37:
             assert torch.isnan(out[r]) if w[r] == 0 else out[r] == float("inf") * w[r]
+
+
+@pytest.mark.parametrize("B", [3, 40, 200])
+@pytest.mark.parametrize("n", [100, 33100])
+def test_undefined_blocks_of_four_bit_contexts(B, n):
+    W = scaled_whole(n, 260, 6)
+    W[37, 100] = float("nan")
+    x = whole(B, 260, 7)
+    x[:, ::32] = 6.0
+    exact = x.double().cuda()
+    x[1, 259] = float("inf")
+    out = D.quant_product(D.quantize_rows(x.cuda()), D.quantize_rows(W.cuda()))
+    bad = torch.zeros((B, n), dtype=torch.bool, device="cuda")
+    bad[1], bad[:, 37] = True, True
+    W[37] = 0.0
+    assert torch.equal(torch.isnan(out), bad)
+    assert torch.equal(out[~bad].double(), (exact @ W.double().cuda().t().contiguous())[~bad])
 
 
 def test_large_values_of_fp32_contexts():
@@ -340,10 +378,15 @@ def test_binding_refuses():
         D.quantize_rows(x.t())
     with pytest.raises(ValueError):
         D.quantize_rows(x[:3], out=q)
-    with pytest.raises(D.DynaError):
+    with pytest.raises(ValueError):
         D.quantize_rows(torch.zeros((2, 8193), device="cuda"))
-    with pytest.raises(D.DynaError):
+    with pytest.raises(ValueError):
         D.quantize_rows(x[:0])
+    for data in (q.data[:-1], q.data.cpu().float(), torch.zeros(2 * q.data.numel(), dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError):
+            D.QuantRows(4, 64, data)
+    with pytest.raises(ValueError):
+        D.dequantize_rows(D.QuantRows(4, 64, q.data.cpu()))
     with pytest.raises(ValueError):
         D.dequantize_rows(q, out=torch.zeros((4, 63), device="cuda"))
     with pytest.raises(ValueError):

@@ -151,8 +151,11 @@ def test_product_refuses():
                    dict(B=-1), dict(ws=None), dict(ws=P + 3), dict(a=None, a4=_quant(5)), dict(a=None, a4=_quant(4, 256)),
                    dict(a=None, a4=_quant(4, 128, out))):
         assert call(**change) == D.ERR_INVALID_ARG, change
-    assert call(bytes=0) == D.ERR_WORKSPACE
+    assert call(bytes=255) == D.ERR_WORKSPACE
     assert call(B=(1 << 24) + 1) == D.ERR_UNSUPPORTED
+    # 2^32 threads are more than a launch takes
+    big = dict(W=_quant(1 << 24, 32), n=1 << 24, stride=32, ostride=1 << 24, a=1 << 60, out=1 << 61)
+    assert call(B=1 << 14, **big) == D.ERR_UNSUPPORTED
 
 
 def _layout(V=1000, d=64, M=10):
