@@ -104,9 +104,10 @@ __device__ __forceinline__ int token_of_slot(const ScoreArgs& a, const RowSlots&
 // A thread's share of a row, in powers of two with c = log2(e) / T: its largest logit
 // m, and relative to `base`, which is m c, the sums of w = 2^(z c - base) and of w (z c
 // - base).  z c - base is one fused multiply-add with base rounded to 32 bits, and the
-// sums' base is that rounded number; past 2^20, where its rounding would move the
-// weights by more than 2^(1/32), it is (z - m) c, relative to m c itself.  Weights are 32 bits, summed 32 at a time by pairs, or in runs
-// of four, and from there on in 64.
+// sums' base is that rounded number; past 2^20, where the largest logit's own y, the
+// rounding of m c, would reach 2^-5 and more, it is (z - m) c, relative to m c itself.
+// Weights are 32 bits, summed 32 at a time by pairs, or in runs of four, and from there
+// on in 64.
 struct RowSum {
     float m = kNegInf, ref = 0.0f;
     bool wide = false;
@@ -219,7 +220,8 @@ __device__ __forceinline__ float kth_of_threads(TopLds& w, float mine, int k) {
     return w.floor;
 }
 
-// A count over the workgroup.
+// A count over the workgroup.  Calls that follow each other without a barrier between
+// them take turns: a wave may still read the last one's counts.
 __device__ __forceinline__ int block_count(TopLds& w, int mine, int turn) {
     mine = __builtin_amdgcn_readlane(wave_inclusive_scan(mine), kWave - 1);
     if (lane_id() == 0) w.counts[turn & 1][threadIdx.x / kWave] = mine;
@@ -237,7 +239,8 @@ template <int E>
 __device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], int k) {
     uint64_t found = 0;
     int reach = 0;  // keys that reach `found`
-    for (int b = 63; b >= 0; --b) {
+    int turn = 1;
+    for (int b = 63; b >= 0; --b, ++turn) {
         if (b == 31) {
             if (reach == k) break;
             found |= 0xffe00000ull;
@@ -247,7 +250,7 @@ __device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], i
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < E; ++i) mine += x[i] >= want;
-        const int n = block_count(w, mine, b);
+        const int n = block_count(w, mine, turn);
         if (n >= k) {
             found = want;
             reach = n;
