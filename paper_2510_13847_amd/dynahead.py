@@ -1027,6 +1027,8 @@ def quant_shortlist_logits(layout: Layout, W: QuantRows, h, sel_sorted, sel_rowo
     if stream is not None:
         with _on(stream, dev):
             return quant_shortlist_logits(layout, W, h, sel_sorted, sel_rowoff, row_len, cap, ws, out)
+    if layout.perm.device != dev:
+        raise ValueError(f"layout is on {layout.perm.device}, not on {dev}")
     B, k = _dims(sel_sorted, "sel_sorted", 2)
     _typed(sel_sorted, "sel_sorted", torch.int32, (B, k), dev)
     _typed(sel_rowoff, "sel_rowoff", torch.int32, (B, k + 1), dev)
