@@ -21,6 +21,7 @@ constexpr int kSweep = kFlight * kVecStep;  // columns that a workgroup goes thr
 constexpr int kSoft = 512;
 constexpr int kCap = kSoft + (DYNA_MAX_KT - 1) * 8 * kFlight + DYNA_MAX_KT;
 constexpr int kMaxParts = 64;
+constexpr int kSt2 = 128;
 constexpr int kGradLen = 32768;             // columns of a gradient's work item
 
 // ---------------------------------------------------------------- rows
@@ -111,6 +112,7 @@ __device__ __forceinline__ int token_of_slot(const ScoreArgs& a, const RowSlots&
 struct RowSum {
     float m = kNegInf, ref = 0.0f;
     bool wide = false;
+    bool masked = false;  // masked logits have been met
     double s = 0.0, u = 0.0;
     __device__ __forceinline__ double base(float c) const { return wide ? (double)m * (double)c : (double)ref; }
     __device__ __forceinline__ void raise(float top, float c) {
@@ -127,23 +129,34 @@ struct RowSum {
             }
         }
     }
-    // A NaN or +inf logit makes s NaN and with it the row.
+    // A NaN or +inf logit makes s NaN and with it the row.  A masked one makes its weight
+    // times y NaN: from the first on, y is held above -1000, where weights are 0.
     template <int F>
     __device__ __forceinline__ void add(const float (&z)[F][8], float c) {
-        if (wide) add_from<F, true>(z, c);
-        else add_from<F, false>(z, c);
+        float part, dot;
+        if (__ballot(wide || masked) == 0) {
+            sums_of<F, false, false>(z, c, part, dot);
+            masked = dot != dot;
+        }
+        if (__ballot(wide || masked) != 0) {
+            if (wide) sums_of<F, true, true>(z, c, part, dot);
+            else sums_of<F, false, true>(z, c, part, dot);
+        }
+        s += (double)part;
+        u += (double)dot;
     }
-    template <int F, bool WIDE>
-    __device__ __forceinline__ void add_from(const float (&z)[F][8], float c) {
+    template <int F, bool WIDE, bool MASKED>
+    __device__ __forceinline__ void sums_of(const float (&z)[F][8], float c, float& part_sum, float& dot_sum) const {
         float part[F], dot[F];
 #pragma unroll
         for (int i = 0; i < F; ++i) {
             float e[8], y[8];
+            __builtin_amdgcn_sched_barrier(0);  // a vector at a time: fewer registers, more waves
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 y[k] = WIDE ? (z[i][k] - m) * c : fmaf(z[i][k], c, -ref);
                 e[k] = __builtin_amdgcn_exp2f(y[k]);
-                y[k] = fmaxf(y[k], -1000.0f);  // a masked logit adds 0, not 0 times infinity
+                if (MASKED) y[k] = fmaxf(y[k], -1000.0f);
             }
             part[i] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
             dot[i] = fmaf(e[3], y[3], fmaf(e[2], y[2], fmaf(e[1], y[1], e[0] * y[0]))) +
@@ -156,8 +169,8 @@ struct RowSum {
                 part[i] += part[i + n];
                 dot[i] += dot[i + n];
             }
-        s += (double)part[0];
-        u += (double)dot[0];
+        part_sum = part[0];
+        dot_sum = dot[0];
     }
 };
 
@@ -291,6 +304,7 @@ __device__ __forceinline__ void each_ranked(const TopLds& w, int n, int top, F&&
     for (int own = threadIdx.x; own < n; own += kST) {
         const uint64_t key = w.keys[own];
         int rank = 0;
+#pragma unroll 8
         for (int i = 0; i < n; ++i) rank += w.keys[i] > key;
         if (rank < top) f(rank, key);
     }
@@ -318,13 +332,33 @@ __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& ro
         if (p < kCap) w.keys[p] = sel_key(x, (uint32_t)token_of_slot(a, row, slot));
     };
     lds_barrier();  // `before` and the floor have been read
-    if (most >= floor && most > kNegInf)
+    const float least = fmaxf(floor, -kF32Max);
+    if (most >= least) {
+        // one copy of the code that adds a candidate: with one for each of a thread's
+        // logits, rows of 64 alternatives waited for its instructions (a part of 8192
+        // columns 10 us, now TODO)
+        uint32_t hits = 0;
 #pragma unroll
         for (int i = 0; i < F; ++i)
-            if (tops[i] >= floor)
+            if (tops[i] >= least)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (z[i][e] >= floor && z[i][e] > kNegInf) push(z[i][e], at + i * kVecStep + e);
+                for (int e = 0; e < 8; ++e) hits |= (z[i][e] >= least ? 1u : 0u) << (i * 8 + e);
+#pragma unroll 1
+        for (; hits != 0; hits &= hits - 1) {
+            const int b = __builtin_ctz(hits);
+            float x[F * 8];
+#pragma unroll
+            for (int q = 0; q < F * 8; ++q) x[q] = z[q / 8][q % 8];
+#pragma unroll
+            for (int n = F * 4, s = 0; n > 0; n /= 2, ++s)
+#pragma unroll
+                for (int q = 0; q < n; ++q) {
+                    const float even = x[2 * q], odd = x[2 * q + 1];
+                    x[q] = (b >> s) & 1 ? odd : even;
+                }
+            push(x[0], at + (b >> 3) * kVecStep + (b & 7));
+        }
+    }
     lds_barrier();
     int n = w.n;
     if (n > kCap) {
@@ -448,12 +482,25 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     int sweep = 0;
     for (int base = v0; base < v1; base += kSweep, ++sweep) {
         float z[kFlight][8], tops[kFlight], most = kNegInf;
+        if (base + 2 * kSweep <= v1) {
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) {
+                in[i].get(z[i]);
+                in[i].load(row + base + kSweep + i * kVecStep + t * 8);
+            }
+        } else {
+            if (base + kSweep > v1) sum.masked = true;  // as columns past the row are
+#pragma unroll
+            for (int i = 0; i < kFlight; ++i) {
+                const int at = base + i * kVecStep + t * 8, next = at + kSweep;
+                __builtin_amdgcn_sched_barrier(0);
+                if (at + 8 <= v1) in[i].get(z[i]);
+                else load_part(row + at, v1 - at, kNegInf, z[i]);
+                if (next + 8 <= v1) in[i].load(row + next);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kFlight; ++i) {
-            const int at = base + i * kVecStep + t * 8, next = at + kSweep;
-            if (at + 8 <= v1) in[i].get(z[i]);
-            else load_part(row + at, v1 - at, kNegInf, z[i]);
-            if (next + 8 <= v1) in[i].load(row + next);
             tops[i] = max8(z[i]);
             most = fmaxf(most, tops[i]);
         }
@@ -519,7 +566,7 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
     if constexpr (TOP) {
         // the keys that reach the k-th largest of the threads' best, all where there are few
-        const float floor = all <= kSoft ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
+        const float floor = all <= kSt2 ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (x[i] != 0 && key_val(x[i]) >= floor) {
@@ -622,7 +669,7 @@ __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
 void split_rows(int32_t N, int32_t V, int32_t* splits, int32_t* len) {
     int64_t parts = 1;
     if (V > 2 * kSweep && N < 1024) {
-        parts = std::min<int64_t>(kMaxParts, std::max<int64_t>(1, 2048 / N));
+        parts = std::min<int64_t>(kMaxParts, std::max<int64_t>(1, 1024 / N));
         parts = std::min<int64_t>(parts, (V + 2 * kVecStep - 1) / (2 * kVecStep));
     }
     int64_t each = (V + parts - 1) / parts;
