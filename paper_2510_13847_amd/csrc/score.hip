@@ -4,6 +4,23 @@
 //   s = sum exp((z - m) / T)           u = sum exp((z - m) / T) (z - m) / T
 //   log p_v = (z_v - m) / T - log s    H = log s - u / s
 //   dz_v = 1 / T (sum_t g_t ([v = t] - p_v) - e p_v (log p_v + H))
+//
+// Both directions are streams: the forward pass reads each logit once, the gradient
+// reads it once more and writes as much.
+//
+// Forward: one pass with a running m, s and u in every thread, which are joined at
+// the row's end (or, for few rows, the parts' by a second kernel).  The same pass
+// keeps the candidates for the best tokens: those that reach a floor which k logits
+// are known to reach, so almost all logits cost one comparison per eight.  4096 x
+// 128256 bf16 (1.05 GB) takes 200 us (5.3 TB/s), with 20 alternatives 249; 2048 x
+// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 200.  The memory would take 155.
+// bf16 rows have twice the exponentials to a byte: one exponential (four times an
+// instruction's time) and six other operations to a logit are 130 us of the vector
+// units by themselves, and what they do not hide is the rest.  Few rows: 1 x 128256 13
+// us, of which the two launches are 6.
+//
+// Gradient: 4096 x 128256 bf16 in 405 us, 5.2 TB/s, the rate of a copy; nothing is
+// gained by more in flight.
 #include <algorithm>
 
 #include "rowstat.h"
@@ -12,7 +29,7 @@
 namespace dyna {
 namespace {
 
-constexpr int kST = 256;  // threads
+constexpr int kST = 256;                    // threads
 constexpr int kFlight = 4;                  // vectors of 8 a thread has in flight
 constexpr int kVecStep = kST * 8;
 constexpr int kSweep = kFlight * kVecStep;  // columns that a workgroup goes through between two looks at its list
@@ -21,7 +38,7 @@ constexpr int kSweep = kFlight * kVecStep;  // columns that a workgroup goes thr
 constexpr int kSoft = 512;
 constexpr int kCap = kSoft + (DYNA_MAX_KT - 1) * 8 * kFlight + DYNA_MAX_KT;
 constexpr int kMaxParts = 64;
-constexpr int kSt2 = 128;
+constexpr int kFew = 128;                   // keys that are ranked rather than cut
 constexpr int kGradLen = 32768;             // columns of a gradient's work item
 
 // ---------------------------------------------------------------- rows
@@ -200,8 +217,9 @@ __device__ __forceinline__ void block_sums(double& s, double& u, double (&tmp)[2
 }
 
 // ---------------------------------------------------------------- best tokens
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 struct TopLds {
-    uint64_t keys[kCap];
+    __attribute__((aligned(16))) uint64_t keys[kCap];
     uint32_t groups[kST];
     int counts[2][kST / kWave];
     int n;
@@ -298,16 +316,28 @@ __device__ __forceinline__ void shorten_list(TopLds& w, int n, int k) {
     keep_best<E>(w, x, k);
 }
 
-// f(rank, key) of the `top` largest of the list's n <= kSoft keys.
+// f(rank, key) of the `top` largest of the list's n <= kSoft keys; every thread calls it
+// behind a barrier.  A thread ranks up to two keys, and reads two at a time.
 template <typename F>
-__device__ __forceinline__ void each_ranked(const TopLds& w, int n, int top, F&& f) {
-    for (int own = threadIdx.x; own < n; own += kST) {
-        const uint64_t key = w.keys[own];
-        int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < n; ++i) rank += w.keys[i] > key;
-        if (rank < top) f(rank, key);
+__device__ __forceinline__ void each_ranked(TopLds& w, int n, int top, F&& f) {
+    static_assert(kSoft <= 2 * kST && kCap > kSoft, "two keys to a thread");
+    if (n % 2 != 0) {
+        if (threadIdx.x == 0) w.keys[n] = 0;  // a pair's other half: below all
+        lds_barrier();
     }
+    const int own = threadIdx.x;
+    if (own >= n) return;
+    const bool two = own + kST < n;
+    const uint64_t key = w.keys[own], other = two ? w.keys[own + kST] : 0;
+    int rank = 0, other_rank = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; i += 2) {
+        const u64x2 x = *reinterpret_cast<const u64x2*>(w.keys + i);
+        rank += (int)(x[0] > key) + (int)(x[1] > key);
+        other_rank += (int)(x[0] > other) + (int)(x[1] > other);
+    }
+    if (rank < top) f(rank, key);
+    if (two && other_rank < top) f(other_rank, other);
 }
 
 template <typename T>
@@ -335,8 +365,8 @@ __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& ro
     const float least = fmaxf(floor, -kF32Max);
     if (most >= least) {
         // one copy of the code that adds a candidate: with one for each of a thread's
-        // logits, rows of 64 alternatives waited for its instructions (a part of 8192
-        // columns 10 us, now TODO)
+        // logits, rows of many alternatives wait for its instructions (4096 x 128256 bf16
+        // with 64 327 us, 291 as it is; with 20 257 and 249)
         uint32_t hits = 0;
 #pragma unroll
         for (int i = 0; i < F; ++i)
@@ -566,7 +596,7 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
     if (t < a.T) a.out_logprobs[(int64_t)r * a.T + t] = there ? q.logprob(given, a.inv_t) : kNegInf;
     if constexpr (TOP) {
         // the keys that reach the k-th largest of the threads' best, all where there are few
-        const float floor = all <= kSt2 ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
+        const float floor = all <= kFew ? kNegInf : kth_of_threads<32>(best, most ? key_val(most) : kNegInf, a.top);
 #pragma unroll
         for (int i = 0; i < E; ++i)
             if (x[i] != 0 && key_val(x[i]) >= floor) {
@@ -664,8 +694,10 @@ __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
     }
 }
 
-// Parts of a row: whole rows where there are enough of them for the device's
-// compute units.
+// Parts of a row: whole rows where there are enough of them for the device's compute
+// units, else as many as fit these at once (four to each: 128 rows of 128256 with 64
+// alternatives 27.4 us, with parts for two or eight to each 33.5 and 29.7), of 4096
+// columns at least.
 void split_rows(int32_t N, int32_t V, int32_t* splits, int32_t* len) {
     int64_t parts = 1;
     if (V > 2 * kSweep && N < 1024) {
