@@ -1,5 +1,5 @@
 // Four-bit rows: their form in memory, and the arguments of the kernels that
-// write and read them (quant.hip, quant_rows.hip).
+// write and read them (quant.hip, quant_rows.hip, quant_tile.hip).
 //
 // 16 rows are a group, 128 columns a step and four steps a unit.  A group is its
 // units one after the other: a unit's steps of 1 KiB, then 256 bytes of scales.

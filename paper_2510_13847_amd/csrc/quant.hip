@@ -1,6 +1,13 @@
 // Rows to four-bit form and back (OCP microscaling: e2m1 values, one e8m0 scale
-// to 32 columns).  Both are streams: each input byte is read once and each output
-// byte written once.
+// to 32 columns).  A block's scale is 2^(floor(log2 a) - 2) for its largest magnitude
+// a, so that a lies in [4, 8) scales and 6, the largest e2m1 value, is reached or
+// saturated; its values are x / scale, an exact product with a power of two, rounded
+// once to nearest even.  No row needs more than its own bits: a comes from the
+// exponent field, without a logarithm.
+//
+// Both are streams, bound by HBM: each input byte is read once and each output byte
+// written once.  128256 x 4096 bf16: 256 us to four bits (1.33 GB, 5.2 TB/s, the rate
+// of a copy), 226 back (5.9 TB/s); 16 x 3584 4.9 and 3.4 us, which is a launch.
 #include "quant.h"
 #include "rowstat.h"
 
@@ -17,7 +24,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 
 // A wave takes a unit of a group: 16 rows of 512 columns, 8 to a lane, so that a
 // load is a whole 1 KiB piece of one row (2 KiB for fp32).  The codes change
-// places through LDS, and leave as 1 KiB stores.
+// places through LDS, and leave as 1 KiB stores.  All 16 rows' loads are in flight
+// before the first is used (eight of fp32: 64 registers either way).
 template <typename T>
 __global__ __launch_bounds__(kQuantWaves* kWave) void quantize_kernel(const T* __restrict__ x, int64_t row_stride,
                                                                        QuantView q, uint8_t* __restrict__ data,
@@ -92,6 +100,9 @@ __device__ __forceinline__ void values_of(uint32_t code, uint32_t scale, float (
     v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
 }
 
+// The same unit the other way: a lane takes eight columns of each of the 16 rows, so
+// a row's stores are whole pieces of 1 KiB (2 KiB for fp32); the codes' loads are four
+// bytes a lane, but a unit's together are its bytes once.
 template <typename T>
 __global__ __launch_bounds__(kQuantWaves* kWave) void dequantize_kernel(QuantView q, T* __restrict__ out,
                                                                          int64_t row_stride, int64_t n_items) {

@@ -1,5 +1,15 @@
 // Four-bit rows times many contexts: LDS-staged tiles on the matrix cores.
 //
+// The products and their precision are those of the row-streaming kernel.  What bounds
+// it: rows' and products' bytes up to about 64 contexts (128256 x 4096: 279 MB of rows
+// and 33 MB of fp32 products; 67 us, where the bytes take 46 and a library's bf16
+// product 55), above it the matrix cores: 256 contexts 218 us (1.23 PFLOP/s, a
+// library's bf16 rate), fp32 ones three times the work (64 in 215 us).  2048 four-bit
+// contexts 562 us (3.8 PFLOP/s; the instruction alone reaches 7.4): there the loads
+// bound it, the same time without products.  A tile of 256 by 256 reads 512 rows' bytes
+// for 65536 products a column, and the 32 by 32 instruction, which does a third more
+// than 16 by 16, wants two operands of 1 KiB for every 44 cycles.
+//
 // A workgroup's tile is 32 WR NR rows by 32 WC NC contexts, a wave's 32 NR rows by
 // 32 NC contexts, and a stage 128 columns.  Rows go from memory to registers as
 // operands of 32 rows by 64 columns, and are converted there; contexts go straight
@@ -172,10 +182,10 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
         }
         if constexpr (!Sh::ROWS_LDS)
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+            for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                ws_next[r][h] = *reinterpret_cast<const uint32_t*>(wp[r] + at + row_at / 4 + h * 128);
+                for (int h = 0; h < 2; ++h)
+                    ws_next[r][h] = *reinterpret_cast<const uint32_t*>(wp[r] + at + row_at / 4 + h * 128);
     };
     // stage `step` into ring place p: contexts to LDS, rows to registers.  Stages
     // past the last one repeat it.
@@ -204,9 +214,9 @@ __global__ __launch_bounds__(kWave* WR* WC, 2) void quant_tile_kernel(QuantProdu
         const int64_t at = step_at(min(step, steps - 1));
         if constexpr (!Sh::ROWS_LDS)
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+            for (int r = 0; r < NR; ++r)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w[p][r][h] = *reinterpret_cast<const u32x4*>(wp[r] + at + row_at + h * 512);
+                for (int h = 0; h < 2; ++h) w[p][r][h] = *reinterpret_cast<const u32x4*>(wp[r] + at + row_at + h * 512);
     };
 
     f32x16 acc[NR][NC];

@@ -12,8 +12,8 @@
 // the row's end (or, for few rows, the parts' by a second kernel).  The same pass
 // keeps the candidates for the best tokens: those that reach a floor which k logits
 // are known to reach, so almost all logits cost one comparison per eight.  4096 x
-// 128256 bf16 (1.05 GB) takes 200 us (5.3 TB/s), with 20 alternatives 249; 2048 x
-// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 200.  The memory would take 155.
+// 128256 bf16 (1.05 GB) takes 203 us (5.2 TB/s), with 20 alternatives 236; 2048 x
+// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 197.  The memory would take 155.
 // bf16 rows have twice the exponentials to a byte: one exponential (four times an
 // instruction's time) and six other operations to a logit are 130 us of the vector
 // units by themselves, and what they do not hide is the rest.  Few rows: 1 x 128256 13
@@ -223,7 +223,7 @@ struct TopLds {
     uint32_t groups[kST];
     int counts[2][kST / kWave];
     int n;
-    float floor;
+    float kth;
 };
 
 // A value that at least k of the workgroup's threads' values `mine` reach: the
@@ -245,10 +245,10 @@ __device__ __forceinline__ float kth_of_threads(TopLds& w, float mine, int k) {
             for (int i = 0; i < kST / kWave; ++i) n += __popcll(__ballot(x[i] >= want));
             if (n >= k) found = want;
         }
-        if (threadIdx.x == 0) w.floor = found > ord_f32(kNegInf) ? ord_to_f32(found) : kNegInf;
+        if (threadIdx.x == 0) w.kth = found > ord_f32(kNegInf) ? ord_to_f32(found) : kNegInf;
     }
     lds_barrier();
-    return w.floor;
+    return w.kth;
 }
 
 // A count over the workgroup.  Calls that follow each other without a barrier between
@@ -290,22 +290,20 @@ __device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], i
     return found;
 }
 
-// Leaves the k largest of the keys in the list (in any order): all of its n <= k,
-// or those not below the k-th, which becomes the floor.
+// Leaves the k largest of the n > k keys in the list (in any order), and returns the
+// k-th's logit.
 template <int E>
-__device__ __forceinline__ void keep_best(TopLds& w, const uint64_t (&x)[E], int k) {
+__device__ __forceinline__ float keep_best(TopLds& w, const uint64_t (&x)[E], int k) {
     const uint64_t last = kth_key<E>(w, x, k);
-    if (threadIdx.x == 0) {
-        w.n = 0;
-        w.floor = key_val(last);
-    }
+    if (threadIdx.x == 0) w.n = 0;
     lds_barrier();  // everyone has its keys in registers
 #pragma unroll
     for (int i = 0; i < E; ++i)
         if (x[i] >= last) w.keys[atomicAdd(&w.n, 1)] = x[i];
     lds_barrier();
+    return key_val(last);
 }
-__device__ __forceinline__ void shorten_list(TopLds& w, int n, int k) {
+__device__ __forceinline__ float shorten_list(TopLds& w, int n, int k) {
     constexpr int E = (kCap + kST - 1) / kST;
     uint64_t x[E];
 #pragma unroll
@@ -313,7 +311,7 @@ __device__ __forceinline__ void shorten_list(TopLds& w, int n, int k) {
         const int at = i * kST + (int)threadIdx.x;
         x[i] = at < n ? w.keys[at] : 0;
     }
-    keep_best<E>(w, x, k);
+    return keep_best<E>(w, x, k);
 }
 
 // f(rank, key) of the `top` largest of the list's n <= kSoft keys; every thread calls it
@@ -343,30 +341,25 @@ __device__ __forceinline__ void each_ranked(TopLds& w, int n, int top, F&& f) {
 template <typename T>
 __device__ __forceinline__ float logit_at(const T* row, int v, int v1) { return v < v1 ? to_f32(row[v]) : kNegInf; }
 
+__device__ __forceinline__ void push_key(const ScoreArgs& a, const RowSlots& row, TopLds& w, float x, int slot) {
+    const int p = atomicAdd(&w.n, 1);
+    if (p < kCap) w.keys[p] = sel_key(x, (uint32_t)token_of_slot(a, row, slot));
+}
+
 // Adds a sweep's candidates to the list: the logits that reach `floor`, which at least
 // k of this sweep and those before do.  The floor is the k-th largest of the threads'
-// largest logits so far (`highest`), found again after 1, 2, 4, .. sweeps (`look`), so
-// that a row adds about k candidates each time it doubles.  Where a sweep's are too
-// many for the list (equal logits), it starts again behind a floor of its own: at most
-// k - 1 threads have a logit above the k-th largest of the threads' maxima, and of
-// those equal to it the k lowest tokens are enough.  Those logits are read again.
-template <typename T, int F>
+// largest logits so far, found again after 1, 2, 4, .. sweeps, so that a row adds about
+// k candidates each time it doubles.  Only then, and at the row's end, the waves wait
+// for each other (4096 x 128256 bf16 with 20 alternatives 236 us; with three barriers at
+// every sweep 249).
+template <int F>
 __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& row, TopLds& w, const float (&z)[F][8],
-                                          const float (&tops)[F], float most, float highest, bool look, const T* logits,
-                                          int at, int v1, int k) {
-    float floor = w.floor;
-    const int before = w.n;
-    if (look) floor = fmaxf(floor, kth_of_threads<16>(w, highest, k));
-    auto push = [&](float x, int slot) {
-        const int p = atomicAdd(&w.n, 1);
-        if (p < kCap) w.keys[p] = sel_key(x, (uint32_t)token_of_slot(a, row, slot));
-    };
-    lds_barrier();  // `before` and the floor have been read
+                                          const float (&tops)[F], float most, float floor, int at) {
     const float least = fmaxf(floor, -kF32Max);
     if (most >= least) {
         // one copy of the code that adds a candidate: with one for each of a thread's
         // logits, rows of many alternatives wait for its instructions (4096 x 128256 bf16
-        // with 64 327 us, 291 as it is; with 20 257 and 249)
+        // with 64 327 us against 291)
         uint32_t hits = 0;
 #pragma unroll
         for (int i = 0; i < F; ++i)
@@ -386,49 +379,79 @@ __device__ __forceinline__ void add_sweep(const ScoreArgs& a, const RowSlots& ro
                     const float even = x[2 * q], odd = x[2 * q + 1];
                     x[q] = (b >> s) & 1 ? odd : even;
                 }
-            push(x[0], at + (b >> 3) * kVecStep + (b & 7));
+            push_key(a, row, w, x[0], at + (b >> 3) * kVecStep + (b & 7));
         }
     }
+}
+
+// A sweep whose candidates, with those beside it, are too many for the list (equal
+// logits, rising ones): it has a floor of its own.  At most k - 1 threads have a logit
+// above the k-th largest of the threads' maxima, and of those equal to it the k lowest
+// tokens are enough.  The logits are read again.  Behind a barrier; returns the list's
+// length.
+template <typename T>
+__device__ __forceinline__ int add_full_sweep(const ScoreArgs& a, const RowSlots& row, TopLds& w, const T* logits,
+                                              int at, int v1, int k, float& floor) {
+    auto each = [&](auto&& f) {
+#pragma unroll 1
+        for (int i = 0; i < kFlight * 8; ++i) {
+            const int slot = at + (i >> 3) * kVecStep + (i & 7);
+            f(logit_at(logits, slot, v1), slot);
+        }
+    };
+    float most = kNegInf;
+    each([&](float x, int) { most = fmaxf(most, x); });
+    const float least = fmaxf(floor, kth_of_threads<32>(w, most, k));  // with barriers
+    if (most > least)
+        each([&](float x, int slot) {
+            if (x > least) push_key(a, row, w, x, slot);
+        });
+    // the tokens of equal logits up to `last`, k of them or all
+    int equal = 0;
+    each([&](float x, int) { equal += x == least && x > kNegInf; });
+    int last = INT32_MAX;
+    if (block_count(w, equal, 0) > k) {
+        last = 0;
+        for (int b = 20; b >= 0; --b) {  // the largest number with fewer than k tokens below it
+            int below = 0;
+            if (equal)
+                each([&](float x, int slot) { below += x == least && token_of_slot(a, row, slot) < (last | (1 << b)); });
+            if (block_count(w, below, b + 1) < k) last |= 1 << b;
+        }
+    }
+    if (equal)
+        each([&](float x, int slot) {
+            if (x == least && token_of_slot(a, row, slot) <= last) push_key(a, row, w, x, slot);
+        });
     lds_barrier();
     int n = w.n;
-    if (n > kCap) {
-        auto each = [&](auto&& f) {
-#pragma unroll 1
-            for (int i = 0; i < F * 8; ++i) {
-                const int slot = at + (i >> 3) * kVecStep + (i & 7);
-                f(logit_at(logits, slot, v1), slot);
-            }
-        };
-        lds_barrier();
-        if (threadIdx.x == 0) w.n = before;
-        floor = fmaxf(floor, kth_of_threads<32>(w, most, k));  // with barriers
-        if (most > floor)
-            each([&](float x, int slot) {
-                if (x > floor) push(x, slot);
-            });
-        // the tokens of equal logits up to `last`, k of them or all
-        int equal = 0;
-        each([&](float x, int) { equal += x == floor && x > kNegInf; });
-        int last = INT32_MAX;
-        if (block_count(w, equal, 0) > k) {
-            last = 0;
-            for (int b = 20; b >= 0; --b) {  // the largest number with fewer than k tokens below it
-                int below = 0;
-                if (equal)
-                    each([&](float x, int slot) { below += x == floor && token_of_slot(a, row, slot) < (last | (1 << b)); });
-                if (block_count(w, below, b + 1) < k) last |= 1 << b;
-            }
-        }
-        if (equal)
-            each([&](float x, int slot) {
-                if (x == floor && token_of_slot(a, row, slot) <= last) push(x, slot);
-            });
-        lds_barrier();
-        n = w.n;
+    if (n > kSoft) {
+        floor = fmaxf(floor, shorten_list(w, n, k));
+        n = k;
     }
-    if (n > kSoft) shorten_list(w, n, k);
-    else if (threadIdx.x == 0) w.floor = floor;
-    lds_barrier();
+    lds_barrier();  // n has been read
+    return n;
+}
+
+// Brings the list to kSoft keys at most behind the sweeps of columns [from, to), in
+// which it had `kept` keys before; returns how many there are now.  A barrier has to
+// follow before the next key is added.
+template <typename T>
+__device__ __forceinline__ int settle_list(const ScoreArgs& a, const RowSlots& row, TopLds& w, const T* logits,
+                                           int from, int to, int v1, int kept, int k, float& floor) {
+    lds_barrier();  // every candidate has been added
+    int n = w.n;
+    if (n > kCap) {
+        lds_barrier();  // n has been read
+        if (threadIdx.x == 0) w.n = kept;
+        lds_barrier();
+        for (int base = from; base < to; base += kSweep)
+            n = add_full_sweep(a, row, w, logits, base + (int)threadIdx.x * 8, v1, k, floor);
+    } else if (n > kSoft) {
+        floor = fmaxf(floor, shorten_list(w, n, k));
+        n = k;
+    }
+    return n;
 }
 
 // ---------------------------------------------------------------- results
@@ -500,17 +523,22 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
     }
     fill_table<kST>(a, w, table);
     if constexpr (TOP) {
-        if (t == 0) {
-            best.n = 0;
-            best.floor = kNegInf;
-        }
+        if (t == 0) best.n = 0;
     }
     lds_barrier();
     bool there = false;
     const float given = whole ? given_logit(a, r, row, w, &there) : 0.0f;
     RowSum sum;
-    int sweep = 0;
+    int sweep = 0, n = 0, from = v0;  // the list's keys and the columns since it was settled
+    float floor = kNegInf;
     for (int base = v0; base < v1; base += kSweep, ++sweep) {
+        const bool look = (sweep & (sweep + 1)) == 0;
+        if constexpr (TOP) {
+            if (look) {
+                n = settle_list(a, w, best, row, from, base, v1, n, a.top, floor);
+                from = base;
+            }
+        }
         float z[kFlight][8], tops[kFlight], most = kNegInf;
         if (base + 2 * kSweep <= v1) {
 #pragma unroll
@@ -536,15 +564,16 @@ __global__ __launch_bounds__(kST) void score_pass_kernel(ScoreArgs a) {
         }
         sum.raise(most, c);
         sum.add(z, c);
-        if constexpr (TOP)
-            add_sweep(a, w, best, z, tops, most, sum.m, (sweep & (sweep + 1)) == 0, row, base + t * 8, v1, a.top);
+        if constexpr (TOP) {
+            if (look) floor = fmaxf(floor, kth_of_threads<16>(best, sum.m, a.top));
+            add_sweep(a, w, best, z, tops, most, floor, base + t * 8);
+        }
     }
+    if constexpr (TOP) n = settle_list(a, w, best, row, from, v1, v1, n, a.top, floor);
     const float m = block_max_f32<kST>(sum.m, tmp_f);
     double s = sum.s, u = sum.u;
     if (sum.m > kNegInf) seen_from((double)m * (double)c, s, u, sum.base(c));
     block_sums(s, u, tmp_d);
-    int n = 0;
-    if constexpr (TOP) n = best.n;
     if (whole) {
         const RowResult q(m, s, u);
         if (t == 0) q.write(a, r);

@@ -142,6 +142,38 @@ def test_masks_and_undefined_logits(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_masks_that_begin_late_in_long_rows(dtype):
+    """Masked logits met by some threads only, from the first, second or last columns on, in rows of one workgroup each."""
+    V, N = 40000, 1040
+    z = rows(8, V, dtype, 3)
+    z[0, 9000] = -float("inf")
+    z[1, 20000:] = -float("inf")
+    z[2, V - 1] = -float("inf")
+    z[3, :30000] = -float("inf")
+    z[4, 8192 * 2:8192 * 3] = -float("inf")
+    z[5, 17000::2048] = -float("inf")
+    z[6, 9000] = float("nan")
+    z[7, 8192 * 4:] = -float("inf")
+    t = torch.tensor([[0, 9000, 20001, V - 1]], dtype=torch.int32).expand(8, 4).contiguous().cuda()
+    for temperature in (1.0, 1e-7):  # the second with its weights by the difference
+        got = D.token_logprobs(z.repeat(N // 8, 1), t.repeat(N // 8, 1), temperature=temperature, top=10)
+        for name in ("logprobs", "entropy", "top_ids", "top_logprobs"):
+            x = getattr(got, name)
+            first = x[:8].repeat(N // 8, *[1] * (x.dim() - 1))
+            assert torch.equal(torch.nan_to_num(x.double(), nan=7.0), torch.nan_to_num(first.double(), nan=7.0))
+            setattr(got, name, x[:8])
+        if temperature == 1.0:
+            check(z, t, 1.0, 10, got)
+        else:  # the largest logit has all the weight, shared where several have it
+            best = z.float().max(1).values
+            assert torch.equal(got.top_logprobs[:, 0].isnan().cpu(), torch.tensor([r == 6 for r in range(8)]))
+            for r in (0, 1, 2, 3, 4, 5, 7):
+                many = int((z[r].float() == best[r]).sum())
+                assert abs(float(got.top_logprobs[r, 0]) + math.log(many)) <= 2.0 ** -18
+                assert abs(float(got.entropy[r]) - math.log(many)) <= 2.0 ** -18
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [300, 9000, 70000])
 @pytest.mark.parametrize("kind", ["equal", "rising", "falling", "two", "steps", "ends"])
 def test_alternatives_of_rows_with_many_equal_or_sorted_logits(kind, V, dtype):
@@ -191,7 +223,8 @@ def shortlists(V, M, k, N, seed, dtype="f32"):
 
 
 @pytest.mark.parametrize("V,M,k,N,T,top", [(100, 5, 2, 4, 3, 7), (3000, 64, 8, 9, 2, 20), (50000, 100, 40, 5, 5, 64),
-                                           (2000, 30, 30, 3, 1, 10), (8191, 2000, 300, 3, 4, 5), (50, 50, 1, 4, 2, 3)])
+                                           (2000, 30, 30, 3, 1, 10), (8191, 2000, 300, 3, 4, 5), (50, 50, 1, 4, 2, 3),
+                                           (9001, 2000, 700, 4, 3, 64), (30000, 1500, 1500, 5, 4, 20)])
 def test_shortlists(V, M, k, N, T, top):
     layout, sel, ids, z, length = shortlists(V, M, k, N, V + k)
     # half of the tokens from the row's own
