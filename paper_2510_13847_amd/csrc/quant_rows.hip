@@ -17,10 +17,10 @@
 // Sums are 32 bits: in an instruction, over a wave's 512 columns, over the waves.
 //
 // What bounds it is the rows' bytes; a wave has 4.25 KiB of the next tile in flight
-// while it multiplies one, two workgroups of 4096 columns 136 KiB to a compute unit.
-// 128256 x 4096 (279 MB): one bf16 context 41 us (6.8 TB/s, what rows stream at), 8 43.5,
-// 16 48; four fp32 ones 51.  Gathered: 128 contexts with 64 of 4096 clusters each over
-// 262144 x 5376 (652 MB) 96 us, 6.8 TB/s; one with 32 of 1024 over 128256 x 4096 8 us.
+// while it multiplies one, the two workgroups of 4096 columns on a compute unit 68 KiB.
+// 128256 x 4096 (279 MB): one bf16 context 42 us (6.7 TB/s, what rows stream at; 5.8
+// where the last cache holds none of them), 8 43.5, 16 48; four fp32 ones 51.  Gathered: 128 contexts with 64 of 4096 clusters each over
+// 262144 x 5376 (652 MB) 95 us, 6.9 TB/s; one with 32 of 1024 over 128256 x 4096 8 us.
 // A run of consecutive chunks to a workgroup, as the plan's order has the contexts of
 // one list side by side: handing chunks out by a counter took 157 us where this took
 // 136, contexts being loaded again for each.

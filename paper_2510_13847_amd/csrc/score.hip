@@ -12,8 +12,8 @@
 // the row's end (or, for few rows, the parts' by a second kernel).  The same pass
 // keeps the candidates for the best tokens: those that reach a floor which k logits
 // are known to reach, so almost all logits cost one comparison per eight.  4096 x
-// 128256 bf16 (1.05 GB) takes 203 us (5.2 TB/s), with 20 alternatives 236; 2048 x
-// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 197.  The memory would take 155.
+// 128256 bf16 (1.05 GB) takes 201 us (5.2 TB/s), with 20 alternatives 236; 2048 x
+// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 189.  The memory would take 155.
 // bf16 rows have twice the exponentials to a byte: one exponential (four times an
 // instruction's time) and six other operations to a logit are 130 us of the vector
 // units by themselves, and what they do not hide is the rest.  Few rows: 1 x 128256 13
