@@ -283,7 +283,13 @@ dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
     const int NW = a.W.units;
     const int64_t tiles = PLAN ? a.max_chunks_bound : ((int64_t)a.n_rows + kMfmaRows - 1) / kMfmaRows;
     const int passes = PLAN ? 1 : (a.B + contexts_per_pass(ACT) - 1) / contexts_per_pass(ACT);
-    const int64_t resident = 256 * (int64_t)std::max(1, 16 / NW);
+    // Workgroups that a compute unit's registers hold at once, so that none runs alone
+    // behind the others: 16 waves; of the instances of few waves, which take more
+    // registers, 12, or 8 where gathered fp32 contexts are put together (262144 x 1536, 16
+    // waves and 12: a bf16 context 44 and 38 us, four fp32 ones 61 and 49; 128 fp32
+    // contexts' 64 of 2048 clusters of 151936 x 1536, 16, 12 and 8: 131, 134 and 117)
+    const int waves = MAXW > 3 || ACT == kActFour ? 16 : PLAN && ACT == kActF32 ? 8 : 12;
+    const int64_t resident = 256 * (int64_t)std::max(1, waves / NW);
     const int64_t blocks = std::max<int64_t>(1, std::min(tiles, resident));
     launch_timed_kernel(quant_rows_kernel<ACT, PLAN, MAXW, OT>, dim3((unsigned)blocks, (unsigned)passes), dim3(NW * kWave),
                         0, stream, a);
