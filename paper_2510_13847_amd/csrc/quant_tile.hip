@@ -4,7 +4,7 @@
 // it: rows' and products' bytes up to about 64 contexts (128256 x 4096: 279 MB of rows
 // and 33 MB of fp32 products; 67 us, where the bytes take 46 and a library's bf16
 // product 55), above it the matrix cores: 256 contexts 218 us (1.23 PFLOP/s, a
-// library's bf16 rate), fp32 ones three times the work (64 in 215 us).  2048 four-bit
+// library's bf16 rate), fp32 ones three times the work (64 in 174 us).  2048 four-bit
 // contexts 562 us (3.8 PFLOP/s; the instruction alone reaches 7.4): there the loads
 // bound it, the same time without products.  A tile of 256 by 256 reads 512 rows' bytes
 // for 65536 products a column, and the 32 by 32 instruction, which does a third more
@@ -437,22 +437,38 @@ int operand_groups(int32_t B) {
     return (groups + kMostGroups - 1) / kMostGroups * kMostGroups;
 }
 
-// Tiles by the contexts, so that few columns of the products are computed for nothing
-// and rows are read few times, with the most rows that still leave every compute unit a
-// tile.  bf16 contexts over 128256 x 4096, us: 32 contexts 53 (tiles of 32); 64 73 (64);
-// 70 121 (128; 134 with two of 64, or eight waves of 64 by 64); 128 133 (138, 142; 187
-// with one of 256); 192 207 (256).  fp32 contexts' three terms fill LDS with 64.
+// Tiles of 256 rows by 256, 128, 64 or 32 contexts: the widest that leaves every compute
+// unit a tile and computes few columns of nothing (an eighth over what the narrowest
+// would); tiles of 64 by 64 where there are no more of those than compute units, and for
+// four-bit contexts where no other fits.  Wide tiles read rows fewer times, narrow ones
+// have more waves.  us by width:
+//                                64x64    32     64    128    256
+//   8192 x 4096, 64 bf16          18.8   21.7   36     59     80
+//   32000 x 4096, 64 bf16         28.2   25.1   37     61     81
+//   32000 x 4096, 256 bf16        89     70     64     69     85
+//   100000 x 4096, 64 bf16        75     63     58     91    158
+//   100000 x 4096, 192 bf16      215    158    149    191    180
+//   100000 x 4096, 256 bf16      284    206    208    209    192
+//   100000 x 4096, 512 four-bit  272     -     194    159    152
+// The three terms of fp32 contexts fill LDS with 64 (100000 x 4096, 64 contexts: 188 us,
+// two tiles of 32 150).
 template <int ACT, typename OT>
 dyna_status launch_shape(const QuantProductArgs& a, const TileGrid& g, hipStream_t stream) {
-    const int64_t tiles = ((int64_t)a.n_rows + 255) / 256;
-    if (tiles * ((a.B + 63) / 64) < 256) return launch_tile<ACT, 1, 1, 2, 2, OT>(a, g, stream);
+    constexpr int64_t kUnits = 256, kLeast = ACT == kActFour ? 64 : 32;
+    const int64_t tiles = ((int64_t)a.n_rows + 255) / 256, least = (a.B + kLeast - 1) / kLeast * kLeast;
+    auto fits = [&](int64_t width) {
+        const int64_t columns = (a.B + width - 1) / width;
+        return tiles * columns >= kUnits && columns * width * 8 <= least * 9;
+    };
+    if (((int64_t)a.n_rows + 63) / 64 * ((a.B + 63) / 64) <= kUnits)
+        return launch_tile<ACT, 1, 1, 2, 2, OT>(a, g, stream);
     if constexpr (ACT != kActF32) {
-        if (a.B > 128) return launch_tile<ACT, 2, 4, 4, 2, OT>(a, g, stream);
-        if (a.B > 64) return launch_tile<ACT, 2, 4, 4, 1, OT>(a, g, stream);
+        if (fits(256)) return launch_tile<ACT, 2, 4, 4, 2, OT>(a, g, stream);
+        if (fits(128)) return launch_tile<ACT, 2, 4, 4, 1, OT>(a, g, stream);
+        if (fits(64)) return launch_tile<ACT, 2, 2, 4, 1, OT>(a, g, stream);
     }
-    if constexpr (ACT != kActFour)
-        if (a.B <= 32) return launch_tile<ACT, 2, 1, 4, 1, OT>(a, g, stream);
-    return launch_tile<ACT, 2, 2, 4, 1, OT>(a, g, stream);
+    if constexpr (ACT != kActFour) return launch_tile<ACT, 2, 1, 4, 1, OT>(a, g, stream);
+    return launch_tile<ACT, 1, 1, 2, 2, OT>(a, g, stream);
 }
 
 template <typename T, int TERMS>
@@ -472,7 +488,8 @@ size_t quant_product_ws_bytes(int32_t B, int32_t d, int32_t terms) {
 }
 
 bool quant_product_fits(int32_t n_rows, int32_t B, int32_t d) {
-    // threads of the tiles' launch (at most 512 to 256 rows by 64 contexts) and of the operands'
+    // threads of the tiles' launch (at most 512 to 256 rows by 64 contexts, of small tiles
+    // 1024, of which there are fewer than 2048) and of the operands'
     const int64_t threads = ((int64_t)n_rows / 256 + 9) * ((int64_t)B / 64 + 1) * 512;
     const int64_t items = (int64_t)quant_view(nullptr, 1, d).steps * operand_groups(B);
     return threads <= 0xffffffffll && items * kWave <= 0xffffffffll;

@@ -157,7 +157,8 @@ def test_whole_numbers_are_exact(B, n, d, kind):
 # tables of rows long enough for the large tiles: of 32, 64, 128 and 256 contexts by 256 rows, ends inside a tile and
 # inside every place of a unit of four steps
 TALL = [(20, 66000, 130), (31, 65537, 384), (33, 65600, 513), (64, 65537, 256), (65, 66001, 640), (128, 65600, 96),
-        (129, 33000, 385), (200, 33100, 700), (257, 33000, 1000), (300, 65793, 60)]
+        (129, 33000, 385), (200, 33100, 700), (257, 33000, 1000), (300, 65793, 60),
+        (256, 65600, 200), (500, 33000, 385), (90, 17000, 300), (17, 30000, 1000)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "four"])
