@@ -597,7 +597,7 @@ dyna_status dyna_quant_shortlist_logits(const dyna_layout* L, const dyna_quant* 
 /* The shortlists that rows of draft logits span, as dyna_shortlist wrote them
  * (k entries a row; shared: one row of them for every row of logits).  */
 typedef struct dyna_shortlist_rows {
-    const dyna_layout* L;        /* perm and offsets are read */
+    const dyna_layout* L;        /* perm and offsets are read; any V, past the columns of a row too */
     const int32_t* token_rows;   /* device [V, 2], dyna_token_rows of L */
     const int32_t* sel_sorted;   /* device [N, k] or [1, k] */
     const int32_t* sel_rowoff;   /* device [N, k + 1] or [1, k + 1] */

@@ -63,6 +63,8 @@ dyna_status check_score(const void* logits, int32_t dtype, int32_t V, int64_t ro
         a->k = rows->k;
         a->shared = rows->shared != 0;
     }
+    a->id_bits = 1;
+    while (a->id_bits < 31 && a->vocab > 1 << a->id_bits) ++a->id_bits;
     return DYNA_OK;
 }
 

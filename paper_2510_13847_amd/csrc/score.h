@@ -27,7 +27,8 @@ struct ScoreArgs {
     const int32_t* row_len;
     int32_t k;
     bool shared;
-    int32_t vocab;           // tokens of the layout
+    int32_t vocab;           // tokens: of the layout, or columns
+    int32_t id_bits;         // a token is below 2^id_bits (1 to 31)
     const int32_t* tokens;   // [N, T]
     int32_t T;
     double inv_t;

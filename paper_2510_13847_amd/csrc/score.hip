@@ -264,18 +264,18 @@ __device__ __forceinline__ int block_count(TopLds& w, int mine, int turn) {
 }
 
 // The k-th largest of n > k keys, E to a thread (0: none); keys differ.  Bit by bit:
-// the logits' 32, then, where equal ones are too many, those of the tokens (below 2^20:
-// the first 11 of their complement are ones).
+// the logits' 32, then, where equal ones are too many, those of the tokens (below
+// 2^id_bits: the complement's others are ones).
 template <int E>
-__device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], int k) {
+__device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], int k, int id_bits) {
     uint64_t found = 0;
     int reach = 0;  // keys that reach `found`
     int turn = 1;
     for (int b = 63; b >= 0; --b, ++turn) {
         if (b == 31) {
             if (reach == k) break;
-            found |= 0xffe00000ull;
-            b = 20;
+            found |= 0xffffffffu << id_bits;
+            b = id_bits - 1;
         }
         const uint64_t want = found | (1ull << b);
         int mine = 0;
@@ -293,8 +293,8 @@ __device__ __forceinline__ uint64_t kth_key(TopLds& w, const uint64_t (&x)[E], i
 // Leaves the k largest of the n > k keys in the list (in any order), and returns the
 // k-th's logit.
 template <int E>
-__device__ __forceinline__ float keep_best(TopLds& w, const uint64_t (&x)[E], int k) {
-    const uint64_t last = kth_key<E>(w, x, k);
+__device__ __forceinline__ float keep_best(TopLds& w, const uint64_t (&x)[E], int k, int id_bits) {
+    const uint64_t last = kth_key<E>(w, x, k, id_bits);
     if (threadIdx.x == 0) w.n = 0;
     lds_barrier();  // everyone has its keys in registers
 #pragma unroll
@@ -303,7 +303,7 @@ __device__ __forceinline__ float keep_best(TopLds& w, const uint64_t (&x)[E], in
     lds_barrier();
     return key_val(last);
 }
-__device__ __forceinline__ float shorten_list(TopLds& w, int n, int k) {
+__device__ __forceinline__ float shorten_list(TopLds& w, int n, int k, int id_bits) {
     constexpr int E = (kCap + kST - 1) / kST;
     uint64_t x[E];
 #pragma unroll
@@ -311,7 +311,7 @@ __device__ __forceinline__ float shorten_list(TopLds& w, int n, int k) {
         const int at = i * kST + (int)threadIdx.x;
         x[i] = at < n ? w.keys[at] : 0;
     }
-    return keep_best<E>(w, x, k);
+    return keep_best<E>(w, x, k, id_bits);
 }
 
 // f(rank, key) of the `top` largest of the list's n <= kSoft keys; every thread calls it
@@ -412,11 +412,11 @@ __device__ __forceinline__ int add_full_sweep(const ScoreArgs& a, const RowSlots
     int last = INT32_MAX;
     if (block_count(w, equal, 0) > k) {
         last = 0;
-        for (int b = 20; b >= 0; --b) {  // the largest number with fewer than k tokens below it
+        for (int b = a.id_bits - 1, turn = 1; b >= 0; --b, ++turn) {  // the largest number with fewer than k tokens below it
             int below = 0;
             if (equal)
                 each([&](float x, int slot) { below += x == least && token_of_slot(a, row, slot) < (last | (1 << b)); });
-            if (block_count(w, below, b + 1) < k) last |= 1 << b;
+            if (block_count(w, below, turn) < k) last |= 1 << b;
         }
     }
     if (equal)
@@ -426,7 +426,7 @@ __device__ __forceinline__ int add_full_sweep(const ScoreArgs& a, const RowSlots
     lds_barrier();
     int n = w.n;
     if (n > kSoft) {
-        floor = fmaxf(floor, shorten_list(w, n, k));
+        floor = fmaxf(floor, shorten_list(w, n, k, a.id_bits));
         n = k;
     }
     lds_barrier();  // n has been read
@@ -448,7 +448,7 @@ __device__ __forceinline__ int settle_list(const ScoreArgs& a, const RowSlots& r
         for (int base = from; base < to; base += kSweep)
             n = add_full_sweep(a, row, w, logits, base + (int)threadIdx.x * 8, v1, k, floor);
     } else if (n > kSoft) {
-        floor = fmaxf(floor, shorten_list(w, n, k));
+        floor = fmaxf(floor, shorten_list(w, n, k, a.id_bits));
         n = k;
     }
     return n;
@@ -635,10 +635,10 @@ __global__ __launch_bounds__(kST) void score_finish_kernel(ScoreArgs a) {
         lds_barrier();
         int n = best.n;
         if (n > kCap) {  // equal logits
-            keep_best<E>(best, x, a.top);
+            keep_best<E>(best, x, a.top, a.id_bits);
             n = a.top;
         } else if (n > kSoft) {
-            shorten_list(best, n, a.top);
+            shorten_list(best, n, a.top, a.id_bits);
             n = a.top;
         }
         write_best(a, r, best, n, q);
