@@ -626,7 +626,9 @@ size_t dyna_token_logprobs_workspace_bytes(int32_t N, int32_t V, int32_t T, int3
  *               exp((z - m) / temperature) and the entropy, for dyna_token_logprobs_grad
  * A masked logit (-inf) has p = 0.  A row that allows no token (empty, or masked
  * throughout) has every log-probability -inf and entropy 0.  A NaN or +inf logit
- * makes its row's log-probabilities and entropy NaN. */
+ * makes its row's log-probabilities and entropy NaN.  No log-probability is above 0
+ * and no entropy below; a token that is almost certain has its log p = -log(1 + r) as
+ * right as r is, down to r of 2^-53. */
 dyna_status dyna_token_logprobs(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
                                 const dyna_shortlist_rows* rows, const int32_t* tokens, int32_t T, float temperature,
                                 int32_t top, float* out_logprobs, float* out_entropy, int32_t* out_top_ids,

@@ -6,10 +6,12 @@
 namespace dyna {
 
 // Sums of a part of a row relative to its largest logit m: w = exp((z - m) / T),
-// and w times (z - m) / T in powers of two.
+// and w times (z - m) / T in powers of two.  lead: the columns that m was added with,
+// the first of them and their sums as added.
 struct ScorePart {
     double s, u;
-    float m, pad;
+    float m, lead_part, lead_dot;
+    int32_t lead_at;
 };
 
 struct ScoreArgs {
