@@ -644,7 +644,8 @@ dyna_status dyna_token_logprobs(const void* logits, int32_t dtype, int32_t V, in
  *               its shortlist) are left as they were; the spans of both, gaps between rows
  *               included, must not overlap
  * A row whose g (at its tokens) and e are all 0 is padding: nothing of its logits
- * is read, its gradient is 0.  So is the gradient of a row that allows no token. */
+ * is read, its gradient is 0.  So is the gradient of a row that allows no token.
+ * Elements of given tokens are as right as 1 - p is in stats. */
 dyna_status dyna_token_logprobs_grad(const void* logits, int32_t dtype, int32_t V, int64_t row_stride, int32_t N,
                                      const dyna_shortlist_rows* rows, const int32_t* tokens, int32_t T,
                                      float temperature, const double* stats, const float* grad_logprobs,
