@@ -80,7 +80,10 @@ enum { DYNA_SEL_ARGMAX = 1, DYNA_SEL_TOPK = 2, DYNA_SEL_SAMPLE = 4, DYNA_SEL_UNI
 typedef struct dyna_layout {
     int32_t V, d, M;
     int32_t wdtype;            /* dyna_dtype of W_perm */
-    const void* W_perm;        /* device [V, d], 16-byte aligned */
+    const void* W_perm;        /* device [V, d], 16-byte aligned; may be NULL (a head
+                                * kept in four bits alone) for dyna_shortlist,
+                                * dyna_draft_select, dyna_token_rows, dyna_verify_chain,
+                                * dyna_quant_shortlist_logits, dyna_shortlist_rows */
     const int32_t* perm;       /* device [V] */
     const int32_t* offsets;    /* device [M + 1] */
     const int32_t* cap_by_k;   /* HOST [M + 1]: sum of the k largest cluster sizes */

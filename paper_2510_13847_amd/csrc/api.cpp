@@ -227,7 +227,7 @@ static Carve carve(const dyna_layout* L, const dyna_router* r, int32_t B, int32_
         if (!(cond)) return set_error(DYNA_ERR_INVALID_ARG, __VA_ARGS__); \
     } while (0)
 
-dyna_status check_layout(const dyna_layout* L) {
+dyna_status check_layout(const dyna_layout* L, bool reads_rows) {
     REQUIRE(L != nullptr, "layout is NULL");
     REQUIRE(L->V >= 1 && L->d >= 8 && L->M >= 1, "layout: bad sizes V=%d d=%d M=%d", L->V, L->d, L->M);
     REQUIRE(L->M <= L->V, "layout: M=%d > V=%d", L->M, L->V);
@@ -236,8 +236,9 @@ dyna_status check_layout(const dyna_layout* L) {
     REQUIRE(valid_dtype(L->wdtype), "layout: bad wdtype %d", L->wdtype);
     REQUIRE(L->d % 8 == 0, "layout: d=%d is not a multiple of 8", L->d);
     if (L->d > 8192) return set_error(DYNA_ERR_UNSUPPORTED, "layout: d=%d > 8192", L->d);
-    REQUIRE(L->W_perm && L->perm && L->offsets && L->cap_by_k, "layout: NULL array");
-    REQUIRE(aligned16(L->W_perm), "layout: W_perm not 16-byte aligned");
+    REQUIRE(L->perm && L->offsets && L->cap_by_k, "layout: NULL array");
+    REQUIRE(!reads_rows || (L->W_perm != nullptr && aligned16(L->W_perm)),
+            "layout: W_perm NULL or not 16-byte aligned");
     REQUIRE(L->max_cluster >= 1 && L->max_cluster <= L->V, "layout: bad max_cluster %d", L->max_cluster);
     return DYNA_OK;
 }
@@ -609,7 +610,7 @@ DYNA_API dyna_status dyna_route(const dyna_router* r, const void* x, int32_t xdt
 DYNA_API dyna_status dyna_shortlist(const dyna_layout* L, const int32_t* topk_ids, int32_t B, int32_t k,
                                     int32_t* sel_sorted, int32_t* sel_rowoff, int32_t* row_len,
                                     int32_t* shortlist_ids, int32_t cap, hipStream_t stream) {
-    TRY(check_layout(L));
+    TRY(check_layout(L, false));
     TRY(check_k(L, k));
     REQUIRE(B >= 0, "B=%d < 0", B);
     if (B == 0) return DYNA_OK;
@@ -641,7 +642,7 @@ DYNA_API dyna_status dyna_quant_shortlist_logits(const dyna_layout* L, const dyn
                                                  int32_t hdtype, int32_t B, int32_t k, const int32_t* sel_sorted,
                                                  const int32_t* sel_rowoff, const int32_t* row_len, float* logits,
                                                  int32_t cap, void* ws, size_t ws_bytes, hipStream_t stream) {
-    TRY(check_layout(L));
+    TRY(check_layout(L, false));
     TRY(check_quant(W, "W"));
     REQUIRE(W->rows == L->V && W->d == L->d, "W: rows=%d d=%d, not the layout's V=%d d=%d", W->rows, W->d, L->V, L->d);
     TRY(check_k(L, k));
@@ -676,7 +677,7 @@ DYNA_API dyna_status dyna_draft_select(const dyna_layout* L, const float* logits
                                        float* out_logprobs,
                                        int32_t* out_sample, float* out_sample_logprob, void* ws,
                                        size_t ws_bytes, hipStream_t stream) {
-    TRY(check_layout(L));
+    TRY(check_layout(L, false));
     TRY(check_k(L, k));
     TRY(check_cap(L, k, cap));
     TRY(check_select(mode, &k_t, temperature, uniforms, out_ids, out_sample));

@@ -81,7 +81,7 @@ void launch_timed_kernel(K kernel, dim3 grid, dim3 block, uint32_t shmem, hipStr
 // Launch error -> status with a message.
 dyna_status set_error(dyna_status s, const char* fmt, ...);
 dyna_status check_launch(const char* what);
-dyna_status check_layout(const dyna_layout* L);
+dyna_status check_layout(const dyna_layout* L, bool reads_rows = true);  // false: W_perm may be NULL
 
 // ---------------- launchers (defined in the .hip files) ----------------
 

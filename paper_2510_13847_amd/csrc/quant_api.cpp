@@ -47,7 +47,7 @@ dyna_status check_score(const void* logits, int32_t dtype, int32_t V, int64_t ro
     a->inv_t = 1.0 / (double)temperature;
     a->vocab = V;
     if (rows != nullptr) {
-        TRY(check_layout(rows->L));
+        TRY(check_layout(rows->L, false));
         REQUIRE(rows->token_rows != nullptr && aligned_to(rows->token_rows, 8),
                 "token_rows NULL or not 8-byte aligned");
         REQUIRE(rows->sel_sorted && rows->sel_rowoff && rows->row_len, "shortlists: NULL argument");

@@ -75,7 +75,7 @@ dyna_status check_distill_sizes(int32_t dtype, int32_t V, int32_t N, int32_t vdt
 
 // ------------------------------------------------------------------ verification
 DYNA_API dyna_status dyna_token_rows(const dyna_layout* L, int32_t* token_rows, hipStream_t stream) {
-    TRY(check_layout(L));
+    TRY(check_layout(L, false));
     REQUIRE(token_rows != nullptr && aligned_to(token_rows, 8), "token_rows NULL or not 8-byte aligned");
     return launch_token_rows(L->perm, L->offsets, L->V, L->M, token_rows, stream);
 }
@@ -123,7 +123,7 @@ DYNA_API dyna_status dyna_verify_chain(const void* target, int32_t tdtype, int32
         if ((int64_t)B * d.k > (1 << 30)) return set_error(DYNA_ERR_UNSUPPORTED, "step %d: B=%d k=%d", i, B, d.k);
     }
     if (clusters) {
-        TRY(check_layout(L));
+        TRY(check_layout(L, false));
         REQUIRE(L->V == V, "layout: V=%d differs from the target's %d", L->V, V);
         REQUIRE(token_rows != nullptr && aligned_to(token_rows, 8), "token_rows NULL or not 8-byte aligned");
         for (int i = 0; i < n; ++i) {

@@ -186,7 +186,8 @@ def kernel_timing(reset=True):
 # --------------------------------------------------------------------------
 @dataclass
 class Layout:
-    """Device layout from build_layout (tensors are kept alive here)."""
+    """Device layout from build_layout (tensors are kept alive here).  W_perm None: a head whose rows are kept in
+    four bits alone, for the calls that do not read them."""
     V: int
     d: int
     M: int
@@ -197,12 +198,12 @@ class Layout:
     max_cluster: int
 
     def __post_init__(self):
-        self._c = _Layout(self.V, self.d, self.M, _dtype_code(self.W_perm), _ptr(self.W_perm),
-                          _ptr(self.perm), _ptr(self.offsets),
+        dtype = BF16 if self.W_perm is None else _dtype_code(self.W_perm)
+        self._c = _Layout(self.V, self.d, self.M, dtype, _ptr(self.W_perm), _ptr(self.perm), _ptr(self.offsets),
                           self.cap_by_k.ctypes.data_as(ctypes.c_void_p).value, self.max_cluster)
 
     def with_weights(self, W_perm) -> "Layout":
-        """The same layout over another copy of the permuted head (replicas)."""
+        """The same layout over another copy of the permuted head (replicas), or without one (None)."""
         return Layout(self.V, self.d, self.M, W_perm, self.perm, self.offsets, self.cap_by_k,
                       self.max_cluster)
 
@@ -1020,7 +1021,8 @@ def quant_product(a, W: QuantRows, n_rows: Optional[int] = None, out=None, out_d
 def quant_shortlist_logits(layout: Layout, W: QuantRows, h, sel_sorted, sel_rowoff, row_len, cap=None, ws=None,
                            out=None, stream=None):
     """dyna_quant_shortlist_logits -> logits [B, cap] fp32 (slots past row_len untouched): shortlist_logits over
-    four-bit rows, W = quantize_rows(layout.W_perm); ws = workspace(layout, None, B, k, cap)."""
+    four-bit rows, W = quantize_rows(layout.W_perm); ws = workspace(layout, None, B, k, cap).  W_perm is not read:
+    layout.with_weights(None) lets go of it."""
     import torch
     _quant(W, "W", getattr(W, "device", None))
     dev = W.device
