@@ -33,6 +33,7 @@ namespace {
 template <typename T>
 using sptr = const __attribute__((address_space(4))) T*;  // read through the scalar unit
 __host__ __device__ constexpr int contexts_per_pass(int act) { return act == kActF32 ? kRowsMostF32 : kRowsMost; }
+// (without a plan there is one pass: more contexts go to the tiles)
 
 // One tile and the contexts that it is multiplied with.
 struct QuantTile {
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
         if (at < c1) cur = read_tile(at, 0);
     } else {
         at = blockIdx.x;
-        if ((int64_t)at * kMfmaRows < a.n_rows) cur = read_tile(at, blockIdx.y * CPP);
+        if ((int64_t)at * kMfmaRows < a.n_rows) cur = read_tile(at, 0);
     }
     // The tile behind cur: plans walk the chunks of one context list once for each
     // CPP of its contexts.
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
         } else {
             if (i * kMfmaRows >= a.n_rows) return kNone;
             at = (int)i;
-            return read_tile(at, cur.first);
+            return read_tile(at, 0);
         }
     };
 
@@ -152,16 +153,15 @@ __global__ __launch_bounds__(MAXW* kWave, MAXW == 3 ? 2 : MAXW / 4) void quant_r
     auto load_contexts = [&](int c) __attribute__((always_inline)) {
         c = max(c, 0);
         if constexpr (ACT == kActFour) {
-            const uint8_t* p = a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes + wv * kQuantUnitBytes +
-                               (c % kMfmaRows) * 16 + g * 256;
+            // (one group: no plan, so 16 contexts at most)
+            const uint8_t* p = a.a4.data + wv * kQuantUnitBytes + c * 16 + g * 256;
 #pragma unroll
             for (int j = 0; j < kQuantUnitSteps; ++j) {
                 b[j][0] = u32x4{0u, 0u, 0u, 0u};
                 if (j < steps) b[j][0] = *reinterpret_cast<const u32x4*>(p + j * kQuantStepBytes);
             }
-            bs = *reinterpret_cast<const uint32_t*>(a.a4.data + (int64_t)(c / kMfmaRows) * a.a4.group_bytes +
-                                                    wv * kQuantUnitBytes + steps * kQuantStepBytes +
-                                                    (c % kMfmaRows) * 4 + g * 64);
+            bs = *reinterpret_cast<const uint32_t*>(a.a4.data + wv * kQuantUnitBytes + steps * kQuantStepBytes +
+                                                    c * 4 + g * 64);
         } else {
             using T = typename std::conditional<ACT == kActBf16, uint16_t, float>::type;
             const int k0 = wv * kQuantUnit + g * kQuantBlock;
@@ -282,7 +282,6 @@ template <int ACT, bool PLAN, int MAXW, typename OT>
 dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
     const int NW = a.W.units;
     const int64_t tiles = PLAN ? a.max_chunks_bound : ((int64_t)a.n_rows + kMfmaRows - 1) / kMfmaRows;
-    const int passes = PLAN ? 1 : (a.B + contexts_per_pass(ACT) - 1) / contexts_per_pass(ACT);
     // Workgroups that a compute unit's registers hold at once, so that none runs alone
     // behind the others: 16 waves; of the instances of few waves, which take more
     // registers, 12, or 8 where gathered fp32 contexts are put together (262144 x 1536, 16
@@ -291,8 +290,7 @@ dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
     const int waves = MAXW > 3 || ACT == kActFour ? 16 : PLAN && ACT == kActF32 ? 8 : 12;
     const int64_t resident = 256 * (int64_t)std::max(1, waves / NW);
     const int64_t blocks = std::max<int64_t>(1, std::min(tiles, resident));
-    launch_timed_kernel(quant_rows_kernel<ACT, PLAN, MAXW, OT>, dim3((unsigned)blocks, (unsigned)passes), dim3(NW * kWave),
-                        0, stream, a);
+    launch_timed_kernel(quant_rows_kernel<ACT, PLAN, MAXW, OT>, dim3((unsigned)blocks), dim3(NW * kWave), 0, stream, a);
     return check_launch("quant_rows_kernel");
 }
 template <int ACT, bool PLAN, typename OT>
