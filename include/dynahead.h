@@ -580,7 +580,8 @@ size_t dyna_quant_product_workspace_bytes(int32_t B, int32_t d);
  *  out       device, dtype odtype, row b is n_rows elements at b * out_stride;
  *            elements behind a row are left as they were
  * The products of the values are exact and summed in 32 bits: fp32 contexts are
- * taken as three bf16 terms each, which hold all 24 bits.  B = 0 is a no-op. */
+ * taken as three bf16 terms each, which hold all 24 bits of magnitudes of 2^-110 and
+ * more, and smaller values to 2^-134.  B = 0 is a no-op. */
 dyna_status dyna_quant_product(const dyna_quant* W, int32_t n_rows, const void* a, int32_t adtype, int64_t a_stride,
                                const dyna_quant* a4, int32_t B, void* out, int32_t odtype, int64_t out_stride,
                                void* ws, size_t ws_bytes, hipStream_t stream);

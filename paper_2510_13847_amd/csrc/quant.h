@@ -10,8 +10,8 @@
 // instruction of 16 rows by 128 columns takes from it with one instruction, lane
 // after lane, and a group of whole rows is consecutive too.  (With a row's four
 // blocks side by side, 64 bytes, a load is the same 1 KiB in another order of lanes:
-// 2048 four-bit contexts over 128256 x 4096 651 us against 599, 128 contexts'
-// shortlists over 262144 x 5376 134 against 131.)
+// with the tiles as they were then, 2048 four-bit contexts over 128256 x 4096 took 651 us
+// against 599, and 128 contexts' shortlists over 262144 x 5376 134 against 131.)
 // Rows past the last one and columns past d are zeros.
 #pragma once
 

@@ -7,7 +7,9 @@
 //
 // Both are streams, bound by HBM: each input byte is read once and each output byte
 // written once.  128256 x 4096 bf16: 256 us to four bits (1.33 GB, 5.2 TB/s, the rate
-// of a copy), 226 back (5.9 TB/s); 16 x 3584 4.9 and 3.4 us, which is a launch.
+// of a copy), 226 back (5.9 TB/s); 16 x 3584 4.9 and 3.4 us, which is a launch.  fp32:
+// 468 us to four bits (5.1 TB/s), 614 back (3.9 TB/s: a lane's two stores of 16 bytes are
+// 32 apart).
 #include "quant.h"
 #include "rowstat.h"
 

@@ -50,7 +50,9 @@ __device__ __forceinline__ f32x16 four_bit_product(const u32x4& x, uint32_t xs, 
 }
 
 // Term t of three of an fp32 value, each cut off behind eight bits (so the sum is
-// the value, and no term overflows); an infinity or NaN is its own first term.
+// the value, and no term overflows); an infinity or NaN is its own first term.  As bf16
+// numbers the terms hold all 24 bits of magnitudes of 2^-110 and more; below, the last
+// one is rounded to a multiple of 2^-133, and the value is taken to 2^-134.
 __device__ __forceinline__ float term_of(float x, int t) {
     const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
     if (t == 0) return x == x ? a : x;

@@ -9,7 +9,8 @@
 // products are added through LDS in wave order (bit-identical from run to run).
 //
 // An fp32 context is three columns of bf16: its 24 bits cut in three terms of
-// eight, whose products with a four-bit value are exact.
+// eight, whose products with a four-bit value are exact (from magnitudes of 2^-110 on;
+// below, the last term ends at bf16's smallest number).
 //
 // bf16 and fp32 contexts take the bf16 instructions, whose products are exact too: an
 // e2m1 value over its scale is a bf16 number, so the rows' four bits are the only
@@ -17,10 +18,15 @@
 // Sums are 32 bits: in an instruction, over a wave's 512 columns, over the waves.
 //
 // What bounds it is the rows' bytes; a wave has 4.25 KiB of the next tile in flight
-// while it multiplies one, the two workgroups of 4096 columns on a compute unit 68 KiB.
+// while it multiplies one, the two workgroups of 4096 columns on a compute unit 68 KiB
+// (dense; of gathered ones, which take more registers, one of 4096 columns runs at a time).
 // 128256 x 4096 (279 MB): one bf16 context 42 us (6.7 TB/s, what rows stream at; 5.8
-// where the last cache holds none of them), 8 43.5, 16 48; four fp32 ones 51.  Gathered: 128 contexts with 64 of 4096 clusters each over
-// 262144 x 5376 (652 MB) 95 us, 6.9 TB/s; one with 32 of 1024 over 128256 x 4096 8 us.
+// where the last cache holds none of them), 8 43.5, 16 47; four fp32 ones 48.  Gathered:
+// 128 contexts with 64 of 4096 clusters each over 262144 x 5376 (652 MB) 95 to 99 us
+// where the last cache holds some of the rows; one with 32 of 1024 over 128256 x 4096 8 us.
+// Gathered fp32 contexts, whose terms are cut again in every pass of five, are far from
+// their rows' bytes: 64 with 32 of 1024 clusters of 128256 x 4096 167 us a call, bf16 ones
+// 50, the bytes 16.
 // A run of consecutive chunks to a workgroup, as the plan's order has the contexts of
 // one list side by side: handing chunks out by a counter took 157 us where this took
 // 136, contexts being loaded again for each.
@@ -283,8 +289,9 @@ dyna_status launch_t(const QuantProductArgs& a, hipStream_t stream) {
     const int NW = a.W.units;
     const int64_t tiles = PLAN ? a.max_chunks_bound : ((int64_t)a.n_rows + kMfmaRows - 1) / kMfmaRows;
     // Workgroups that a compute unit's registers hold at once, so that none runs alone
-    // behind the others: 16 waves; of the instances of few waves, which take more
-    // registers, 12, or 8 where gathered fp32 contexts are put together (262144 x 1536, 16
+    // behind the others: 16 waves (of gathered instances of 8 and 12 waves, with 140 and
+    // 147 registers, 12 of these run at once: some workgroups do come behind); of the
+    // instances of few waves, which take more registers, 12, or 8 where gathered fp32 contexts are put together (262144 x 1536, 16
     // waves and 12: a bf16 context 44 and 38 us, four fp32 ones 61 and 49; 128 fp32
     // contexts' 64 of 2048 clusters of 151936 x 1536, 16, 12 and 8: 131, 134 and 117)
     const int waves = MAXW > 3 || ACT == kActFour ? 16 : PLAN && ACT == kActF32 ? 8 : 12;

@@ -2,9 +2,9 @@
 //
 // The products and their precision are those of the row-streaming kernel.  What bounds
 // it: rows' and products' bytes up to about 64 contexts (128256 x 4096: 279 MB of rows
-// and 33 MB of fp32 products; 67 us, where the bytes take 46 and a library's bf16
-// product 55), above it the matrix cores: 256 contexts 218 us (1.23 PFLOP/s, a
-// library's bf16 rate), fp32 ones three times the work (64 in 174 us).  2048 four-bit
+// and 33 MB of fp32 products; 67 us, where the bytes take 46 and the products 55 at
+// 1.22 PFLOP/s, what a library's largest bf16 products reach), above it the matrix cores:
+// 256 contexts 215 us (1.25 PFLOP/s), fp32 ones three times the work (64 in 174 us).  2048 four-bit
 // contexts 562 us (3.8 PFLOP/s; the instruction alone reaches 7.4): there the loads
 // bound it, the same time without products.  A tile of 256 by 256 reads 512 rows' bytes
 // for 65536 products a column, and the 32 by 32 instruction, which does a third more

@@ -13,15 +13,15 @@
 // is almost certain of one token is log1p of what the others weigh.  The same pass
 // keeps the candidates for the best tokens: those that reach a floor which k logits
 // are known to reach, so almost all logits cost one comparison per eight.  4096 x
-// 128256 bf16 (1.05 GB) takes 201 us (5.2 TB/s), with 20 alternatives 236; 2048 x
-// 128256 fp32, the same bytes, 178 (5.9 TB/s) and 189.  The memory would take 155.
+// 128256 bf16 (1.05 GB) takes 187 us (5.6 TB/s), with 20 alternatives 220 to 235; 2048 x
+// 128256 fp32, the same bytes, 177 (5.9 TB/s) and 190.  The memory would take 155.
 // bf16 rows have twice the exponentials to a byte: one exponential (four times an
 // instruction's time) and six other operations to a logit are 130 us of the vector
 // units by themselves, and what they do not hide is the rest.  Few rows: 1 x 128256 13
 // us, of which the two launches are 6.
 //
-// Gradient: 4096 x 128256 bf16 in 405 us, 5.2 TB/s, the rate of a copy; nothing is
-// gained by more in flight.
+// Gradient: 4096 x 128256 bf16 in 402 us, 5.2 TB/s, the rate of a copy, 2048 x 128256
+// fp32 in 427; nothing is gained by more in flight.
 #include <algorithm>
 
 #include "rowstat.h"
@@ -821,9 +821,13 @@ __global__ __launch_bounds__(kST) void score_grad_kernel(ScoreArgs a) {
 }
 
 // Parts of a row: whole rows where there are enough of them for the device's compute
-// units, else as many as fit these at once (four to each: 128 rows of 128256 with 64
+// units, else as many as make four workgroups to each (128 rows of 128256 with 64
 // alternatives 27.4 us, with parts for two or eight to each 33.5 and 29.7), of 4096
-// columns at least.
+// columns at least.  Four run at once, of fp32 rows with alternatives three.  From 513
+// rows on a row is one part, and compute units have two to four of them: rows of 128256
+// without and with 20 alternatives, bf16: 300 rows 24 and 34 us (the bytes 11), 600 33
+// and 49 (23), 900 43 and 58 (34), 1024 47 and 58 (39); fp32: 32 and 47 (23), 57 and 62
+// (45), 85 and 108 (68), 92 and 114 (77).
 void split_rows(int32_t N, int32_t V, int32_t* splits, int32_t* len) {
     int64_t parts = 1;
     if (V > 2 * kSweep && N < 1024) {
